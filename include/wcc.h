@@ -48,7 +48,8 @@ typedef enum {
     WCC_ERR_WORKSPACE = 7,   /* ws_bytes smaller than wcc_workspace_bytes(...) */
     WCC_ERR_CUDA = 8,        /* a CUDA runtime call or launch failed */
     WCC_ERR_TIMEOUT = 9,     /* a bounded device-side wait ran out (reported by wcc_last_status) */
-    WCC_ERR_NONFINITE = 10   /* reserved */
+    WCC_ERR_NONFINITE = 10,  /* reserved */
+    WCC_ERR_INDEX = 11       /* an adapter index out of range (reported by wcc_last_status) */
 } wcc_status;
 
 typedef enum { WCC_F32 = 0, WCC_BF16 = 1 } wcc_dtype;   /* element type of activations x and y */
@@ -304,9 +305,66 @@ wcc_status wcc_forward_staged(const void* x, const float* Wt, int N, int Cin, in
                               void* ws, size_t ws_bytes, void* stream, const wcc_taps* taps);
 
 /*
+ * Layer norm over the channels of a map: every position of every image is normalised over its C channels,
+ *     mean = 1/C sum_c x,  rstd = (1/C sum_c (x - mean)^2 + eps)^-1/2,  y = (x - mean) * rstd * gamma[c] + beta[c]
+ * (the paper's networks normalise over the batch, which folds into the weights; networks of pointwise and depthwise convolutions
+ * that normalise per position need this in front of the layer).  H = Wd = 1 is a batch of N rows of C contiguous channels.
+ *   x     in : [N][C][H][Wd] of dt          gamma, beta in: fp32 [C], each may be NULL (1 and 0)
+ *   y     out: as x; may be x itself        mean, rstd out: fp32 [N][H*Wd], each may be NULL; the backward pass reads them
+ *   eps      : >= 0 and finite.  With eps = 0 a position whose channels are all equal gives NaN, as the formula does.
+ * H and Wd are any positive numbers (no multiples), C <= WCC_MAX_CHANNELS, N * H * Wd <= 2^30.  fp32 arithmetic; the variance
+ * is a sum of squared deviations from the mean, so a large common offset of the channels costs it no digits.
+ */
+wcc_status wcc_layernorm_fwd(const void* x, const float* gamma, const float* beta, int N, int C, int H, int Wd, float eps, wcc_dtype dt,
+                             void* y, float* mean, float* rstd, void* stream);
+/*
+ * Its backward pass.  With xh = (x - mean) * rstd and g = dy * gamma[c]:
+ *     dx = rstd * (g - 1/C sum_c g - xh * 1/C sum_c g xh),   dgamma[c] = sum_{n,p} dy xh,   dbeta[c] = sum_{n,p} dy
+ *   dy, x in: [N][C][H][Wd] of dt           mean, rstd in: what the forward pass returned
+ *   dx   out: as x; may be dy or x itself   dgamma, dbeta out: fp32 [C], each may be NULL (both NULL: ws is not used and may be NULL)
+ *   ws      : scratch of at least wcc_layernorm_bwd_workspace_bytes(...) bytes, 16-byte aligned
+ * The sums over images and positions are fp32, in an order that depends on the sizes alone: the same call gives the same bits.
+ */
+size_t wcc_layernorm_bwd_workspace_bytes(int N, int C, int H, int Wd, wcc_dtype dt);
+wcc_status wcc_layernorm_bwd(const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, int N, int C, int H,
+                             int Wd, wcc_dtype dt, void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Low-rank adapters of many requests at once beside a shared projection (a WCC layer whose weights stay as they are): image n of the batch
+ * is a request with adapter a = ids[n], any negative id for none,
+ *     y_n = base_n + scale[a] * B_a (A_a x_n)            (a < 0: y_n = base_n)
+ * over the channels at every position.  Added to a layer: wcc_adapters_fwd writes into y (with the layer's own residual, if it has one, as base),
+ * then wcc_forward_ex runs with residual = y into the same y; the layer's ReLU then comes after the sum.
+ *   x     in : [N][Cin][H][Wd] of dt                A in: [R][rank][Cin] of dt          B in: [R][Cout][rank] of dt
+ *   scale in : fp32 [R], or NULL for 1              ids in: int32 [N] on the DEVICE     base in: [N][Cout][H][Wd] of dt, or NULL for 0
+ *   y     out: [N][Cout][H][Wd] of dt; may be base, must not overlap x
+ *   ws       : scratch of at least wcc_adapters_workspace_bytes(..., 0) bytes, 16-byte aligned
+ * rank is 1 .. WCC_MAX_RANK; adapters of smaller rank are padded with zero rows of A and columns of B.  H and Wd are any positive numbers,
+ * H = Wd = 1 is a batch of single tokens.  N * H * Wd <= 2^30, R <= 65535.  An id of R or more counts as none, and wcc_last_status then
+ * reports WCC_ERR_INDEX.  Sums are fp32; the products of rank size keep at least 16 bits (bf16 maps) or 21 bits (fp32 maps) of a factor.
+ * A position with a NaN or an infinity among its channels gives NaN or infinity at that position alone.
+ */
+#define WCC_MAX_RANK 64
+size_t wcc_adapters_workspace_bytes(int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, int backward);
+wcc_status wcc_adapters_fwd(const void* x, const void* A, const void* B, const float* scale, const int32_t* ids, const void* base, int N,
+                            int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, void* y, void* ws, size_t ws_bytes, void* stream);
+/*
+ * Its backward pass: with V_n = scale[a] * B_a^T dy_n and U_n = A_a x_n,
+ *     dx_n = base_n + A_a^T V_n,   dA_a = sum_n V_n x_n^T,   dB_a = scale[a] * sum_n dy_n U_n^T   (over the images of the adapter and all positions)
+ *   dy   in : [N][Cout][H][Wd] of dt                 base in: [N][Cin][H][Wd] of dt, what dx is added to (the shared projection's own gradient), or NULL
+ *   dx   out: [N][Cin][H][Wd] of dt, may be base, must not overlap x or dy; NULL: not wanted
+ *   dA, dB out: fp32 [R][rank][Cin] and [R][Cout][rank], zeros for adapters without an image; both NULL: not wanted (x may then be NULL)
+ *   ws      : scratch of at least wcc_adapters_workspace_bytes(..., 1) bytes, 16-byte aligned
+ * The sums over images and positions are fp32, in an order that depends on the sizes and the ids alone: the same call gives the same bits.
+ */
+wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const void* B, const float* scale, const int32_t* ids,
+                            const void* base, int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, void* dx, float* dA,
+                            float* dB, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns the device-side status word of the calling thread's current device:
  * WCC_OK, or WCC_ERR_TIMEOUT if a bounded wait inside a kernel gave up (the output of that call is then
- * undefined).  Reading clears the word.
+ * undefined), or WCC_ERR_INDEX if an adapter index was out of range.  Reading clears the word.
  */
 wcc_status wcc_last_status(void* stream);
 

@@ -10,6 +10,8 @@
 #include "scatter.cuh"
 #include "select.cuh"
 #include "contract.cuh"
+#include "norm.cuh"
+#include "adapters.cuh"
 #include "pass2.cuh"
 #include "wavelet.cuh"
 
@@ -1082,6 +1084,90 @@ wcc_status wcc_forward_debug(const void* x, const float* Wt, int N, int Cin, int
                         static_cast<cudaStream_t>(stream), taps);
 }
 
+// ---- layer norm over the channels ---------------------------------------------------------------
+wcc_status wcc_layernorm_fwd(const void* x, const float* gamma, const float* beta, int N, int C, int H, int Wd, float eps, wcc_dtype dt,
+                             void* y, float* mean, float* rstd, void* stream)
+{
+    if (!x || !y) return WCC_ERR_NULL;
+    wcc_status s = check_norm_args(N, C, H, Wd, dt);
+    if (s != WCC_OK) return s;
+    if (!(eps >= 0.0f) || eps > 3.0e38f) return WCC_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(gamma) || !aligned16(beta) || !aligned16(y) || !aligned16(mean) || !aligned16(rstd)) return WCC_ERR_ALIGN;
+    const ln::Plan p = ln::plan_of(N, C, (size_t)H * Wd, dt == WCC_BF16 ? 2 : 4, false);
+    if (!p.rows && (long long)p.q.items * p.q.cl > 0x7FFFFFFFLL) return WCC_ERR_SHAPE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dt == WCC_BF16 ? ln::forward<__nv_bfloat16>(p, x, gamma, beta, y, mean, rstd, N, C, eps, st)
+                          : ln::forward<float>(p, x, gamma, beta, y, mean, rstd, N, C, eps, st);
+}
+
+size_t wcc_layernorm_bwd_workspace_bytes(int N, int C, int H, int Wd, wcc_dtype dt)
+{
+    if (check_norm_args(N, C, H, Wd, dt) != WCC_OK) return 0;
+    return ln::bwd_ws_bytes(ln::plan_of(N, C, (size_t)H * Wd, dt == WCC_BF16 ? 2 : 4, true), N, C);
+}
+
+wcc_status wcc_layernorm_bwd(const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, int N, int C, int H,
+                             int Wd, wcc_dtype dt, void* dx, float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream)
+{
+    const bool params = dgamma || dbeta;
+    if (!dy || !x || !mean || !rstd || !dx || (params && !ws)) return WCC_ERR_NULL;
+    wcc_status s = check_norm_args(N, C, H, Wd, dt);
+    if (s != WCC_OK) return s;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(gamma) || !aligned16(mean) || !aligned16(rstd) || !aligned16(dx) || !aligned16(dgamma) ||
+        !aligned16(dbeta) || !aligned16(ws)) return WCC_ERR_ALIGN;
+    const ln::Plan p = ln::plan_of(N, C, (size_t)H * Wd, dt == WCC_BF16 ? 2 : 4, true);
+    if (params && ws_bytes < ln::bwd_ws_bytes(p, N, C)) return WCC_ERR_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    float* part = params ? static_cast<float*>(ws) : nullptr;
+    s = dt == WCC_BF16 ? ln::backward<__nv_bfloat16>(p, dy, x, gamma, mean, rstd, dx, part, N, C, st)
+                       : ln::backward<float>(p, dy, x, gamma, mean, rstd, dx, part, N, C, st);
+    if (s != WCC_OK || !params) return s;
+    const int rows = ln::bwd_ctas(p, N) / (p.rows ? 1 : p.q.cl);
+    return launch_overlapped(ln::ln_reduce, dim3((unsigned)ceil_div(2 * C, 32)), dim3(32, 32), 0, st, true, 1, part, rows, C, dgamma, dbeta);
+}
+
+// ---- low-rank adapters beside a shared projection -------------------------------------------------
+size_t wcc_adapters_workspace_bytes(int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, int backward)
+{
+    if (check_adapter_args(N, Cin, Cout, H, Wd, R, rank, dt) != WCC_OK) return 0;
+    const size_t P = (size_t)H * Wd;
+    const size_t n = dt == WCC_BF16 ? ad::carve<__nv_bfloat16>(nullptr, N, Cin, Cout, P, R, rank, backward != 0).total
+                                    : ad::carve<float>(nullptr, N, Cin, Cout, P, R, rank, backward != 0).total;
+    return std::max<size_t>(n, 256);
+}
+
+wcc_status wcc_adapters_fwd(const void* x, const void* A, const void* B, const float* scale, const int32_t* ids, const void* base, int N,
+                            int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, void* y, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!x || !A || !B || !ids || !y || !ws) return WCC_ERR_NULL;
+    wcc_status s = check_adapter_args(N, Cin, Cout, H, Wd, R, rank, dt);
+    if (s != WCC_OK) return s;
+    if (!aligned16(x) || !aligned16(A) || !aligned16(B) || !aligned16(scale) || !aligned16(ids) || !aligned16(base) || !aligned16(y) || !aligned16(ws))
+        return WCC_ERR_ALIGN;
+    if (ws_bytes < wcc_adapters_workspace_bytes(N, Cin, Cout, H, Wd, R, rank, dt, 0)) return WCC_ERR_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const size_t P = (size_t)H * Wd;
+    return dt == WCC_BF16 ? ad::forward<__nv_bfloat16>(x, A, B, scale, ids, base, N, Cin, Cout, P, R, rank, y, ws, st)
+                          : ad::forward<float>(x, A, B, scale, ids, base, N, Cin, Cout, P, R, rank, y, ws, st);
+}
+
+wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const void* B, const float* scale, const int32_t* ids,
+                            const void* base, int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, void* dx, float* dA,
+                            float* dB, void* ws, size_t ws_bytes, void* stream)
+{
+    if (!dy || !A || !B || !ids || !ws || (!dx && !dA) || (!dA != !dB) || (dA && !x) || (base && !dx)) return WCC_ERR_NULL;
+    wcc_status s = check_adapter_args(N, Cin, Cout, H, Wd, R, rank, dt);
+    if (s != WCC_OK) return s;
+    if (!aligned16(dy) || !aligned16(x) || !aligned16(A) || !aligned16(B) || !aligned16(scale) || !aligned16(ids) || !aligned16(base) ||
+        !aligned16(dx) || !aligned16(dA) || !aligned16(dB) || !aligned16(ws)) return WCC_ERR_ALIGN;
+    if (ws_bytes < wcc_adapters_workspace_bytes(N, Cin, Cout, H, Wd, R, rank, dt, 1)) return WCC_ERR_WORKSPACE;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const size_t P = (size_t)H * Wd;
+    return dt == WCC_BF16 ? ad::backward<__nv_bfloat16>(dy, x, A, B, scale, ids, base, N, Cin, Cout, P, R, rank, dx, dA, dB, ws, st)
+                          : ad::backward<float>(dy, x, A, B, scale, ids, base, N, Cin, Cout, P, R, rank, dx, dA, dB, ws, st);
+}
+
+// ---- status ---------------------------------------------------------------------------------------
 wcc_status wcc_last_status(void* stream)
 {
     if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return WCC_ERR_CUDA;
@@ -1156,6 +1242,7 @@ const char* wcc_status_str(wcc_status s)
         case WCC_ERR_CUDA: return "CUDA error";
         case WCC_ERR_TIMEOUT: return "device wait timed out";
         case WCC_ERR_NONFINITE: return "non-finite input";
+        case WCC_ERR_INDEX: return "adapter index out of range";
     }
     return "unknown status";
 }

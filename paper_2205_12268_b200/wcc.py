@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libwcc.so")
 F32, BF16 = 0, 1
 _STATUS = {0: "ok", 1: "null pointer", 2: "bad shape", 3: "k out of range", 4: "bad bits", 5: "bad dtype",
            6: "misaligned pointer", 7: "workspace too small", 8: "CUDA error", 9: "device wait timed out",
-           10: "non-finite input"}
+           10: "non-finite input", 11: "adapter index out of range"}
+MAX_RANK = 64
 
 EXPORTS = ("wcc_staged_workspace_bytes", "wcc_forward_staged", "wcc_workspace_bytes", "wcc_select_workspace_bytes", "wcc_haar_fwd", "wcc_haar_inv", "wcc_select_topk",
            "wcc_forward", "wcc_forward_debug", "wcc_kpad", "wcc_last_status", "wcc_status_str",
@@ -24,7 +25,9 @@ EXPORTS = ("wcc_staged_workspace_bytes", "wcc_forward_staged", "wcc_workspace_by
            "wcc_debug_set_wait_limit", "wcc_debug_wait_selftest", "wcc_debug_select", "wcc_forward_ex", "wcc_chain_workspace_bytes",
            "wcc_chain_forward", "wcc_select_bitmap_workspace_bytes", "wcc_select_topk_bitmap",
            "wcc_padded_workspace_bytes", "wcc_forward_padded", "wcc_dwconv_haar_fwd", "wcc_block_workspace_bytes",
-           "wcc_block_forward", "wcc_dwt_fwd", "wcc_dwt_inv", "wcc_wavelet_workspace_bytes", "wcc_forward_wavelet")
+           "wcc_block_forward", "wcc_dwt_fwd", "wcc_dwt_inv", "wcc_wavelet_workspace_bytes", "wcc_forward_wavelet",
+           "wcc_layernorm_fwd", "wcc_layernorm_bwd_workspace_bytes", "wcc_layernorm_bwd", "wcc_adapters_workspace_bytes",
+           "wcc_adapters_fwd", "wcc_adapters_bwd")
 STATIC_SCRATCH_BYTES = 512 * 1024
 STAGES = ("haar_fwd_norms", "select_topk", "weight_quant", "gather_quant", "contract", "scatter_inv")   # wcc_forward_staged
 FUSED_STAGES = ("clear", "haar_norms", "select_topk", "fused_pass2")                                      # wcc_forward
@@ -113,8 +116,7 @@ def lib() -> C.CDLL:
         L.wcc_chain_workspace_bytes.argtypes = [C.POINTER(ChainLayer), i, i, i, i, i, i, i, i]
         L.wcc_chain_forward.restype = i
         L.wcc_chain_forward.argtypes = [vp, C.POINTER(ChainLayer), i, i, i, i, i, i, i, vp, i, vp, sz, vp]
-        L.wcc_last_status.restype = i
-        L.wcc_last_status.argtypes = [vp]
+        _operator_prototypes(L)
         L.wcc_profile_enable.restype = i
         L.wcc_profile_enable.argtypes = [i]
         L.wcc_profile_read.restype = i
@@ -131,6 +133,25 @@ def lib() -> C.CDLL:
         L.wcc_status_str.argtypes = [i]
         _lib = L
     return _lib
+
+
+def _operator_prototypes(L):
+    """Layer norm, adapters and the status word."""
+    i, vp, sz, f = C.c_int, C.c_void_p, C.c_size_t, C.c_float
+    L.wcc_layernorm_fwd.restype = i
+    L.wcc_layernorm_fwd.argtypes = [vp, vp, vp, i, i, i, i, f, i, vp, vp, vp, vp]
+    L.wcc_layernorm_bwd_workspace_bytes.restype = sz
+    L.wcc_layernorm_bwd_workspace_bytes.argtypes = [i] * 5
+    L.wcc_layernorm_bwd.restype = i
+    L.wcc_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
+    L.wcc_adapters_workspace_bytes.restype = sz
+    L.wcc_adapters_workspace_bytes.argtypes = [i] * 9
+    L.wcc_adapters_fwd.restype = i
+    L.wcc_adapters_fwd.argtypes = [vp] * 6 + [i] * 8 + [vp, vp, sz, vp]
+    L.wcc_adapters_bwd.restype = i
+    L.wcc_adapters_bwd.argtypes = [vp] * 7 + [i] * 8 + [vp, vp, vp, vp, sz, vp]
+    L.wcc_last_status.restype = i
+    L.wcc_last_status.argtypes = [vp]
 
 
 def _check(code: int, where: str):
@@ -370,6 +391,180 @@ class Workspace:
         if n == 0:
             raise WccError(2, "wcc_workspace_bytes")
         return cls(n, x.device)
+
+    @classmethod
+    def for_layernorm_backward(cls, x: torch.Tensor):
+        n = int(lib().wcc_layernorm_bwd_workspace_bytes(*_map_shape(x, "x"), _dt(x)))
+        if n == 0:
+            raise WccError(2, "wcc_layernorm_bwd_workspace_bytes")
+        return cls(n, x.device)
+
+
+def _map_shape(x: torch.Tensor, name: str):
+    """(N, C, H, W) of a map [N][C][H][W] or of rows [N][C], which are maps of one position."""
+    _dev(x, name)
+    if x.dim() == 2:
+        return (x.shape[0], x.shape[1], 1, 1)
+    if x.dim() != 4:
+        raise ValueError("%s must be [N][C][H][W] or [N][C]" % name)
+    return tuple(x.shape)
+
+
+def _same(t: torch.Tensor, like: torch.Tensor, name: str, what: str):
+    """t is a tensor of `like`'s shape, type and device, contiguous as every map."""
+    _dev(t, name)
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError("%s must have the shape, type and device of %s" % (name, what))
+
+
+def _fp32(t, shape, like: torch.Tensor, name: str):
+    if t is not None:
+        _dev(t, name)
+        if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or t.device != like.device:
+            raise ValueError("%s must be float32 %s on the device of the map" % (name, list(shape)))
+
+
+def _on(t: torch.Tensor):
+    """The library launches on the current device's current stream: tensors of another device are refused."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("the map is on %s, which is not the current device" % t.device)
+
+
+def layernorm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5,
+              y: torch.Tensor | None = None, stats: bool = False):
+    """Layer norm over the channels of a map [N][C][H][W] (or of rows [N][C]), fp32 ``gamma`` and ``beta`` [C] or None.
+    Returns y (``y`` may be x), or with ``stats`` (y, mean, rstd), the statistics fp32 [N][H*W] as the backward pass reads them."""
+    N, Cc, H, W = _map_shape(x, "x")
+    dt = _dt(x)
+    _on(x)
+    _fp32(gamma, (Cc,), x, "gamma")
+    _fp32(beta, (Cc,), x, "beta")
+    if y is None:
+        y = torch.empty_like(x)
+    elif y is not x:
+        _same(y, x, "y", "x")
+    mean = rstd = None
+    if stats:
+        mean = torch.empty((N, H * W), dtype=torch.float32, device=x.device)
+        rstd = torch.empty((N, H * W), dtype=torch.float32, device=x.device)
+    _check(lib().wcc_layernorm_fwd(x.data_ptr(), _ptr(gamma), _ptr(beta), N, Cc, H, W, eps, dt, y.data_ptr(), _ptr(mean), _ptr(rstd),
+                                   _stream()), "wcc_layernorm_fwd")
+    return (y, mean, rstd) if stats else y
+
+
+def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: torch.Tensor | None = None,
+                       dx: torch.Tensor | None = None, params: bool = True, ws: Workspace | None = None):
+    """The gradients of ``layernorm``: (dx, dgamma, dbeta), the last two fp32 [C] and None without ``params``.
+    ``dx`` may be dy or x.  ``ws`` is a ``Workspace.for_layernorm_backward``, allocated here if it is not given."""
+    N, Cc, H, W = _map_shape(x, "x")
+    dt = _dt(x)
+    _on(x)
+    _same(dy, x, "dy", "x")
+    _fp32(mean, (N, H * W), x, "mean")
+    _fp32(rstd, (N, H * W), x, "rstd")
+    _fp32(gamma, (Cc,), x, "gamma")
+    if dx is None:
+        dx = torch.empty_like(x)
+    elif dx is not x and dx is not dy:
+        _same(dx, x, "dx", "x")
+    dgamma = dbeta = None
+    if params:
+        dgamma = torch.empty((Cc,), dtype=torch.float32, device=x.device)
+        dbeta = torch.empty((Cc,), dtype=torch.float32, device=x.device)
+        if ws is None:
+            ws = Workspace.for_layernorm_backward(x)
+    _check(lib().wcc_layernorm_bwd(dy.data_ptr(), x.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), N, Cc, H, W, dt,
+                                   dx.data_ptr(), _ptr(dgamma), _ptr(dbeta), ws.buf.data_ptr() if params else None,
+                                   ws.nbytes if params else 0, _stream()), "wcc_layernorm_bwd")
+    return dx, dgamma, dbeta
+
+
+class Adapters:
+    """Low-rank adapters beside a shared projection: factors ``A`` [R][rank][Cin] and ``B`` [R][Cout][rank] of the maps' type, ``scale`` fp32 [R]
+    or None for 1.  The tensors are kept, not copied: a call sees what they hold when it runs.
+
+    ``adapters(x, ids)`` -> base + scale * B (A x) with the adapter ids[n] (int32 [N] on the device, negative: none) for image n of x
+    [N][Cin][H][W] (or of rows [N][Cin]); ``adapters.backward(dy, x, ids)`` -> (dx, dA, dB).  See wcc_adapters_fwd and wcc_adapters_bwd."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
+        for t, name in ((A, "A"), (B, "B")):
+            _dev(t, name)
+            if t.dim() != 3:
+                raise ValueError("A [R][rank][Cin] and B [R][Cout][rank] expected")
+        self.dt = _dt(A)
+        self.R, self.rank, self.Cin = A.shape
+        self.Cout = B.shape[1]
+        if B.dtype != A.dtype or B.device != A.device or tuple(B.shape) != (self.R, self.Cout, self.rank):
+            raise ValueError("B must be [R][Cout][rank] of A's type on A's device")
+        if not 1 <= self.rank <= MAX_RANK:
+            raise ValueError("the rank must be 1 to %d" % MAX_RANK)
+        _fp32(scale, (self.R,), A, "scale")
+        self.A, self.B, self.scale = A, B, scale
+
+    def workspace(self, x: torch.Tensor, backward: bool = True) -> Workspace:
+        """Scratch for calls on maps of x's shape; that for the backward pass also serves the forward pass."""
+        N, _, H, W = self._args(x, None)
+        n = [int(lib().wcc_adapters_workspace_bytes(N, self.Cin, self.Cout, H, W, self.R, self.rank, self.dt, b)) for b in ((0, 1) if backward else (0,))]
+        if min(n) == 0:
+            raise WccError(2, "wcc_adapters_workspace_bytes")
+        return Workspace(max(n), x.device)
+
+    def _args(self, x, ids):
+        shape = _map_shape(x, "x")
+        if _dt(x) != self.dt or shape[1] != self.Cin or x.device != self.A.device:
+            raise ValueError("x must have the adapters' type, Cin channels and device")
+        if ids is not None:
+            _dev(ids, "ids")
+            if ids.dtype != torch.int32 or tuple(ids.shape) != (shape[0],) or ids.device != x.device:
+                raise ValueError("ids must be int32 [N] on the device of the map")
+        return shape
+
+    def _map(self, t, x, C, name):
+        """A map of x's sizes with C channels."""
+        if _map_shape(t, name) != (x.shape[0], C) + tuple(x.shape[2:] if x.dim() == 4 else (1, 1)) or t.dtype != x.dtype or t.device != x.device:
+            raise ValueError("%s must be a map of %d channels with x's sizes, type and device" % (name, C))
+
+    def __call__(self, x: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None, y: torch.Tensor | None = None,
+                 ws: Workspace | None = None) -> torch.Tensor:
+        N, _, H, W = self._args(x, ids)
+        _on(x)
+        if base is not None:
+            self._map(base, x, self.Cout, "base")
+        if y is None:
+            y = torch.empty((N, self.Cout) + tuple(x.shape[2:]), dtype=x.dtype, device=x.device)
+        else:
+            self._map(y, x, self.Cout, "y")
+            if y.data_ptr() == x.data_ptr():
+                raise ValueError("y must not be x")
+        if ws is None:
+            ws = self.workspace(x, backward=False)
+        _check(lib().wcc_adapters_fwd(x.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), ids.data_ptr(), _ptr(base), N, self.Cin,
+                                      self.Cout, H, W, self.R, self.rank, self.dt, y.data_ptr(), ws.buf.data_ptr(), ws.nbytes, _stream()),
+               "wcc_adapters_fwd")
+        return y
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                 params: bool = True, ws: Workspace | None = None):
+        """(dx, dA, dB): dx = base + the adapters' part of the map's gradient, dA and dB fp32 in the factors' shapes (None without ``params``)."""
+        N, _, H, W = self._args(x, ids)
+        _on(x)
+        self._map(dy, x, self.Cout, "dy")
+        if base is not None:
+            self._map(base, x, self.Cin, "base")
+        if dx is None:
+            dx = torch.empty_like(x)
+        else:
+            self._map(dx, x, self.Cin, "dx")
+            if dx.data_ptr() in (x.data_ptr(), dy.data_ptr()):
+                raise ValueError("dx must not be x or dy")
+        dA = torch.empty(self.A.shape, dtype=torch.float32, device=x.device) if params else None
+        dB = torch.empty(self.B.shape, dtype=torch.float32, device=x.device) if params else None
+        if ws is None:
+            ws = self.workspace(x)
+        _check(lib().wcc_adapters_bwd(dy.data_ptr(), x.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), ids.data_ptr(), _ptr(base),
+                                      N, self.Cin, self.Cout, H, W, self.R, self.rank, self.dt, dx.data_ptr(), _ptr(dA), _ptr(dB),
+                                      ws.buf.data_ptr(), ws.nbytes, _stream()), "wcc_adapters_bwd")
+        return dx, dA, dB
 
 
 def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits: int = 8, y: torch.Tensor | None = None,
