@@ -25,11 +25,17 @@ namespace ad {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int MAX_RANK = 64;
+#ifndef AD_HALF
+#define AD_HALF 8
+#define AD_FILL 12LL
+#endif
 
 template <typename T> struct Geo;
 template <> struct Geo<__nv_bfloat16> { static constexpr int NP = 8, TP = 64, CL = 8, GC = 32, PARTS = 1; };
 template <> struct Geo<float> { static constexpr int NP = 4, TP = 32, CL = 4, GC = 16, PARTS = 2; };
-// NP positions of a lane, TP of a warp's tile, CL channels of a lane in a group of GC, PARTS parts of a factor's element
+// NP positions of a lane (16 bytes) and TP of a warp's tile in the widest form, CL channels of a lane in a group of GC, PARTS parts of a factor's
+// element.  For the largest ranks a lane takes half as many positions, which halves the sums it has to hold.
+template <typename T> __host__ __device__ constexpr int lane_positions(int rb) { return rb >= AD_HALF ? Geo<T>::NP / 2 : Geo<T>::NP; }
 
 // steps of the second product's summation index, ranks in blocks of 8
 template <typename T> __host__ __device__ constexpr int steps2(int rb) { return sizeof(T) == 2 ? (rb + 1) / 2 : rb; }
@@ -66,41 +72,94 @@ __device__ __forceinline__ void split_bf16(float u0, float u1, uint32_t& hi, uin
     lo = pack_bf16x2(u0 - bf16lo(hi), u1 - bf16hi(hi));
 }
 
-// 16 bytes of a channel's row: NP positions from p on, those at P and beyond as zeros.  VEC: rows start on 16 bytes.
-template <typename T, bool VEC>
-__device__ __forceinline__ uint4 load_positions(const T* row, size_t p, size_t P)
+// NP positions of a channel's row from p on as they lie in memory, those at P and beyond as zeros.  VEC: rows start on multiples of NP positions.
+// Otherwise the two aligned pieces around them are loaded and shifted into place (`end`: behind the tensor's last element, nothing is read from
+// there on): single loads of 2 bytes cost eight times the instructions, a layer's odd map 76 us instead of the figure below.
+template <int WORDS> struct Words { uint32_t w[WORDS]; };
+template <int W> __device__ __forceinline__ Words<W> load_words(const void* p)
 {
-    if (VEC) return p < P ? *reinterpret_cast<const uint4*>(row + p) : make_uint4(0u, 0u, 0u, 0u);
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (sizeof(T) == 2) {
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(row);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (p + i < P) w[i >> 1] |= (uint32_t)q[p + i] << (16 * (i & 1));
+    Words<W> r;
+    if constexpr (W == 8) {
+        // volatile, so that it stays ahead of the products it is issued before
+        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+            : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+            : "l"(p));
+    } else if constexpr (W == 4) {
+        const uint4 u = *static_cast<const uint4*>(p);
+        r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
     } else {
-        const uint32_t* q = reinterpret_cast<const uint32_t*>(row);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (p + i < P) w[i] = q[p + i];
+        const uint2 u = *static_cast<const uint2*>(p);
+        r.w[0] = u.x; r.w[1] = u.y;
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return r;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void store_positions(T* row, size_t p, size_t P, uint4 v)
+template <int W> __device__ __forceinline__ void store_words(void* p, const Words<W>& v)
 {
-    if (VEC) { if (p < P) *reinterpret_cast<uint4*>(row + p) = v; return; }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    if (sizeof(T) == 2) {
-        uint16_t* q = reinterpret_cast<uint16_t*>(row);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (p + i < P) q[p + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    if constexpr (W == 8)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]), "r"(v.w[3]), "r"(v.w[4]), "r"(v.w[5]), "r"(v.w[6]), "r"(v.w[7]) : "memory");
+    else if constexpr (W == 4) *static_cast<uint4*>(p) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+    else *static_cast<uint2*>(p) = make_uint2(v.w[0], v.w[1]);
+}
+template <typename T, int NP, bool VEC>
+__device__ __forceinline__ Words<NP * (int)sizeof(T) / 4> load_row(const T* row, size_t p, size_t P, const T* end)
+{
+    constexpr int W = NP * (int)sizeof(T) / 4;
+    Words<W> r{};
+    if (p >= P) return r;
+    if constexpr (VEC) {
+        return load_words<W>(row + p);
     } else {
-        uint32_t* q = reinterpret_cast<uint32_t*>(row);
+        const T* q = row + p;
+        const int m = (int)((reinterpret_cast<uintptr_t>(q) / sizeof(T)) % NP);
+        q -= m;                                                         // (a tensor starts on 16 bytes)
+        uint32_t w[2 * W];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (p + i < P) q[p + i] = w[i];
+        for (int i = 0; i < 2 * W; ++i) w[i] = 0u;
+#pragma unroll
+        for (int h = 0; h < 2; ++h, q += NP) {
+            if (h == 1 && m == 0) break;
+            if (q + NP <= end) {
+                const Words<W> u = load_words<W>(q);
+#pragma unroll
+                for (int i = 0; i < W; ++i) w[h * W + i] = u.w[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+                    if (q + i < end) {
+                        if (sizeof(T) == 2) w[(h * W + (i >> 1)) % (2 * W)] |= (uint32_t)reinterpret_cast<const uint16_t*>(q)[i] << (16 * (i & 1));
+                        else w[(h * W + i) % (2 * W)] = reinterpret_cast<const uint32_t*>(q)[i];
+                    }
+            }
+        }
+        const int sw = sizeof(T) == 2 ? m >> 1 : m;                     // whole words first
+#pragma unroll
+        for (int step = W / 2; step >= 1; step /= 2)
+            if (sw & step) {
+#pragma unroll
+                for (int i = 0; i + step < 2 * W; ++i) w[i] = w[i + step];
+            }
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            r.w[i] = sizeof(T) == 2 ? __funnelshift_r(w[i], w[i + 1], 16 * (m & 1)) : w[i];
+            if (p + NP > P) {
+                if (sizeof(T) == 2) {
+                    if (p + 2 * i >= P) r.w[i] = 0u;
+                    else if (p + 2 * i + 1 >= P) r.w[i] &= 0xFFFFu;
+                } else if (p + i >= P) r.w[i] = 0u;
+            }
+        }
+        return r;
     }
+}
+template <typename T> __device__ __forceinline__ float load_one(const T* p)
+{
+    return sizeof(T) == 4 ? *reinterpret_cast<const float*>(p) : __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+}
+template <typename T> __device__ __forceinline__ void store_one(T* p, float v)
+{
+    if (sizeof(T) == 4) *reinterpret_cast<float*>(p) = v;
+    else *reinterpret_cast<uint16_t*>(p) = (uint16_t)pack_bf16x2(v, 0.0f);
 }
 
 // ---- factors in the order of the matrix instructions -----------------------------------------
@@ -238,10 +297,13 @@ struct ApplyArgs {
     int* status;
 };
 
-template <typename T, int RB, bool VEC>
+// VEC: 0 single loads, 1 rows start on the NP positions of a lane's first product, 2 also on the 2 NP of the second.
+template <typename T, int RB, int VEC>
 __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, float4* sm)
 {
-    constexpr int NP = Geo<T>::NP, TP = Geo<T>::TP, CL = Geo<T>::CL, GC = Geo<T>::GC, PARTS = Geo<T>::PARTS, MB = NP / 2;
+    constexpr int NP = lane_positions<T>(RB), TP = 8 * NP, CL = Geo<T>::CL, GC = Geo<T>::GC, PARTS = Geo<T>::PARTS, MB = NP / 2;
+    constexpr int NO = VEC == 2 ? 2 * NP : NP, PIECES = 2 * NP / NO;    // positions of a load or store of the second product
+    constexpr bool HALF = sizeof(T) == 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int n = item / q.tiles;
     const int per = (int)(blockDim.x >> 5) / q.ks;                    // position tiles of the CTA
@@ -250,21 +312,37 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
     const int a = adapter_of(q.ids, n, q.R, q.status);
     const size_t P = q.P;
     const int mo_n = (q.M + 15) / 16;
+    const size_t pw = p0 + (size_t)(2 * NP * t);
 
     if (a < 0) {                                                        // (the whole CTA: it has one image)
         if (!q.w2 || q.dst == q.base || p0 >= P) return;
-        for (int mo = kw; mo < mo_n; mo += q.ks)
+        // the warps of the tile copy its rows, eight pieces of 16 or 8 bytes (or 32 single elements) a row
+        const T* from = q.base + (size_t)n * q.M * P;
+        T* to = q.dst + (size_t)n * q.M * P;
+        constexpr int BATCH = 8;                                        // loads before the first store: the two may be the same map
+        if constexpr (VEC > 0) {
+            constexpr int W = NP * (int)sizeof(T) / 4;
+            const size_t p = p0 + (size_t)NP * (lane & 7);
+            if (p < P)
+                for (int o0 = 4 * kw + (lane >> 3); o0 < q.M; o0 += BATCH * 4 * q.ks) {
+                    Words<W> v[BATCH];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int o = 16 * mo + g + 8 * h;
-                if (o >= q.M) continue;
-                const size_t row = ((size_t)n * q.M + o) * P;
+                    for (int i = 0; i < BATCH; ++i) v[i] = q.base ? load_words<W>(from + min(o0 + 4 * i * q.ks, q.M - 1) * P + p) : Words<W>{};
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const size_t p = p0 + (size_t)(2 * NP * t + NP * e);
-                    store_positions<T, VEC>(q.dst + row, p, P, q.base ? load_positions<T, VEC>(q.base + row, p, P) : make_uint4(0u, 0u, 0u, 0u));
+                    for (int i = 0; i < BATCH; ++i)
+                        if (o0 + 4 * i * q.ks < q.M) store_words(to + (o0 + 4 * i * q.ks) * P + p, v[i]);
                 }
-            }
+        } else {
+            for (size_t p = p0 + lane; p < min(P, p0 + TP); p += 32)
+                for (int o0 = kw; o0 < q.M; o0 += BATCH * q.ks) {
+                    float v[BATCH];
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) v[i] = q.base ? load_one(from + min(o0 + i * q.ks, q.M - 1) * P + p) : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i)
+                        if (o0 + i * q.ks < q.M) store_one(to + (o0 + i * q.ks) * P + p, v[i]);
+                }
+        }
         return;
     }
 
@@ -277,30 +355,35 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
             for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
 
     const int groups = (q.K + GC - 1) / GC;
-    const T* src = q.src + (size_t)n * q.K * P;
     const size_t pl = p0 + (size_t)NP * g;
+    const T* src = q.src + (size_t)n * q.K * P;
+    const size_t pc = pl < P ? pl : 0;
+    const T* src_end = q.src + (size_t)q.N * q.K * P;
     const uint4* w1 = q.w1 + (size_t)a * first_words<T>(RB, q.K) + lane;
+    const size_t limit = q.tap ? q.Pp : P;                             // the tap is zero behind P
     if (p0 < P)
 #pragma unroll 2
         for (int grp = kw; grp < groups; grp += q.ks) {
-            uint4 xr[CL];
+            // Channels behind the last one meet zeros in the factor, positions behind the last one are never stored: both load something else that
+            // exists, so that all loads of a group go out together.
+            Words<NP * (int)sizeof(T) / 4> x[CL];
 #pragma unroll
             for (int i = 0; i < CL; ++i) {
-                const int c = grp * GC + t * CL + i;
-                xr[i] = c < q.K ? load_positions<T, VEC>(src + (size_t)c * P, pl, P) : make_uint4(0u, 0u, 0u, 0u);
+                const T* xp = src + (size_t)min(grp * GC + t * CL + i, q.K - 1) * P;
+                if constexpr (VEC > 0) x[i] = load_words<NP * (int)sizeof(T) / 4>(xp + pc);
+                else x[i] = load_row<T, NP, false>(xp, pl, P, src_end);
             }
-            const uint32_t(*xw)[4] = reinterpret_cast<const uint32_t(*)[4]>(xr);
             const uint4* wg = w1 + (size_t)grp * RB * PARTS * 32;
-            if constexpr (sizeof(T) == 2) {
+            if constexpr (HALF) {
                 uint32_t fa[2][MB][4];
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int mb = 0; mb < MB; ++mb) {
-                        fa[s][mb][0] = __byte_perm(xw[4 * s][mb], xw[4 * s + 1][mb], 0x5410);
-                        fa[s][mb][1] = __byte_perm(xw[4 * s][mb], xw[4 * s + 1][mb], 0x7632);
-                        fa[s][mb][2] = __byte_perm(xw[4 * s + 2][mb], xw[4 * s + 3][mb], 0x5410);
-                        fa[s][mb][3] = __byte_perm(xw[4 * s + 2][mb], xw[4 * s + 3][mb], 0x7632);
+                        fa[s][mb][0] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x5410);
+                        fa[s][mb][1] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x7632);
+                        fa[s][mb][2] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x5410);
+                        fa[s][mb][3] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x7632);
                     }
 #pragma unroll
                 for (int jb = 0; jb < RB; ++jb) {
@@ -320,7 +403,7 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
 #pragma unroll
                     for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) split_tf32(xw[2 * s + (i >> 1)][2 * mb + (i & 1)], hi[s][mb][i], lo[s][mb][i]);
+                        for (int i = 0; i < 4; ++i) split_tf32(x[2 * s + (i >> 1)].w[2 * mb + (i & 1)], hi[s][mb][i], lo[s][mb][i]);
 #pragma unroll
                 for (int jb = 0; jb < RB; ++jb) {
                     const uint4 wh = __ldg(wg + (jb * 2) * 32), wl = __ldg(wg + (jb * 2 + 1) * 32);
@@ -360,7 +443,7 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
                 acc[mb][jb][0] = v.x; acc[mb][jb][1] = v.y; acc[mb][jb][2] = v.z; acc[mb][jb][3] = v.w;
             }
     }
-    if (p0 >= P) return;
+    if (p0 >= limit) return;
     const float sc = q.scale ? q.scale[a] : 1.0f;
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
@@ -370,45 +453,86 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
             for (int i = 0; i < 4; ++i) acc[mb][jb][i] *= sc;
 
     if (q.tap && kw == 0) {
+        if (pl >= P) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int jb = 0; jb < RB; ++jb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
+        }
         // rank j = 8 jb + 2 t + e: this lane's positions p0 + NP g + b are accumulators [b / 2][jb][2 (b % 2) + e]
 #pragma unroll
         for (int jb = 0; jb < RB; ++jb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const size_t at = ((size_t)n * (8 * RB) + 8 * jb + 2 * t + e) * q.Pp + pl;
-                if constexpr (sizeof(T) == 2) {
-                    uint32_t hi[4], mid[4], lo[4];
+                if constexpr (HALF) {
+                    Words<MB> hi, mid, lo;
 #pragma unroll
-                    for (int mb = 0; mb < 4; ++mb) {
+                    for (int mb = 0; mb < MB; ++mb) {
                         const float v0 = acc[mb][jb][e], v1 = acc[mb][jb][2 + e];
-                        hi[mb] = pack_bf16x2(v0, v1);
-                        split_bf16(v0 - bf16lo(hi[mb]), v1 - bf16hi(hi[mb]), mid[mb], lo[mb]);
+                        hi.w[mb] = pack_bf16x2(v0, v1);
+                        split_bf16(v0 - bf16lo(hi.w[mb]), v1 - bf16hi(hi.w[mb]), mid.w[mb], lo.w[mb]);
                     }
-                    __nv_bfloat16* plane = static_cast<__nv_bfloat16*>(q.tap) + at;
+                    T* plane = static_cast<T*>(q.tap) + at;
                     const size_t next = (size_t)q.N * (8 * RB) * q.Pp;
-                    *reinterpret_cast<uint4*>(plane) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4*>(plane + next) = make_uint4(mid[0], mid[1], mid[2], mid[3]);
-                    *reinterpret_cast<uint4*>(plane + 2 * next) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    store_words(plane, hi);
+                    store_words(plane + next, mid);
+                    store_words(plane + 2 * next, lo);
                 } else {
-                    *reinterpret_cast<float4*>(static_cast<float*>(q.tap) + at) = make_float4(acc[0][jb][e], acc[0][jb][2 + e], acc[1][jb][e], acc[1][jb][2 + e]);
+                    Words<NP> v;
+#pragma unroll
+                    for (int b = 0; b < NP; ++b) v.w[b] = __float_as_uint(acc[b >> 1][jb][2 * (b & 1) + e]);
+                    store_words(static_cast<T*>(q.tap) + at, v);
                 }
             }
     }
-    if (!q.w2) return;
+    if (!q.w2 || p0 >= P) return;
 
+    // the accumulators as operands: of position b, block jb of ranks
+    constexpr int UW = HALF ? 1 : 2;
+    uint32_t uh[NP][RB][UW], ul[NP][RB][UW];
+#pragma unroll
+    for (int b = 0; b < NP; ++b)
+#pragma unroll
+        for (int jb = 0; jb < RB; ++jb) {
+            const float u0 = acc[b >> 1][jb][2 * (b & 1)], u1 = acc[b >> 1][jb][2 * (b & 1) + 1];
+            if constexpr (HALF) split_bf16(u0, u1, uh[b][jb][0], ul[b][jb][0]);
+            else {
+                split_tf32(__float_as_uint(u0), uh[b][jb][0], ul[b][jb][0]);
+                split_tf32(__float_as_uint(u1), uh[b][jb][UW - 1], ul[b][jb][UW - 1]);
+            }
+        }
+    float* out = reinterpret_cast<float*>(sm) + (q.ks > 1 ? (size_t)(blockDim.x >> 5) * (MB * RB * 128) : 0) + warp * 16 * (TP + 4);
     const uint4* w2 = q.w2 + (size_t)a * second_words<T>(RB, q.M) + lane;
     constexpr int NS = steps2<T>(RB);
-    for (int mo = kw; mo < mo_n; mo += q.ks) {
-        uint4 bs[2][2];
-        const size_t pw = p0 + (size_t)(2 * NP * t);
+    // the base of the next 16 channels is loaded while these are computed: the loads of one iteration would be waited for in every one
+    using Piece = Words<NO * (int)sizeof(T) / 4>;
+    auto load_base = [&](int mo, Piece(&b)[2][PIECES]) {
+        if (VEC > 0 && q.base && mo < mo_n) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int o = 16 * mo + g + 8 * h;
-            const bool have = q.base && o < q.M;
-            const T* row = q.base + ((size_t)n * q.M + o) * P;
-            bs[h][0] = have ? load_positions<T, VEC>(row, pw, P) : make_uint4(0u, 0u, 0u, 0u);
-            bs[h][1] = have ? load_positions<T, VEC>(row, pw + NP, P) : make_uint4(0u, 0u, 0u, 0u);
+            for (int h = 0; h < 2; ++h) {
+                const T* row = q.base + ((size_t)n * q.M + min(16 * mo + g + 8 * h, q.M - 1)) * P;
+#pragma unroll
+                for (int e = 0; e < PIECES; ++e) b[h][e] = load_words<NO * (int)sizeof(T) / 4>(row + (pw + NO * e < P ? pw + NO * e : 0));
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < PIECES; ++e) b[h][e] = Piece{};
         }
+    };
+    Piece next[2][PIECES];
+    load_base(kw, next);
+    for (int mo = kw; mo < mo_n; mo += q.ks) {
+        Piece bs[2][PIECES];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < PIECES; ++e) bs[h][e] = next[h][e];
+        load_base(mo + q.ks, next);
         float d[NP][4];
 #pragma unroll
         for (int b = 0; b < NP; ++b)
@@ -417,52 +541,75 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
         const uint4* wm = w2 + (size_t)mo * NS * PARTS * 32;
 #pragma unroll
         for (int ks = 0; ks < NS; ++ks) {
-            if constexpr (sizeof(T) == 2) {
+            if constexpr (HALF) {
                 const uint4 w = __ldg(wm + ks * 32);
 #pragma unroll
                 for (int b = 0; b < NP; ++b) {
-                    uint32_t h0, l0, h1 = 0u, l1 = 0u;
-                    split_bf16(acc[b >> 1][2 * ks][2 * (b & 1)], acc[b >> 1][2 * ks][2 * (b & 1) + 1], h0, l0);
-                    if (2 * ks + 1 < RB) split_bf16(acc[b >> 1][(2 * ks + 1) % RB][2 * (b & 1)], acc[b >> 1][(2 * ks + 1) % RB][2 * (b & 1) + 1], h1, l1);
-                    mma_bf16(d[b], w.x, w.y, w.z, w.w, l0, l1);
-                    mma_bf16(d[b], w.x, w.y, w.z, w.w, h0, h1);
+                    mma_bf16(d[b], w.x, w.y, w.z, w.w, ul[b][2 * ks][0], 2 * ks + 1 < RB ? ul[b][(2 * ks + 1) % RB][0] : 0u);
+                    mma_bf16(d[b], w.x, w.y, w.z, w.w, uh[b][2 * ks][0], 2 * ks + 1 < RB ? uh[b][(2 * ks + 1) % RB][0] : 0u);
                 }
             } else {
                 const uint4 wh = __ldg(wm + (ks * 2) * 32), wl = __ldg(wm + (ks * 2 + 1) * 32);
 #pragma unroll
                 for (int b = 0; b < NP; ++b) {
-                    uint32_t h0, l0, h1, l1;
-                    split_tf32(__float_as_uint(acc[b >> 1][ks][2 * (b & 1)]), h0, l0);
-                    split_tf32(__float_as_uint(acc[b >> 1][ks][2 * (b & 1) + 1]), h1, l1);
-                    mma_tf32(d[b], wl.x, wl.y, wl.z, wl.w, h0, h1);
-                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, l0, l1);
-                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, h0, h1);
+                    mma_tf32(d[b], wl.x, wl.y, wl.z, wl.w, uh[b][ks][0], uh[b][ks][UW - 1]);
+                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, ul[b][ks][0], ul[b][ks][UW - 1]);
+                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, uh[b][ks][0], uh[b][ks][UW - 1]);
                 }
             }
         }
-        // channel g + 8 h: accumulators 2 h + e hold position pw + NP e + b
+        // channel g + 8 h: accumulators 2 h + e of b are position pw + NP e + b
+        if constexpr (VEC == 0) {
+            // rows that start anywhere: through shared memory, so that the lanes of a warp write neighbours
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int b = 0; b < NP; b += 2)
+                        *reinterpret_cast<float2*>(out + (g + 8 * h) * (TP + 4) + 2 * NP * t + NP * e + b) = make_float2(d[b][2 * h + e], d[b + 1][2 * h + e]);
+            __syncwarp();
+            const int rows = min(16, q.M - 16 * mo);
+            const size_t at = ((size_t)n * q.M + 16 * mo) * P + p0, here = P - p0;
+#pragma unroll 8
+            for (int i = lane; i < 16 * TP; i += 32) {
+                const int r = i / TP, c = i % TP;
+                if (r < rows && (size_t)c < here) {
+                    const size_t j = at + r * P + c;
+                    float v = out[r * (TP + 4) + c];
+                    if (q.base) v += load_one(q.base + j);
+                    store_one(q.dst + j, v);
+                }
+            }
+        } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int o = 16 * mo + g + 8 * h;
             if (o >= q.M) continue;
             T* row = q.dst + ((size_t)n * q.M + o) * P;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t bw[4] = {bs[h][e].x, bs[h][e].y, bs[h][e].z, bs[h][e].w};
-                uint32_t w[4];
+            for (int e = 0; e < PIECES; ++e) {
+                Piece v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (sizeof(T) == 2) w[i] = pack_bf16x2(d[2 * i][2 * h + e] + bf16lo(bw[i]), d[2 * i + 1][2 * h + e] + bf16hi(bw[i]));
-                    else w[i] = __float_as_uint(d[i][2 * h + e] + __uint_as_float(bw[i]));
+                for (int i = 0; i < NO * (int)sizeof(T) / 4; ++i) {
+                    if constexpr (HALF) {
+                        const int at = NO * e + 2 * i;                  // of the lane's 2 NP positions
+                        v.w[i] = pack_bf16x2(d[at % NP][2 * h + at / NP] + bf16lo(bs[h][e].w[i]), d[at % NP + 1][2 * h + at / NP] + bf16hi(bs[h][e].w[i]));
+                    } else {
+                        const int at = NO * e + i;
+                        v.w[i] = __float_as_uint(d[at % NP][2 * h + at / NP] + __uint_as_float(bs[h][e].w[i]));
+                    }
                 }
-                store_positions<T, VEC>(row, pw + NP * e, P, make_uint4(w[0], w[1], w[2], w[3]));
+                if (pw + NO * e < P) store_words(row + pw + NO * e, v);
             }
+        }
         }
     }
 }
 
 // Up to two maps in one launch (the backward pass projects dy and x): the second takes the CTAs from q0.items on.
-template <typename T, int RB, bool VEC>
+template <typename T, int RB, int VEC>
 __global__ void __launch_bounds__(256) apply_kernel(ApplyArgs<T> q0, ApplyArgs<T> q1)
 {
     extern __shared__ float4 apply_sm[];
@@ -570,6 +717,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs<T> q)
     const bool side = blk >= q.blocks[0];
     const int c0 = 16 * (side ? blk - q.blocks[0] : blk), C = side ? q.C[1] : q.C[0];
     const T* map = side ? q.map[1] : q.map[0];
+    const T* map_end = map + (size_t)q.N * C * q.P;
     const void* plane = side ? q.plane[1] : q.plane[0];
     const long long total = (long long)q.start[q.R] * q.tiles, share = (total + q.ranges - 1) / q.ranges;
     const long long u0 = k * share, u1 = min(total, u0 + share);
@@ -596,23 +744,24 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs<T> q)
         const T* m0 = map + ((size_t)n * C + c0 + g) * q.P;
         const T* m1 = m0 + 8 * q.P;
         const size_t pb = (size_t)tile * TP;
-        uint4 xr[2][2];                 // [half of the tile][channel g, g + 8]: this lane's NP positions of it
+        Words<4> xr[2][2];              // [half of the tile][channel g, g + 8]: this lane's NP positions of it
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const size_t p = pb + h * (TP / 2) + t * NP;
-            xr[h][0] = c0 + g < C ? load_positions<T, VEC>(m0, p, q.P) : make_uint4(0u, 0u, 0u, 0u);
-            xr[h][1] = c0 + g + 8 < C ? load_positions<T, VEC>(m1, p, q.P) : make_uint4(0u, 0u, 0u, 0u);
+            xr[h][0] = xr[h][1] = Words<4>{};
+            if (c0 + g < C) xr[h][0] = load_row<T, NP, VEC>(m0, p, q.P, map_end);
+            if (c0 + g + 8 < C) xr[h][1] = load_row<T, NP, VEC>(m1, p, q.P, map_end);
         }
 #pragma unroll
         for (int jb = 0; jb < RB; ++jb) {
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t(*xw)[4] = reinterpret_cast<const uint32_t(*)[4]>(xr[h]);
+                const Words<4>(&xw)[2] = xr[h];
                 const size_t at = ((size_t)n * (8 * RB) + 8 * jb + g) * q.Pp + pb + h * (TP / 2) + t * NP;
                 if constexpr (sizeof(T) == 2) {
                     const __nv_bfloat16* pl = static_cast<const __nv_bfloat16*>(plane) + at;
-                    const uint32_t a0[4] = {xw[0][0], xw[1][0], xw[0][1], xw[1][1]}, a1[4] = {xw[0][2], xw[1][2], xw[0][3], xw[1][3]};
+                    const uint32_t a0[4] = {xw[0].w[0], xw[1].w[0], xw[0].w[1], xw[1].w[1]}, a1[4] = {xw[0].w[2], xw[1].w[2], xw[0].w[3], xw[1].w[3]};
 #pragma unroll
                     for (int part = 2; part >= 0; --part) {
                         const uint4 v = *reinterpret_cast<const uint4*>(pl + (size_t)part * q.N * (8 * RB) * q.Pp);
@@ -626,7 +775,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs<T> q)
                     for (int s = 0; s < 2; ++s) {
                         uint32_t ah[4], al[4], bh[2], bl[2];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) split_tf32(xw[i & 1][2 * s + (i >> 1)], ah[i], al[i]);
+                        for (int i = 0; i < 4; ++i) split_tf32(xw[i & 1].w[2 * s + (i >> 1)], ah[i], al[i]);
                         split_tf32(vw[2 * s], bh[0], bl[0]);
                         split_tf32(vw[2 * s + 1], bh[1], bl[1]);
                         mma_tf32(d, al, bh[0], bh[1]);
@@ -727,39 +876,43 @@ static Ws carve(void* ws, int N, int Cin, int Cout, size_t P, int R, int rank, b
 }
 
 // Warps that share a tile: more only while the tiles alone do not fill the GPU.
-template <typename T>
-static void plan_apply(ApplyArgs<T>& q, int rb, int& warps, size_t& smem)
+// Partial sums of warps that share a tile, and the tiles on their way out where rows start anywhere.
+template <typename T> static size_t apply_smem(int warps, int rb, int ks, bool vec)
 {
-    const long long tiles = (long long)((q.P + Geo<T>::TP - 1) / Geo<T>::TP);
+    const int np = lane_positions<T>(rb);
+    return (size_t)warps * ((ks > 1 ? (np / 2) * rb * 512 : 0) + (vec ? 0 : 16 * (8 * np + 4) * 4));
+}
+template <typename T>
+static void plan_apply(ApplyArgs<T>& q, int rb, int& warps)
+{
+    const int tp = 8 * lane_positions<T>(rb);
+    const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
     const int parts = std::max(ceil_div(q.K, Geo<T>::GC), q.w2 ? ceil_div(q.M, 16) : 1);
     q.ks = 1;
-    while (q.ks < 8 && q.ks * 2 <= parts && (long long)q.N * tiles * q.ks < 12LL * B200_SMS) q.ks *= 2;
+    while (q.ks < 8 && q.ks * 2 <= parts && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
     warps = q.ks == 8 ? 8 : 4;
     const int per = warps / q.ks;
     q.tiles = (int)((tiles + per - 1) / per);
-    smem = q.ks > 1 ? (size_t)warps * (Geo<T>::NP / 2) * rb * 32 * 16 : 0;
 }
 
-template <typename T, int RB, bool VEC>
+template <typename T, int RB, int VEC>
 static wcc_status run_apply(ApplyArgs<T> q0, ApplyArgs<T>* q1, int dev, cudaStream_t st)
 {
     int warps, warps1 = 0;
-    size_t smem, smem1 = 0;
-    plan_apply(q0, RB, warps, smem);
+    plan_apply(q0, RB, warps);
     if (q1) {
-        plan_apply(*q1, RB, warps1, smem1);
+        plan_apply(*q1, RB, warps1);
         if (warps1 != warps) {          // one block size for the launch: the larger, whose other map then has more tiles a CTA
-            const int w = std::max(warps, warps1);
+            warps = std::max(warps, warps1);
             for (ApplyArgs<T>* p : {&q0, q1}) {
-                const long long tiles = (long long)((p->P + Geo<T>::TP - 1) / Geo<T>::TP);
-                p->tiles = (int)((tiles + w / p->ks - 1) / (w / p->ks));
+                const int tp = 8 * lane_positions<T>(RB);
+                const long long tiles = (long long)(((p->tap ? p->Pp : p->P) + tp - 1) / tp);
+                p->tiles = (int)((tiles + warps / p->ks - 1) / (warps / p->ks));
             }
-            if (q0.ks > 1) smem = (size_t)w * (Geo<T>::NP / 2) * RB * 512;
-            if (q1->ks > 1) smem1 = (size_t)w * (Geo<T>::NP / 2) * RB * 512;
-            warps = w;
         }
-        smem = std::max(smem, smem1);
     }
+    size_t smem = apply_smem<T>(warps, RB, q0.ks, VEC > 0);
+    if (q1) smem = std::max(smem, apply_smem<T>(warps, RB, q1->ks, VEC > 0));
     const long long items = (long long)q0.N * q0.tiles, items1 = q1 ? (long long)q1->N * q1->tiles : 0;
     if (items + items1 > 0x7FFFFFFFLL) return WCC_ERR_SHAPE;
     q0.items = (int)items;
@@ -769,10 +922,12 @@ static wcc_status run_apply(ApplyArgs<T> q0, ApplyArgs<T>* q1, int dev, cudaStre
     return launch_overlapped(apply_kernel<T, RB, VEC>, dim3((unsigned)(items + items1)), dim3((unsigned)(32 * warps)), smem, st, true, 1, q0, q1 ? *q1 : q0);
 }
 template <typename T>
-static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb, bool vec, int dev, cudaStream_t st)
+static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb, int dev, cudaStream_t st)
 {
-#define WCC_AD_APPLY(RB_) \
-    if (rb == (RB_)) return vec ? run_apply<T, RB_, true>(q0, q1, dev, st) : run_apply<T, RB_, false>(q0, q1, dev, st);
+    const int np = lane_positions<T>(rb), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
+#define WCC_AD_APPLY(RB_)                                                                      \
+    if (rb == (RB_))                                                                           \
+        return vec == 2 ? run_apply<T, RB_, 2>(q0, q1, dev, st) : vec == 1 ? run_apply<T, RB_, 1>(q0, q1, dev, st) : run_apply<T, RB_, 0>(q0, q1, dev, st);
     WCC_AD_APPLY(1) WCC_AD_APPLY(2) WCC_AD_APPLY(4) WCC_AD_APPLY(8)
 #undef WCC_AD_APPLY
     return WCC_ERR_SHAPE;
@@ -813,7 +968,7 @@ static wcc_status forward(const void* x, const void* A, const void* B, const flo
     q.src = static_cast<const T*>(x); q.w1 = static_cast<const uint4*>(w.first[0]); q.w2 = static_cast<const uint4*>(w.second[0]);
     q.scale = scale; q.ids = ids; q.base = static_cast<const T*>(base); q.dst = static_cast<T*>(y);
     q.P = P; q.N = N; q.K = Cin; q.M = Cout; q.R = R; q.status = di.status;
-    return launch_apply<T>(q, nullptr, rb, P % Geo<T>::NP == 0, di.dev, st);
+    return launch_apply<T>(q, nullptr, rb, di.dev, st);
 }
 
 template <typename T>
@@ -841,7 +996,7 @@ static wcc_status backward(const void* dy, const void* x, const void* A, const v
     u = q;
     u.src = static_cast<const T*>(x); u.w1 = static_cast<const uint4*>(w.first[1]); u.w2 = nullptr; u.scale = nullptr; u.base = nullptr;
     u.dst = nullptr; u.tap = w.tap[1]; u.K = Cin; u.M = 0;
-    if ((s = launch_apply<T>(q, params ? &u : nullptr, rb, vec, di.dev, st)) != WCC_OK || !params) return s;
+    if ((s = launch_apply<T>(q, params ? &u : nullptr, rb, di.dev, st)) != WCC_OK || !params) return s;
     GradArgs<T> h{};
     h.map[0] = static_cast<const T*>(x); h.map[1] = static_cast<const T*>(dy); h.plane[0] = w.tap[0]; h.plane[1] = w.tap[1];
     h.part = w.part; h.order = w.order; h.start = w.start; h.ids = ids; h.P = P; h.Pp = w.Pp;

@@ -1118,11 +1118,14 @@ wcc_status wcc_layernorm_bwd(const void* dy, const void* x, const float* gamma, 
     const ln::Plan p = ln::plan_of(N, C, (size_t)H * Wd, dt == WCC_BF16 ? 2 : 4, true);
     if (params && ws_bytes < ln::bwd_ws_bytes(p, N, C)) return WCC_ERR_WORKSPACE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    float* part = params ? static_cast<float*>(ws) : nullptr;
-    s = dt == WCC_BF16 ? ln::backward<__nv_bfloat16>(p, dy, x, gamma, mean, rstd, dx, part, N, C, st)
-                       : ln::backward<float>(p, dy, x, gamma, mean, rstd, dx, part, N, C, st);
-    if (s != WCC_OK || !params) return s;
-    const int rows = ln::bwd_ctas(p, N) / (p.rows ? 1 : p.q.cl);
+    // one row of partial sums is the gradients
+    const int rows = ln::bwd_rows(p, N);
+    float* part = static_cast<float*>(ws);
+    ln::Partials out{};
+    if (params) out = rows == 1 ? ln::Partials{dgamma, dbeta, 0} : ln::Partials{part, part + C, (size_t)2 * C};
+    s = dt == WCC_BF16 ? ln::backward<__nv_bfloat16>(p, dy, x, gamma, mean, rstd, dx, out, N, C, st)
+                       : ln::backward<float>(p, dy, x, gamma, mean, rstd, dx, out, N, C, st);
+    if (s != WCC_OK || !params || rows == 1) return s;
     return launch_overlapped(ln::ln_reduce, dim3((unsigned)ceil_div(2 * C, 32)), dim3(32, 32), 0, st, true, 1, part, rows, C, dgamma, dbeta);
 }
 

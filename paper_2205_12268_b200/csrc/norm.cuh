@@ -17,12 +17,14 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "tma.cuh"
 
 namespace wcc {
 namespace ln {
 
-constexpr int NT = 256;                 // threads of a CTA
+constexpr int NT = 256;                 // threads of a CTA over rows
 constexpr int WARPS = NT / 32;
+constexpr int MAX_WARPS = 16;           // of a CTA over a map
 constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // V elements of type T as they lie in memory.
@@ -45,10 +47,38 @@ struct Vec {
         else if (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     }
+    // Element i from p[i * stride]; only the first n.
+    __device__ __forceinline__ void load(const T* p, int stride, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (sizeof(T) == 4) { if (i < n) w[i % WORDS] = *reinterpret_cast<const uint32_t*>(p + i * stride); }
+            else {
+                uint32_t u = 0u;
+                if (i < n) u = *reinterpret_cast<const uint16_t*>(p + i * stride);
+                w[(i >> 1) % WORDS] |= u << (16 * (i & 1));
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T* p, int stride, int n) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) {
+                if (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i * stride) = w[i % WORDS];
+                else *reinterpret_cast<uint16_t*>(p + i * stride) = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
+            }
+    }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
         for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+    }
+    // The values are unpacked again behind this: kept unpacked across a barrier they would take twice the registers.
+    __device__ __forceinline__ void forget()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) asm volatile("" : "+r"(w[i]));
     }
     __device__ __forceinline__ float get(int i) const
     {
@@ -95,6 +125,76 @@ __device__ __forceinline__ void store_floats(float* p, const float (&f)[V])
     }
 }
 
+// Element-wise fp32 arithmetic, two at a time where there are two.
+__device__ __forceinline__ void add2(float& x0, float& x1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
+        : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void mul2(float& x0, float& x1, float a0, float a1, float b0, float b1)
+{
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
+        : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ void fma2(float& x0, float& x1, float a0, float a1, float b0, float b1, float c0, float c1)
+{
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}"
+        : "=f"(x0), "=f"(x1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+template <int V> struct F {
+    float f[V];
+    __device__ __forceinline__ F() {}
+    __device__ __forceinline__ explicit F(float s)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = s;
+    }
+};
+template <int V> __device__ __forceinline__ F<V> operator+(const F<V>& a, const F<V>& b)
+{
+    F<V> r;
+    if constexpr (V == 1) { r.f[0] = a.f[0] + b.f[0]; }
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) add2(r.f[i], r.f[i + 1], a.f[i], a.f[i + 1], b.f[i], b.f[i + 1]);
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ F<V> operator*(const F<V>& a, const F<V>& b)
+{
+    F<V> r;
+    if constexpr (V == 1) { r.f[0] = a.f[0] * b.f[0]; }
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) mul2(r.f[i], r.f[i + 1], a.f[i], a.f[i + 1], b.f[i], b.f[i + 1]);
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ F<V> fma(const F<V>& a, const F<V>& b, const F<V>& c)
+{
+    F<V> r;
+    if constexpr (V == 1) { r.f[0] = fmaf(a.f[0], b.f[0], c.f[0]); }
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2) fma2(r.f[i], r.f[i + 1], a.f[i], a.f[i + 1], b.f[i], b.f[i + 1], c.f[i], c.f[i + 1]);
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ F<V> operator-(const F<V>& a)
+{
+    F<V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.f[i] = -a.f[i];
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ F<V> floats(const Vec<T, V>& v)
+{
+    F<V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.f[i] = v.get(i);
+    return r;
+}
+
 __device__ __forceinline__ uint32_t cluster_addr(const void* p, int rank)
 {
     uint32_t a;
@@ -117,138 +217,256 @@ struct MapGeom {
     int C, Cs;                          // channels, and those of one CTA of a cluster
     int tiles, items;                   // tiles of an image, of the batch
     int segl_log2;
+    int warps, groups_log2;             // of a CTA: warps, groups of lanes
+    int pw_log2;                        // warps side by side over the positions (segl = 32)
     int cl;                             // CTAs of a cluster
 };
 
-// Sums of a tile's NS * V values per lane over all channels: over the groups of a warp, over the warps through shared memory and over the CTAs of a
-// cluster; every thread ends up with the same bits.  Calls alternate between two buffers, each of tile_floats(), so one barrier a call is
-// enough: a buffer is written again only behind the barrier of the call in between.
-__host__ __device__ inline int tile_parts(int segl_log2) { return (NT >> segl_log2) < WARPS ? (NT >> segl_log2) : WARPS; }
-__host__ __device__ inline int tile_floats(const MapGeom& q, int tpos) { return (tile_parts(q.segl_log2) + (q.cl > 1 ? 1 : 0)) * 2 * tpos; }
+// Sums of a tile's NS * V values per lane over all channels: over the groups of a warp, then over the warps, a thread per sum, through shared
+// memory, and over the CTAs of a cluster.  Every thread ends up with the same bits.  Calls alternate between two buffers for the result:
+// a neighbour of the cluster may still read the one before.
+__host__ __device__ inline int tile_floats(const MapGeom& q, int tpos) { return ((q.warps >> q.pw_log2) + 2) * 2 * tpos; }
 template <int V, int NS>
-__device__ __forceinline__ void tile_sum(float (&s)[2 * V], float* sm, const MapGeom& q, int l, int g, int buf)
+__device__ __forceinline__ void tile_sum(F<V> (&s)[NS], float* sm, const MapGeom& q, int l, int buf)
 {
-    const int segl = 1 << q.segl_log2, tpos = segl * V, parts = tile_parts(q.segl_log2);
+    const int segl = 1 << q.segl_log2, tpos = (segl << q.pw_log2) * V, parts = q.warps >> q.pw_log2;
+    if (parts == 1 && segl == 32 && q.cl == 1) return;               // a warp has all channels of its positions
     for (int o = segl; o < 32; o <<= 1) {
 #pragma unroll
-        for (int i = 0; i < NS * V; ++i) s[i] += __shfl_xor_sync(FULL, s[i], o);
-    }
-    sm += buf * tile_floats(q, tpos);
-    const int part = segl < 32 ? (int)threadIdx.x >> 5 : g;
-    if ((threadIdx.x & 31) < segl || segl >= 32) {
+        for (int j = 0; j < NS; ++j)
 #pragma unroll
-        for (int i = 0; i < NS * V; ++i) sm[(part * 2 + i / V) * tpos + l * V + i % V] = s[i];
+            for (int i = 0; i < V; ++i) s[j].f[i] += __shfl_xor_sync(FULL, s[j].f[i], o);
+    }
+    if ((int)(threadIdx.x & 31) < segl) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j) store_floats<V>(sm + ((threadIdx.x >> (5 + q.pw_log2)) * NS + j) * tpos + l * V, s[j].f);
     }
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NS * V; ++i) s[i] = sm[(i / V) * tpos + l * V + i % V];
-    for (int w = 1; w < parts; ++w) {
-#pragma unroll
-        for (int i = 0; i < NS * V; ++i) s[i] += sm[(w * 2 + i / V) * tpos + l * V + i % V];
+    float* res = sm + (parts + buf) * 2 * tpos;
+    for (int i = threadIdx.x; i < NS * tpos; i += 32 * q.warps) {
+        float a = sm[i];
+        for (int w = 1; w < parts; ++w) a += sm[w * NS * tpos + i];
+        res[i] = a;
     }
     if (q.cl > 1) {
-        float* mine = sm + parts * 2 * tpos;
-        if (g == 0) {
-#pragma unroll
-            for (int i = 0; i < NS * V; ++i) mine[(i / V) * tpos + l * V + i % V] = s[i];
-        }
         cluster_sync();
 #pragma unroll
-        for (int i = 0; i < NS * V; ++i) s[i] = 0.0f;
+        for (int j = 0; j < NS; ++j) s[j] = F<V>(0.0f);
         for (int b = 0; b < q.cl; ++b) {
-            const uint32_t a = cluster_addr(mine, b);
+            const uint32_t a = cluster_addr(res, b);
 #pragma unroll
-            for (int i = 0; i < NS * V; ++i) s[i] += cluster_ld(a + 4u * ((i / V) * tpos + l * V + i % V));
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[j].f[i] += cluster_ld(a + 4u * (j * tpos + l * V + i));
+        }
+    } else {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NS; ++j) load_floats<V>(res + j * tpos + l * V, s[j].f);
+    }
+}
+
+// Where a thread stands in a tile: column l of its positions, group g of its channels; its V positions run from `first` on, in a vector, or with
+// STR every segl-th (rows that do not start on a vector: single loads, each of them coalesced).
+template <int V, bool STR>
+struct Place {
+    int l, g, first, stride;
+    __device__ __forceinline__ explicit Place(const MapGeom& q)
+    {
+        const int lane = threadIdx.x & 31, segl = 1 << q.segl_log2, wp = (threadIdx.x >> 5) & ((1 << q.pw_log2) - 1);
+        l = wp * segl + (lane & (segl - 1));
+        g = ((int)(threadIdx.x >> (5 + q.pw_log2)) << (5 - q.segl_log2)) + (lane >> q.segl_log2);
+        first = STR ? wp * segl * V + (lane & (segl - 1)) : l * V;
+        stride = segl;
+    }
+    // how many of the V positions from p on exist
+    __device__ __forceinline__ int valid(size_t p, size_t P) const
+    {
+        if (p >= P) return 0;
+        if (!STR) return V;
+        const size_t n = (P - p + stride - 1) / stride;
+        return n < V ? (int)n : V;
+    }
+};
+template <typename T, int V, bool STR>
+__device__ __forceinline__ void load_at(Vec<T, V>& v, const T* p, int stride, int nv)
+{
+    if (STR) v.load(p, stride, nv);
+    else if (nv) v.load(p);
+}
+template <int V, bool STR>
+__device__ __forceinline__ void load_floats_at(const float* p, int stride, int nv, float (&f)[V])
+{
+    if constexpr (STR) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < nv) f[i] = p[i * stride];
+    } else if (nv) load_floats<V>(p, f);
+}
+template <int V, bool STR>
+__device__ __forceinline__ void store_floats_at(float* p, int stride, int nv, const float (&f)[V])
+{
+    if constexpr (STR) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < nv) p[i * stride] = f[i];
+    } else if (nv) store_floats<V>(p, f);
+}
+
+template <typename T, int V, int K>
+__device__ __forceinline__ void forget(Vec<T, V> (&v)[K])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k].forget();
+}
+// A position's mean and reciprocal deviation from the channels that the tile's threads hold.  A first mean, then the sums of the deviations
+// from it and of their squares: they correct it, and what it was off by enters the variance in second order only.
+template <typename T, int V, int K>
+__device__ __forceinline__ void statistics(Vec<T, V> (&v)[K], int nk, float eps, float* sm, const MapGeom& q, int l, F<V>& m, F<V>& r)
+{
+    const float inv_C = 1.0f / (float)q.C;
+    F<V> s[2], one[1];
+    one[0] = F<V>(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) one[0] = one[0] + floats(v[k]);      // (zeros where there is no channel)
+    forget<T, V, K>(v);
+    tile_sum<V, 1>(one, sm, q, l, 0);
+    m = one[0] * F<V>(inv_C);
+    s[0] = s[1] = F<V>(0.0f);
+    const F<V> neg = -m;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k < nk) {
+            const F<V> d = floats(v[k]) + neg;
+            s[0] = s[0] + d;
+            s[1] = fma(d, d, s[1]);
+        }
+    forget<T, V, K>(v);
+    tile_sum<V, 2>(s, sm, q, l, 1);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float e = s[0].f[i] * inv_C, var = fmaf(s[1].f[i], inv_C, -e * e);
+        m.f[i] += e;
+        r.f[i] = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);      // (a NaN stays one)
+    }
+}
+// y of a thread's channels, stored `step` elements apart; its k-th channel's parameters are at k * cstep.
+template <typename T, int V, int K, bool STR>
+__device__ __forceinline__ void normalise(Vec<T, V> (&v)[K], int nk, const F<V>& m, const F<V>& r, const float* pg, const float* pb, int cstep, T* py,
+                                          size_t step, int stride, int nv)
+{
+    const F<V> neg = -m;
+#pragma unroll
+    for (int k = 0; k < K; ++k, py += step)
+        if (k < nk) {
+            const float ga = pg ? pg[k * cstep] : 1.0f, be = pb ? pb[k * cstep] : 0.0f;
+            const F<V> o = fma((floats(v[k]) + neg) * r, F<V>(ga), F<V>(be));
+            v[k].set(o.f);
+            if constexpr (STR) v[k].store(py, stride, nv);
+            else v[k].store(py);
+        }
+}
+// The sums over the channels that a gradient needs (s: of g and of g xh), and this tile's share of the parameters' gradients.
+template <typename T, int V, int K>
+__device__ __forceinline__ void gradient_sums(const Vec<T, V> (&vx)[K], const Vec<T, V> (&vd)[K], int nk, const F<V>& neg, const F<V>& r, const float* pg,
+                                              int cstep, F<V> (&s)[2], float (&dg)[K], float (&db)[K])
+{
+    s[0] = s[1] = F<V>(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (k < nk) {
+            const F<V> d = floats(vd[k]), xh = (floats(vx[k]) + neg) * r, gg = pg ? d * F<V>(pg[k * cstep]) : d;
+            s[0] = s[0] + gg;
+            s[1] = fma(gg, xh, s[1]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) { dg[k] = fmaf(d.f[i], xh.f[i], dg[k]); db[k] += d.f[i]; }
+        }
+}
+template <typename T, int V, int K, bool STR>
+__device__ __forceinline__ void gradient(Vec<T, V> (&vx)[K], const Vec<T, V> (&vd)[K], int nk, const F<V>& neg, const F<V>& r, const float* pg, int cstep,
+                                         const F<V> (&s)[2], float inv_C, T* po, size_t step, int stride, int nv)
+{
+    const F<V> c1 = s[0] * F<V>(-inv_C), c2 = s[1] * F<V>(-inv_C);
+#pragma unroll
+    for (int k = 0; k < K; ++k, po += step)
+        if (k < nk) {
+            const F<V> xh = (floats(vx[k]) + neg) * r;
+            const F<V> o = r * fma(xh, c2, fma(floats(vd[k]), F<V>(pg ? pg[k * cstep] : 1.0f), c1));
+            vx[k].set(o.f);
+            if constexpr (STR) vx[k].store(po, stride, nv);
+            else vx[k].store(po);
+        }
+}
+// Where the sums of the parameters' gradients go: rows of partial sums [row][2][C], or, if there is one row only, the gradients themselves.
+struct Partials {
+    float *g, *b;                       // either may be NULL
+    size_t pitch;
+};
+// The lanes of a channel add up and write row `row`; c: the thread's first channel.
+template <int K>
+__device__ __forceinline__ void store_partials(float (&dg)[K], float (&db)[K], int nk, int segl, int cstep, const Partials& out, int C, int row, int c)
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        for (int o = 1; o < segl; o <<= 1) { dg[k] += __shfl_xor_sync(FULL, dg[k], o); db[k] += __shfl_xor_sync(FULL, db[k], o); }
+        if ((threadIdx.x & (segl - 1)) == 0 && k < nk) {
+            if (out.g) out.g[row * out.pitch + c + k * cstep] = dg[k];
+            if (out.b) out.b[row * out.pitch + c + k * cstep] = db[k];
         }
     }
 }
 
 // ---- forward, maps --------------------------------------------------------------------------
-template <typename T, int V, int K>
-__global__ void __launch_bounds__(NT) ln_fwd_map(const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
-                                                 float* __restrict__ mean_out, float* __restrict__ rstd_out, MapGeom q, float eps)
+template <typename T, int V, int K, bool STR>
+__global__ void __launch_bounds__(32 * MAX_WARPS, K * Vec<T, V>::WORDS <= 16 ? 2 : 1) ln_fwd_map(const T* x, const float* __restrict__ gamma,
+                                                                                                 const float* __restrict__ beta, T* y,
+                                                                                                 float* __restrict__ mean, float* __restrict__ rstd,
+                                                                                                 MapGeom q, float eps)
 {
     extern __shared__ float sm[];
-    const int tid = threadIdx.x;
-    const int segl = 1 << q.segl_log2, tpos = segl * V, G = NT >> q.segl_log2;
-    const int l = tid & (segl - 1), g = tid >> q.segl_log2;
+    const Place<V, STR> w(q);
     const int item = blockIdx.x / q.cl, crank = blockIdx.x - item * q.cl;
     const int n = item / q.tiles;
-    const size_t p = (size_t)(item - n * q.tiles) * tpos + (size_t)l * V;
-    const bool in = p < q.P;
-    const int c0 = crank * q.Cs, c1 = min(q.C, c0 + q.Cs);
-    const size_t at = ((size_t)n * q.C + c0 + g) * q.P + p, step = (size_t)G * q.P;
+    const size_t p = (size_t)(item - n * q.tiles) * ((size_t)V << (q.segl_log2 + q.pw_log2)) + w.first;
+    const int nv = w.valid(p, q.P);
+    const int c = crank * q.Cs + w.g, left = min(q.C, crank * q.Cs + q.Cs) - c;      // this thread's first channel, and how many there are from it on
+    const int nk = (left + (1 << q.groups_log2) - 1) >> q.groups_log2;
+    const size_t at = ((size_t)n * q.C + c) * q.P + p, step = q.P << q.groups_log2;
 
     Vec<T, V> v[K];
+    const T* px = x + at;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k, px += step) {
         v[k].zero();
-        if (in && c0 + g + k * G < c1) v[k].load(x + at + k * step);
+        if (k < nk) load_at<T, V, STR>(v[k], px, w.stride, nv);
     }
-
-    // a first mean, then the sums of the deviations from it and of their squares: they correct it, and what it was off by enters the
-    // variance in second order only
-    const float inv_C = 1.0f / (float)q.C;
-    float m[V], s[2 * V];
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) s[i] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] += v[k].get(i);              // (zeros where there is no channel)
-    tile_sum<V, 1>(s, sm, q, l, g, 0);
-#pragma unroll
-    for (int i = 0; i < V; ++i) { m[i] = s[i] * inv_C; s[i] = 0.0f; }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (c0 + g + k * G < c1) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = v[k].get(i) - m[i]; s[i] += d; s[V + i] = fmaf(d, d, s[V + i]); }
-        }
-    tile_sum<V, 2>(s, sm, q, l, g, 1);
+    F<V> m, r;
+    statistics<T, V, K>(v, nk, eps, sm, q, w.l, m, r);
     if (q.cl > 1) cluster_sync();       // nobody leaves while a neighbour reads
-    float r[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float e = s[i] * inv_C;
-        m[i] += e;
-        const float var = fmaf(s[V + i], inv_C, -e * e);
-        r[i] = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);        // (a NaN stays one)
+    if (w.g == 0 && crank == 0) {
+        if (mean) store_floats_at<V, STR>(mean + (size_t)n * q.P + p, w.stride, nv, m.f);
+        if (rstd) store_floats_at<V, STR>(rstd + (size_t)n * q.P + p, w.stride, nv, r.f);
     }
-    if (!in) return;
-    if (g == 0 && crank == 0) {
-        if (mean_out) store_floats<V>(mean_out + (size_t)n * q.P + p, m);
-        if (rstd_out) store_floats<V>(rstd_out + (size_t)n * q.P + p, r);
-    }
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int c = c0 + g + k * G;
-        if (c < c1) {
-            const float ga = gamma ? gamma[c] : 1.0f, be = beta ? beta[c] : 0.0f;
-            float f[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = fmaf((v[k].get(i) - m[i]) * r[i], ga, be);
-            v[k].set(f);
-            v[k].store(y + at + k * step);
-        }
-    }
+    if (STR || nv) normalise<T, V, K, STR>(v, nk, m, r, gamma ? gamma + c : nullptr, beta ? beta + c : nullptr, 1 << q.groups_log2, y + at, step, w.stride, nv);
 }
 
 // ---- backward, maps -------------------------------------------------------------------------
 // Persistent: a thread keeps its channels from tile to tile, so the sums of the parameters' gradients stay in its registers; at the
 // end each cluster writes one row of partial sums and ln_reduce adds the rows in a fixed order.
-template <typename T, int V, int K>
-__global__ void __launch_bounds__(NT) ln_bwd_map(const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
-                                                 const float* __restrict__ rstd, T* dx, float* __restrict__ part_out, MapGeom q)
+template <typename T, int V, int K, bool STR>
+__global__ void __launch_bounds__(32 * MAX_WARPS, K * Vec<T, V>::WORDS <= 8 ? 2 : 1) ln_bwd_map(const T* dy, const T* x, const float* __restrict__ gamma,
+                                                                                                const float* __restrict__ mean,
+                                                                                                const float* __restrict__ rstd, T* dx,
+                                                                                                Partials out, MapGeom q)
 {
     extern __shared__ float sm[];
-    const int tid = threadIdx.x;
-    const int segl = 1 << q.segl_log2, tpos = segl * V, G = NT >> q.segl_log2;       // segl <= 32
-    const int l = tid & (segl - 1), g = tid >> q.segl_log2;
+    const Place<V, STR> w(q);
     const int cid = blockIdx.x / q.cl, clusters = gridDim.x / q.cl, crank = blockIdx.x - cid * q.cl;
-    const int c0 = crank * q.Cs, c1 = min(q.C, c0 + q.Cs);
-    const size_t step = (size_t)G * q.P;
+    const int c = crank * q.Cs + w.g, left = min(q.C, crank * q.Cs + q.Cs) - c;
+    const int nk = (left + (1 << q.groups_log2) - 1) >> q.groups_log2, cstep = 1 << q.groups_log2;
+    const size_t step = q.P << q.groups_log2;
     const float inv_C = 1.0f / (float)q.C;
+    const float* pg = gamma ? gamma + c : nullptr;
 
     float dg[K], db[K];
 #pragma unroll
@@ -256,64 +474,165 @@ __global__ void __launch_bounds__(NT) ln_bwd_map(const T* dy, const T* x, const 
     int buf = 0;
     for (int item = cid; item < q.items; item += clusters, buf ^= 1) {
         const int n = item / q.tiles;
-        const size_t p = (size_t)(item - n * q.tiles) * tpos + (size_t)l * V;
-        const bool in = p < q.P;
-        const size_t at = ((size_t)n * q.C + c0 + g) * q.P + p;
+        const size_t p = (size_t)(item - n * q.tiles) * ((size_t)V << (q.segl_log2 + q.pw_log2)) + w.first;
+        const int nv = w.valid(p, q.P);
+        const size_t at = ((size_t)n * q.C + c) * q.P + p;
         Vec<T, V> vx[K], vd[K];
+        const T *px = x + at, *pd = dy + at;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
+        for (int k = 0; k < K; ++k, px += step, pd += step) {
             vx[k].zero(); vd[k].zero();
-            if (in && c0 + g + k * G < c1) { vx[k].load(x + at + k * step); vd[k].load(dy + at + k * step); }
+            if (k < nk) { load_at<T, V, STR>(vx[k], px, w.stride, nv); load_at<T, V, STR>(vd[k], pd, w.stride, nv); }
         }
-        float mu[V], r[V], s[2 * V];      // s: sums of g and of g xh
-#pragma unroll
-        for (int i = 0; i < V; ++i) { mu[i] = 0.0f; r[i] = 0.0f; s[i] = 0.0f; s[V + i] = 0.0f; }
-        if (in) { load_floats<V>(mean + (size_t)n * q.P + p, mu); load_floats<V>(rstd + (size_t)n * q.P + p, r); }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int c = c0 + g + k * G;
-            if (c < c1) {
-                const float ga = gamma ? gamma[c] : 1.0f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = vd[k].get(i), xh = (vx[k].get(i) - mu[i]) * r[i], gg = d * ga;
-                    dg[k] = fmaf(d, xh, dg[k]);
-                    db[k] += d;
-                    s[i] += gg;
-                    s[V + i] = fmaf(gg, xh, s[V + i]);
-                }
-            }
-        }
-        tile_sum<V, 2>(s, sm, q, l, g, buf);
-        if (in) {
-#pragma unroll
-            for (int i = 0; i < 2 * V; ++i) s[i] *= inv_C;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int c = c0 + g + k * G;
-                if (c < c1) {
-                    const float ga = gamma ? gamma[c] : 1.0f;
-                    float f[V];
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float xh = (vx[k].get(i) - mu[i]) * r[i];
-                        f[i] = r[i] * (fmaf(vd[k].get(i), ga, -s[i]) - xh * s[V + i]);
-                    }
-                    vx[k].set(f);
-                    vx[k].store(dx + at + k * step);
-                }
-            }
-        }
+        F<V> neg(0.0f), r(0.0f), s[2];    // s: sums of g and of g xh
+        load_floats_at<V, STR>(mean + (size_t)n * q.P + p, w.stride, nv, neg.f);
+        load_floats_at<V, STR>(rstd + (size_t)n * q.P + p, w.stride, nv, r.f);
+        neg = -neg;
+        gradient_sums<T, V, K>(vx, vd, nk, neg, r, pg, cstep, s, dg, db);
+        forget<T, V, K>(vx);
+        forget<T, V, K>(vd);
+        tile_sum<V, 2>(s, sm, q, w.l, buf);
+        if (STR || nv) gradient<T, V, K, STR>(vx, vd, nk, neg, r, pg, cstep, s, inv_C, dx + at, step, w.stride, nv);
     }
     if (q.cl > 1) cluster_sync();       // nobody leaves while a neighbour reads
     pdl_launch();
-    if (!part_out) return;
-    float* row = part_out + (size_t)cid * 2 * q.C;
+    const int wp = (threadIdx.x >> 5) & ((1 << q.pw_log2) - 1);
+    store_partials<K>(dg, db, nk, 1 << q.segl_log2, cstep, out, q.C, (cid << q.pw_log2) + wp, c);
+}
+
+// ---- large maps: tiles through a ring in shared memory -----------------------------------------
+// The same arithmetic on tiles that TMA copies in and out, so that the copies of the next tiles and of the last one run while a tile is
+// worked on, whatever the registers hold.  A stage is [rows][TP] of x (backward: then the same of dy), rows = channels in boxes of at most 256; the
+// result takes x's place.  Persistent CTAs; thread 0 issues the copies.  A stage is loaded again when its store has read it, which thread 0
+// waits for one tile later.
+constexpr int STAGES = 3;
+struct RingGeom {
+    MapGeom q;
+    int boxes, box_rows, tp;            // rows of a stage = boxes * box_rows, positions of a tile
+    uint32_t half;                      // bytes of x's part of a stage
+};
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+template <typename T, int V, int K, bool BWD>
+__global__ void __launch_bounds__(32 * MAX_WARPS, 1) ln_ring(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmd,
+                                                             const __grid_constant__ CUtensorMap tmo, const float* __restrict__ gamma,
+                                                             const float* __restrict__ beta, float* __restrict__ mean, float* __restrict__ rstd,
+                                                             Partials out, RingGeom h, float eps, int* __restrict__ status)
+{
+    extern __shared__ uint8_t ring_raw[];
+    __shared__ uint64_t full[STAGES];
+    const MapGeom& q = h.q;
+    uint8_t* ring = ring_raw + ((128u - (tc::smem_u32(ring_raw) & 127u)) & 127u);
+    const uint32_t stage_bytes = h.half * (BWD ? 2 : 1);
+    float* sm = reinterpret_cast<float*>(ring + (size_t)STAGES * stage_bytes);
+    float* par = sm + tile_floats(q, h.tp);                             // gamma [C], beta [C]
+    for (int c = threadIdx.x; c < q.C; c += 32 * q.warps) {
+        par[c] = gamma ? gamma[c] : 1.0f;
+        if (!BWD) par[q.C + c] = beta ? beta[c] : 0.0f;
+    }
+    const int segl = 1 << q.segl_log2;
+    const int l = threadIdx.x & (segl - 1), g = threadIdx.x >> q.segl_log2;
+    const int cstep = 1 << q.groups_log2, left = q.C - g, nk = (left + cstep - 1) >> q.groups_log2;
+    const size_t step = (size_t)h.tp << q.groups_log2;
+    const float inv_C = 1.0f / (float)q.C;
+
+    auto issue = [&](int i) {           // (thread 0) tile i of this CTA into its stage
+        const long long item = (long long)blockIdx.x + (long long)i * gridDim.x;
+        if (item >= q.items) return;
+        const int n = (int)item / q.tiles, p = ((int)item - n * q.tiles) * h.tp;
+        const uint32_t dst = tc::smem_u32(ring) + (uint32_t)(i % STAGES) * stage_bytes, bar = tc::smem_u32(&full[i % STAGES]);
+        tc::mbar_expect_tx(bar, stage_bytes);
+        const uint32_t box = (uint32_t)(h.box_rows * h.tp * (int)sizeof(T));
+        for (int b = 0; b < h.boxes; ++b) {
+            tma_load_3d(dst + b * box, &tmx, p, b * h.box_rows, n, bar);
+            if (BWD) tma_load_3d(dst + h.half + b * box, &tmd, p, b * h.box_rows, n, bar);
+        }
+    };
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) tc::mbar_init(tc::smem_u32(&full[s]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < STAGES; ++i) issue(i);
+    }
+    __syncthreads();
+
+    float dg[BWD ? K : 1], db[BWD ? K : 1];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        for (int o = 1; o < segl; o <<= 1) { dg[k] += __shfl_xor_sync(FULL, dg[k], o); db[k] += __shfl_xor_sync(FULL, db[k], o); }
-        const int c = c0 + g + k * G;
-        if (l == 0 && c < c1) { row[c] = dg[k]; row[q.C + c] = db[k]; }
+    for (int k = 0; k < (BWD ? K : 1); ++k) { dg[k] = 0.0f; db[k] = 0.0f; }
+    bool ok = true;
+    int i = 0;
+    for (int item = blockIdx.x; item < q.items; item += gridDim.x, ++i) {
+        const int n = item / q.tiles;
+        const size_t p = (size_t)(item - n * q.tiles) * h.tp + (size_t)l * V;
+        const bool in = p < q.P;
+        const size_t at = (size_t)n * q.P + p;
+        F<V> m(0.0f), r(0.0f);
+        if (BWD && in) { load_floats<V>(mean + at, m.f); load_floats<V>(rstd + at, r.f); }
+        ok = tc::mbar_wait(tc::smem_u32(&full[i % STAGES]), (uint32_t)(i / STAGES) & 1u);
+        if (__syncthreads_or(!ok)) { ok = false; break; }
+        T* tile = reinterpret_cast<T*>(ring + (size_t)(i % STAGES) * stage_bytes) + (size_t)g * h.tp + l * V;
+        Vec<T, V> v[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k].zero();
+            if (k < nk) v[k].load(tile + k * step);
+        }
+        if constexpr (BWD) {
+            Vec<T, V> vd[K];
+            const T* td = tile + h.half / sizeof(T);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                vd[k].zero();
+                if (k < nk) vd[k].load(td + k * step);
+            }
+            F<V> s[2];
+            const F<V> neg = -m;
+            const float* pg = par + g;
+            gradient_sums<T, V, K>(v, vd, nk, neg, r, pg, cstep, s, dg, db);
+            forget<T, V, K>(v);
+            forget<T, V, K>(vd);
+            tile_sum<V, 2>(s, sm, q, l, i & 1);
+            gradient<T, V, K, false>(v, vd, nk, neg, r, pg, cstep, s, inv_C, tile, step, 0, V);
+        } else {
+            statistics<T, V, K>(v, nk, eps, sm, q, l, m, r);
+            if (g == 0 && in) {
+                if (mean) store_floats<V>(mean + at, m.f);
+                if (rstd) store_floats<V>(rstd + at, r.f);
+            }
+            normalise<T, V, K, false>(v, nk, m, r, par + g, par + q.C + g, cstep, tile, step, 0, V);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const uint32_t src = tc::smem_u32(ring) + (uint32_t)(i % STAGES) * stage_bytes, box = (uint32_t)(h.box_rows * h.tp * (int)sizeof(T));
+            const int p0 = (item - n * q.tiles) * h.tp;
+            for (int b = 0; b < h.boxes; ++b) tma_store_3d(&tmo, src + b * box, p0, b * h.box_rows, n);
+            store_commit();
+            store_wait_read<1>();       // the store of the tile before has left its stage
+            if (i >= 1) issue(i - 1 + STAGES);
+        }
+    }
+    if (!ok) {
+        // let the copies that are under way land before the shared memory goes away
+        if (threadIdx.x == 0) atomicExch(status, (int)WCC_ERR_TIMEOUT);
+        for (int w = 0; w < 2000; ++w) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) store_wait_all();
+    if constexpr (BWD) {
+        pdl_launch();
+        store_partials<K>(dg, db, nk, segl, cstep, out, q.C, blockIdx.x, g);
     }
 }
 
@@ -397,9 +716,9 @@ __global__ void __launch_bounds__(NT) ln_fwd_rows(const T* x, const float* __res
 
 template <typename T, int V, int K, int TR>
 __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
-                                                  const float* __restrict__ rstd, T* dx, float* __restrict__ part_out, int N, int C)
+                                                  const float* __restrict__ rstd, T* dx, Partials out, int N, int C)
 {
-    extern __shared__ float acc_sm[];   // TR < 256: [2][C], the sums of the CTA's row groups
+    extern __shared__ float acc_sm[];   // TR < 256: [2][C], the sums of the CTA's warps
     __shared__ float2 sm[WARPS];
     const int t = threadIdx.x % TR, sub = threadIdx.x / TR;
     constexpr int R = NT / TR;
@@ -464,11 +783,21 @@ __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const
         }
     }
     pdl_launch();
-    if (!part_out) return;
-    float* row = part_out + (size_t)blockIdx.x * 2 * C;
-    // the row groups add up one after the other: a fixed order
-    for (int w = 0; w < R; ++w) {
-        if (sub == w) {
+    if (!out.g && !out.b) return;
+    // the row groups of a warp add up, then the warps one after the other: a fixed order
+#pragma unroll
+    for (int o = TR; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                dg[k][i] += __shfl_xor_sync(FULL, dg[k][i], o);
+                db[k][i] += __shfl_xor_sync(FULL, db[k][i], o);
+            }
+    constexpr int TURNS = TR < NT ? WARPS : 1;
+    const size_t row = blockIdx.x * out.pitch;
+    for (int w = 0; w < TURNS; ++w) {
+        if (TURNS == 1 || ((int)(threadIdx.x >> 5) == w && (int)(threadIdx.x & 31) < TR)) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int c = (t + k * TR) * V;
@@ -476,14 +805,17 @@ __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         float a = dg[k][i], b = db[k][i];
-                        if (R > 1 && w > 0) { a += acc_sm[c + i]; b += acc_sm[C + c + i]; }
-                        if (R > 1 && w + 1 < R) { acc_sm[c + i] = a; acc_sm[C + c + i] = b; }
-                        else { row[c + i] = a; row[C + c + i] = b; }
+                        if (w > 0) { a += acc_sm[c + i]; b += acc_sm[C + c + i]; }
+                        if (w + 1 < TURNS) { acc_sm[c + i] = a; acc_sm[C + c + i] = b; }
+                        else {
+                            if (out.g) out.g[row + c + i] = a;
+                            if (out.b) out.b[row + c + i] = b;
+                        }
                     }
                 }
             }
         }
-        if (R > 1) __syncthreads();
+        if (TURNS > 1) __syncthreads();
     }
 }
 
@@ -511,12 +843,19 @@ __global__ void __launch_bounds__(1024) ln_reduce(const float* __restrict__ part
 // ---- plans and launches -----------------------------------------------------------------------
 struct Plan {
     bool rows;
-    int V, K, TR;                       // TR: rows only
+    int es, V, K, TR;                       // TR: rows only
+    bool ring, strided;
     MapGeom q;
+    RingGeom h;                         // ring only; h.q == q
+    int ctas;                           // ring only: CTAs of the launch
     size_t smem;
 };
 
-// Elements of a vector: 16 bytes while rows of `len` elements start on that.
+#ifndef LN_KF
+#define LN_KF 16
+#define LN_KB 8
+#endif
+// Elements of a vector
 inline int vec_elems(size_t len, int es)
 {
     int v = 16 / es;
@@ -524,10 +863,57 @@ inline int vec_elems(size_t len, int es)
     return v;
 }
 
+#ifndef LN_RING_TILE
+#define LN_RING_TILE 32768
+#define LN_RING_VB 8
+#define LN_RING_MIN 2
+#endif
+// The ring, where rows start on 16 bytes and there are tiles enough to keep it busy.
+inline bool ring_plan(Plan& p, int N, int C, size_t P, int es, bool bwd)
+{
+    if (P * es % 16 != 0 || P * es < 64 || C < 8) return false;
+    int row = 512;                                                       // bytes of a tile's row
+    const int most = LN_RING_TILE >> (bwd ? 1 : 0);
+    while (row > 64 && (long long)row * C > most) row /= 2;
+    while (row > 64 && (size_t)row > P * es) row /= 2;
+    RingGeom& h = p.h;
+    h.boxes = ceil_div(C, 256);
+    h.box_rows = ceil_div(ceil_div(C, h.boxes), 2) * 2;                  // boxes start on 128 bytes of shared memory
+    h.tp = row / es;
+    h.half = (uint32_t)(h.boxes * h.box_rows * row);
+    if (h.half > 65536u >> (bwd ? 1 : 0)) return false;
+    const size_t tiles = (P + h.tp - 1) / h.tp;
+    if (tiles * N > 0x7FFFFFFFull) return false;
+    const int vb = std::min(row / 4, LN_RING_VB);
+    p.V = vb / es;
+    int lg = 0;
+    while ((vb << lg) < row && lg < 5) ++lg;
+    if ((vb << lg) != row) { p.V *= 2; if (p.V * es > 16) return false; }
+    int warps = 4;
+    const int kmax = (bwd ? 16 : 32) / (p.V * es / 4);
+    while (warps < MAX_WARPS && ceil_div(C, warps << (5 - lg)) > kmax) warps *= 2;
+    const int k = ceil_div(C, warps << (5 - lg));
+    if (k > kmax) return false;
+    p.K = k <= 2 ? 2 : k <= 4 ? 4 : k <= 8 ? 8 : 16;
+    MapGeom& q = p.q;
+    q.P = P; q.C = C; q.Cs = C; q.cl = 1; q.segl_log2 = lg; q.warps = warps;
+    q.groups_log2 = 5 - lg + (warps == 4 ? 2 : warps == 8 ? 3 : 4);
+    q.tiles = (int)tiles;
+    q.items = N * q.tiles;
+    h.q = q;
+    p.smem = 128 + (size_t)STAGES * h.half * (bwd ? 2 : 1) + (size_t)tile_floats(q, h.tp) * 4 + (size_t)(bwd ? 1 : 2) * C * 4;
+    const int per_sm = std::max(1, std::min((int)(225 * 1024 / (p.smem + 1200)), 512 / (32 * warps)));
+    p.ctas = std::min(q.items, per_sm * B200_SMS);
+    if (q.items < LN_RING_MIN * p.ctas) return false;
+    p.ring = true;
+    return true;
+}
+
 // Registers: a thread of the forward pass holds K vectors, one of the backward pass 2 K (and 2 K sums).
 inline Plan plan_of(int N, int C, size_t P, int es, bool bwd)
 {
     Plan p{};
+    p.es = es;
     if (P == 1) {
         p.rows = true;
         p.V = C % (16 / es) == 0 ? 16 / es : 1;
@@ -539,41 +925,52 @@ inline Plan plan_of(int N, int C, size_t P, int es, bool bwd)
         p.smem = bwd && p.TR < NT ? (size_t)2 * C * 4 : 0;
         return p;
     }
+    if (ring_plan(p, N, C, P, es, bwd)) return p;
+    // single loads where rows start on no vector (a vector of two bf16 is hardly better)
     p.V = vec_elems(P, es);
-    const int kmax = bwd ? (p.V * es <= 4 ? 16 : 8) : (p.V * es <= 4 ? 32 : 16), kgood = 8;
+    p.strided = p.V * es < (es == 2 ? 4 : 8);
+    if (p.strided) p.V = 16 / es;
+    const int words = p.V * es / 4, kmax = (bwd ? 16 : 32) / words, kgood = (bwd ? LN_KB : LN_KF) / words;
     int lg = 0;
-    const int top = bwd ? 5 : 8;
-    while (lg < top && ((size_t)p.V << lg) < P) ++lg;
-    // the widest segments that leave K at kgood; narrower down to a sector for more tiles than the GPU has room for at once, or for K
-    auto K_of = [&](int s, int c) { return ceil_div(c, NT >> s); };
+    while (lg < 5 && ((size_t)p.V << lg) < P) ++lg;
     auto tiles_of = [&](int s) { return (P + ((size_t)p.V << s) - 1) / ((size_t)p.V << s); };
-    const int sector = [&] { int s = 0; while ((p.V << s) * es < 32 && s < lg) ++s; return s; }();
-    while (lg > sector && K_of(lg, C) > kgood) --lg;
-    while (lg > sector && (size_t)N * tiles_of(lg) < 2 * B200_SMS) --lg;
+    auto K_of = [&](int s, int w, int c) { return ceil_div(c, w << (5 - s)); };
+    const int sector = [&] { int s = 0; while ((p.strided ? es << s : (p.V << s) * es) < 32 && s < lg) ++s; return s; }();
     int cl = 1;
-    while (K_of(lg, ceil_div(C, cl)) > kmax && cl < 8) cl *= 2;
-    while (K_of(lg, ceil_div(C, cl)) > kmax) --lg;
+    while (lg > sector && K_of(lg, MAX_WARPS, C) > kmax) --lg;
+    while (lg > sector && (size_t)N * tiles_of(lg) < 2 * B200_SMS) --lg;
+    while (K_of(lg, MAX_WARPS, ceil_div(C, cl)) > kmax && cl < 8) cl *= 2;
+    while (K_of(lg, MAX_WARPS, ceil_div(C, cl)) > kmax) --lg;
+    int warps = 1;
+    while (warps < MAX_WARPS && K_of(lg, warps, ceil_div(C, cl)) > kgood) warps *= 2;
     p.q.P = P; p.q.C = C; p.q.cl = cl; p.q.Cs = ceil_div(C, cl); p.q.segl_log2 = lg;
-    p.q.tiles = (int)tiles_of(lg);
-    p.q.items = N * p.q.tiles;
-    const int k = K_of(lg, p.q.Cs);
+    p.q.groups_log2 = 5 - lg;
+    for (int w = 1; w < warps; w *= 2) ++p.q.groups_log2;
+    const int k = K_of(lg, warps, p.q.Cs);
     p.K = k <= 2 ? 2 : k <= 4 ? 4 : k <= 8 ? 8 : k <= 16 ? 16 : 32;
+    // few channels: warps side by side
+    while (lg == 5 && warps < 8 && (size_t)N * tiles_of(lg + p.q.pw_log2 + 1) >= 2 * B200_SMS) { ++p.q.pw_log2; warps *= 2; }
+    while (warps < 4 && lg < 5) { warps *= 2; ++p.q.groups_log2; }
+    p.q.warps = warps;
+    p.q.tiles = (int)tiles_of(lg + p.q.pw_log2);
+    p.q.items = N * p.q.tiles;
+    lg += p.q.pw_log2;
     const int tpos = p.V << lg;
-    p.smem = (size_t)2 * tile_floats(p.q, tpos) * 4;
+    p.smem = (size_t)tile_floats(p.q, tpos) * 4;
     return p;
 }
 
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool STR>
 static wcc_status fwd_map(const Plan& p, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, float eps, cudaStream_t st)
 {
-    return launch_overlapped(ln_fwd_map<T, V, K>, dim3((unsigned)(p.q.items * p.q.cl)), dim3(NT), p.smem, st, false, p.q.cl,
+    return launch_overlapped(ln_fwd_map<T, V, K, STR>, dim3((unsigned)(p.q.items * p.q.cl)), dim3((unsigned)(32 * p.q.warps)), p.smem, st, false, p.q.cl,
                              static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, p.q, eps);
 }
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool STR>
 static wcc_status bwd_map(const Plan& p, int ctas, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
-                          float* part, cudaStream_t st)
+                          const Partials& part, cudaStream_t st)
 {
-    return launch_overlapped(ln_bwd_map<T, V, K>, dim3((unsigned)ctas), dim3(NT), p.smem, st, false, p.q.cl, static_cast<const T*>(dy),
+    return launch_overlapped(ln_bwd_map<T, V, K, STR>, dim3((unsigned)ctas), dim3((unsigned)(32 * p.q.warps)), p.smem, st, false, p.q.cl, static_cast<const T*>(dy),
                              static_cast<const T*>(x), gamma, mean, rstd, static_cast<T*>(dx), part, p.q);
 }
 template <typename T, int V, int K, int TR>
@@ -584,26 +981,63 @@ static wcc_status fwd_rows(const void* x, const float* gamma, const float* beta,
 }
 template <typename T, int V, int K, int TR>
 static wcc_status bwd_rows(const Plan& p, int ctas, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
-                           float* part, int N, int C, cudaStream_t st)
+                           const Partials& part, int N, int C, cudaStream_t st)
 {
     return launch_overlapped(ln_bwd_rows<T, V, K, TR>, dim3((unsigned)ctas), dim3(NT), p.smem, st, false, 1, static_cast<const T*>(dy),
                              static_cast<const T*>(x), gamma, mean, rstd, static_cast<T*>(dx), part, N, C);
 }
 
+inline bool ring_map(CUtensorMap* tm, const void* ptr, int es, const Plan& p, int N)
+{
+    tc::EncodeTiledFn fn = tc::encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)p.q.P, (cuuint64_t)p.q.C, (cuuint64_t)N};
+    cuuint64_t strides[2] = {(cuuint64_t)p.q.P * es, (cuuint64_t)p.q.P * p.q.C * es};
+    cuuint32_t box[3] = {(cuuint32_t)p.h.tp, (cuuint32_t)p.h.box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(tm, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+template <typename T, int V, int K, bool BWD>
+static wcc_status run_ring(const Plan& p, const void* x, const void* dy, void* out, const float* gamma, const float* beta, float* mean, float* rstd,
+                           const Partials& part, int N, float eps, cudaStream_t st)
+{
+    CUtensorMap tx, td, to;
+    if (!ring_map(&tx, x, sizeof(T), p, N) || !ring_map(&td, BWD ? dy : x, sizeof(T), p, N) || !ring_map(&to, out, sizeof(T), p, N)) return WCC_ERR_CUDA;
+    DeviceInfo di;
+    wcc_status s = device_info(di);
+    if (s != WCC_OK) return s;
+    if ((s = allow_smem<ln_ring<T, V, K, BWD>>(di.dev, (int)p.smem)) != WCC_OK) return s;
+    return launch_overlapped(ln_ring<T, V, K, BWD>, dim3((unsigned)p.ctas), dim3((unsigned)(32 * p.q.warps)), p.smem, st, false, 1, tx, td, to, gamma, beta,
+                             mean, rstd, part, p.h, eps, di.status);
+}
+template <typename T, bool BWD>
+static wcc_status ring(const Plan& p, const void* x, const void* dy, void* out, const float* gamma, const float* beta, float* mean, float* rstd,
+                       const Partials& part, int N, float eps, cudaStream_t st)
+{
+    constexpr int V4 = 4 / (int)sizeof(T);
+#define WCC_LN_RING(V_, K_) \
+    if (p.V == (V_) && p.K == (K_)) return run_ring<T, V_, K_, BWD>(p, x, dy, out, gamma, beta, mean, rstd, part, N, eps, st);
+    WCC_LN_RING(2 * V4, 2) WCC_LN_RING(2 * V4, 4) WCC_LN_RING(2 * V4, 8) WCC_LN_RING(4 * V4, 2) WCC_LN_RING(4 * V4, 4)
+    if constexpr (!BWD) { WCC_LN_RING(2 * V4, 16) WCC_LN_RING(4 * V4, 8) }
+#undef WCC_LN_RING
+    return WCC_ERR_SHAPE;
+}
+
 // CTAs of the backward pass = rows of partial sums (times the cluster): as many as run at once.
 inline int bwd_ctas(const Plan& p, int N)
 {
+    if (p.ring) return p.ctas;
     if (p.rows) {
         const long long want = ((long long)N * p.TR + NT - 1) / NT;
         return (int)(want < 2 * B200_SMS ? want : 2 * B200_SMS);
     }
-    const int room = 2 * B200_SMS / p.q.cl;
+    const int words = p.K * std::max(1, p.V * p.es / 4), room = B200_SMS * std::min(16, (words <= 8 ? 1024 : 512) / (32 * p.q.warps)) / p.q.cl;
     return (p.q.items < room ? p.q.items : room) * p.q.cl;
 }
-inline size_t bwd_ws_bytes(const Plan& p, int N, int C)
-{
-    return align_up((size_t)bwd_ctas(p, N) / (p.rows ? 1 : p.q.cl) * 2 * C * 4, 256);
-}
+// Rows of partial sums.
+inline int bwd_rows(const Plan& p, int N) { return p.rows || p.ring ? bwd_ctas(p, N) : (bwd_ctas(p, N) / p.q.cl) << p.q.pw_log2; }
+inline size_t bwd_ws_bytes(const Plan& p, int N, int C) { return align_up((size_t)bwd_rows(p, N) * 2 * C * 4, 256); }
 
 template <typename T>
 static wcc_status forward(const Plan& p, const void* x, const float* gamma, const float* beta, void* y, float* mean, float* rstd, int N, int C, float eps,
@@ -618,19 +1052,21 @@ static wcc_status forward(const Plan& p, const void* x, const float* gamma, cons
 #undef WCC_LN_ROWS
         return WCC_ERR_SHAPE;
     }
-#define WCC_LN_MAP(V_, K_) \
-    if (p.V == (V_) && p.K == (K_)) return fwd_map<T, V_, K_>(p, x, gamma, beta, y, mean, rstd, eps, st);
-    WCC_LN_MAP(VM, 2) WCC_LN_MAP(VM, 4) WCC_LN_MAP(VM, 8) WCC_LN_MAP(VM, 16)
-    WCC_LN_MAP(VM / 2, 2) WCC_LN_MAP(VM / 2, 4) WCC_LN_MAP(VM / 2, 8) WCC_LN_MAP(VM / 2, 16)
-    WCC_LN_MAP(VM / 4, 2) WCC_LN_MAP(VM / 4, 4) WCC_LN_MAP(VM / 4, 8) WCC_LN_MAP(VM / 4, 16) WCC_LN_MAP(VM / 4, 32)
-    if constexpr (VM == 8) { WCC_LN_MAP(1, 2) WCC_LN_MAP(1, 4) WCC_LN_MAP(1, 8) WCC_LN_MAP(1, 16) WCC_LN_MAP(1, 32) }
+    if (p.ring) return ring<T, false>(p, x, nullptr, y, gamma, beta, mean, rstd, Partials{}, N, eps, st);
+#define WCC_LN_MAP(V_, K_, STR_) \
+    if (p.V == (V_) && p.K == (K_) && p.strided == (STR_)) return fwd_map<T, V_, K_, STR_>(p, x, gamma, beta, y, mean, rstd, eps, st);
+    constexpr int V4 = 4 / (int)sizeof(T);
+    WCC_LN_MAP(4 * V4, 2, false) WCC_LN_MAP(4 * V4, 4, false) WCC_LN_MAP(4 * V4, 8, false)
+    WCC_LN_MAP(2 * V4, 2, false) WCC_LN_MAP(2 * V4, 4, false) WCC_LN_MAP(2 * V4, 8, false) WCC_LN_MAP(2 * V4, 16, false)
+    WCC_LN_MAP(4 * V4, 2, true) WCC_LN_MAP(4 * V4, 4, true) WCC_LN_MAP(4 * V4, 8, true)
+    if constexpr (V4 == 2) { WCC_LN_MAP(V4, 2, false) WCC_LN_MAP(V4, 4, false) WCC_LN_MAP(V4, 8, false) WCC_LN_MAP(V4, 16, false) WCC_LN_MAP(V4, 32, false) }
 #undef WCC_LN_MAP
     return WCC_ERR_SHAPE;
 }
 
 template <typename T>
 static wcc_status backward(const Plan& p, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
-                           float* part, int N, int C, cudaStream_t st)
+                           const Partials& part, int N, int C, cudaStream_t st)
 {
     constexpr int VM = 16 / (int)sizeof(T);
     const int ctas = bwd_ctas(p, N);
@@ -642,12 +1078,14 @@ static wcc_status backward(const Plan& p, const void* dy, const void* x, const f
 #undef WCC_LN_ROWS
         return WCC_ERR_SHAPE;
     }
-#define WCC_LN_MAP(V_, K_) \
-    if (p.V == (V_) && p.K == (K_)) return bwd_map<T, V_, K_>(p, ctas, dy, x, gamma, mean, rstd, dx, part, st);
-    WCC_LN_MAP(VM, 2) WCC_LN_MAP(VM, 4) WCC_LN_MAP(VM, 8)
-    WCC_LN_MAP(VM / 2, 2) WCC_LN_MAP(VM / 2, 4) WCC_LN_MAP(VM / 2, 8)
-    WCC_LN_MAP(VM / 4, 2) WCC_LN_MAP(VM / 4, 4) WCC_LN_MAP(VM / 4, 8) WCC_LN_MAP(VM / 4, 16)
-    if constexpr (VM == 8) { WCC_LN_MAP(1, 2) WCC_LN_MAP(1, 4) WCC_LN_MAP(1, 8) WCC_LN_MAP(1, 16) }
+    if (p.ring) return ring<T, true>(p, x, dy, dx, gamma, nullptr, const_cast<float*>(mean), const_cast<float*>(rstd), part, N, 0.0f, st);
+#define WCC_LN_MAP(V_, K_, STR_) \
+    if (p.V == (V_) && p.K == (K_) && p.strided == (STR_)) return bwd_map<T, V_, K_, STR_>(p, ctas, dy, x, gamma, mean, rstd, dx, part, st);
+    constexpr int V4 = 4 / (int)sizeof(T);
+    WCC_LN_MAP(4 * V4, 2, false) WCC_LN_MAP(4 * V4, 4, false)
+    WCC_LN_MAP(2 * V4, 2, false) WCC_LN_MAP(2 * V4, 4, false) WCC_LN_MAP(2 * V4, 8, false)
+    WCC_LN_MAP(4 * V4, 2, true) WCC_LN_MAP(4 * V4, 4, true)
+    if constexpr (V4 == 2) { WCC_LN_MAP(V4, 2, false) WCC_LN_MAP(V4, 4, false) WCC_LN_MAP(V4, 8, false) WCC_LN_MAP(V4, 16, false) }
 #undef WCC_LN_MAP
     return WCC_ERR_SHAPE;
 }
