@@ -28,6 +28,10 @@ constexpr int MAX_RANK = 64;
 #ifndef AD_HALF
 #define AD_HALF 8
 #define AD_FILL 12LL
+#define AD_FUSED 296
+#define AD_STAGES 3
+#define AD_CTAS 3
+#define AD_RUNS 3LL
 #endif
 
 template <typename T> struct Geo;
@@ -167,30 +171,78 @@ template <typename T> __device__ __forceinline__ void store_one(T* p, float v)
 template <typename T>
 struct Factor { const T* p; long long sa; int sj, sc; };
 
-// First product: [adapter][group of GC channels][block of 8 ranks][part][lane] 16 bytes (CL channels of rank g).
-// Second product: [adapter][block of 16 channels][step][part][lane] 16 bytes.
+// First product: [group of GC channels][block of 8 ranks][part][lane] 16 bytes (CL channels of rank g).
+// Second product: [block of 16 channels][step][part][lane] 16 bytes.
 template <typename T> __host__ __device__ inline size_t first_words(int rb, int K) { return (size_t)((K + Geo<T>::GC - 1) / Geo<T>::GC) * rb * Geo<T>::PARTS * 32; }
 template <typename T> __host__ __device__ inline size_t second_words(int rb, int M) { return (size_t)((M + 15) / 16) * steps2<T>(rb) * Geo<T>::PARTS * 32; }
 
 template <typename T>
-__device__ __forceinline__ uint32_t element(const Factor<T>& f, int a, int j, int c, int r, int C)
+__device__ __forceinline__ uint32_t element(const T* f, int j, int c, int sj, int sc, int r, int C)
 {
     if (j >= r || c >= C) return 0u;
-    const T* q = f.p + a * f.sa + (long long)j * f.sj + (long long)c * f.sc;
+    const T* q = f + (long long)j * sj + (long long)c * sc;
     return sizeof(T) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(q) : *reinterpret_cast<const uint32_t*>(q);
 }
-
+// Adapter a's factor into `out`; this thread takes words i0, i0 + step, ...
 template <typename T>
-struct PrepArgs {
-    Factor<T> first[2], second[2];      // of up to two products of each kind (p NULL: none)
-    uint4* first_out[2];
-    uint4* second_out[2];
-    int K[2], M[2];
-    int R, r, rb, N;
-    const int32_t* ids;
-    int32_t* order;                     // backward: images with an adapter by adapter, and per adapter the first of them [R + 1]
-    int32_t* start;
-};
+__device__ __forceinline__ void lay_first(const Factor<T>& f, int a, int r, int rb, int K, uint4* out, int i0, int step)
+{
+    constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PARTS = Geo<T>::PARTS;
+    const T* p = f.p + a * f.sa;
+    const int n = (int)(first_words<T>(rb, K) / PARTS);
+    const bool wide = f.sc == 1 && K % CL == 0;                          // a lane's channels are 16 aligned bytes
+    for (int i = i0; i < n; i += step) {
+        const int lane = i & 31, jb = (i >> 5) % rb, grp = (i >> 5) / rb;
+        const int j = 8 * jb + (lane >> 2), c = grp * GC + (lane & 3) * CL;
+        uint32_t w[4] = {0u, 0u, 0u, 0u}, lo[4];
+        if (wide) {
+            if (j < r && c < K) {
+                const uint4 u = *reinterpret_cast<const uint4*>(p + (long long)j * f.sj + c);
+                w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < CL; ++k) {
+                const uint32_t e = element(p, j, c + k, f.sj, f.sc, r, K);
+                if (sizeof(T) == 2) w[(k >> 1) & 3] |= e << (16 * (k & 1));
+                else w[k & 3] = e;
+            }
+        }
+        if (PARTS == 2) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split_tf32(w[k], w[k], lo[k]);
+        }
+        uint4* o = out + (i >> 5) * (PARTS * 32) + lane;
+        o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        if (PARTS == 2) o[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void lay_second(const Factor<T>& f, int a, int r, int rb, int M, uint4* out, int i0, int step)
+{
+    constexpr int PARTS = Geo<T>::PARTS;
+    const T* p = f.p + a * f.sa;
+    const int ns = steps2<T>(rb), n = (int)(second_words<T>(rb, M) / PARTS);
+    const bool pairs = sizeof(T) == 2 && f.sj == 1 && r % 2 == 0;        // two neighbouring ranks are one aligned word
+    for (int i = i0; i < n; i += step) {
+        const int lane = i & 31, ks = (i >> 5) % ns, mo = (i >> 5) / ns, g = lane >> 2, t = lane & 3;
+        uint32_t w[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {                                   // registers: channel g, g + 8, then the other half of the step's ranks
+            const int o = 16 * mo + g + 8 * (k & 1);
+            if (sizeof(T) == 2) {
+                const int j = 16 * ks + 8 * (k >> 1) + 2 * t;
+                if (pairs) w[k] = j < r && o < M ? *reinterpret_cast<const uint32_t*>(p + (long long)o * f.sc + j) : 0u;
+                else w[k] = element(p, j, o, f.sj, f.sc, r, M) | (element(p, j + 1, o, f.sj, f.sc, r, M) << 16);
+            } else {
+                split_tf32(element(p, 8 * ks + 2 * t + (k >> 1), o, f.sj, f.sc, r, M), w[k], lo[k]);
+            }
+        }
+        uint4* op = out + (i >> 5) * (PARTS * 32) + lane;
+        op[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        if (PARTS == 2) op[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
 
 // The ids of a call as the kernels take them: anything but 0 .. R - 1 is no adapter, and one at R or beyond is an error.
 __device__ __forceinline__ int adapter_of(const int32_t* ids, int n, int R, int* status)
@@ -200,6 +252,19 @@ __device__ __forceinline__ int adapter_of(const int32_t* ids, int n, int R, int*
     if (status) atomicExch(status, (int)WCC_ERR_INDEX);
     return -1;
 }
+
+// What the larger problems prepare in memory: factors too large for a CTA's shared memory, and the order of the images for grad_kernel.
+template <typename T>
+struct PrepArgs {
+    Factor<T> first[2], second;         // p NULL: none
+    uint4* first_out[2];
+    uint4* second_out;
+    int K[2], M;
+    int R, r, rb, N;
+    const int32_t* ids;
+    int32_t* order;                     // images with an adapter by adapter, and per adapter the first of them [R + 1]; or NULL
+    int32_t* start;
+};
 
 // CTA = one adapter (grid.x) and one stripe of its words (grid.y).  An adapter that no image uses is skipped.
 template <typename T>
@@ -230,184 +295,77 @@ __global__ void __launch_bounds__(256) prep_kernel(PrepArgs<T> q)
             }
     }
     if (!used) return;
-    constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PARTS = Geo<T>::PARTS;
-    for (int side = 0; side < 2; ++side) {
-        if (q.first[side].p) {
-            const size_t words = first_words<T>(q.rb, q.K[side]);
-            uint4* out = q.first_out[side] + a * words;
-            for (size_t i = (size_t)blockIdx.y * 256 + threadIdx.x; i < words / PARTS; i += (size_t)gridDim.y * 256) {
-                const int lane = (int)(i & 31), jb = (int)((i >> 5) % q.rb), grp = (int)((i >> 5) / q.rb);
-                const int j = 8 * jb + (lane >> 2), c = grp * GC + (lane & 3) * CL;
-                uint32_t e[CL], w[4], lo[4];
+    const int i0 = blockIdx.y * 256 + threadIdx.x, step = gridDim.y * 256;
 #pragma unroll
-                for (int k = 0; k < CL; ++k) e[k] = element(q.first[side], a, j, c + k, q.r, q.K[side]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (sizeof(T) == 2) w[k] = e[(2 * k) % CL] | (e[(2 * k + 1) % CL] << 16);
-                    else split_tf32(e[k], w[k], lo[k]);
-                }
-                uint4* o = out + (i >> 5) * (PARTS * 32) + lane;
-                o[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                if (PARTS == 2) o[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            }
-        }
-        if (q.second[side].p) {
-            const int ns = steps2<T>(q.rb);
-            const size_t words = second_words<T>(q.rb, q.M[side]);
-            uint4* out = q.second_out[side] + a * words;
-            for (size_t i = (size_t)blockIdx.y * 256 + threadIdx.x; i < words / PARTS; i += (size_t)gridDim.y * 256) {
-                const int lane = (int)(i & 31), ks = (int)((i >> 5) % ns), mo = (int)((i >> 5) / ns), g = lane >> 2, t = lane & 3;
-                const int o0 = 16 * mo + g, M = q.M[side];
-                const Factor<T>& f = q.second[side];
-                uint32_t w[4], lo[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {           // registers: channel o0, o0 + 8, then the other half of the step's ranks
-                    const int o = o0 + 8 * (k & 1);
-                    if (sizeof(T) == 2) {
-                        const int j = 16 * ks + 8 * (k >> 1) + 2 * t;
-                        w[k] = element(f, a, j, o, q.r, M) | (element(f, a, j + 1, o, q.r, M) << 16);
-                    } else {
-                        split_tf32(element(f, a, 8 * ks + 2 * t + (k >> 1), o, q.r, M), w[k], lo[k]);
-                    }
-                }
-                uint4* op = out + (i >> 5) * (PARTS * 32) + lane;
-                op[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                if (PARTS == 2) op[32] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            }
-        }
-    }
+    for (int side = 0; side < 2; ++side)
+        if (q.first[side].p) lay_first<T>(q.first[side], a, q.r, q.rb, q.K[side], q.first_out[side] + a * first_words<T>(q.rb, q.K[side]), i0, step);
+    if (q.second.p) lay_second<T>(q.second, a, q.r, q.rb, q.M, q.second_out + a * second_words<T>(q.rb, q.M), i0, step);
 }
 
-// ---- both products over a tile of positions -----------------------------------------------------
-template <typename T>
-struct ApplyArgs {
-    const T* src;                       // [N][K][P]
-    const uint4* w1;
-    const uint4* w2;                    // NULL: the first product alone (tap)
-    const float* scale;                 // NULL: 1
-    const int32_t* ids;
-    const T* base;                      // NULL: 0
-    T* dst;                             // [N][M][P]
-    void* tap;                          // first product with the scale: three bf16 parts, or fp32, [N][8 RB][Pp] each; NULL: not kept
-    size_t P, Pp;
-    int N, K, M, R;
-    int tiles;                          // groups of CTA tiles of an image
-    int ks;                             // warps that share a position tile
-    int items;
-    int* status;
-};
-
-// VEC: 0 single loads, 1 rows start on the NP positions of a lane's first product, 2 also on the 2 NP of the second.
-template <typename T, int RB, int VEC>
-__device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, float4* sm)
-{
-    constexpr int NP = lane_positions<T>(RB), TP = 8 * NP, CL = Geo<T>::CL, GC = Geo<T>::GC, PARTS = Geo<T>::PARTS, MB = NP / 2;
-    constexpr int NO = VEC == 2 ? 2 * NP : NP, PIECES = 2 * NP / NO;    // positions of a load or store of the second product
-    constexpr bool HALF = sizeof(T) == 2;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int n = item / q.tiles;
-    const int per = (int)(blockDim.x >> 5) / q.ks;                    // position tiles of the CTA
-    const int kw = warp % q.ks, tile = (item - n * q.tiles) * per + warp / q.ks;
-    const size_t p0 = (size_t)tile * TP;
-    const int a = adapter_of(q.ids, n, q.R, q.status);
-    const size_t P = q.P;
-    const int mo_n = (q.M + 15) / 16;
-    const size_t pw = p0 + (size_t)(2 * NP * t);
-
-    if (a < 0) {                                                        // (the whole CTA: it has one image)
-        if (!q.w2 || q.dst == q.base || p0 >= P) return;
-        // the warps of the tile copy its rows, eight pieces of 16 or 8 bytes (or 32 single elements) a row
-        const T* from = q.base + (size_t)n * q.M * P;
-        T* to = q.dst + (size_t)n * q.M * P;
-        constexpr int BATCH = 8;                                        // loads before the first store: the two may be the same map
-        if constexpr (VEC > 0) {
-            constexpr int W = NP * (int)sizeof(T) / 4;
-            const size_t p = p0 + (size_t)NP * (lane & 7);
-            if (p < P)
-                for (int o0 = 4 * kw + (lane >> 3); o0 < q.M; o0 += BATCH * 4 * q.ks) {
-                    Words<W> v[BATCH];
+// ---- the two products over a warp's tile of positions ---------------------------------------------
+template <typename T, int RB> struct Tile {
+    static constexpr int NP = lane_positions<T>(RB), TP = 8 * NP, MB = NP / 2;
+    float acc[MB][RB][4];               // of position NP g + b, rank 8 jb + 2 t + e: [b / 2][jb][2 (b % 2) + e]
+    __device__ __forceinline__ void zero()
+    {
 #pragma unroll
-                    for (int i = 0; i < BATCH; ++i) v[i] = q.base ? load_words<W>(from + min(o0 + 4 * i * q.ks, q.M - 1) * P + p) : Words<W>{};
+        for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                    for (int i = 0; i < BATCH; ++i)
-                        if (o0 + 4 * i * q.ks < q.M) store_words(to + (o0 + 4 * i * q.ks) * P + p, v[i]);
-                }
-        } else {
-            for (size_t p = p0 + lane; p < min(P, p0 + TP); p += 32)
-                for (int o0 = kw; o0 < q.M; o0 += BATCH * q.ks) {
-                    float v[BATCH];
+            for (int jb = 0; jb < RB; ++jb)
 #pragma unroll
-                    for (int i = 0; i < BATCH; ++i) v[i] = q.base ? load_one(from + min(o0 + i * q.ks, q.M - 1) * P + p) : 0.0f;
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i)
-                        if (o0 + i * q.ks < q.M) store_one(to + (o0 + i * q.ks) * P + p, v[i]);
-                }
-        }
-        return;
+                for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
     }
+    __device__ __forceinline__ void scale(float s)
+    {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int jb = 0; jb < RB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[mb][jb][i] *= s;
+    }
+};
+template <bool SM> __device__ __forceinline__ uint4 load_factor(const uint4* p) { return SM ? *p : __ldg(p); }
 
-    float acc[MB][RB][4];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int jb = 0; jb < RB; ++jb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
-
-    const int groups = (q.K + GC - 1) / GC;
-    const size_t pl = p0 + (size_t)NP * g;
-    const T* src = q.src + (size_t)n * q.K * P;
-    const size_t pc = pl < P ? pl : 0;
-    const T* src_end = q.src + (size_t)q.N * q.K * P;
-    const uint4* w1 = q.w1 + (size_t)a * first_words<T>(RB, q.K) + lane;
-    const size_t limit = q.tap ? q.Pp : P;                             // the tap is zero behind P
-    if (p0 < P)
-#pragma unroll 2
-        for (int grp = kw; grp < groups; grp += q.ks) {
-            // Channels behind the last one meet zeros in the factor, positions behind the last one are never stored: both load something else that
-            // exists, so that all loads of a group go out together.
-            Words<NP * (int)sizeof(T) / 4> x[CL];
-#pragma unroll
-            for (int i = 0; i < CL; ++i) {
-                const T* xp = src + (size_t)min(grp * GC + t * CL + i, q.K - 1) * P;
-                if constexpr (VEC > 0) x[i] = load_words<NP * (int)sizeof(T) / 4>(xp + pc);
-                else x[i] = load_row<T, NP, false>(xp, pl, P, src_end);
-            }
-            const uint4* wg = w1 + (size_t)grp * RB * PARTS * 32;
-            if constexpr (HALF) {
+// Adds a group of channels to the first product: x holds this lane's channels of it, wg points at this lane's words of the factor.
+template <typename T, int RB, bool SM>
+__device__ __forceinline__ void first_step(Tile<T, RB>& tile, const Words<Tile<T, RB>::NP * (int)sizeof(T) / 4> (&x)[Geo<T>::CL], const uint4* wg)
+{
+    constexpr int MB = Tile<T, RB>::MB, CL = Geo<T>::CL;
+            if constexpr (sizeof(T) == 2) {
                 uint32_t fa[2][MB][4];
-#pragma unroll
+    #pragma unroll
                 for (int s = 0; s < 2; ++s)
-#pragma unroll
+    #pragma unroll
                     for (int mb = 0; mb < MB; ++mb) {
                         fa[s][mb][0] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x5410);
                         fa[s][mb][1] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x7632);
                         fa[s][mb][2] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x5410);
                         fa[s][mb][3] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x7632);
                     }
-#pragma unroll
+    #pragma unroll
                 for (int jb = 0; jb < RB; ++jb) {
-                    const uint4 w = __ldg(wg + jb * 32);
-#pragma unroll
+                    const uint4 w = load_factor<SM>(wg + jb * 32);
+    #pragma unroll
                     for (int mb = 0; mb < MB; ++mb) {
                         float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                         mma_bf16(d, fa[0][mb], w.x, w.y);
                         mma_bf16(d, fa[1][mb], w.z, w.w);
-                        add(acc[mb][jb], d);
+                        add(tile.acc[mb][jb], d);
                     }
                 }
             } else {
                 uint32_t hi[2][MB][4], lo[2][MB][4];
-#pragma unroll
+    #pragma unroll
                 for (int s = 0; s < 2; ++s)
-#pragma unroll
+    #pragma unroll
                     for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
+    #pragma unroll
                         for (int i = 0; i < 4; ++i) split_tf32(x[2 * s + (i >> 1)].w[2 * mb + (i & 1)], hi[s][mb][i], lo[s][mb][i]);
-#pragma unroll
+    #pragma unroll
                 for (int jb = 0; jb < RB; ++jb) {
-                    const uint4 wh = __ldg(wg + (jb * 2) * 32), wl = __ldg(wg + (jb * 2 + 1) * 32);
-#pragma unroll
+                    const uint4 wh = load_factor<SM>(wg + (jb * 2) * 32), wl = load_factor<SM>(wg + (jb * 2 + 1) * 32);
+    #pragma unroll
                     for (int mb = 0; mb < MB; ++mb) {
                         float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                         mma_tf32(d, lo[0][mb], wh.x, wh.y);
@@ -416,80 +374,118 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
                         mma_tf32(d, hi[1][mb], wl.z, wl.w);
                         mma_tf32(d, hi[0][mb], wh.x, wh.y);
                         mma_tf32(d, hi[1][mb], wh.z, wh.w);
-                        add(acc[mb][jb], d);
+                        add(tile.acc[mb][jb], d);
                     }
                 }
             }
-        }
+}
 
-    if (q.ks > 1) {
-        // the warps of a tile add their partial sums, every warp all of them in the same order
-        float4* mine = sm + (size_t)warp * (MB * RB * 32) + lane;
+// The maps of first products on their way through shared memory, where rows start on vectors: a warp copies the groups of channels ahead of
+// their use, also those of its next tile while it writes the last one, and waits for nobody else.  One group in a stage, [GC rows][8 pieces of
+// NP positions], pieces exchanged so that the eight lanes of a phase (two g, four t) read from different banks.  Rows behind the last channel and
+// pieces behind the last position arrive as zeros.  With plain loads into registers the maps came no faster than 4.9 TB/s (headline batch 57 us).
+template <typename T, int RB>
+struct Feed {
+    static constexpr int NP = Tile<T, RB>::NP, GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), STAGE = GC * 8 * PIECE, S = AD_STAGES;
+    uint32_t base;
+    int head, tail;                     // stages filled and used so far
+    __device__ __forceinline__ explicit Feed(void* warp_smem) : base((uint32_t)__cvta_generic_to_shared(warp_smem)), head(0), tail(0) {}
+    // A stage of a first product's group, or (BASE) of 16 channels of a second product's base: rows from `row0` (its first channel, at position 0),
+    // `left` channels of them exist.  left <= 0: an empty stage.
+    template <bool BASE>
+    __device__ __forceinline__ void issue(const T* row0, int left, size_t P, size_t p0)
+    {
+        constexpr int ROWS = BASE ? 16 : GC;
+        const int lane = threadIdx.x & 31, r0 = lane >> 3, c = lane & 7;
+        const bool in = p0 + (size_t)(NP * c) < P;
+        const T* src = row0 + (size_t)r0 * P + (in ? p0 + (size_t)(NP * c) : 0);
+        const uint32_t dst = base + (uint32_t)(head % S) * STAGE;
+        if (left > 0) {
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int jb = 0; jb < RB; ++jb) mine[(mb * RB + jb) * 32] = make_float4(acc[mb][jb][0], acc[mb][jb][1], acc[mb][jb][2], acc[mb][jb][3]);
-        __syncthreads();
-        const float4* all = sm + (size_t)(warp - kw) * (MB * RB * 32) + lane;
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int jb = 0; jb < RB; ++jb) {
-                float4 v = all[(mb * RB + jb) * 32];
-                for (int w = 1; w < q.ks; ++w) {
-                    const float4 u = all[(size_t)w * (MB * RB * 32) + (mb * RB + jb) * 32];
-                    v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-                }
-                acc[mb][jb][0] = v.x; acc[mb][jb][1] = v.y; acc[mb][jb][2] = v.z; acc[mb][jb][3] = v.w;
+            for (int k = 0; k < ROWS / 4; ++k) {
+                const int r = r0 + 4 * k;
+                const bool have = r < left;
+                const uint32_t d = dst + (uint32_t)((r * 8 + (c ^ (BASE ? r & 1 : swap(r)))) * PIECE);
+                const T* q = have ? src + (size_t)(4 * k) * P : row0;
+                const int bytes = have && in ? PIECE : 0;
+                if constexpr (PIECE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(q), "r"(bytes) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(d), "l"(q), "r"(bytes) : "memory");
             }
-    }
-    if (p0 >= limit) return;
-    const float sc = q.scale ? q.scale[a] : 1.0f;
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int jb = 0; jb < RB; ++jb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[mb][jb][i] *= sc;
-
-    if (q.tap && kw == 0) {
-        if (pl >= P) {
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int jb = 0; jb < RB; ++jb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
         }
-        // rank j = 8 jb + 2 t + e: this lane's positions p0 + NP g + b are accumulators [b / 2][jb][2 (b % 2) + e]
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        ++head;
+    }
+    static __device__ __forceinline__ int swap(int r) { return PIECE == 16 ? 2 * ((r / CL) & 3) : 4 * ((r / CL) & 1); }
+    // Waits for the next stage; the stage before it may be filled again behind this.
+    __device__ __forceinline__ void wait()
+    {
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+        __syncwarp();
+    }
+    __device__ __forceinline__ void take(Words<PIECE / 4> (&x)[CL])
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const uint32_t src = base + (uint32_t)(tail % S) * STAGE;
 #pragma unroll
-        for (int jb = 0; jb < RB; ++jb)
+        for (int i = 0; i < CL; ++i) {
+            const int r = t * CL + i;
+            const uint32_t d = src + (uint32_t)((r * 8 + (g ^ swap(r))) * PIECE);
+            if constexpr (PIECE == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[i].w[0]), "=r"(x[i].w[1]), "=r"(x[i].w[2 % (PIECE / 4)]), "=r"(x[i].w[3 % (PIECE / 4)]) : "r"(d));
+            else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[i].w[0]), "=r"(x[i].w[1]) : "r"(d));
+        }
+        ++tail;
+    }
+    // 2 NP positions of channels g and g + 8
+    __device__ __forceinline__ void take_base(Words<PIECE / 2> (&x)[2])
+    {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const uint32_t src = base + (uint32_t)(tail % S) * STAGE;
+        constexpr int W = PIECE / 4;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const size_t at = ((size_t)n * (8 * RB) + 8 * jb + 2 * t + e) * q.Pp + pl;
-                if constexpr (HALF) {
-                    Words<MB> hi, mid, lo;
-#pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) {
-                        const float v0 = acc[mb][jb][e], v1 = acc[mb][jb][2 + e];
-                        hi.w[mb] = pack_bf16x2(v0, v1);
-                        split_bf16(v0 - bf16lo(hi.w[mb]), v1 - bf16hi(hi.w[mb]), mid.w[mb], lo.w[mb]);
-                    }
-                    T* plane = static_cast<T*>(q.tap) + at;
-                    const size_t next = (size_t)q.N * (8 * RB) * q.Pp;
-                    store_words(plane, hi);
-                    store_words(plane + next, mid);
-                    store_words(plane + 2 * next, lo);
-                } else {
-                    Words<NP> v;
-#pragma unroll
-                    for (int b = 0; b < NP; ++b) v.w[b] = __float_as_uint(acc[b >> 1][jb][2 * (b & 1) + e]);
-                    store_words(static_cast<T*>(q.tap) + at, v);
-                }
+                const int r = g + 8 * h;
+                const uint32_t d = src + (uint32_t)((r * 8 + ((2 * t + e) ^ (r & 1))) * PIECE);
+                if constexpr (PIECE == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[h].w[e * W]), "=r"(x[h].w[e * W + 1]), "=r"(x[h].w[e * W + 2 % W]), "=r"(x[h].w[e * W + 3 % W]) : "r"(d));
+                else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[h].w[e * W]), "=r"(x[h].w[e * W + 1]) : "r"(d));
             }
+        ++tail;
     }
-    if (!q.w2 || p0 >= P) return;
+    static __device__ __forceinline__ void drain() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+};
 
+// Adds the first product over the channel groups kw, kw + ks, ... of an image (src: its first channel, end: behind the tensor) at the tile
+// that starts at p0, loaded as it is needed: rows that start anywhere.  w1 already points at this lane.
+template <typename T, int RB, bool SM>
+__device__ __forceinline__ void first_product(Tile<T, RB>& tile, const T* src, const T* end, int K, size_t P, size_t p0, const uint4* w1, int kw, int ks)
+{
+    constexpr int NP = Tile<T, RB>::NP, CL = Geo<T>::CL, GC = Geo<T>::GC, PARTS = Geo<T>::PARTS;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int groups = (K + GC - 1) / GC;
+    for (int grp = kw; grp < groups; grp += ks) {
+        // channels behind the last one meet zeros in the factor: they load something else that exists, so that all loads of a group go out together
+        Words<NP * (int)sizeof(T) / 4> x[CL];
+#pragma unroll
+        for (int i = 0; i < CL; ++i)
+            x[i] = load_row<T, NP, false>(src + (size_t)min(grp * GC + t * CL + i, K - 1) * P, p0 + (size_t)NP * g, P, end);
+        first_step<T, RB, SM>(tile, x, w1 + (size_t)grp * RB * PARTS * 32);
+    }
+}
+
+// dst = base + second product, of the blocks kw, kw + ks, ... of 16 channels of an image (base, dst: its first channel; base may be NULL).
+// next_base(x): this lane's part of the next block's base from the feed (VEC > 0).  VEC 2: rows also start on 2 NP positions.  out: this warp's
+// 16 x (TP + 4) floats, VEC 0 only.
+template <typename T, int RB, int VEC, bool SM, typename Next>
+__device__ __forceinline__ void second_product(const Tile<T, RB>& tile, const T* base, T* dst, int M, size_t P, size_t p0, const uint4* w2, int kw, int ks,
+                                               float* out, Next next_base)
+{
+    constexpr int NP = Tile<T, RB>::NP, TP = 8 * NP, PARTS = Geo<T>::PARTS;
+    constexpr int NO = VEC == 2 ? 2 * NP : NP, PIECES = 2 * NP / NO;    // positions of a load or store
+    constexpr bool HALF = sizeof(T) == 2;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int mo_n = (M + 15) / 16;
+    const size_t pw = p0 + (size_t)(2 * NP * t);
     // the accumulators as operands: of position b, block jb of ranks
     constexpr int UW = HALF ? 1 : 2;
     uint32_t uh[NP][RB][UW], ul[NP][RB][UW];
@@ -497,42 +493,16 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
     for (int b = 0; b < NP; ++b)
 #pragma unroll
         for (int jb = 0; jb < RB; ++jb) {
-            const float u0 = acc[b >> 1][jb][2 * (b & 1)], u1 = acc[b >> 1][jb][2 * (b & 1) + 1];
+            const float u0 = tile.acc[b >> 1][jb][2 * (b & 1)], u1 = tile.acc[b >> 1][jb][2 * (b & 1) + 1];
             if constexpr (HALF) split_bf16(u0, u1, uh[b][jb][0], ul[b][jb][0]);
             else {
                 split_tf32(__float_as_uint(u0), uh[b][jb][0], ul[b][jb][0]);
                 split_tf32(__float_as_uint(u1), uh[b][jb][UW - 1], ul[b][jb][UW - 1]);
             }
         }
-    float* out = reinterpret_cast<float*>(sm) + (q.ks > 1 ? (size_t)(blockDim.x >> 5) * (MB * RB * 128) : 0) + warp * 16 * (TP + 4);
-    const uint4* w2 = q.w2 + (size_t)a * second_words<T>(RB, q.M) + lane;
     constexpr int NS = steps2<T>(RB);
-    // the base of the next 16 channels is loaded while these are computed: the loads of one iteration would be waited for in every one
     using Piece = Words<NO * (int)sizeof(T) / 4>;
-    auto load_base = [&](int mo, Piece(&b)[2][PIECES]) {
-        if (VEC > 0 && q.base && mo < mo_n) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const T* row = q.base + ((size_t)n * q.M + min(16 * mo + g + 8 * h, q.M - 1)) * P;
-#pragma unroll
-                for (int e = 0; e < PIECES; ++e) b[h][e] = load_words<NO * (int)sizeof(T) / 4>(row + (pw + NO * e < P ? pw + NO * e : 0));
-            }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < PIECES; ++e) b[h][e] = Piece{};
-        }
-    };
-    Piece next[2][PIECES];
-    load_base(kw, next);
-    for (int mo = kw; mo < mo_n; mo += q.ks) {
-        Piece bs[2][PIECES];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < PIECES; ++e) bs[h][e] = next[h][e];
-        load_base(mo + q.ks, next);
+    for (int mo = kw; mo < mo_n; mo += ks) {
         float d[NP][4];
 #pragma unroll
         for (int b = 0; b < NP; ++b)
@@ -540,21 +510,21 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
             for (int i = 0; i < 4; ++i) d[b][i] = 0.0f;
         const uint4* wm = w2 + (size_t)mo * NS * PARTS * 32;
 #pragma unroll
-        for (int ks = 0; ks < NS; ++ks) {
+        for (int s = 0; s < NS; ++s) {
             if constexpr (HALF) {
-                const uint4 w = __ldg(wm + ks * 32);
+                const uint4 w = load_factor<SM>(wm + s * 32);
 #pragma unroll
                 for (int b = 0; b < NP; ++b) {
-                    mma_bf16(d[b], w.x, w.y, w.z, w.w, ul[b][2 * ks][0], 2 * ks + 1 < RB ? ul[b][(2 * ks + 1) % RB][0] : 0u);
-                    mma_bf16(d[b], w.x, w.y, w.z, w.w, uh[b][2 * ks][0], 2 * ks + 1 < RB ? uh[b][(2 * ks + 1) % RB][0] : 0u);
+                    mma_bf16(d[b], w.x, w.y, w.z, w.w, ul[b][2 * s][0], 2 * s + 1 < RB ? ul[b][(2 * s + 1) % RB][0] : 0u);
+                    mma_bf16(d[b], w.x, w.y, w.z, w.w, uh[b][2 * s][0], 2 * s + 1 < RB ? uh[b][(2 * s + 1) % RB][0] : 0u);
                 }
             } else {
-                const uint4 wh = __ldg(wm + (ks * 2) * 32), wl = __ldg(wm + (ks * 2 + 1) * 32);
+                const uint4 wh = load_factor<SM>(wm + (s * 2) * 32), wl = load_factor<SM>(wm + (s * 2 + 1) * 32);
 #pragma unroll
                 for (int b = 0; b < NP; ++b) {
-                    mma_tf32(d[b], wl.x, wl.y, wl.z, wl.w, uh[b][ks][0], uh[b][ks][UW - 1]);
-                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, ul[b][ks][0], ul[b][ks][UW - 1]);
-                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, uh[b][ks][0], uh[b][ks][UW - 1]);
+                    mma_tf32(d[b], wl.x, wl.y, wl.z, wl.w, uh[b][s][0], uh[b][s][UW - 1]);
+                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, ul[b][s][0], ul[b][s][UW - 1]);
+                    mma_tf32(d[b], wh.x, wh.y, wh.z, wh.w, uh[b][s][0], uh[b][s][UW - 1]);
                 }
             }
         }
@@ -570,54 +540,242 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, floa
                     for (int b = 0; b < NP; b += 2)
                         *reinterpret_cast<float2*>(out + (g + 8 * h) * (TP + 4) + 2 * NP * t + NP * e + b) = make_float2(d[b][2 * h + e], d[b + 1][2 * h + e]);
             __syncwarp();
-            const int rows = min(16, q.M - 16 * mo);
-            const size_t at = ((size_t)n * q.M + 16 * mo) * P + p0, here = P - p0;
+            const int rows = min(16, M - 16 * mo);
+            const size_t at = (size_t)(16 * mo) * P + p0, here = P - p0;
 #pragma unroll 8
             for (int i = lane; i < 16 * TP; i += 32) {
                 const int r = i / TP, c = i % TP;
                 if (r < rows && (size_t)c < here) {
                     const size_t j = at + r * P + c;
                     float v = out[r * (TP + 4) + c];
-                    if (q.base) v += load_one(q.base + j);
-                    store_one(q.dst + j, v);
+                    if (base) v += load_one(base + j);
+                    store_one(dst + j, v);
                 }
             }
         } else {
+            Words<NP * (int)sizeof(T) / 2> bs[2]{};
+            if (base) next_base(bs);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int o = 16 * mo + g + 8 * h;
-            if (o >= q.M) continue;
-            T* row = q.dst + ((size_t)n * q.M + o) * P;
+            for (int h = 0; h < 2; ++h) {
+                const int o = 16 * mo + g + 8 * h;
+                if (o >= M) continue;
+                T* row = dst + (size_t)o * P;
 #pragma unroll
-            for (int e = 0; e < PIECES; ++e) {
-                Piece v;
+                for (int e = 0; e < PIECES; ++e) {
+                    Piece v;
 #pragma unroll
-                for (int i = 0; i < NO * (int)sizeof(T) / 4; ++i) {
-                    if constexpr (HALF) {
-                        const int at = NO * e + 2 * i;                  // of the lane's 2 NP positions
-                        v.w[i] = pack_bf16x2(d[at % NP][2 * h + at / NP] + bf16lo(bs[h][e].w[i]), d[at % NP + 1][2 * h + at / NP] + bf16hi(bs[h][e].w[i]));
-                    } else {
-                        const int at = NO * e + i;
-                        v.w[i] = __float_as_uint(d[at % NP][2 * h + at / NP] + __uint_as_float(bs[h][e].w[i]));
+                    for (int i = 0; i < NO * (int)sizeof(T) / 4; ++i) {
+                        const uint32_t bw = bs[h].w[e * (NO * (int)sizeof(T) / 4) + i];
+                        if constexpr (HALF) {
+                            const int at = NO * e + 2 * i;              // of the lane's 2 NP positions
+                            v.w[i] = pack_bf16x2(d[at % NP][2 * h + at / NP] + bf16lo(bw), d[at % NP + 1][2 * h + at / NP] + bf16hi(bw));
+                        } else {
+                            const int at = NO * e + i;
+                            v.w[i] = __float_as_uint(d[at % NP][2 * h + at / NP] + __uint_as_float(bw));
+                        }
                     }
+                    if (pw + NO * e < P) store_words(row + pw + NO * e, v);
                 }
-                if (pw + NO * e < P) store_words(row + pw + NO * e, v);
             }
-        }
         }
     }
 }
 
-// Up to two maps in one launch (the backward pass projects dy and x): the second takes the CTAs from q0.items on.
-template <typename T, int RB, int VEC>
-__global__ void __launch_bounds__(256) apply_kernel(ApplyArgs<T> q0, ApplyArgs<T> q1)
+// dst = base (or 0) at a tile of TP positions: what an image without an adapter gets.  The ks warps of the tile take turns at the rows.
+template <typename T, int TP, bool VEC>
+__device__ __forceinline__ void copy_tile(const T* base, T* dst, int M, size_t P, size_t p0, int kw, int ks)
 {
-    extern __shared__ float4 apply_sm[];
+    constexpr int NP = TP / 8, W = NP * (int)sizeof(T) / 4, BATCH = 8;   // loads before the first store: the two may be the same map
+    const int lane = threadIdx.x & 31;
+    if constexpr (VEC) {
+        const size_t p = p0 + (size_t)NP * (lane & 7);
+        if (p >= P) return;
+        for (int o0 = 4 * kw + (lane >> 3); o0 < M; o0 += BATCH * 4 * ks) {
+            Words<W> v[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) v[i] = base ? load_words<W>(base + min(o0 + 4 * i * ks, M - 1) * P + p) : Words<W>{};
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (o0 + 4 * i * ks < M) store_words(dst + (o0 + 4 * i * ks) * P + p, v[i]);
+        }
+    } else {
+        for (size_t p = p0 + lane; p < min(P, p0 + TP); p += 32)
+            for (int o0 = kw; o0 < M; o0 += BATCH * ks) {
+                float v[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) v[i] = base ? load_one(base + min(o0 + i * ks, M - 1) * P + p) : 0.0f;
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i)
+                    if (o0 + i * ks < M) store_one(dst + (o0 + i * ks) * P + p, v[i]);
+            }
+    }
+}
+
+// This lane's part of a tile as planes of a [ranks][pitch] array, `at` = element (0, NP g): bf16 three parts `next` elements apart, or fp32.
+template <typename T, int RB>
+__device__ __forceinline__ void store_planes(const Tile<T, RB>& tile, T* plane, size_t pitch, size_t next)
+{
+    constexpr int NP = Tile<T, RB>::NP, MB = NP / 2;
+    const int t = threadIdx.x & 3;
+#pragma unroll
+    for (int jb = 0; jb < RB; ++jb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            T* q = plane + (8 * jb + 2 * t + e) * pitch;
+            if constexpr (sizeof(T) == 2) {
+                Words<MB> hi, mid, lo;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) {
+                    const float v0 = tile.acc[mb][jb][e], v1 = tile.acc[mb][jb][2 + e];
+                    hi.w[mb] = pack_bf16x2(v0, v1);
+                    split_bf16(v0 - bf16lo(hi.w[mb]), v1 - bf16hi(hi.w[mb]), mid.w[mb], lo.w[mb]);
+                }
+                store_words(q, hi);
+                store_words(q + next, mid);
+                store_words(q + 2 * next, lo);
+            } else {
+                Words<NP> v;
+#pragma unroll
+                for (int b = 0; b < NP; ++b) v.w[b] = __float_as_uint(tile.acc[b >> 1][jb][2 * (b & 1) + e]);
+                store_words(q, v);
+            }
+        }
+}
+
+template <typename T>
+struct ApplyArgs {
+    const T* src;                       // [N][K][P]
+    Factor<T> f1, f2;                   // f2.p NULL: the first product alone (tap)
+    const uint4* w1;                    // laid out in memory, or NULL: each CTA lays them out in shared memory
+    const uint4* w2;
+    const float* scale;                 // NULL: 1
+    const int32_t* ids;
+    const T* base;                      // NULL: 0
+    T* dst;                             // [N][M][P]
+    T* tap;                             // first product with the scale as planes [N][8 RB][Pp], zero behind P; NULL: not kept
+    size_t P, Pp;
+    int N, K, M, R, r;
+    int ks;                             // warps that share a position tile
+    int groups, parts, per_part;        // of an image: tiles of a CTA's warps, CTAs, groups of a CTA
+    int items;
+    int* status;
+};
+
+// A CTA takes a run of tiles of one image.  Shared memory: the factors (SM), partial sums of warps that share a tile, tiles on their way out.
+template <typename T, int RB, int VEC, bool SM>
+__device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, uint4* sm)
+{
+    using Ti = Tile<T, RB>;
+    constexpr int TP = Ti::TP, MB = Ti::MB;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int n = item / q.parts, per = warps / q.ks;                   // per: position tiles at once
+    const int kw = warp % q.ks;
+    const int g0 = (item - n * q.parts) * q.per_part, g1 = min(q.groups, g0 + q.per_part);
+    const int a = adapter_of(q.ids, n, q.R, q.status);
+    const size_t P = q.P;
+    const T* base = q.base ? q.base + (size_t)n * q.M * P : nullptr;
+    T* dst = q.dst + (size_t)n * q.M * P;
+
+    if (a < 0) {                                                        // (the whole CTA: it has one image)
+        if (q.f2.p && q.dst != q.base)
+            for (int gr = g0; gr < g1; ++gr) copy_tile<T, TP, (VEC > 0)>(base, dst, q.M, P, (size_t)(gr * per + warp / q.ks) * TP, kw, q.ks);
+        return;
+    }
+    const size_t n1 = first_words<T>(RB, q.K), n2 = q.f2.p ? second_words<T>(RB, q.M) : 0;
+    const uint4 *w1 = sm + lane, *w2 = sm + n1 + lane;
+    if (SM) {
+        lay_first<T>(q.f1, a, q.r, RB, q.K, sm, threadIdx.x, blockDim.x);
+        if (n2) lay_second<T>(q.f2, a, q.r, RB, q.M, sm + n1, threadIdx.x, blockDim.x);
+        sm += n1 + n2;
+        __syncthreads();
+    } else {
+        w1 = q.w1 + a * n1 + lane;
+        w2 = q.w2 + a * n2 + lane;
+    }
+    float4* red = reinterpret_cast<float4*>(sm);
+    char* tail = reinterpret_cast<char*>(sm) + (q.ks > 1 ? (size_t)warps * (MB * RB * 512) : 0);      // tiles on their way out, or in
+    float* out = reinterpret_cast<float*>(tail) + warp * 16 * (TP + 4);
+    void* feed_sm = tail + (size_t)warp * Feed<T, RB>::S * Feed<T, RB>::STAGE;
+    const float sc = q.scale ? q.scale[a] : 1.0f;
+    const T* src = q.src + (size_t)n * q.K * P;
+    const size_t limit = q.tap ? q.Pp : P;
+
+    using Fd = Feed<T, RB>;
+    constexpr int GC = Geo<T>::GC;
+    Fd feed(feed_sm);
+    // What the feed copies next: the fi-th stage of the tile in round fr, this warp's groups of the map and then its blocks of the base.
+    const int groups = (q.K + GC - 1) / GC, nx = groups > kw ? (groups - kw + q.ks - 1) / q.ks : 0;
+    const int blocks = (q.M + 15) / 16, nb = base && q.f2.p && blocks > kw ? (blocks - kw + q.ks - 1) / q.ks : 0;
+    int fr = g0, fi = 0;
+    auto ahead = [&]() {
+        size_t p = (size_t)(fr * per + warp / q.ks) * TP;
+        while (fr < g1 && fi >= nx + (p < P ? nb : 0)) { fi = 0; ++fr; p = (size_t)(fr * per + warp / q.ks) * TP; if (nx + nb == 0) break; }
+        if (fr >= g1 || nx + nb == 0) feed.template issue<false>(src, 0, P, 0);
+        else if (fi < nx) { const int c = (kw + fi * q.ks) * GC; feed.template issue<false>(src + (size_t)c * P, q.K - c, P, p); }
+        else { const int c = (kw + (fi - nx) * q.ks) * 16; feed.template issue<true>(base + (size_t)c * P, q.M - c, P, p); }
+        ++fi;
+    };
+    auto next_base = [&](Words<Fd::PIECE / 2> (&x)[2]) { feed.wait(); ahead(); feed.take_base(x); };
+    if constexpr (VEC > 0)
+        for (int i = 0; i < Fd::S - 1; ++i) ahead();
+    for (int gr = g0; gr < g1; ++gr) {
+        const size_t p0 = (size_t)(gr * per + warp / q.ks) * TP;
+        Ti tile;
+        tile.zero();
+        if constexpr (VEC > 0) {
+            for (int grp = kw; grp < groups; grp += q.ks) {
+                Words<Fd::PIECE / 4> x[Fd::CL];
+                feed.wait();
+                ahead();
+                feed.take(x);
+                first_step<T, RB, SM>(tile, x, w1 + (size_t)grp * RB * Geo<T>::PARTS * 32);
+            }
+        } else if (p0 < P) first_product<T, RB, SM>(tile, src, q.src + (size_t)q.N * q.K * P, q.K, P, p0, w1, kw, q.ks);
+        if (q.ks > 1) {
+            // the warps of a tile add their partial sums, every warp all of them in the same order
+            if (gr > g0) __syncthreads();                               // those of the group before have been read
+            float4* mine = red + (size_t)warp * (MB * RB * 32) + lane;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int jb = 0; jb < RB; ++jb)
+                    mine[(mb * RB + jb) * 32] = make_float4(tile.acc[mb][jb][0], tile.acc[mb][jb][1], tile.acc[mb][jb][2], tile.acc[mb][jb][3]);
+            __syncthreads();
+            const float4* all = red + (size_t)(warp - kw) * (MB * RB * 32) + lane;
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int jb = 0; jb < RB; ++jb) {
+                    float4 v = all[(mb * RB + jb) * 32];
+                    for (int w = 1; w < q.ks; ++w) {
+                        const float4 u = all[(size_t)w * (MB * RB * 32) + (mb * RB + jb) * 32];
+                        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+                    }
+                    tile.acc[mb][jb][0] = v.x; tile.acc[mb][jb][1] = v.y; tile.acc[mb][jb][2] = v.z; tile.acc[mb][jb][3] = v.w;
+                }
+        }
+        if (p0 >= limit) continue;
+        tile.scale(sc);
+        if (q.tap && kw == 0) {
+            const size_t pl = p0 + (size_t)Ti::NP * (lane >> 2);
+            if (pl >= P) tile.zero();
+            store_planes<T, RB>(tile, q.tap + (size_t)n * (8 * RB) * q.Pp + pl, q.Pp, (size_t)q.N * (8 * RB) * q.Pp);
+        }
+        if (q.f2.p && p0 < P) second_product<T, RB, VEC, SM>(tile, base, dst, q.M, P, p0, w2, kw, q.ks, out, next_base);
+    }
+    if constexpr (VEC > 0) Fd::drain();
+}
+
+// Up to two maps in one launch (the backward pass projects dy and x): the second takes the CTAs from q0.items on.
+template <typename T, int RB, int VEC, bool SM>
+__global__ void __launch_bounds__(256, RB <= 2 ? 2 : 1) apply_kernel(ApplyArgs<T> q0, ApplyArgs<T> q1)
+{
+    extern __shared__ uint4 apply_sm[];
     pdl_wait();
     pdl_launch();
     const int item = blockIdx.x;
-    if (item < q0.items) apply_body<T, RB, VEC>(q0, item, apply_sm);
-    else apply_body<T, RB, VEC>(q1, item - q0.items, apply_sm);
+    if (item < q0.items) apply_body<T, RB, VEC, SM>(q0, item, apply_sm);
+    else apply_body<T, RB, VEC, SM>(q1, item - q0.items, apply_sm);
 }
 
 // ---- single tokens (one position an image) --------------------------------------------------------
@@ -690,6 +848,36 @@ __global__ void __launch_bounds__(256) token_kernel(const T* __restrict__ x, con
 // contiguous.  The images are taken in the order of their adapters, cut into `ranges` equal runs of tiles; a warp takes one run and 16
 // channels, keeps its 16 x 8 RB sums in registers and writes them out where the adapter changes, to slot (run + adapter): runs and adapters
 // only ascend, so no slot is written twice, and grad_reduce adds an adapter's slots in ascending order.
+// One half tile of G[c][j] += map[c][p] plane[j][p]: 4 NP positions, channels g and g + 8 in x0 and x1, pl at rank g and this lane's positions.
+template <typename T>
+__device__ __forceinline__ void grad_step(float (&d)[4], const Words<Geo<T>::NP * (int)sizeof(T) / 4>& x0, const Words<Geo<T>::NP * (int)sizeof(T) / 4>& x1,
+                                          const T* pl, size_t next)
+{
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t a0[4] = {x0.w[0], x1.w[0], x0.w[1], x1.w[1]}, a1[4] = {x0.w[2], x1.w[2], x0.w[3], x1.w[3]};
+#pragma unroll
+        for (int part = 2; part >= 0; --part) {
+            const uint4 v = *reinterpret_cast<const uint4*>(pl + part * next);
+            mma_bf16(d, a0, v.x, v.y);
+            mma_bf16(d, a1, v.z, v.w);
+        }
+    } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(pl);
+        const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            uint32_t ah[4], al[4], bh[2], bl[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) split_tf32(i & 1 ? x1.w[2 * s + (i >> 1)] : x0.w[2 * s + (i >> 1)], ah[i], al[i]);
+            split_tf32(vw[2 * s], bh[0], bl[0]);
+            split_tf32(vw[2 * s + 1], bh[1], bl[1]);
+            mma_tf32(d, al, bh[0], bh[1]);
+            mma_tf32(d, ah, bl[0], bl[1]);
+            mma_tf32(d, ah, bh[0], bh[1]);
+        }
+    }
+}
+
 template <typename T>
 struct GradArgs {
     const T* map[2];                    // x (with the plane of V) and dy (with that of U)
@@ -756,34 +944,9 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs<T> q)
         for (int jb = 0; jb < RB; ++jb) {
             float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const Words<4>(&xw)[2] = xr[h];
-                const size_t at = ((size_t)n * (8 * RB) + 8 * jb + g) * q.Pp + pb + h * (TP / 2) + t * NP;
-                if constexpr (sizeof(T) == 2) {
-                    const __nv_bfloat16* pl = static_cast<const __nv_bfloat16*>(plane) + at;
-                    const uint32_t a0[4] = {xw[0].w[0], xw[1].w[0], xw[0].w[1], xw[1].w[1]}, a1[4] = {xw[0].w[2], xw[1].w[2], xw[0].w[3], xw[1].w[3]};
-#pragma unroll
-                    for (int part = 2; part >= 0; --part) {
-                        const uint4 v = *reinterpret_cast<const uint4*>(pl + (size_t)part * q.N * (8 * RB) * q.Pp);
-                        mma_bf16(d, a0, v.x, v.y);
-                        mma_bf16(d, a1, v.z, v.w);
-                    }
-                } else {
-                    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const float*>(plane) + at);
-                    const uint32_t vw[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        uint32_t ah[4], al[4], bh[2], bl[2];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) split_tf32(xw[i & 1].w[2 * s + (i >> 1)], ah[i], al[i]);
-                        split_tf32(vw[2 * s], bh[0], bl[0]);
-                        split_tf32(vw[2 * s + 1], bh[1], bl[1]);
-                        mma_tf32(d, al, bh[0], bh[1]);
-                        mma_tf32(d, ah, bl[0], bl[1]);
-                        mma_tf32(d, ah, bh[0], bh[1]);
-                    }
-                }
-            }
+            for (int h = 0; h < 2; ++h)
+                grad_step<T>(d, xr[h][0], xr[h][1], static_cast<const T*>(plane) + ((size_t)n * (8 * RB) + 8 * jb + g) * q.Pp + pb + h * (TP / 2) + t * NP,
+                             (size_t)q.N * (8 * RB) * q.Pp);
             add(acc[jb], d);
         }
         if (++tile == q.tiles) {
@@ -828,10 +991,264 @@ __global__ void __launch_bounds__(256) grad_reduce(const float* __restrict__ par
     }
 }
 
+// ---- the whole backward pass in one kernel --------------------------------------------------------
+// Small ranks and maps with tiles enough.  A CTA takes a run of units of 4 warp tiles, in the order of the images.  For a unit its warps compute
+// V and dx and then U of their tiles, leave V and U in shared memory, and then each of them takes blocks of 16 channels of x and dy over
+// the unit's positions: G[c][j] += map[c][p] plane[j][p], from rows that were just read and come from the L1 or L2.  So x and dy cross the
+// memory bus once.  The sums stay in registers until the image changes; run and image only ascend, so slot (run + image) is written once.
+constexpr int BW = 4;                                                   // warps of a CTA
+template <typename T>
+struct BwdArgs {
+    const T *dy, *x, *base;
+    T* dx;                              // NULL: not wanted
+    Factor<T> fB, fAt, fA;              // dy -> V, V -> dx, x -> U
+    const float* scale;
+    const int32_t* ids;
+    float* part;                        // [slot][block of 16 channels][16][8 RB]
+    size_t P;
+    int N, Cin, Cout, R, r;
+    int units, share;                   // units of an image, of a run
+    int* status;
+};
+template <typename T> __host__ __device__ constexpr int plane_pitch(int np) { return BW * 8 * np + 64 / (int)sizeof(T); }      // 16 banks off per rank
+template <typename T>
+static size_t bwd_smem(int rb, int Cin, int Cout, bool dx, bool vec)
+{
+    const int np = lane_positions<T>(rb);
+    return 16 * (first_words<T>(rb, Cout) + first_words<T>(rb, Cin) + (dx ? second_words<T>(rb, Cin) : 0)) +
+           (size_t)2 * (sizeof(T) == 2 ? 3 : 1) * 8 * rb * plane_pitch<T>(np) * sizeof(T) + (size_t)BW * (vec ? AD_STAGES * Geo<T>::GC * 8 * np * sizeof(T) : 16 * (8 * np + 4) * 4);
+}
+
+template <typename T, int RB, int VEC, int NB>
+__global__ void __launch_bounds__(32 * BW, NB <= 4 ? 3 : 2) bwd_kernel(BwdArgs<T> q)
+{
+    using Ti = Tile<T, RB>;
+    constexpr int NP = Ti::NP, TP = Ti::TP, PITCH = plane_pitch<T>(NP), PARTS = sizeof(T) == 2 ? 3 : 1, PLANE = 8 * RB * PITCH;
+    extern __shared__ uint4 bwd_sm[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const size_t P = q.P, nB = first_words<T>(RB, q.Cout), nA = first_words<T>(RB, q.Cin), nAt = q.dx ? second_words<T>(RB, q.Cin) : 0;
+    T* planes = reinterpret_cast<T*>(bwd_sm + nB + nA + nAt);           // [U for dy, V for x][part][rank][position]
+    float* out = reinterpret_cast<float*>(planes + 2 * PARTS * PLANE) + warp * 16 * (TP + 4);
+    const int blocks0 = (q.Cin + 15) / 16, all = blocks0 + (q.Cout + 15) / 16;
+    const T *x_end = q.x + (size_t)q.N * q.Cin * P, *dy_end = q.dy + (size_t)q.N * q.Cout * P;
+    const int run = blockIdx.x;
+    const long long total = (long long)q.N * q.units, u0 = (long long)run * q.share, u1 = min(total, u0 + q.share);
+
+    float acc[NB][RB][4];
+    auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int jb = 0; jb < RB; ++jb)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][jb][k] = 0.0f;
+    };
+    auto flush = [&](int n) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            if (warp + BW * i < all) {
+                float* o = q.part + ((size_t)(run + n) * all + warp + BW * i) * (16 * 8 * RB) + 2 * t;
+#pragma unroll
+                for (int jb = 0; jb < RB; ++jb) {
+                    *reinterpret_cast<float2*>(o + g * 8 * RB + 8 * jb) = make_float2(acc[i][jb][0], acc[i][jb][1]);
+                    *reinterpret_cast<float2*>(o + (g + 8) * 8 * RB + 8 * jb) = make_float2(acc[i][jb][2], acc[i][jb][3]);
+                }
+            }
+        clear();
+    };
+    clear();
+    // What the feed copies next: the fi-th stage of unit fu, the groups of dy, the blocks of the base, the groups of x.  Units of images without an
+    // adapter are stepped over.
+    using Fd = Feed<T, RB>;
+    constexpr int GC = Geo<T>::GC;
+    const int gB = (q.Cout + GC - 1) / GC, gA = (q.Cin + GC - 1) / GC, gD = q.dx && q.base ? blocks0 : 0;
+    Fd feed(reinterpret_cast<char*>(planes + 2 * PARTS * PLANE) + (size_t)warp * Fd::S * Fd::STAGE);
+    long long fu = u0 - 1;
+    int fi = 0, fn = -1, fend = 0, fb = 0;                              // stages of the unit, blocks of the base among them
+    size_t fp = 0;
+    bool feeds = false;
+    auto ahead = [&]() {
+        if (fi == fend) {
+            for (++fu; fu < u1; ++fu) {
+                const int n = (int)(fu / q.units);
+                if (n != fn) { fn = n; feeds = q.ids[n] >= 0 && q.ids[n] < q.R; }
+                if (feeds) break;
+            }
+            fi = 0;
+            fp = (size_t)(fu - (long long)fn * q.units) * (BW * TP) + (size_t)warp * TP;
+            fb = fp < P ? gD : 0;
+            fend = gB + fb + gA;
+        }
+        if (fu >= u1) { feed.template issue<false>(q.dy, 0, P, 0); fi = fend; return; }
+        if (fi < gB) feed.template issue<false>(q.dy + ((size_t)fn * q.Cout + fi * GC) * P, q.Cout - fi * GC, P, fp);
+        else if (fi < gB + fb) { const int c = (fi - gB) * 16; feed.template issue<true>(q.base + ((size_t)fn * q.Cin + c) * P, q.Cin - c, P, fp); }
+        else { const int c = (fi - gB - fb) * GC; feed.template issue<false>(q.x + ((size_t)fn * q.Cin + c) * P, q.Cin - c, P, fp); }
+        ++fi;
+    };
+    auto next_base = [&](Words<Fd::PIECE / 2> (&x)[2]) { feed.wait(); ahead(); feed.take_base(x); };
+    auto consume = [&](Ti& tile, const uint4* w) {
+        Words<Fd::PIECE / 4> x[Fd::CL];
+        feed.wait();
+        ahead();
+        feed.take(x);
+        first_step<T, RB, true>(tile, x, w);
+    };
+    if constexpr (VEC > 0)
+        for (int i = 0; i < Fd::S - 1; ++i) ahead();
+    int last = -1, a = -1, laid = -1;                                   // image at work, its adapter, the adapter in shared memory
+    float sc = 1.0f;
+    for (long long u = u0; u < u1; ++u) {
+        const int n = (int)(u / q.units);
+        const size_t pu = (size_t)(u - (long long)n * q.units) * (BW * TP), p0 = pu + (size_t)warp * TP;
+        if (n != last) {
+            if (a >= 0) flush(last);
+            last = n;
+            a = adapter_of(q.ids, n, q.R, q.status);
+            if (a >= 0 && a != laid) {
+                __syncthreads();
+                lay_first<T>(q.fB, a, q.r, RB, q.Cout, bwd_sm, threadIdx.x, 32 * BW);
+                lay_first<T>(q.fA, a, q.r, RB, q.Cin, bwd_sm + nB, threadIdx.x, 32 * BW);
+                if (nAt) lay_second<T>(q.fAt, a, q.r, RB, q.Cin, bwd_sm + nB + nA, threadIdx.x, 32 * BW);
+                laid = a;
+                sc = q.scale ? q.scale[a] : 1.0f;
+                __syncthreads();
+            }
+        }
+        const T* base = q.base ? q.base + (size_t)n * q.Cin * P : nullptr;
+        T* dx = q.dx + (size_t)n * q.Cin * P;
+        if (a < 0) {
+            if (q.dx && q.dx != q.base) copy_tile<T, TP, (VEC > 0)>(base, dx, q.Cin, P, p0, 0, 1);
+            continue;
+        }
+        const T *xn = q.x + (size_t)n * q.Cin * P, *dyn = q.dy + (size_t)n * q.Cout * P;
+        const bool behind = p0 + (size_t)NP * g >= P;
+        T* mine = planes + warp * TP + NP * g;
+        Ti tile;
+        tile.zero();
+        if constexpr (VEC > 0) {
+            for (int grp = 0; grp < gB; ++grp) consume(tile, bwd_sm + lane + (size_t)grp * RB * Geo<T>::PARTS * 32);
+        } else {
+            if (p0 < P) first_product<T, RB, true>(tile, dyn, dy_end, q.Cout, P, p0, bwd_sm + lane, 0, 1);
+            if (behind) tile.zero();
+        }
+        tile.scale(sc);
+        store_planes<T, RB>(tile, mine + PARTS * PLANE, PITCH, PLANE);
+        if (nAt && p0 < P) second_product<T, RB, VEC, true>(tile, base, dx, q.Cin, P, p0, bwd_sm + nB + nA + lane, 0, 1, out, next_base);
+        tile.zero();
+        if constexpr (VEC > 0) {
+            for (int grp = 0; grp < gA; ++grp) consume(tile, bwd_sm + nB + lane + (size_t)grp * RB * Geo<T>::PARTS * 32);
+        } else {
+            if (p0 < P) first_product<T, RB, true>(tile, xn, x_end, q.Cin, P, p0, bwd_sm + nB + lane, 0, 1);
+            if (behind) tile.zero();
+        }
+        store_planes<T, RB>(tile, mine, PITCH, PLANE);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int blk = warp + BW * i;
+            if (blk >= all) continue;
+            const bool side = blk >= blocks0;                           // dy
+            const int c0 = 16 * (side ? blk - blocks0 : blk), C = side ? q.Cout : q.Cin;
+            const T* m0 = (side ? dyn : xn) + (size_t)min(c0 + g, C - 1) * P;     // channels behind the last one: sums that nobody reads
+            const T* m1 = (side ? dyn : xn) + (size_t)min(c0 + g + 8, C - 1) * P;
+            const T* end = side ? dy_end : x_end;
+            const T* plane = planes + (side ? 0 : PARTS * PLANE) + t * NP;
+#pragma unroll 2
+            for (int w = 0; w < BW; ++w) {
+                Words<NP * (int)sizeof(T) / 4> xw[2][2];                // [half of the tile][channel g, g + 8]
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const size_t p = pu + w * TP + h * (TP / 2) + t * NP;
+                    xw[h][0] = load_row<T, NP, (VEC > 0)>(m0, p, P, end);
+                    xw[h][1] = load_row<T, NP, (VEC > 0)>(m1, p, P, end);
+                }
+#pragma unroll
+                for (int jb = 0; jb < RB; ++jb) {
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const T* pl = plane + (8 * jb + g) * PITCH + w * TP + h * (TP / 2);
+                        grad_step<T>(d, xw[h][0], xw[h][1], pl, PLANE);
+                    }
+                    add(acc[i][jb], d);
+                }
+            }
+        }
+        __syncthreads();                                                // the planes are written again
+    }
+    if (a >= 0) flush(last);
+    if constexpr (VEC > 0) Fd::drain();
+    pdl_launch();
+}
+
+// dA and dB from the slots of bwd_kernel: 32 elements (channel in blocks of 16, rank) a CTA, eight threads an element, added in a fixed order.
+template <int RB>
+__global__ void __launch_bounds__(256) bwd_reduce(const float* __restrict__ part, const int32_t* __restrict__ ids, const float* __restrict__ scale,
+                                                  float* __restrict__ dA, float* __restrict__ dB, int N, int Cin, int Cout, int blocks0, int all, int r,
+                                                  int units, int share)
+{
+    __shared__ float sm[8][33];
+    pdl_wait();
+    const int a = blockIdx.y, e = blockIdx.x * 32 + threadIdx.x;        // (all * 16 * 8 RB is a multiple of 32)
+    const size_t pitch = (size_t)all * (16 * 8 * RB);
+    float s = 0.0f;
+    int count = 0;                                                      // slots of the adapter so far
+    for (int n = 0; n < N; ++n) {
+        if (ids[n] != a) continue;
+        const int k0 = (int)((long long)n * units / share), k1 = (int)(((long long)(n + 1) * units - 1) / share);
+        const int skip = (int)((threadIdx.y - (unsigned)count) & 7u);
+#pragma unroll 4
+        for (int k = k0 + skip; k <= k1; k += 8) s += part[(size_t)(k + n) * pitch + e];
+        count += k1 - k0 + 1;
+    }
+    sm[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += sm[i][threadIdx.x];
+    const int j = e % (8 * RB), c = e / (8 * RB);
+    if (j >= r) return;
+    if (c < 16 * blocks0) {
+        if (c < Cin) dA[((size_t)a * r + j) * Cin + c] = s;
+    } else {
+        const int o = c - 16 * blocks0;
+        if (o < Cout) dB[((size_t)a * Cout + o) * r + j] = scale ? scale[a] * s : s;
+    }
+}
+
 // ---- plans and launches -----------------------------------------------------------------------------
+inline int blocks_of(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : rank <= 32 ? 4 : 8; }
+
+// The one-kernel backward pass: its sums are 4 NB RB registers a thread, its unit is 4 tiles.
+template <typename T>
+struct Fused {
+    bool ok;
+    int nb, units, share, runs;
+};
+template <typename T>
+static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
+{
+    Fused<T> f{};
+    const int rb = blocks_of(rank), all = ceil_div(Cin, 16) + ceil_div(Cout, 16), unit = BW * Geo<T>::TP;
+    f.nb = all <= 2 * BW ? 2 : all <= 4 * BW ? 4 : 8;
+    f.units = (int)((P + unit - 1) / unit);
+    const long long total = (long long)N * f.units;
+    if (rb > 2 || all > 8 * BW || N > 4096 || total < AD_FUSED) return f;
+    const size_t smem = std::max(bwd_smem<T>(rb, Cin, Cout, true, false), bwd_smem<T>(rb, Cin, Cout, true, true));
+    if (smem > 113 * 1024) return f;                                      // two CTAs an SM
+    f.runs = (int)std::min(total, AD_RUNS * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
+    f.share = (int)((total + f.runs - 1) / f.runs);
+    f.runs = (int)((total + f.share - 1) / f.share);
+    f.ok = true;
+    return f;
+}
+
+// Factors that a CTA lays out for itself: while four CTAs of an SM have the room.
+template <typename T> static bool staged(int rb, int K, int M) { return 16 * (first_words<T>(rb, K) + (M ? second_words<T>(rb, M) : 0)) <= 40 * 1024; }
+
 struct Ws {
     void* first[2];
-    void* second[2];
+    void* second;
     void* tap[2];
     int32_t* order;
     int32_t* start;
@@ -841,32 +1258,36 @@ struct Ws {
     size_t total;
 };
 
-inline int blocks_of(int rank) { return rank <= 8 ? 1 : rank <= 16 ? 2 : rank <= 32 ? 4 : 8; }
-
 template <typename T>
 static Ws carve(void* ws, int N, int Cin, int Cout, size_t P, int R, int rank, bool bwd)
 {
     Ws w{};
-    const int rb = blocks_of(rank), TP = Geo<T>::TP;
+    const int rb = blocks_of(rank), TP = Geo<T>::TP, all = ceil_div(Cin, 16) + ceil_div(Cout, 16);
     size_t off = 0;
     char* b = static_cast<char*>(ws);
     auto take = [&](size_t bytes) { char* p = b ? b + off : nullptr; off += align_up(bytes, 256); return p; };
     if (!bwd) {
-        if (P > 1) {
+        if (P > 1 && !staged<T>(rb, Cin, Cout)) {
             w.first[0] = take((size_t)R * first_words<T>(rb, Cin) * 16);
-            w.second[0] = take((size_t)R * second_words<T>(rb, Cout) * 16);
+            w.second = take((size_t)R * second_words<T>(rb, Cout) * 16);
         }
         w.total = off;
         return w;
     }
+    // dy -> V -> dx alone, x -> U, and what the sums of the gradients need
+    w.first[0] = take((size_t)R * first_words<T>(rb, Cout) * 16);
+    w.second = take((size_t)R * second_words<T>(rb, Cin) * 16);
+    w.first[1] = take((size_t)R * first_words<T>(rb, Cin) * 16);
+    const Fused<T> f = fused_of<T>(N, Cin, Cout, P, rank);
+    if (f.ok) {
+        w.part = reinterpret_cast<float*>(take((size_t)(f.runs + N) * all * 16 * 8 * rb * 4));
+        w.total = off;
+        return w;
+    }
     w.Pp = (P + TP - 1) / TP * TP;
-    w.first[0] = take((size_t)R * first_words<T>(rb, Cout) * 16);       // B^T: dy -> V
-    w.second[0] = take((size_t)R * second_words<T>(rb, Cin) * 16);      // A^T: V -> dx
-    w.first[1] = take((size_t)R * first_words<T>(rb, Cin) * 16);        // A: x -> U
     for (int i = 0; i < 2; ++i) w.tap[i] = take((size_t)N * 8 * rb * w.Pp * (sizeof(T) == 2 ? 6 : 4));
     w.order = reinterpret_cast<int32_t*>(take((size_t)N * 4));
     w.start = reinterpret_cast<int32_t*>(take((size_t)(R + 1) * 4));
-    const int all = ceil_div(Cin, 16) + ceil_div(Cout, 16);
     const long long units = (long long)N * (w.Pp / TP);
     const long long want = (16LL * B200_SMS + all - 1) / all;
     w.ranges = (int)std::max(1LL, std::min(want, units));
@@ -876,59 +1297,71 @@ static Ws carve(void* ws, int N, int Cin, int Cout, size_t P, int R, int rank, b
 }
 
 // Warps that share a tile: more only while the tiles alone do not fill the GPU.
-// Partial sums of warps that share a tile, and the tiles on their way out where rows start anywhere.
-template <typename T> static size_t apply_smem(int warps, int rb, int ks, bool vec)
-{
-    const int np = lane_positions<T>(rb);
-    return (size_t)warps * ((ks > 1 ? (np / 2) * rb * 512 : 0) + (vec ? 0 : 16 * (8 * np + 4) * 4));
-}
 template <typename T>
 static void plan_apply(ApplyArgs<T>& q, int rb, int& warps)
 {
     const int tp = 8 * lane_positions<T>(rb);
     const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
-    const int parts = std::max(ceil_div(q.K, Geo<T>::GC), q.w2 ? ceil_div(q.M, 16) : 1);
+    const int most = std::max(ceil_div(q.K, Geo<T>::GC), q.f2.p ? ceil_div(q.M, 16) : 1);
     q.ks = 1;
-    while (q.ks < 8 && q.ks * 2 <= parts && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
-    warps = q.ks == 8 ? 8 : 4;
-    const int per = warps / q.ks;
-    q.tiles = (int)((tiles + per - 1) / per);
+    while (q.ks < 8 && q.ks * 2 <= most && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
+    if (!warps) warps = q.ks == 8 ? 8 : 4;
+    if (q.ks == 8) warps = 8;
+}
+template <typename T>
+static void plan_parts(ApplyArgs<T>& q, int rb, int warps, bool sm)
+{
+    const int tp = 8 * lane_positions<T>(rb), per = warps / q.ks;
+    const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
+    q.groups = (int)((tiles + per - 1) / per);
+    // a CTA that lays out its factors takes as many groups as leave four CTAs an SM (eight warps: two)
+    const int ctas = AD_CTAS * B200_SMS * (warps == 8 ? 2 : 4);
+    q.per_part = sm ? (int)std::max(1LL, std::min((long long)q.groups, (long long)q.N * q.groups / ctas)) : 1;
+    q.parts = ceil_div(q.groups, q.per_part);
+}
+// Factors, partial sums of warps that share a tile, and the tiles on their way out where rows start anywhere.
+template <typename T> static size_t apply_smem(const ApplyArgs<T>& q, int warps, int rb, bool vec, bool sm)
+{
+    const int np = lane_positions<T>(rb);
+    return (sm ? 16 * (first_words<T>(rb, q.K) + (q.f2.p ? second_words<T>(rb, q.M) : 0)) : 0) +
+           (size_t)warps * ((q.ks > 1 ? (np / 2) * rb * 512 : 0) + (vec ? AD_STAGES * Geo<T>::GC * 8 * np * (int)sizeof(T) : 16 * (8 * np + 4) * 4));
 }
 
-template <typename T, int RB, int VEC>
-static wcc_status run_apply(ApplyArgs<T> q0, ApplyArgs<T>* q1, int dev, cudaStream_t st)
+template <typename T, int RB, int VEC, bool SM>
+static wcc_status run_apply(ApplyArgs<T> q0, ApplyArgs<T>* q1, int dev, bool overlap, cudaStream_t st)
 {
-    int warps, warps1 = 0;
+    int warps = 0;
     plan_apply(q0, RB, warps);
+    if (q1) plan_apply(*q1, RB, warps);
+    plan_parts(q0, RB, warps, SM);
+    size_t smem = apply_smem(q0, warps, RB, VEC > 0, SM);
+    long long items1 = 0;
     if (q1) {
-        plan_apply(*q1, RB, warps1);
-        if (warps1 != warps) {          // one block size for the launch: the larger, whose other map then has more tiles a CTA
-            warps = std::max(warps, warps1);
-            for (ApplyArgs<T>* p : {&q0, q1}) {
-                const int tp = 8 * lane_positions<T>(RB);
-                const long long tiles = (long long)(((p->tap ? p->Pp : p->P) + tp - 1) / tp);
-                p->tiles = (int)((tiles + warps / p->ks - 1) / (warps / p->ks));
-            }
-        }
+        plan_parts(*q1, RB, warps, SM);
+        smem = std::max(smem, apply_smem(*q1, warps, RB, VEC > 0, SM));
+        items1 = (long long)q1->N * q1->parts;
     }
-    size_t smem = apply_smem<T>(warps, RB, q0.ks, VEC > 0);
-    if (q1) smem = std::max(smem, apply_smem<T>(warps, RB, q1->ks, VEC > 0));
-    const long long items = (long long)q0.N * q0.tiles, items1 = q1 ? (long long)q1->N * q1->tiles : 0;
+    const long long items = (long long)q0.N * q0.parts;
     if (items + items1 > 0x7FFFFFFFLL) return WCC_ERR_SHAPE;
     q0.items = (int)items;
     if (q1) q1->items = (int)items1;
-    wcc_status s = allow_smem<apply_kernel<T, RB, VEC>>(dev, (int)smem);
+    wcc_status s = allow_smem<apply_kernel<T, RB, VEC, SM>>(dev, (int)smem);
     if (s != WCC_OK) return s;
-    return launch_overlapped(apply_kernel<T, RB, VEC>, dim3((unsigned)(items + items1)), dim3((unsigned)(32 * warps)), smem, st, true, 1, q0, q1 ? *q1 : q0);
+    return launch_overlapped(apply_kernel<T, RB, VEC, SM>, dim3((unsigned)(items + items1)), dim3((unsigned)(32 * warps)), smem, st, overlap, 1, q0,
+                             q1 ? *q1 : q0);
 }
+// overlap: the kernel before it in the stream is the preparation.
 template <typename T>
-static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb, int dev, cudaStream_t st)
+static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb, int dev, bool overlap, cudaStream_t st)
 {
     const int np = lane_positions<T>(rb), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
-#define WCC_AD_APPLY(RB_)                                                                      \
-    if (rb == (RB_))                                                                           \
-        return vec == 2 ? run_apply<T, RB_, 2>(q0, q1, dev, st) : vec == 1 ? run_apply<T, RB_, 1>(q0, q1, dev, st) : run_apply<T, RB_, 0>(q0, q1, dev, st);
-    WCC_AD_APPLY(1) WCC_AD_APPLY(2) WCC_AD_APPLY(4) WCC_AD_APPLY(8)
+    const bool sm = !q0.w1;
+#define WCC_AD_APPLY(RB_, SM_)                                                                                                           \
+    if (rb == (RB_) && sm == (SM_))                                                                                                      \
+        return vec == 2 ? run_apply<T, RB_, 2, SM_>(q0, q1, dev, overlap, st) : vec == 1 ? run_apply<T, RB_, 1, SM_>(q0, q1, dev, overlap, st) \
+                                                                                         : run_apply<T, RB_, 0, SM_>(q0, q1, dev, overlap, st);
+    WCC_AD_APPLY(1, true) WCC_AD_APPLY(2, true) WCC_AD_APPLY(4, true) WCC_AD_APPLY(8, true)
+    WCC_AD_APPLY(1, false) WCC_AD_APPLY(2, false) WCC_AD_APPLY(4, false) WCC_AD_APPLY(8, false)
 #undef WCC_AD_APPLY
     return WCC_ERR_SHAPE;
 }
@@ -936,8 +1369,8 @@ static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb,
 template <typename T>
 static wcc_status launch_prep(const PrepArgs<T>& q, cudaStream_t st)
 {
-    const size_t words = std::max({q.first[0].p ? first_words<T>(q.rb, q.K[0]) : 0, q.first[1].p ? first_words<T>(q.rb, q.K[1]) : 0,
-                                   q.second[0].p ? second_words<T>(q.rb, q.M[0]) : 0, q.second[1].p ? second_words<T>(q.rb, q.M[1]) : 0});
+    const size_t words = std::max({q.first[0].p ? first_words<T>(q.rb, q.K[0]) : 1, q.first[1].p ? first_words<T>(q.rb, q.K[1]) : 1,
+                                   q.second.p ? second_words<T>(q.rb, q.M) : 1});
     const int stripes = (int)std::min<size_t>(64, (words + 255) / 256);
     return launch_overlapped(prep_kernel<T>, dim3((unsigned)q.R, (unsigned)stripes), dim3(256), 0, st, false, 1, q);
 }
@@ -958,17 +1391,20 @@ static wcc_status forward(const void* x, const void* A, const void* B, const flo
     }
     const Ws w = carve<T>(ws, N, Cin, Cout, P, R, rank, false);
     const int rb = blocks_of(rank);
-    PrepArgs<T> p{};
-    p.first[0] = Factor<T>{static_cast<const T*>(A), (long long)rank * Cin, Cin, 1};
-    p.second[0] = Factor<T>{static_cast<const T*>(B), (long long)Cout * rank, 1, rank};
-    p.first_out[0] = static_cast<uint4*>(w.first[0]); p.second_out[0] = static_cast<uint4*>(w.second[0]);
-    p.K[0] = Cin; p.M[0] = Cout; p.R = R; p.r = rank; p.rb = rb; p.N = N; p.ids = ids;
-    if ((s = launch_prep(p, st)) != WCC_OK) return s;
     ApplyArgs<T> q{};
-    q.src = static_cast<const T*>(x); q.w1 = static_cast<const uint4*>(w.first[0]); q.w2 = static_cast<const uint4*>(w.second[0]);
-    q.scale = scale; q.ids = ids; q.base = static_cast<const T*>(base); q.dst = static_cast<T*>(y);
-    q.P = P; q.N = N; q.K = Cin; q.M = Cout; q.R = R; q.status = di.status;
-    return launch_apply<T>(q, nullptr, rb, di.dev, st);
+    q.f1 = Factor<T>{static_cast<const T*>(A), (long long)rank * Cin, Cin, 1};
+    q.f2 = Factor<T>{static_cast<const T*>(B), (long long)Cout * rank, 1, rank};
+    if (w.first[0]) {
+        PrepArgs<T> p{};
+        p.first[0] = q.f1; p.second = q.f2;
+        p.first_out[0] = static_cast<uint4*>(w.first[0]); p.second_out = static_cast<uint4*>(w.second);
+        p.K[0] = Cin; p.M = Cout; p.R = R; p.r = rank; p.rb = rb; p.N = N; p.ids = ids;
+        if ((s = launch_prep(p, st)) != WCC_OK) return s;
+        q.w1 = p.first_out[0]; q.w2 = p.second_out;
+    }
+    q.src = static_cast<const T*>(x); q.scale = scale; q.ids = ids; q.base = static_cast<const T*>(base); q.dst = static_cast<T*>(y);
+    q.P = P; q.N = N; q.K = Cin; q.M = Cout; q.R = R; q.r = rank; q.status = di.status;
+    return launch_apply<T>(q, nullptr, rb, di.dev, q.w1 != nullptr, st);
 }
 
 template <typename T>
@@ -979,30 +1415,62 @@ static wcc_status backward(const void* dy, const void* x, const void* A, const v
     wcc_status s = device_info(di);
     if (s != WCC_OK) return s;
     const Ws w = carve<T>(ws, N, Cin, Cout, P, R, rank, true);
-    const int rb = blocks_of(rank);
+    const int rb = blocks_of(rank), all = ceil_div(Cin, 16) + ceil_div(Cout, 16);
     const bool vec = P % Geo<T>::NP == 0, params = dA != nullptr;
-    PrepArgs<T> p{};
-    p.first[0] = Factor<T>{static_cast<const T*>(B), (long long)Cout * rank, 1, rank};
-    if (dx) p.second[0] = Factor<T>{static_cast<const T*>(A), (long long)rank * Cin, Cin, 1};
-    if (params) p.first[1] = Factor<T>{static_cast<const T*>(A), (long long)rank * Cin, Cin, 1};
-    p.first_out[0] = static_cast<uint4*>(w.first[0]); p.first_out[1] = static_cast<uint4*>(w.first[1]); p.second_out[0] = static_cast<uint4*>(w.second[0]);
-    p.K[0] = Cout; p.K[1] = Cin; p.M[0] = Cin; p.R = R; p.r = rank; p.rb = rb; p.N = N; p.ids = ids;
-    if (params) { p.order = w.order; p.start = w.start; }
-    if ((s = launch_prep(p, st)) != WCC_OK) return s;
+    const Factor<T> fB{static_cast<const T*>(B), (long long)Cout * rank, 1, rank}, fAt{static_cast<const T*>(A), (long long)rank * Cin, Cin, 1}, fA = fAt;
+    const Fused<T> f = fused_of<T>(N, Cin, Cout, P, rank);
+    if (params && f.ok) {
+        BwdArgs<T> q{};
+        q.dy = static_cast<const T*>(dy); q.x = static_cast<const T*>(x); q.base = static_cast<const T*>(base); q.dx = static_cast<T*>(dx);
+        q.fB = fB; q.fAt = fAt; q.fA = fA; q.scale = scale; q.ids = ids; q.part = w.part; q.P = P; q.N = N; q.Cin = Cin; q.Cout = Cout; q.R = R;
+        q.r = rank; q.units = f.units; q.share = f.share; q.status = di.status;
+        const int v = P % (2 * Geo<T>::NP) == 0 ? 2 : vec ? 1 : 0;
+        const size_t smem = bwd_smem<T>(rb, Cin, Cout, dx != nullptr, v > 0);
+        const dim3 rgrid((unsigned)(all * 4 * rb), (unsigned)R);
+#define WCC_AD_BWD(RB_, VEC_, NB_)                                                                                                                \
+    if (rb == (RB_) && v == (VEC_) && f.nb == (NB_)) {                                                                                            \
+        if ((s = allow_smem<bwd_kernel<T, RB_, VEC_, NB_>>(di.dev, (int)smem)) != WCC_OK) return s;                                               \
+        s = launch_overlapped(bwd_kernel<T, RB_, VEC_, NB_>, dim3((unsigned)f.runs), dim3(32 * BW), smem, st, false, 1, q);                       \
+        if (s != WCC_OK) return s;                                                                                                                \
+        return launch_overlapped(bwd_reduce<RB_>, rgrid, dim3(32, 8), 0, st, true, 1, w.part, ids, scale, dA, dB, N, Cin, Cout, ceil_div(Cin, 16), \
+                                 all, rank, f.units, f.share);                                                                                    \
+    }
+#define WCC_AD_BWDS(RB_, VEC_) WCC_AD_BWD(RB_, VEC_, 2) WCC_AD_BWD(RB_, VEC_, 4) WCC_AD_BWD(RB_, VEC_, 8)
+        WCC_AD_BWDS(1, 0) WCC_AD_BWDS(1, 1) WCC_AD_BWDS(1, 2) WCC_AD_BWDS(2, 0) WCC_AD_BWDS(2, 1) WCC_AD_BWDS(2, 2)
+#undef WCC_AD_BWDS
+#undef WCC_AD_BWD
+        return WCC_ERR_SHAPE;
+    }
+    const bool sm = staged<T>(rb, Cout, dx ? Cin : 0) && (!params || staged<T>(rb, Cin, 0));
     ApplyArgs<T> q{}, u{};
-    q.src = static_cast<const T*>(dy); q.w1 = static_cast<const uint4*>(w.first[0]); q.w2 = dx ? static_cast<const uint4*>(w.second[0]) : nullptr;
-    q.scale = scale; q.ids = ids; q.base = static_cast<const T*>(base); q.dst = static_cast<T*>(dx); q.tap = params ? w.tap[0] : nullptr;
-    q.P = P; q.Pp = w.Pp; q.N = N; q.K = Cout; q.M = Cin; q.R = R; q.status = di.status;
+    q.f1 = fB;
+    if (dx) q.f2 = fAt;
+    if (!sm || params) {
+        PrepArgs<T> p{};
+        if (!sm) {
+            p.first[0] = fB;
+            if (dx) p.second = fAt;
+            if (params) p.first[1] = fA;
+            p.first_out[0] = static_cast<uint4*>(w.first[0]); p.first_out[1] = static_cast<uint4*>(w.first[1]); p.second_out = static_cast<uint4*>(w.second);
+            q.w1 = p.first_out[0]; q.w2 = p.second_out;
+        }
+        p.K[0] = Cout; p.K[1] = Cin; p.M = Cin; p.R = R; p.r = rank; p.rb = rb; p.N = N; p.ids = ids;
+        if (params) { p.order = w.order; p.start = w.start; }
+        if ((s = launch_prep(p, st)) != WCC_OK) return s;
+    }
+    q.src = static_cast<const T*>(dy); q.scale = scale; q.ids = ids; q.base = static_cast<const T*>(base); q.dst = static_cast<T*>(dx);
+    q.tap = params ? static_cast<T*>(w.tap[0]) : nullptr;
+    q.P = P; q.Pp = w.Pp; q.N = N; q.K = Cout; q.M = Cin; q.R = R; q.r = rank; q.status = di.status;
     u = q;
-    u.src = static_cast<const T*>(x); u.w1 = static_cast<const uint4*>(w.first[1]); u.w2 = nullptr; u.scale = nullptr; u.base = nullptr;
-    u.dst = nullptr; u.tap = w.tap[1]; u.K = Cin; u.M = 0;
-    if ((s = launch_apply<T>(q, params ? &u : nullptr, rb, di.dev, st)) != WCC_OK || !params) return s;
+    u.src = static_cast<const T*>(x); u.f1 = fA; u.f2 = Factor<T>{}; u.scale = nullptr; u.base = nullptr; u.dst = nullptr;
+    u.tap = static_cast<T*>(w.tap[1]); u.K = Cin; u.M = 0;
+    if (!sm) u.w1 = static_cast<uint4*>(w.first[1]);
+    if ((s = launch_apply<T>(q, params ? &u : nullptr, rb, di.dev, !sm || params, st)) != WCC_OK || !params) return s;
     GradArgs<T> h{};
     h.map[0] = static_cast<const T*>(x); h.map[1] = static_cast<const T*>(dy); h.plane[0] = w.tap[0]; h.plane[1] = w.tap[1];
     h.part = w.part; h.order = w.order; h.start = w.start; h.ids = ids; h.P = P; h.Pp = w.Pp;
     h.C[0] = Cin; h.C[1] = Cout; h.blocks[0] = ceil_div(Cin, 16); h.blocks[1] = ceil_div(Cout, 16);
     h.N = N; h.R = R; h.ranges = w.ranges; h.tiles = (int)(w.Pp / Geo<T>::TP);
-    const int all = h.blocks[0] + h.blocks[1];
     const dim3 grid((unsigned)(((long long)w.ranges * all + 7) / 8)), rgrid((unsigned)ceil_div(16 * all * 8 * rb, 256), (unsigned)R);
 #define WCC_AD_GRAD(RB_)                                                                                                                          \
     if (rb == (RB_)) {                                                                                                                            \

@@ -403,31 +403,35 @@ class Workspace:
 def _map_shape(x: torch.Tensor, name: str):
     """(N, C, H, W) of a map [N][C][H][W] or of rows [N][C], which are maps of one position."""
     _dev(x, name)
-    if x.dim() == 2:
-        return (x.shape[0], x.shape[1], 1, 1)
-    if x.dim() != 4:
+    if x.dim() == 4:
+        return x.shape
+    if x.dim() != 2:
         raise ValueError("%s must be [N][C][H][W] or [N][C]" % name)
-    return tuple(x.shape)
+    return (x.shape[0], x.shape[1], 1, 1)
 
 
-def _same(t: torch.Tensor, like: torch.Tensor, name: str, what: str):
-    """t is a tensor of `like`'s shape, type and device, contiguous as every map."""
-    _dev(t, name)
-    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError("%s must have the shape, type and device of %s" % (name, what))
+def _here(x: torch.Tensor) -> int:
+    """The device of a call's map.  The library launches on the current device's current stream: maps of another device are refused."""
+    dev = x.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError("the map is on cuda:%d, which is not the current device" % dev)
+    return dev
 
 
-def _fp32(t, shape, like: torch.Tensor, name: str):
-    if t is not None:
-        _dev(t, name)
-        if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or t.device != like.device:
-            raise ValueError("%s must be float32 %s on the device of the map" % (name, list(shape)))
+def _same(t: torch.Tensor, like: torch.Tensor, dev: int, name: str, what: str) -> int:
+    """The address of t, which must have `like`'s shape and type on device `dev`, contiguous as every map."""
+    if not (t.get_device() == dev and t.is_contiguous() and t.dtype == like.dtype and t.shape == like.shape):
+        raise ValueError("%s must be contiguous, of the shape, type and device of %s" % (name, what))
+    return t.data_ptr()
 
 
-def _on(t: torch.Tensor):
-    """The library launches on the current device's current stream: tensors of another device are refused."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("the map is on %s, which is not the current device" % t.device)
+def _floats(t, n: int, dev: int, name: str, rows: int = 0):
+    """The address of t, None or fp32 [n] (with `rows`: [rows][n]) on device `dev`."""
+    if t is None:
+        return None
+    if not (t.get_device() == dev and t.is_contiguous() and t.dtype == torch.float32 and t.shape == ((rows, n) if rows else (n,))):
+        raise ValueError("%s must be contiguous float32 %s on the device of the map" % (name, [rows, n] if rows else [n]))
+    return t.data_ptr()
 
 
 def layernorm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5,
@@ -435,20 +439,18 @@ def layernorm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Te
     """Layer norm over the channels of a map [N][C][H][W] (or of rows [N][C]), fp32 ``gamma`` and ``beta`` [C] or None.
     Returns y (``y`` may be x), or with ``stats`` (y, mean, rstd), the statistics fp32 [N][H*W] as the backward pass reads them."""
     N, Cc, H, W = _map_shape(x, "x")
-    dt = _dt(x)
-    _on(x)
-    _fp32(gamma, (Cc,), x, "gamma")
-    _fp32(beta, (Cc,), x, "beta")
+    dt, dev = _dt(x), _here(x)
+    pg, pb = _floats(gamma, Cc, dev, "gamma"), _floats(beta, Cc, dev, "beta")
     if y is None:
         y = torch.empty_like(x)
-    elif y is not x:
-        _same(y, x, "y", "x")
-    mean = rstd = None
+        py = y.data_ptr()
+    else:
+        py = _same(y, x, dev, "y", "x")
+    mean = rstd = pm = pr = None
     if stats:
-        mean = torch.empty((N, H * W), dtype=torch.float32, device=x.device)
-        rstd = torch.empty((N, H * W), dtype=torch.float32, device=x.device)
-    _check(lib().wcc_layernorm_fwd(x.data_ptr(), _ptr(gamma), _ptr(beta), N, Cc, H, W, eps, dt, y.data_ptr(), _ptr(mean), _ptr(rstd),
-                                   _stream()), "wcc_layernorm_fwd")
+        mean, rstd = x.new_empty((N, H * W), dtype=torch.float32), x.new_empty((N, H * W), dtype=torch.float32)
+        pm, pr = mean.data_ptr(), rstd.data_ptr()
+    _check(lib().wcc_layernorm_fwd(x.data_ptr(), pg, pb, N, Cc, H, W, eps, dt, py, pm, pr, _stream()), "wcc_layernorm_fwd")
     return (y, mean, rstd) if stats else y
 
 
@@ -457,25 +459,22 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
     """The gradients of ``layernorm``: (dx, dgamma, dbeta), the last two fp32 [C] and None without ``params``.
     ``dx`` may be dy or x.  ``ws`` is a ``Workspace.for_layernorm_backward``, allocated here if it is not given."""
     N, Cc, H, W = _map_shape(x, "x")
-    dt = _dt(x)
-    _on(x)
-    _same(dy, x, "dy", "x")
-    _fp32(mean, (N, H * W), x, "mean")
-    _fp32(rstd, (N, H * W), x, "rstd")
-    _fp32(gamma, (Cc,), x, "gamma")
+    dt, dev = _dt(x), _here(x)
+    pdy, pg = _same(dy, x, dev, "dy", "x"), _floats(gamma, Cc, dev, "gamma")
+    pm, pr = _floats(mean, H * W, dev, "mean", N), _floats(rstd, H * W, dev, "rstd", N)
     if dx is None:
         dx = torch.empty_like(x)
-    elif dx is not x and dx is not dy:
-        _same(dx, x, "dx", "x")
-    dgamma = dbeta = None
+        pdx = dx.data_ptr()
+    else:
+        pdx = _same(dx, x, dev, "dx", "x")
+    dgamma = dbeta = pdg = pdb = pw = None
+    nw = 0
     if params:
-        dgamma = torch.empty((Cc,), dtype=torch.float32, device=x.device)
-        dbeta = torch.empty((Cc,), dtype=torch.float32, device=x.device)
+        dgamma, dbeta = x.new_empty((Cc,), dtype=torch.float32), x.new_empty((Cc,), dtype=torch.float32)
         if ws is None:
             ws = Workspace.for_layernorm_backward(x)
-    _check(lib().wcc_layernorm_bwd(dy.data_ptr(), x.data_ptr(), _ptr(gamma), mean.data_ptr(), rstd.data_ptr(), N, Cc, H, W, dt,
-                                   dx.data_ptr(), _ptr(dgamma), _ptr(dbeta), ws.buf.data_ptr() if params else None,
-                                   ws.nbytes if params else 0, _stream()), "wcc_layernorm_bwd")
+        pdg, pdb, pw, nw = dgamma.data_ptr(), dbeta.data_ptr(), ws.buf.data_ptr(), ws.nbytes
+    _check(lib().wcc_layernorm_bwd(pdy, x.data_ptr(), pg, pm, pr, N, Cc, H, W, dt, pdx, pdg, pdb, pw, nw, _stream()), "wcc_layernorm_bwd")
     return dx, dgamma, dbeta
 
 
@@ -498,72 +497,84 @@ class Adapters:
             raise ValueError("B must be [R][Cout][rank] of A's type on A's device")
         if not 1 <= self.rank <= MAX_RANK:
             raise ValueError("the rank must be 1 to %d" % MAX_RANK)
-        _fp32(scale, (self.R,), A, "scale")
+        _floats(scale, self.R, A.get_device(), "scale")
         self.A, self.B, self.scale = A, B, scale
+        self._ws_bytes = {}
 
     def workspace(self, x: torch.Tensor, backward: bool = True) -> Workspace:
         """Scratch for calls on maps of x's shape; that for the backward pass also serves the forward pass."""
-        N, _, H, W = self._args(x, None)
-        n = [int(lib().wcc_adapters_workspace_bytes(N, self.Cin, self.Cout, H, W, self.R, self.rank, self.dt, b)) for b in ((0, 1) if backward else (0,))]
-        if min(n) == 0:
-            raise WccError(2, "wcc_adapters_workspace_bytes")
-        return Workspace(max(n), x.device)
+        N, _, H, W = self._shape(x)
+        n = self._bytes(N, H, W, False)
+        return Workspace(max(n, self._bytes(N, H, W, True)) if backward else n, x.device)
 
-    def _args(self, x, ids):
+    def _bytes(self, N, H, W, backward):
+        n = self._ws_bytes.get((N, H, W, backward))
+        if n is None:
+            n = int(lib().wcc_adapters_workspace_bytes(N, self.Cin, self.Cout, H, W, self.R, self.rank, self.dt, int(backward)))
+            if n == 0:
+                raise WccError(2, "wcc_adapters_workspace_bytes")
+            self._ws_bytes[N, H, W, backward] = n
+        return n
+
+    def _scratch(self, x, N, H, W, backward, ws):
+        if ws is not None:
+            return ws.buf, ws.nbytes
+        n = self._bytes(N, H, W, backward)
+        return x.new_empty((n,), dtype=torch.uint8), n
+
+    def _shape(self, x):
         shape = _map_shape(x, "x")
-        if _dt(x) != self.dt or shape[1] != self.Cin or x.device != self.A.device:
+        if x.dtype != self.A.dtype or shape[1] != self.Cin or x.get_device() != self.A.get_device():
             raise ValueError("x must have the adapters' type, Cin channels and device")
-        if ids is not None:
-            _dev(ids, "ids")
-            if ids.dtype != torch.int32 or tuple(ids.shape) != (shape[0],) or ids.device != x.device:
-                raise ValueError("ids must be int32 [N] on the device of the map")
         return shape
 
-    def _map(self, t, x, C, name):
-        """A map of x's sizes with C channels."""
-        if _map_shape(t, name) != (x.shape[0], C) + tuple(x.shape[2:] if x.dim() == 4 else (1, 1)) or t.dtype != x.dtype or t.device != x.device:
-            raise ValueError("%s must be a map of %d channels with x's sizes, type and device" % (name, C))
+    @staticmethod
+    def _ids(ids, N, dev):
+        if not (ids.get_device() == dev and ids.is_contiguous() and ids.dtype == torch.int32 and ids.shape == (N,)):
+            raise ValueError("ids must be contiguous int32 [N] on the device of the map")
+        return ids.data_ptr()
+
+    @staticmethod
+    def _map(t, x, C, dev, name):
+        """The address of a map of x's sizes with C channels; None stays None."""
+        if t is None:
+            return None
+        if not (t.get_device() == dev and t.is_contiguous() and t.dtype == x.dtype and t.dim() == x.dim() and t.shape[0] == x.shape[0] and
+                t.shape[1] == C and t.shape[2:] == x.shape[2:]):
+            raise ValueError("%s must be a contiguous map of %d channels with x's sizes, type and device" % (name, C))
+        return t.data_ptr()
 
     def __call__(self, x: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None, y: torch.Tensor | None = None,
                  ws: Workspace | None = None) -> torch.Tensor:
-        N, _, H, W = self._args(x, ids)
-        _on(x)
-        if base is not None:
-            self._map(base, x, self.Cout, "base")
+        N, _, H, W = self._shape(x)
+        dev, px = _here(x), x.data_ptr()
+        pi, pb = self._ids(ids, N, dev), self._map(base, x, self.Cout, dev, "base")
         if y is None:
-            y = torch.empty((N, self.Cout) + tuple(x.shape[2:]), dtype=x.dtype, device=x.device)
-        else:
-            self._map(y, x, self.Cout, "y")
-            if y.data_ptr() == x.data_ptr():
-                raise ValueError("y must not be x")
-        if ws is None:
-            ws = self.workspace(x, backward=False)
-        _check(lib().wcc_adapters_fwd(x.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), ids.data_ptr(), _ptr(base), N, self.Cin,
-                                      self.Cout, H, W, self.R, self.rank, self.dt, y.data_ptr(), ws.buf.data_ptr(), ws.nbytes, _stream()),
-               "wcc_adapters_fwd")
+            y = x.new_empty((N, self.Cout) + tuple(x.shape[2:]))
+        py = self._map(y, x, self.Cout, dev, "y")
+        if py == px:
+            raise ValueError("y must not be x")
+        buf, n = self._scratch(x, N, H, W, False, ws)
+        _check(lib().wcc_adapters_fwd(px, self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), pi, pb, N, self.Cin, self.Cout, H, W, self.R,
+                                      self.rank, self.dt, py, buf.data_ptr(), n, _stream()), "wcc_adapters_fwd")
         return y
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None, dx: torch.Tensor | None = None,
                  params: bool = True, ws: Workspace | None = None):
         """(dx, dA, dB): dx = base + the adapters' part of the map's gradient, dA and dB fp32 in the factors' shapes (None without ``params``)."""
-        N, _, H, W = self._args(x, ids)
-        _on(x)
-        self._map(dy, x, self.Cout, "dy")
-        if base is not None:
-            self._map(base, x, self.Cin, "base")
+        N, _, H, W = self._shape(x)
+        dev, px = _here(x), x.data_ptr()
+        pi, pdy, pb = self._ids(ids, N, dev), self._map(dy, x, self.Cout, dev, "dy"), self._map(base, x, self.Cin, dev, "base")
         if dx is None:
             dx = torch.empty_like(x)
-        else:
-            self._map(dx, x, self.Cin, "dx")
-            if dx.data_ptr() in (x.data_ptr(), dy.data_ptr()):
-                raise ValueError("dx must not be x or dy")
-        dA = torch.empty(self.A.shape, dtype=torch.float32, device=x.device) if params else None
-        dB = torch.empty(self.B.shape, dtype=torch.float32, device=x.device) if params else None
-        if ws is None:
-            ws = self.workspace(x)
-        _check(lib().wcc_adapters_bwd(dy.data_ptr(), x.data_ptr(), self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), ids.data_ptr(), _ptr(base),
-                                      N, self.Cin, self.Cout, H, W, self.R, self.rank, self.dt, dx.data_ptr(), _ptr(dA), _ptr(dB),
-                                      ws.buf.data_ptr(), ws.nbytes, _stream()), "wcc_adapters_bwd")
+        pdx = self._map(dx, x, self.Cin, dev, "dx")
+        if pdx == px or pdx == pdy:
+            raise ValueError("dx must not be x or dy")
+        dA = x.new_empty(self.A.shape, dtype=torch.float32) if params else None
+        dB = x.new_empty(self.B.shape, dtype=torch.float32) if params else None
+        buf, n = self._scratch(x, N, H, W, True, ws)
+        _check(lib().wcc_adapters_bwd(pdy, px, self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), pi, pb, N, self.Cin, self.Cout, H, W, self.R,
+                                      self.rank, self.dt, pdx, _ptr(dA), _ptr(dB), buf.data_ptr(), n, _stream()), "wcc_adapters_bwd")
         return dx, dA, dB
 
 

@@ -301,5 +301,5 @@ def test_binding_refusals(wcc):      # noqa: F811
     with pytest.raises(TypeError):
         wcc.Adapters(d["A"].half(), d["B"].half())
     with pytest.raises(wcc.WccError) as e:
-        ad(x, ids, ws=wcc.Workspace(256, x.device))
+        ad.backward(dy, x, ids, ws=wcc.Workspace(256, x.device))
     assert e.value.code == 7
