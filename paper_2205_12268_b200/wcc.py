@@ -581,14 +581,24 @@ class Adapters:
 def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits: int = 8, y: torch.Tensor | None = None,
             ws: Workspace | None = None, taps: bool = False, staged: bool = False, alpha: float = 0.0, wbits: int = 0,
             relu: bool = False, residual: torch.Tensor | None = None, Wq: torch.Tensor | None = None,
-            scale_w: torch.Tensor | None = None):
+            scale_w: torch.Tensor | None = None, adapters: Adapters | None = None, ids: torch.Tensor | None = None):
     """The WCC layer.  Returns y, or (y, dict of intermediate tensors) when ``taps`` is set (True: all of them; or an
     iterable of names out of coef, nrm2, idx, acc, Xq / Xb, scale_a, Wq, scale_w).
     ``staged`` selects wcc_forward_staged (every intermediate in memory) instead of the fused wcc_forward.
     ``alpha``, ``wbits``, ``relu``, ``residual``, ``Wq`` + ``scale_w``: the options of wcc_forward_ex (see wcc.h);
-    with pre-quantized weights ``Wt`` may be None."""
+    with pre-quantized weights ``Wt`` may be None.
+    ``adapters`` with ``ids`` (int32 [N], negative: none): low-rank adapters beside the layer's projection.  Their sum (and ``residual``) is written to y
+    in the map's type and enters the layer as its residual, so the ReLU comes after it."""
     _dev(x, "x")
     N, Cin, H, W = x.shape
+    if adapters is not None:
+        if ids is None:
+            raise ValueError("adapters need ids")
+        if staged:
+            raise ValueError("options are only available on the fused path")
+        if adapters.Cin != Cin or adapters.Cout != (Wt if Wq is None else Wq).shape[0]:
+            raise ValueError("the adapters must have the layer's channels")
+        y = residual = adapters(x, ids, base=residual, y=y)
     use_ex = bool(alpha > 0.0 or wbits or relu or residual is not None or Wq is not None)
     if Wq is not None:
         _dev(Wq, "Wq")
@@ -652,9 +662,14 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
 class Chain:
     """A chain of pointwise WCC layers (wcc_chain_forward): ``weights[i]`` is layer i's fp32 [Cout][Cin] device tensor;
     a ReLU follows every layer but (unless ``relu_last``) the last; ``alphas[i]`` > 0 fixes layer i's clipping parameter.
-    The workspace (intermediate maps included) is allocated once, here."""
+    The workspace (intermediate maps included) is allocated once, here.
 
-    def __init__(self, x: torch.Tensor, weights, levels: int, k: int, bits: int = 8, relu_last: bool = False, alphas=None):
+    ``norms[i]`` = (gamma, beta, eps): layer i's input is normalised over its channels first (``layernorm``; gamma and beta may be None);
+    ``adapters[i]``: ``Adapters`` beside layer i, taken by the ``ids`` of the call.  Either list may hold None for layers without.  Such a chain runs
+    layer by layer."""
+
+    def __init__(self, x: torch.Tensor, weights, levels: int, k: int, bits: int = 8, relu_last: bool = False, alphas=None, norms=None,
+                 adapters=None):
         _dev(x, "x")
         self.N, cin, self.H, self.W = x.shape
         self.levels, self.k, self.bits, self.dt = levels, k, bits, _dt(x)
@@ -672,12 +687,62 @@ class Chain:
         nbytes = int(lib().wcc_chain_workspace_bytes(self.layers, n, self.N, self.H, self.W, levels, k, bits, self.dt))
         if nbytes == 0:
             raise WccError(2, "wcc_chain_workspace_bytes")
+        self.norms, self.adapters = ([None] * n if v is None else list(v) for v in (norms, adapters))
+        if len(self.norms) != n or len(self.adapters) != n:
+            raise ValueError("norms and adapters must have an entry for each layer")
+        self.plain = not any(v is not None for v in self.norms + self.adapters)
+        if not self.plain:
+            self._prepare(x)
+            return
         self.ws = Workspace(nbytes, x.device)
 
-    def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None) -> torch.Tensor:
+    def _prepare(self, x: torch.Tensor):
+        """What a chain that runs layer by layer keeps: two intermediate maps, a normalised one, and scratch for any of its calls."""
+        n, wide, normed, nbytes = len(self.weights), 0, 0, 0
+        for i, layer in enumerate(self.layers):
+            Cin, Cout = layer.Cin, layer.Cout
+            if i + 1 < n:
+                wide = max(wide, Cout)
+            if self.norms[i] is not None:
+                gamma, beta, _ = self.norms[i]
+                _floats(gamma, Cin, x.get_device(), "norms[%d]: gamma" % i)
+                _floats(beta, Cin, x.get_device(), "norms[%d]: beta" % i)
+                normed = max(normed, Cin)
+            if self.adapters[i] is not None:
+                a = self.adapters[i]
+                if (a.Cin, a.Cout, a.dt) != (Cin, Cout, self.dt) or a.A.device != x.device:
+                    raise ValueError("adapters[%d] must have the layer's channels and the map's type and device" % i)
+                nbytes = max(nbytes, a._bytes(self.N, self.H, self.W, False))
+            nbytes = max(nbytes, int(lib().wcc_workspace_bytes(self.N, Cin, Cout, self.H, self.W, self.levels, self.k, self.bits, self.dt)))
+        self.ws = Workspace(nbytes, x.device)
+        room = self.N * self.H * self.W
+        self.between = [x.new_empty((room * wide,)) for _ in range(2 if n > 2 else 1)] if n > 1 else []
+        self.normed = x.new_empty((room * normed,)) if normed else None
+
+    def _run(self, x: torch.Tensor, y: torch.Tensor, ids) -> torch.Tensor:
+        n = len(self.weights)
+        if ids is None and any(a is not None for a in self.adapters):
+            raise ValueError("adapters need ids")
+        for i, layer in enumerate(self.layers):
+            shape = (self.N, layer.Cin, self.H, self.W)
+            if self.norms[i] is not None:
+                gamma, beta, eps = self.norms[i]
+                x = layernorm(x, gamma, beta, eps, y=self.normed[:x.numel()].view(shape))
+            out = y if i + 1 == n else self.between[i % len(self.between)][:self.N * layer.Cout * self.H * self.W].view(self.N, layer.Cout, self.H, self.W)
+            residual = None
+            if self.adapters[i] is not None:
+                residual = self.adapters[i](x, ids, y=out, ws=self.ws)
+            x = forward(x, self.weights[i], self.levels, self.k, self.bits, y=out, ws=self.ws, alpha=layer.alpha, relu=bool(layer.relu), residual=residual)
+        return x
+
+    def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None, ids: torch.Tensor | None = None) -> torch.Tensor:
         _dev(x, "x")
         if y is None:
             y = torch.empty((self.N, self.Cout, self.H, self.W), dtype=x.dtype, device=x.device)
+        if not self.plain:
+            if tuple(x.shape) != (self.N, self.layers[0].Cin, self.H, self.W) or _dt(x) != self.dt:
+                raise ValueError("x must have the shape and type the chain was made for")
+            return self._run(x, y, ids)
         _check(lib().wcc_chain_forward(x.data_ptr(), self.layers, len(self.weights), self.N, self.H, self.W, self.levels,
                                        self.k, self.bits, y.data_ptr(), self.dt, self.ws.buf.data_ptr(), self.ws.nbytes,
                                        _stream()), "wcc_chain_forward")
