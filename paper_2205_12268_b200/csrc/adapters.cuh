@@ -303,8 +303,8 @@ __global__ void __launch_bounds__(256) prep_kernel(PrepArgs<T> q)
 }
 
 // ---- the two products over a warp's tile of positions ---------------------------------------------
-template <typename T, int RB> struct Tile {
-    static constexpr int NP = lane_positions<T>(RB), TP = 8 * NP, MB = NP / 2;
+template <typename T, int RB, int NP_> struct Tile {
+    static constexpr int NP = NP_, TP = 8 * NP, MB = NP / 2;
     float acc[MB][RB][4];               // of position NP g + b, rank 8 jb + 2 t + e: [b / 2][jb][2 (b % 2) + e]
     __device__ __forceinline__ void zero()
     {
@@ -314,6 +314,17 @@ template <typename T, int RB> struct Tile {
             for (int jb = 0; jb < RB; ++jb)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[mb][jb][i] = 0.0f;
+    }
+    // positions from `n` on of this lane's NP are nothing
+    __device__ __forceinline__ void keep(int n)
+    {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int jb = 0; jb < RB; ++jb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (2 * mb + (i >> 1) >= n) acc[mb][jb][i] = 0.0f;
     }
     __device__ __forceinline__ void scale(float s)
     {
@@ -328,10 +339,10 @@ template <typename T, int RB> struct Tile {
 template <bool SM> __device__ __forceinline__ uint4 load_factor(const uint4* p) { return SM ? *p : __ldg(p); }
 
 // Adds a group of channels to the first product: x holds this lane's channels of it, wg points at this lane's words of the factor.
-template <typename T, int RB, bool SM>
-__device__ __forceinline__ void first_step(Tile<T, RB>& tile, const Words<Tile<T, RB>::NP * (int)sizeof(T) / 4> (&x)[Geo<T>::CL], const uint4* wg)
+template <typename T, int RB, bool SM, int NP>
+__device__ __forceinline__ void first_step(Tile<T, RB, NP>& tile, const Words<NP * (int)sizeof(T) / 4> (&x)[Geo<T>::CL], const uint4* wg)
 {
-    constexpr int MB = Tile<T, RB>::MB, CL = Geo<T>::CL;
+    constexpr int MB = NP / 2, CL = Geo<T>::CL;
             if constexpr (sizeof(T) == 2) {
                 uint32_t fa[2][MB][4];
     #pragma unroll
@@ -380,107 +391,139 @@ __device__ __forceinline__ void first_step(Tile<T, RB>& tile, const Words<Tile<T
             }
 }
 
-// The maps of first products on their way through shared memory, where rows start on vectors: a warp copies the groups of channels ahead of
-// their use, also those of its next tile while it writes the last one, and waits for nobody else.  One group in a stage, [GC rows][8 pieces of
-// NP positions], pieces exchanged so that the eight lanes of a phase (two g, four t) read from different banks.  Rows behind the last channel and
-// pieces behind the last position arrive as zeros.  With plain loads into registers the maps came no faster than 4.9 TB/s (headline batch 57 us).
-template <typename T, int RB>
+// The maps of first products and the bases of second ones on their way through shared memory: a warp copies the groups of channels ahead of
+// their use, also those of its next tile while it writes the last one, and waits for nobody else.
+//  - AL, rows that start on vectors: a stage is [GC rows][8 pieces of NP positions], pieces exchanged so that the eight lanes of a phase (two g,
+//    four t) read from different banks.
+//  - rows that start anywhere: the aligned pieces of 16 bytes around the tile's part of each row, as they lie; the reader shifts.  Single loads of 2
+//    bytes cost eight times the instructions, and one after the other: 58 -> 70 channels of 129 x 257 bf16 77 us, shifted in registers 31.
+// Rows behind the last channel arrive as zeros; positions behind the last one as zeros (AL) or as what follows them, and nobody keeps what is
+// made of them.  With plain loads into registers the maps came no faster than 4.9 TB/s (headline batch, 57 us without those of the base).
+template <typename T, int NP, bool AL>
 struct Feed {
-    static constexpr int NP = Tile<T, RB>::NP, GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), STAGE = GC * 8 * PIECE, S = AD_STAGES;
-    uint32_t base;
-    int head, tail;                     // stages filled and used so far
-    __device__ __forceinline__ explicit Feed(void* warp_smem) : base((uint32_t)__cvta_generic_to_shared(warp_smem)), head(0), tail(0) {}
+    static constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), S = AD_STAGES, W = PIECE / 4;
+    static constexpr int ROW = 8 * PIECE, PITCH = ROW + (AL ? 0 : 16), CH = PITCH / 16, STAGE = GC * PITCH;
+    uint32_t base, fill, use;           // shared address, offsets of the stages to fill and to use next
+    size_t off;                         // AL: this lane's first row and piece of a stage, from the stage's first channel at position 0; else p0
+    bool in;                            // that piece exists
+    __device__ __forceinline__ explicit Feed(void* warp_smem) : base((uint32_t)__cvta_generic_to_shared(warp_smem)), fill(0), use(0), off(0), in(false) {}
+    // The following stages are of the tile at p0.
+    __device__ __forceinline__ void at(size_t P, size_t p0)
+    {
+        const int lane = threadIdx.x & 31;
+        const size_t p = p0 + (size_t)(NP * (lane & 7));
+        in = p < P;
+        off = AL ? (size_t)(lane >> 3) * P + (in ? p : 0) : p0;
+    }
     // A stage of a first product's group, or (BASE) of 16 channels of a second product's base: rows from `row0` (its first channel, at position 0),
-    // `left` channels of them exist.  left <= 0: an empty stage.
+    // `left` > 0 channels of them exist; `end`: behind the tensor.  commit() follows; without an issue before it the stage stays empty.
     template <bool BASE>
-    __device__ __forceinline__ void issue(const T* row0, int left, size_t P, size_t p0)
+    __device__ __forceinline__ void issue(const T* row0, int left, size_t P, const T* end)
     {
         constexpr int ROWS = BASE ? 16 : GC;
-        const int lane = threadIdx.x & 31, r0 = lane >> 3, c = lane & 7;
-        const bool in = p0 + (size_t)(NP * c) < P;
-        const T* src = row0 + (size_t)r0 * P + (in ? p0 + (size_t)(NP * c) : 0);
-        const uint32_t dst = base + (uint32_t)(head % S) * STAGE;
-        if (left > 0) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (AL) {
+            const int r0 = lane >> 3, c = lane & 7;
+            const T* src = row0 + off;
+            const uint32_t dst = base + fill + (uint32_t)(r0 * ROW);
 #pragma unroll
-            for (int k = 0; k < ROWS / 4; ++k) {
-                const int r = r0 + 4 * k;
-                const bool have = r < left;
-                const uint32_t d = dst + (uint32_t)((r * 8 + (c ^ (BASE ? r & 1 : swap(r)))) * PIECE);
-                const T* q = have ? src + (size_t)(4 * k) * P : row0;
+            for (int k = 0; k < ROWS / 4; ++k, src += 4 * P) {
+                const bool have = r0 + 4 * k < left;
+                const int sw = BASE ? r0 & 1 : PIECE == 16 ? 2 * ((4 * k / CL) & 3) : 4 * ((4 * k / CL) & 1);      // (r0 < 4 <= CL)
+                const uint32_t d = dst + (uint32_t)(k * 4 * ROW + (c ^ sw) * PIECE);
                 const int bytes = have && in ? PIECE : 0;
-                if constexpr (PIECE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(q), "r"(bytes) : "memory");
-                else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(d), "l"(q), "r"(bytes) : "memory");
+                if constexpr (PIECE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(have ? src : row0), "r"(bytes) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(d), "l"(have ? src : row0), "r"(bytes) : "memory");
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < (ROWS * CH + 31) / 32; ++k) {
+                const int i = lane + 32 * k, r = i / CH, ch = i - r * CH;
+                if (r >= ROWS) break;
+                const bool have = r < left;
+                const T* row = row0 + (size_t)(have ? r : 0) * P;
+                const char* src = reinterpret_cast<const char*>((reinterpret_cast<uintptr_t>(row + off) & ~(uintptr_t)15) + 16 * ch);
+                const bool any = have && off < P && src < reinterpret_cast<const char*>(row + P);
+                const long long rest = reinterpret_cast<const char*>(end) - src;      // (a tensor starts on 16 bytes, it may end anywhere)
+                const int bytes = any ? (rest < 16 ? (int)rest : 16) : 0;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"(base + fill + (uint32_t)(r * PITCH + 16 * ch)), "l"(any ? src : reinterpret_cast<const char*>((reinterpret_cast<uintptr_t>(row0) & ~(uintptr_t)15))), "r"(bytes) : "memory");
             }
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        ++head;
     }
-    static __device__ __forceinline__ int swap(int r) { return PIECE == 16 ? 2 * ((r / CL) & 3) : 4 * ((r / CL) & 1); }
+    __device__ __forceinline__ void commit()
+    {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        fill = fill == (S - 1) * STAGE ? 0 : fill + STAGE;
+    }
     // Waits for the next stage; the stage before it may be filled again behind this.
     __device__ __forceinline__ void wait()
     {
         asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
         __syncwarp();
     }
-    __device__ __forceinline__ void take(Words<PIECE / 4> (&x)[CL])
+    static __device__ __forceinline__ void read(uint32_t a, uint32_t* w)
+    {
+        if constexpr (PIECE == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+        else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
+    }
+    // Where a row that starts at `row` (its address at p0) begins in the 16 bytes that hold it.
+    static __device__ __forceinline__ uint32_t skew(const T* row0, size_t P, size_t p0, int r)
+    {
+        return ((uint32_t)reinterpret_cast<uintptr_t>(row0) + ((uint32_t)p0 + (uint32_t)r * (uint32_t)P) * (uint32_t)sizeof(T)) & 15u;
+    }
+    // row0, p0: as in issue and at (rows that start anywhere)
+    __device__ __forceinline__ void take(Words<W> (&x)[CL], const T* row0, size_t P, size_t p0)
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-        const uint32_t src = base + (uint32_t)(tail % S) * STAGE;
+        if constexpr (AL) {
+            const uint32_t a = base + use + (uint32_t)(t * CL * ROW + (g ^ (PIECE == 16 ? 2 * t : 4 * (t & 1))) * PIECE);
 #pragma unroll
-        for (int i = 0; i < CL; ++i) {
-            const int r = t * CL + i;
-            const uint32_t d = src + (uint32_t)((r * 8 + (g ^ swap(r))) * PIECE);
-            if constexpr (PIECE == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[i].w[0]), "=r"(x[i].w[1]), "=r"(x[i].w[2 % (PIECE / 4)]), "=r"(x[i].w[3 % (PIECE / 4)]) : "r"(d));
-            else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[i].w[0]), "=r"(x[i].w[1]) : "r"(d));
+            for (int i = 0; i < CL; ++i) read(a + (uint32_t)(i * ROW), x[i].w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CL; ++i) {
+                const int r = t * CL + i;
+                const uint32_t m = skew(row0, P, p0, r), a = base + use + (uint32_t)(r * PITCH + g * PIECE) + (m & ~3u);
+                uint32_t w[W + 1];
+#pragma unroll
+                for (int k = 0; k < W + (sizeof(T) == 2 ? 1 : 0); ++k) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[k]) : "r"(a + 4u * k));
+#pragma unroll
+                for (int k = 0; k < W; ++k) x[i].w[k] = sizeof(T) == 2 ? __funnelshift_r(w[k], w[k + 1], 8 * (m & 3u)) : w[k];
+            }
         }
-        ++tail;
+        use = use == (S - 1) * STAGE ? 0 : use + STAGE;
     }
     // 2 NP positions of channels g and g + 8
-    __device__ __forceinline__ void take_base(Words<PIECE / 2> (&x)[2])
+    __device__ __forceinline__ void take_base(Words<2 * W> (&x)[2])
     {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-        const uint32_t src = base + (uint32_t)(tail % S) * STAGE;
-        constexpr int W = PIECE / 4;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = g + 8 * h;
-                const uint32_t d = src + (uint32_t)((r * 8 + ((2 * t + e) ^ (r & 1))) * PIECE);
-                if constexpr (PIECE == 16) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(x[h].w[e * W]), "=r"(x[h].w[e * W + 1]), "=r"(x[h].w[e * W + 2 % W]), "=r"(x[h].w[e * W + 3 % W]) : "r"(d));
-                else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(x[h].w[e * W]), "=r"(x[h].w[e * W + 1]) : "r"(d));
-            }
-        ++tail;
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t a = base + use + (uint32_t)(g * ROW + ((2 * t + e) ^ (g & 1)) * PIECE);
+            read(a, x[0].w + e * W);
+            read(a + 8 * ROW, x[1].w + e * W);
+        }
+        use = use == (S - 1) * STAGE ? 0 : use + STAGE;
+    }
+    // rows that start anywhere: the stage itself
+    __device__ __forceinline__ uint32_t take_stage()
+    {
+        const uint32_t a = base + use;
+        use = use == (S - 1) * STAGE ? 0 : use + STAGE;
+        return a;
     }
     static __device__ __forceinline__ void drain() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 };
 
-// Adds the first product over the channel groups kw, kw + ks, ... of an image (src: its first channel, end: behind the tensor) at the tile
-// that starts at p0, loaded as it is needed: rows that start anywhere.  w1 already points at this lane.
-template <typename T, int RB, bool SM>
-__device__ __forceinline__ void first_product(Tile<T, RB>& tile, const T* src, const T* end, int K, size_t P, size_t p0, const uint4* w1, int kw, int ks)
-{
-    constexpr int NP = Tile<T, RB>::NP, CL = Geo<T>::CL, GC = Geo<T>::GC, PARTS = Geo<T>::PARTS;
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int groups = (K + GC - 1) / GC;
-    for (int grp = kw; grp < groups; grp += ks) {
-        // channels behind the last one meet zeros in the factor: they load something else that exists, so that all loads of a group go out together
-        Words<NP * (int)sizeof(T) / 4> x[CL];
-#pragma unroll
-        for (int i = 0; i < CL; ++i)
-            x[i] = load_row<T, NP, false>(src + (size_t)min(grp * GC + t * CL + i, K - 1) * P, p0 + (size_t)NP * g, P, end);
-        first_step<T, RB, SM>(tile, x, w1 + (size_t)grp * RB * PARTS * 32);
-    }
-}
-
 // dst = base + second product, of the blocks kw, kw + ks, ... of 16 channels of an image (base, dst: its first channel; base may be NULL).
-// next_base(x): this lane's part of the next block's base from the feed (VEC > 0).  VEC 2: rows also start on 2 NP positions.  out: this warp's
+// next_base(x): this lane's part of the next block's base from the feed (VEC 0: the stage's address).  VEC 2: rows also start on 2 NP positions.  out: this warp's
 // 16 x (TP + 4) floats, VEC 0 only.
-template <typename T, int RB, int VEC, bool SM, typename Next>
-__device__ __forceinline__ void second_product(const Tile<T, RB>& tile, const T* base, T* dst, int M, size_t P, size_t p0, const uint4* w2, int kw, int ks,
+template <typename T, int RB, int VEC, bool SM, int NP, typename Next>
+__device__ __forceinline__ void second_product(const Tile<T, RB, NP>& tile, const T* base, T* dst, int M, size_t P, size_t p0, const uint4* w2, int kw, int ks,
                                                float* out, Next next_base)
 {
-    constexpr int NP = Tile<T, RB>::NP, TP = 8 * NP, PARTS = Geo<T>::PARTS;
+    constexpr int TP = 8 * NP, PARTS = Geo<T>::PARTS;
     constexpr int NO = VEC == 2 ? 2 * NP : NP, PIECES = 2 * NP / NO;    // positions of a load or store
     constexpr bool HALF = sizeof(T) == 2;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -540,16 +583,29 @@ __device__ __forceinline__ void second_product(const Tile<T, RB>& tile, const T*
                     for (int b = 0; b < NP; b += 2)
                         *reinterpret_cast<float2*>(out + (g + 8 * h) * (TP + 4) + 2 * NP * t + NP * e + b) = make_float2(d[b][2 * h + e], d[b + 1][2 * h + e]);
             __syncwarp();
-            const int rows = min(16, M - 16 * mo);
-            const size_t at = (size_t)(16 * mo) * P + p0, here = P - p0;
-#pragma unroll 8
-            for (int i = lane; i < 16 * TP; i += 32) {
+            const int rows = min(16, M - 16 * mo), here = (int)min((size_t)TP, P - p0);
+            using Fd = Feed<T, NP, false>;
+            Words<1> none[1];
+            const uint32_t stage = base ? next_base(none) : 0u;
+            T* row = dst + (size_t)(16 * mo) * P + p0;
+#pragma unroll 4
+            for (int i = lane; i < rows * TP; i += 32) {
                 const int r = i / TP, c = i % TP;
-                if (r < rows && (size_t)c < here) {
-                    const size_t j = at + r * P + c;
+                if (c < here) {
                     float v = out[r * (TP + 4) + c];
-                    if (base) v += load_one(base + j);
-                    store_one(dst + j, v);
+                    if (base) {
+                        const uint32_t a = stage + (uint32_t)(r * Fd::PITCH + c * (int)sizeof(T)) + Fd::skew(base + (size_t)(16 * mo) * P, P, p0, r);
+                        if constexpr (HALF) {
+                            uint16_t h;
+                            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(a));
+                            v += __uint_as_float((uint32_t)h << 16);
+                        } else {
+                            uint32_t h;
+                            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(h) : "r"(a));
+                            v += __uint_as_float(h);
+                        }
+                    }
+                    store_one(row + (size_t)r * P + c, v);
                 }
             }
         } else {
@@ -612,10 +668,10 @@ __device__ __forceinline__ void copy_tile(const T* base, T* dst, int M, size_t P
 }
 
 // This lane's part of a tile as planes of a [ranks][pitch] array, `at` = element (0, NP g): bf16 three parts `next` elements apart, or fp32.
-template <typename T, int RB>
-__device__ __forceinline__ void store_planes(const Tile<T, RB>& tile, T* plane, size_t pitch, size_t next)
+template <typename T, int RB, int NP>
+__device__ __forceinline__ void store_planes(const Tile<T, RB, NP>& tile, T* plane, size_t pitch, size_t next)
 {
-    constexpr int NP = Tile<T, RB>::NP, MB = NP / 2;
+    constexpr int MB = NP / 2;
     const int t = threadIdx.x & 3;
 #pragma unroll
     for (int jb = 0; jb < RB; ++jb)
@@ -662,10 +718,10 @@ struct ApplyArgs {
 };
 
 // A CTA takes a run of tiles of one image.  Shared memory: the factors (SM), partial sums of warps that share a tile, tiles on their way out.
-template <typename T, int RB, int VEC, bool SM>
+template <typename T, int RB, int NP, int VEC, bool SM>
 __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, uint4* sm)
 {
-    using Ti = Tile<T, RB>;
+    using Ti = Tile<T, RB, NP>;
     constexpr int TP = Ti::TP, MB = Ti::MB;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     const int n = item / q.parts, per = warps / q.ks;                   // per: position tiles at once
@@ -695,42 +751,58 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, uint
     float4* red = reinterpret_cast<float4*>(sm);
     char* tail = reinterpret_cast<char*>(sm) + (q.ks > 1 ? (size_t)warps * (MB * RB * 512) : 0);      // tiles on their way out, or in
     float* out = reinterpret_cast<float*>(tail) + warp * 16 * (TP + 4);
-    void* feed_sm = tail + (size_t)warp * Feed<T, RB>::S * Feed<T, RB>::STAGE;
+    if (VEC == 0) tail += (size_t)warps * 16 * (TP + 4) * 4;
+    void* feed_sm = tail + (size_t)warp * Feed<T, NP, (VEC > 0)>::S * Feed<T, NP, (VEC > 0)>::STAGE;
     const float sc = q.scale ? q.scale[a] : 1.0f;
-    const T* src = q.src + (size_t)n * q.K * P;
+    const T *src = q.src + (size_t)n * q.K * P, *src_end = q.src + (size_t)q.N * q.K * P, *base_end = q.base + (size_t)q.N * q.M * P;
     const size_t limit = q.tap ? q.Pp : P;
 
-    using Fd = Feed<T, RB>;
+    using Fd = Feed<T, NP, (VEC > 0)>;
     constexpr int GC = Geo<T>::GC;
     Fd feed(feed_sm);
-    // What the feed copies next: the fi-th stage of the tile in round fr, this warp's groups of the map and then its blocks of the base.
-    const int groups = (q.K + GC - 1) / GC, nx = groups > kw ? (groups - kw + q.ks - 1) / q.ks : 0;
-    const int blocks = (q.M + 15) / 16, nb = base && q.f2.p && blocks > kw ? (blocks - kw + q.ks - 1) / q.ks : 0;
-    int fr = g0, fi = 0;
+    // What the feed copies next: `fleft` channels from `fsrc` on, of the map or (fb) of the base, at the tile of round fr; this warp's groups of the
+    // map and then its blocks of the base.
+    const int groups = (q.K + GC - 1) / GC;
+    const T* const base0 = q.f2.p ? base : nullptr;
+    const size_t xstep = (size_t)(q.ks * GC) * P, bstep = (size_t)(q.ks * 16) * P;
+    int fr = g0 - 1, fleft = 0;
+    bool fb = true, fin = false;
+    const T* fsrc = src;
     auto ahead = [&]() {
-        size_t p = (size_t)(fr * per + warp / q.ks) * TP;
-        while (fr < g1 && fi >= nx + (p < P ? nb : 0)) { fi = 0; ++fr; p = (size_t)(fr * per + warp / q.ks) * TP; if (nx + nb == 0) break; }
-        if (fr >= g1 || nx + nb == 0) feed.template issue<false>(src, 0, P, 0);
-        else if (fi < nx) { const int c = (kw + fi * q.ks) * GC; feed.template issue<false>(src + (size_t)c * P, q.K - c, P, p); }
-        else { const int c = (kw + (fi - nx) * q.ks) * 16; feed.template issue<true>(base + (size_t)c * P, q.M - c, P, p); }
-        ++fi;
+        while (fleft <= 0 && fr < g1) {
+            if (!fb && base0 && fin) { fb = true; fsrc = base0 + (size_t)(kw * 16) * P; fleft = q.M - kw * 16; }
+            else {
+                const size_t p = (size_t)(++fr * per + warp / q.ks) * TP;
+                if (fr == g1) break;
+                fin = p < P;
+                feed.at(P, p);
+                fb = false; fsrc = src + (size_t)(kw * GC) * P; fleft = q.K - kw * GC;
+            }
+        }
+        if (fr < g1) {
+            if (fb) { feed.template issue<true>(fsrc, fleft, P, base_end); fsrc += bstep; fleft -= 16 * q.ks; }
+            else { feed.template issue<false>(fsrc, fleft, P, src_end); fsrc += xstep; fleft -= GC * q.ks; }
+        }
+        feed.commit();
     };
-    auto next_base = [&](Words<Fd::PIECE / 2> (&x)[2]) { feed.wait(); ahead(); feed.take_base(x); };
-    if constexpr (VEC > 0)
-        for (int i = 0; i < Fd::S - 1; ++i) ahead();
+    auto next_base = [&](auto& x) -> uint32_t {
+        feed.wait();
+        ahead();
+        if constexpr (VEC > 0) { feed.take_base(x); return 0u; }
+        else return feed.take_stage();
+    };
+    for (int i = 0; i < Fd::S - 1; ++i) ahead();
     for (int gr = g0; gr < g1; ++gr) {
         const size_t p0 = (size_t)(gr * per + warp / q.ks) * TP;
         Ti tile;
         tile.zero();
-        if constexpr (VEC > 0) {
-            for (int grp = kw; grp < groups; grp += q.ks) {
-                Words<Fd::PIECE / 4> x[Fd::CL];
-                feed.wait();
-                ahead();
-                feed.take(x);
-                first_step<T, RB, SM>(tile, x, w1 + (size_t)grp * RB * Geo<T>::PARTS * 32);
-            }
-        } else if (p0 < P) first_product<T, RB, SM>(tile, src, q.src + (size_t)q.N * q.K * P, q.K, P, p0, w1, kw, q.ks);
+        for (int grp = kw; grp < groups; grp += q.ks) {
+            Words<Fd::W> x[Fd::CL];
+            feed.wait();
+            ahead();
+            feed.take(x, src + (size_t)(grp * GC) * P, P, p0);
+            first_step<T, RB, SM, NP>(tile, x, w1 + (size_t)grp * RB * Geo<T>::PARTS * 32);
+        }
         if (q.ks > 1) {
             // the warps of a tile add their partial sums, every warp all of them in the same order
             if (gr > g0) __syncthreads();                               // those of the group before have been read
@@ -757,25 +829,25 @@ __device__ __forceinline__ void apply_body(const ApplyArgs<T>& q, int item, uint
         if (p0 >= limit) continue;
         tile.scale(sc);
         if (q.tap && kw == 0) {
-            const size_t pl = p0 + (size_t)Ti::NP * (lane >> 2);
-            if (pl >= P) tile.zero();
-            store_planes<T, RB>(tile, q.tap + (size_t)n * (8 * RB) * q.Pp + pl, q.Pp, (size_t)q.N * (8 * RB) * q.Pp);
+            const size_t pl = p0 + (size_t)NP * (lane >> 2);
+            if (pl + NP > P) tile.keep(pl < P ? (int)(P - pl) : 0);
+            store_planes<T, RB, NP>(tile, q.tap + (size_t)n * (8 * RB) * q.Pp + pl, q.Pp, (size_t)q.N * (8 * RB) * q.Pp);
         }
-        if (q.f2.p && p0 < P) second_product<T, RB, VEC, SM>(tile, base, dst, q.M, P, p0, w2, kw, q.ks, out, next_base);
+        if (q.f2.p && p0 < P) second_product<T, RB, VEC, SM, NP>(tile, base, dst, q.M, P, p0, w2, kw, q.ks, out, next_base);
     }
-    if constexpr (VEC > 0) Fd::drain();
+    Fd::drain();
 }
 
 // Up to two maps in one launch (the backward pass projects dy and x): the second takes the CTAs from q0.items on.
-template <typename T, int RB, int VEC, bool SM>
+template <typename T, int RB, int NP, int VEC, bool SM>
 __global__ void __launch_bounds__(256, RB <= 2 ? 2 : 1) apply_kernel(ApplyArgs<T> q0, ApplyArgs<T> q1)
 {
     extern __shared__ uint4 apply_sm[];
     pdl_wait();
     pdl_launch();
     const int item = blockIdx.x;
-    if (item < q0.items) apply_body<T, RB, VEC, SM>(q0, item, apply_sm);
-    else apply_body<T, RB, VEC, SM>(q1, item - q0.items, apply_sm);
+    if (item < q0.items) apply_body<T, RB, NP, VEC, SM>(q0, item, apply_sm);
+    else apply_body<T, RB, NP, VEC, SM>(q1, item - q0.items, apply_sm);
 }
 
 // ---- single tokens (one position an image) --------------------------------------------------------
@@ -991,6 +1063,12 @@ __global__ void __launch_bounds__(256) grad_reduce(const float* __restrict__ par
     }
 }
 
+// Shared memory of a warp for its feed, and for its tiles on their way out where rows start anywhere.
+template <typename T> static size_t feed_smem(int np, bool vec)
+{
+    return (size_t)AD_STAGES * Geo<T>::GC * (8 * np * sizeof(T) + (vec ? 0 : 16)) + (vec ? 0 : (size_t)16 * (8 * np + 4) * 4);
+}
+
 // ---- the whole backward pass in one kernel --------------------------------------------------------
 // Small ranks and maps with tiles enough.  A CTA takes a run of units of 4 warp tiles, in the order of the images.  For a unit its warps compute
 // V and dx and then U of their tiles, leave V and U in shared memory, and then each of them takes blocks of 16 channels of x and dy over
@@ -1016,21 +1094,23 @@ static size_t bwd_smem(int rb, int Cin, int Cout, bool dx, bool vec)
 {
     const int np = lane_positions<T>(rb);
     return 16 * (first_words<T>(rb, Cout) + first_words<T>(rb, Cin) + (dx ? second_words<T>(rb, Cin) : 0)) +
-           (size_t)2 * (sizeof(T) == 2 ? 3 : 1) * 8 * rb * plane_pitch<T>(np) * sizeof(T) + (size_t)BW * (vec ? AD_STAGES * Geo<T>::GC * 8 * np * sizeof(T) : 16 * (8 * np + 4) * 4);
+           (size_t)2 * (sizeof(T) == 2 ? 3 : 1) * 8 * rb * plane_pitch<T>(np) * sizeof(T) + BW * feed_smem<T>(np, vec);
 }
 
 template <typename T, int RB, int VEC, int NB>
 __global__ void __launch_bounds__(32 * BW, NB <= 4 ? 3 : 2) bwd_kernel(BwdArgs<T> q)
 {
-    using Ti = Tile<T, RB>;
-    constexpr int NP = Ti::NP, TP = Ti::TP, PITCH = plane_pitch<T>(NP), PARTS = sizeof(T) == 2 ? 3 : 1, PLANE = 8 * RB * PITCH;
+    constexpr int NP = lane_positions<T>(RB);
+    using Ti = Tile<T, RB, NP>;
+    constexpr int TP = Ti::TP, PITCH = plane_pitch<T>(NP), PARTS = sizeof(T) == 2 ? 3 : 1, PLANE = 8 * RB * PITCH;
     extern __shared__ uint4 bwd_sm[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const size_t P = q.P, nB = first_words<T>(RB, q.Cout), nA = first_words<T>(RB, q.Cin), nAt = q.dx ? second_words<T>(RB, q.Cin) : 0;
     T* planes = reinterpret_cast<T*>(bwd_sm + nB + nA + nAt);           // [U for dy, V for x][part][rank][position]
     float* out = reinterpret_cast<float*>(planes + 2 * PARTS * PLANE) + warp * 16 * (TP + 4);
     const int blocks0 = (q.Cin + 15) / 16, all = blocks0 + (q.Cout + 15) / 16;
-    const T *x_end = q.x + (size_t)q.N * q.Cin * P, *dy_end = q.dy + (size_t)q.N * q.Cout * P;
+    const T *x_end = q.x + (size_t)q.N * q.Cin * P, *dy_end = q.dy + (size_t)q.N * q.Cout * P,
+            *base_end = q.base + (size_t)q.N * q.Cin * P;
     const int run = blockIdx.x;
     const long long total = (long long)q.N * q.units, u0 = (long long)run * q.share, u1 = min(total, u0 + q.share);
 
@@ -1057,44 +1137,60 @@ __global__ void __launch_bounds__(32 * BW, NB <= 4 ? 3 : 2) bwd_kernel(BwdArgs<T
         clear();
     };
     clear();
-    // What the feed copies next: the fi-th stage of unit fu, the groups of dy, the blocks of the base, the groups of x.  Units of images without an
-    // adapter are stepped over.
-    using Fd = Feed<T, RB>;
+    // What the feed copies next: `fleft` channels from `fsrc` on, of dy (phase 0), the base (1) and x (2) of unit fu.  Units of images without an adapter
+    // are stepped over.
+    using Fd = Feed<T, NP, (VEC > 0)>;
     constexpr int GC = Geo<T>::GC;
-    const int gB = (q.Cout + GC - 1) / GC, gA = (q.Cin + GC - 1) / GC, gD = q.dx && q.base ? blocks0 : 0;
-    Fd feed(reinterpret_cast<char*>(planes + 2 * PARTS * PLANE) + (size_t)warp * Fd::S * Fd::STAGE);
+    const int gB = (q.Cout + GC - 1) / GC, gA = (q.Cin + GC - 1) / GC;
+    Fd feed(reinterpret_cast<char*>(planes + 2 * PARTS * PLANE) + (VEC > 0 ? 0 : (size_t)BW * 16 * (TP + 4) * 4) + (size_t)warp * Fd::S * Fd::STAGE);
     long long fu = u0 - 1;
-    int fi = 0, fn = -1, fend = 0, fb = 0;                              // stages of the unit, blocks of the base among them
-    size_t fp = 0;
-    bool feeds = false;
+    int fn = -1, fleft = 0, phase = 2;
+    bool feeds = false, fin = false;
+    const T* fsrc = q.dy;
     auto ahead = [&]() {
-        if (fi == fend) {
-            for (++fu; fu < u1; ++fu) {
-                const int n = (int)(fu / q.units);
-                if (n != fn) { fn = n; feeds = q.ids[n] >= 0 && q.ids[n] < q.R; }
-                if (feeds) break;
-            }
-            fi = 0;
-            fp = (size_t)(fu - (long long)fn * q.units) * (BW * TP) + (size_t)warp * TP;
-            fb = fp < P ? gD : 0;
-            fend = gB + fb + gA;
+        if (fleft <= 0 && fu < u1) {
+            if (phase == 2) {
+                for (++fu; fu < u1; ++fu) {
+                    const int n = (int)(fu / q.units);
+                    if (n != fn) { fn = n; feeds = q.ids[n] >= 0 && q.ids[n] < q.R; }
+                    if (feeds) break;
+                }
+                const size_t p = (size_t)(fu - (long long)fn * q.units) * (BW * TP) + (size_t)warp * TP;
+                fin = p < P;
+                feed.at(P, p);
+                phase = 0; fsrc = q.dy + (size_t)fn * q.Cout * P; fleft = q.Cout;
+            } else if (phase == 0 && fin && q.dx && q.base) { phase = 1; fsrc = q.base + (size_t)fn * q.Cin * P; fleft = q.Cin; }
+            else { phase = 2; fsrc = q.x + (size_t)fn * q.Cin * P; fleft = q.Cin; }
         }
-        if (fu >= u1) { feed.template issue<false>(q.dy, 0, P, 0); fi = fend; return; }
-        if (fi < gB) feed.template issue<false>(q.dy + ((size_t)fn * q.Cout + fi * GC) * P, q.Cout - fi * GC, P, fp);
-        else if (fi < gB + fb) { const int c = (fi - gB) * 16; feed.template issue<true>(q.base + ((size_t)fn * q.Cin + c) * P, q.Cin - c, P, fp); }
-        else { const int c = (fi - gB - fb) * GC; feed.template issue<false>(q.x + ((size_t)fn * q.Cin + c) * P, q.Cin - c, P, fp); }
-        ++fi;
+        if (fu < u1) {
+            const int rows = phase == 1 ? 16 : GC;
+            if (phase == 1) feed.template issue<true>(fsrc, fleft, P, base_end);
+            else feed.template issue<false>(fsrc, fleft, P, phase ? x_end : dy_end);
+            fsrc += (size_t)rows * P;
+            fleft -= rows;
+        }
+        feed.commit();
     };
-    auto next_base = [&](Words<Fd::PIECE / 2> (&x)[2]) { feed.wait(); ahead(); feed.take_base(x); };
-    auto consume = [&](Ti& tile, const uint4* w) {
-        Words<Fd::PIECE / 4> x[Fd::CL];
+    auto next_base = [&](auto& x) -> uint32_t {
         feed.wait();
         ahead();
-        feed.take(x);
-        first_step<T, RB, true>(tile, x, w);
+        if constexpr (VEC > 0) { feed.take_base(x); return 0u; }
+        else return feed.take_stage();
     };
-    if constexpr (VEC > 0)
-        for (int i = 0; i < Fd::S - 1; ++i) ahead();
+    // the first product of a map at this warp's tile
+    auto project = [&](Ti& tile, const T* map, int groups, size_t p0, const uint4* w) {
+        tile.zero();
+        for (int grp = 0; grp < groups; ++grp) {
+            Words<Fd::W> x[Fd::CL];
+            feed.wait();
+            ahead();
+            feed.take(x, map + (size_t)(grp * GC) * P, P, p0);
+            first_step<T, RB, true, NP>(tile, x, w + (size_t)grp * RB * Geo<T>::PARTS * 32);
+        }
+        const size_t pl = p0 + (size_t)NP * g;
+        if (pl + NP > P) tile.keep(pl < P ? (int)(P - pl) : 0);
+    };
+    for (int i = 0; i < Fd::S - 1; ++i) ahead();
     int last = -1, a = -1, laid = -1;                                   // image at work, its adapter, the adapter in shared memory
     float sc = 1.0f;
     for (long long u = u0; u < u1; ++u) {
@@ -1121,27 +1217,14 @@ __global__ void __launch_bounds__(32 * BW, NB <= 4 ? 3 : 2) bwd_kernel(BwdArgs<T
             continue;
         }
         const T *xn = q.x + (size_t)n * q.Cin * P, *dyn = q.dy + (size_t)n * q.Cout * P;
-        const bool behind = p0 + (size_t)NP * g >= P;
         T* mine = planes + warp * TP + NP * g;
         Ti tile;
-        tile.zero();
-        if constexpr (VEC > 0) {
-            for (int grp = 0; grp < gB; ++grp) consume(tile, bwd_sm + lane + (size_t)grp * RB * Geo<T>::PARTS * 32);
-        } else {
-            if (p0 < P) first_product<T, RB, true>(tile, dyn, dy_end, q.Cout, P, p0, bwd_sm + lane, 0, 1);
-            if (behind) tile.zero();
-        }
+        project(tile, dyn, gB, p0, bwd_sm + lane);
         tile.scale(sc);
-        store_planes<T, RB>(tile, mine + PARTS * PLANE, PITCH, PLANE);
-        if (nAt && p0 < P) second_product<T, RB, VEC, true>(tile, base, dx, q.Cin, P, p0, bwd_sm + nB + nA + lane, 0, 1, out, next_base);
-        tile.zero();
-        if constexpr (VEC > 0) {
-            for (int grp = 0; grp < gA; ++grp) consume(tile, bwd_sm + nB + lane + (size_t)grp * RB * Geo<T>::PARTS * 32);
-        } else {
-            if (p0 < P) first_product<T, RB, true>(tile, xn, x_end, q.Cin, P, p0, bwd_sm + nB + lane, 0, 1);
-            if (behind) tile.zero();
-        }
-        store_planes<T, RB>(tile, mine, PITCH, PLANE);
+        store_planes<T, RB, NP>(tile, mine + PARTS * PLANE, PITCH, PLANE);
+        if (nAt && p0 < P) second_product<T, RB, VEC, true, NP>(tile, base, dx, q.Cin, P, p0, bwd_sm + nB + nA + lane, 0, 1, out, next_base);
+        project(tile, xn, gA, p0, bwd_sm + nB + lane);
+        store_planes<T, RB, NP>(tile, mine, PITCH, PLANE);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -1177,7 +1260,7 @@ __global__ void __launch_bounds__(32 * BW, NB <= 4 ? 3 : 2) bwd_kernel(BwdArgs<T
         __syncthreads();                                                // the planes are written again
     }
     if (a >= 0) flush(last);
-    if constexpr (VEC > 0) Fd::drain();
+    Fd::drain();
     pdl_launch();
 }
 
@@ -1234,7 +1317,7 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
     f.units = (int)((P + unit - 1) / unit);
     const long long total = (long long)N * f.units;
     if (rb > 2 || all > 8 * BW || N > 4096 || total < AD_FUSED) return f;
-    const size_t smem = std::max(bwd_smem<T>(rb, Cin, Cout, true, false), bwd_smem<T>(rb, Cin, Cout, true, true));
+    const size_t smem = bwd_smem<T>(rb, Cin, Cout, true, P % Geo<T>::NP == 0);
     if (smem > 113 * 1024) return f;                                      // two CTAs an SM
     f.runs = (int)std::min(total, AD_RUNS * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
     f.share = (int)((total + f.runs - 1) / f.runs);
@@ -1245,6 +1328,12 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
 
 // Factors that a CTA lays out for itself: while four CTAs of an SM have the room.
 template <typename T> static bool staged(int rb, int K, int M) { return 16 * (first_words<T>(rb, K) + (M ? second_words<T>(rb, M) : 0)) <= 40 * 1024; }
+// Positions of a lane: half as many for the largest ranks, unless there are full tiles enough for four warps of every SM (rank 64, bf16, us, half /
+// full: 256 -> 1024 on 4 x 128 x 128 159 / 126, 826 -> 899 on 14 x 18 x 72 47 / 54).
+template <typename T> static int positions_of(int rb, int N, size_t P)
+{
+    return (long long)N * ((P + Geo<T>::TP - 1) / Geo<T>::TP) >= 4 * B200_SMS ? Geo<T>::NP : lane_positions<T>(rb);
+}
 
 struct Ws {
     void* first[2];
@@ -1298,20 +1387,20 @@ static Ws carve(void* ws, int N, int Cin, int Cout, size_t P, int R, int rank, b
 
 // Warps that share a tile: more only while the tiles alone do not fill the GPU.
 template <typename T>
-static void plan_apply(ApplyArgs<T>& q, int rb, int& warps)
+static void plan_apply(ApplyArgs<T>& q, int np, int most_ks, int& warps)
 {
-    const int tp = 8 * lane_positions<T>(rb);
+    const int tp = 8 * np;
     const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
     const int most = std::max(ceil_div(q.K, Geo<T>::GC), q.f2.p ? ceil_div(q.M, 16) : 1);
     q.ks = 1;
-    while (q.ks < 8 && q.ks * 2 <= most && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
+    while (q.ks < most_ks && q.ks * 2 <= most && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
     if (!warps) warps = q.ks == 8 ? 8 : 4;
     if (q.ks == 8) warps = 8;
 }
 template <typename T>
-static void plan_parts(ApplyArgs<T>& q, int rb, int warps, bool sm)
+static void plan_parts(ApplyArgs<T>& q, int np, int warps, bool sm)
 {
-    const int tp = 8 * lane_positions<T>(rb), per = warps / q.ks;
+    const int tp = 8 * np, per = warps / q.ks;
     const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
     q.groups = (int)((tiles + per - 1) / per);
     // a CTA that lays out its factors takes as many groups as leave four CTAs an SM (eight warps: two)
@@ -1320,48 +1409,54 @@ static void plan_parts(ApplyArgs<T>& q, int rb, int warps, bool sm)
     q.parts = ceil_div(q.groups, q.per_part);
 }
 // Factors, partial sums of warps that share a tile, and the tiles on their way out where rows start anywhere.
-template <typename T> static size_t apply_smem(const ApplyArgs<T>& q, int warps, int rb, bool vec, bool sm)
+template <typename T> static size_t apply_smem(const ApplyArgs<T>& q, int warps, int rb, int np, bool vec, bool sm)
 {
-    const int np = lane_positions<T>(rb);
     return (sm ? 16 * (first_words<T>(rb, q.K) + (q.f2.p ? second_words<T>(rb, q.M) : 0)) : 0) +
-           (size_t)warps * ((q.ks > 1 ? (np / 2) * rb * 512 : 0) + (vec ? AD_STAGES * Geo<T>::GC * 8 * np * (int)sizeof(T) : 16 * (8 * np + 4) * 4));
+           (size_t)warps * ((q.ks > 1 ? (np / 2) * rb * 512 : 0) + feed_smem<T>(np, vec));
 }
 
-template <typename T, int RB, int VEC, bool SM>
+template <typename T, int RB, int NP, int VEC, bool SM>
 static wcc_status run_apply(ApplyArgs<T> q0, ApplyArgs<T>* q1, int dev, bool overlap, cudaStream_t st)
 {
+    size_t smem = 0;
     int warps = 0;
-    plan_apply(q0, RB, warps);
-    if (q1) plan_apply(*q1, RB, warps);
-    plan_parts(q0, RB, warps, SM);
-    size_t smem = apply_smem(q0, warps, RB, VEC > 0, SM);
     long long items1 = 0;
-    if (q1) {
-        plan_parts(*q1, RB, warps, SM);
-        smem = std::max(smem, apply_smem(*q1, warps, RB, VEC > 0, SM));
-        items1 = (long long)q1->N * q1->parts;
+    for (int most_ks = 8; most_ks >= 4; most_ks /= 2) {                 // eight warps if their shared memory is there
+        warps = 0;
+        plan_apply(q0, NP, most_ks, warps);
+        if (q1) plan_apply(*q1, NP, most_ks, warps);
+        plan_parts(q0, NP, warps, SM);
+        smem = apply_smem(q0, warps, RB, NP, VEC > 0, SM);
+        if (q1) {
+            plan_parts(*q1, NP, warps, SM);
+            smem = std::max(smem, apply_smem(*q1, warps, RB, NP, VEC > 0, SM));
+            items1 = (long long)q1->N * q1->parts;
+        }
+        if (smem <= 227 * 1024) break;
     }
     const long long items = (long long)q0.N * q0.parts;
     if (items + items1 > 0x7FFFFFFFLL) return WCC_ERR_SHAPE;
     q0.items = (int)items;
     if (q1) q1->items = (int)items1;
-    wcc_status s = allow_smem<apply_kernel<T, RB, VEC, SM>>(dev, (int)smem);
+    wcc_status s = allow_smem<apply_kernel<T, RB, NP, VEC, SM>>(dev, (int)smem);
     if (s != WCC_OK) return s;
-    return launch_overlapped(apply_kernel<T, RB, VEC, SM>, dim3((unsigned)(items + items1)), dim3((unsigned)(32 * warps)), smem, st, overlap, 1, q0,
+    return launch_overlapped(apply_kernel<T, RB, NP, VEC, SM>, dim3((unsigned)(items + items1)), dim3((unsigned)(32 * warps)), smem, st, overlap, 1, q0,
                              q1 ? *q1 : q0);
 }
 // overlap: the kernel before it in the stream is the preparation.
 template <typename T>
 static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb, int dev, bool overlap, cudaStream_t st)
 {
-    const int np = lane_positions<T>(rb), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
+    constexpr int FULL_NP = Geo<T>::NP;
     const bool sm = !q0.w1;
-#define WCC_AD_APPLY(RB_, SM_)                                                                                                           \
-    if (rb == (RB_) && sm == (SM_))                                                                                                      \
-        return vec == 2 ? run_apply<T, RB_, 2, SM_>(q0, q1, dev, overlap, st) : vec == 1 ? run_apply<T, RB_, 1, SM_>(q0, q1, dev, overlap, st) \
-                                                                                         : run_apply<T, RB_, 0, SM_>(q0, q1, dev, overlap, st);
-    WCC_AD_APPLY(1, true) WCC_AD_APPLY(2, true) WCC_AD_APPLY(4, true) WCC_AD_APPLY(8, true)
-    WCC_AD_APPLY(1, false) WCC_AD_APPLY(2, false) WCC_AD_APPLY(4, false) WCC_AD_APPLY(8, false)
+    const int np = positions_of<T>(rb, q0.N, q0.P), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
+#define WCC_AD_APPLY(RB_, NP_, SM_)                                                                                                      \
+    if (rb == (RB_) && np == (NP_) && sm == (SM_))                                                                                       \
+        return vec == 2 ? run_apply<T, RB_, NP_, 2, SM_>(q0, q1, dev, overlap, st)                                                        \
+                        : vec == 1 ? run_apply<T, RB_, NP_, 1, SM_>(q0, q1, dev, overlap, st) : run_apply<T, RB_, NP_, 0, SM_>(q0, q1, dev, overlap, st);
+    WCC_AD_APPLY(1, FULL_NP, true) WCC_AD_APPLY(2, FULL_NP, true) WCC_AD_APPLY(4, FULL_NP, true) WCC_AD_APPLY(8, FULL_NP, true)
+    WCC_AD_APPLY(8, FULL_NP / 2, true) WCC_AD_APPLY(8, FULL_NP / 2, false) WCC_AD_APPLY(8, FULL_NP, false)
+    WCC_AD_APPLY(1, FULL_NP, false) WCC_AD_APPLY(2, FULL_NP, false) WCC_AD_APPLY(4, FULL_NP, false)
 #undef WCC_AD_APPLY
     return WCC_ERR_SHAPE;
 }
