@@ -401,7 +401,7 @@ __device__ __forceinline__ void first_step(Tile<T, RB, NP>& tile, const Words<NP
 // made of them.  With plain loads into registers the maps came no faster than 4.9 TB/s (headline batch, 57 us without those of the base).
 template <typename T, int NP, bool AL>
 struct Feed {
-    static constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), S = AD_STAGES, W = PIECE / 4;
+    static constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), S = AL ? AD_STAGES : 2, W = PIECE / 4;
     static constexpr int ROW = 8 * PIECE, PITCH = ROW + (AL ? 0 : 16), CH = PITCH / 16, STAGE = GC * PITCH;
     uint32_t base, fill, use;           // shared address, offsets of the stages to fill and to use next
     size_t off;                         // AL: this lane's first row and piece of a stage, from the stage's first channel at position 0; else p0
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(256) grad_reduce(const float* __restrict__ par
 // Shared memory of a warp for its feed, and for its tiles on their way out where rows start anywhere.
 template <typename T> static size_t feed_smem(int np, bool vec)
 {
-    return (size_t)AD_STAGES * Geo<T>::GC * (8 * np * sizeof(T) + (vec ? 0 : 16)) + (vec ? 0 : (size_t)16 * (8 * np + 4) * 4);
+    return (size_t)(vec ? AD_STAGES : 2) * Geo<T>::GC * (8 * np * sizeof(T) + (vec ? 0 : 16)) + (vec ? 0 : (size_t)16 * (8 * np + 4) * 4);
 }
 
 // ---- the whole backward pass in one kernel --------------------------------------------------------
@@ -1328,13 +1328,6 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
 
 // Factors that a CTA lays out for itself: while four CTAs of an SM have the room.
 template <typename T> static bool staged(int rb, int K, int M) { return 16 * (first_words<T>(rb, K) + (M ? second_words<T>(rb, M) : 0)) <= 40 * 1024; }
-// Positions of a lane: half as many for the largest ranks, unless there are full tiles enough for four warps of every SM (rank 64, bf16, us, half /
-// full: 256 -> 1024 on 4 x 128 x 128 159 / 126, 826 -> 899 on 14 x 18 x 72 47 / 54).
-template <typename T> static int positions_of(int rb, int N, size_t P)
-{
-    return (long long)N * ((P + Geo<T>::TP - 1) / Geo<T>::TP) >= 4 * B200_SMS ? Geo<T>::NP : lane_positions<T>(rb);
-}
-
 struct Ws {
     void* first[2];
     void* second;
@@ -1449,14 +1442,13 @@ static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb,
 {
     constexpr int FULL_NP = Geo<T>::NP;
     const bool sm = !q0.w1;
-    const int np = positions_of<T>(rb, q0.N, q0.P), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
+    const int np = lane_positions<T>(rb), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
 #define WCC_AD_APPLY(RB_, NP_, SM_)                                                                                                      \
     if (rb == (RB_) && np == (NP_) && sm == (SM_))                                                                                       \
         return vec == 2 ? run_apply<T, RB_, NP_, 2, SM_>(q0, q1, dev, overlap, st)                                                        \
                         : vec == 1 ? run_apply<T, RB_, NP_, 1, SM_>(q0, q1, dev, overlap, st) : run_apply<T, RB_, NP_, 0, SM_>(q0, q1, dev, overlap, st);
-    WCC_AD_APPLY(1, FULL_NP, true) WCC_AD_APPLY(2, FULL_NP, true) WCC_AD_APPLY(4, FULL_NP, true) WCC_AD_APPLY(8, FULL_NP, true)
-    WCC_AD_APPLY(8, FULL_NP / 2, true) WCC_AD_APPLY(8, FULL_NP / 2, false) WCC_AD_APPLY(8, FULL_NP, false)
-    WCC_AD_APPLY(1, FULL_NP, false) WCC_AD_APPLY(2, FULL_NP, false) WCC_AD_APPLY(4, FULL_NP, false)
+    WCC_AD_APPLY(1, FULL_NP, true) WCC_AD_APPLY(2, FULL_NP, true) WCC_AD_APPLY(4, FULL_NP, true) WCC_AD_APPLY(8, FULL_NP / 2, true)
+    WCC_AD_APPLY(1, FULL_NP, false) WCC_AD_APPLY(2, FULL_NP, false) WCC_AD_APPLY(4, FULL_NP, false) WCC_AD_APPLY(8, FULL_NP / 2, false)
 #undef WCC_AD_APPLY
     return WCC_ERR_SHAPE;
 }

@@ -319,9 +319,10 @@ __device__ __forceinline__ void forget(Vec<T, V> (&v)[K])
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k].forget();
 }
+// FULL: every thread has all K channels; tests of each left there cost the large maps half of their speed (block's expanded map 73 -> 110 us).
 // A position's mean and reciprocal deviation from the channels that the tile's threads hold.  A first mean, then the sums of the deviations
 // from it and of their squares: they correct it, and what it was off by enters the variance in second order only.
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool FULL>
 __device__ __forceinline__ void statistics(Vec<T, V> (&v)[K], int nk, float eps, float* sm, const MapGeom& q, int l, F<V>& m, F<V>& r)
 {
     const float inv_C = 1.0f / (float)q.C;
@@ -336,7 +337,7 @@ __device__ __forceinline__ void statistics(Vec<T, V> (&v)[K], int nk, float eps,
     const F<V> neg = -m;
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < nk) {
+        if (FULL || k < nk) {
             const F<V> d = floats(v[k]) + neg;
             s[0] = s[0] + d;
             s[1] = fma(d, d, s[1]);
@@ -351,14 +352,14 @@ __device__ __forceinline__ void statistics(Vec<T, V> (&v)[K], int nk, float eps,
     }
 }
 // y of a thread's channels, stored `step` elements apart; its k-th channel's parameters are at k * cstep.
-template <typename T, int V, int K, bool STR>
+template <typename T, int V, int K, bool STR, bool FULL>
 __device__ __forceinline__ void normalise(Vec<T, V> (&v)[K], int nk, const F<V>& m, const F<V>& r, const float* pg, const float* pb, int cstep, T* py,
                                           size_t step, int stride, int nv)
 {
     const F<V> neg = -m;
 #pragma unroll
     for (int k = 0; k < K; ++k, py += step)
-        if (k < nk) {
+        if (FULL || k < nk) {
             const float ga = pg ? pg[k * cstep] : 1.0f, be = pb ? pb[k * cstep] : 0.0f;
             const F<V> o = fma((floats(v[k]) + neg) * r, F<V>(ga), F<V>(be));
             v[k].set(o.f);
@@ -367,14 +368,14 @@ __device__ __forceinline__ void normalise(Vec<T, V> (&v)[K], int nk, const F<V>&
         }
 }
 // The sums over the channels that a gradient needs (s: of g and of g xh), and this tile's share of the parameters' gradients.
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool FULL>
 __device__ __forceinline__ void gradient_sums(const Vec<T, V> (&vx)[K], const Vec<T, V> (&vd)[K], int nk, const F<V>& neg, const F<V>& r, const float* pg,
                                               int cstep, F<V> (&s)[2], float (&dg)[K], float (&db)[K])
 {
     s[0] = s[1] = F<V>(0.0f);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-        if (k < nk) {
+        if (FULL || k < nk) {
             const F<V> d = floats(vd[k]), xh = (floats(vx[k]) + neg) * r, gg = pg ? d * F<V>(pg[k * cstep]) : d;
             s[0] = s[0] + gg;
             s[1] = fma(gg, xh, s[1]);
@@ -382,14 +383,14 @@ __device__ __forceinline__ void gradient_sums(const Vec<T, V> (&vx)[K], const Ve
             for (int i = 0; i < V; ++i) { dg[k] = fmaf(d.f[i], xh.f[i], dg[k]); db[k] += d.f[i]; }
         }
 }
-template <typename T, int V, int K, bool STR>
+template <typename T, int V, int K, bool STR, bool FULL>
 __device__ __forceinline__ void gradient(Vec<T, V> (&vx)[K], const Vec<T, V> (&vd)[K], int nk, const F<V>& neg, const F<V>& r, const float* pg, int cstep,
                                          const F<V> (&s)[2], float inv_C, T* po, size_t step, int stride, int nv)
 {
     const F<V> c1 = s[0] * F<V>(-inv_C), c2 = s[1] * F<V>(-inv_C);
 #pragma unroll
     for (int k = 0; k < K; ++k, po += step)
-        if (k < nk) {
+        if (FULL || k < nk) {
             const F<V> xh = (floats(vx[k]) + neg) * r;
             const F<V> o = r * fma(xh, c2, fma(floats(vd[k]), F<V>(pg ? pg[k * cstep] : 1.0f), c1));
             vx[k].set(o.f);
@@ -441,13 +442,13 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, K * Vec<T, V>::WORDS <= 16 ? 2
         if (k < nk) load_at<T, V, STR>(v[k], px, w.stride, nv);
     }
     F<V> m, r;
-    statistics<T, V, K>(v, nk, eps, sm, q, w.l, m, r);
+    statistics<T, V, K, false>(v, nk, eps, sm, q, w.l, m, r);
     if (q.cl > 1) cluster_sync();       // nobody leaves while a neighbour reads
     if (w.g == 0 && crank == 0) {
         if (mean) store_floats_at<V, STR>(mean + (size_t)n * q.P + p, w.stride, nv, m.f);
         if (rstd) store_floats_at<V, STR>(rstd + (size_t)n * q.P + p, w.stride, nv, r.f);
     }
-    if (STR || nv) normalise<T, V, K, STR>(v, nk, m, r, gamma ? gamma + c : nullptr, beta ? beta + c : nullptr, 1 << q.groups_log2, y + at, step, w.stride, nv);
+    if (STR || nv) normalise<T, V, K, STR, false>(v, nk, m, r, gamma ? gamma + c : nullptr, beta ? beta + c : nullptr, 1 << q.groups_log2, y + at, step, w.stride, nv);
 }
 
 // ---- backward, maps -------------------------------------------------------------------------
@@ -488,11 +489,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, K * Vec<T, V>::WORDS <= 8 ? 2 
         load_floats_at<V, STR>(mean + (size_t)n * q.P + p, w.stride, nv, neg.f);
         load_floats_at<V, STR>(rstd + (size_t)n * q.P + p, w.stride, nv, r.f);
         neg = -neg;
-        gradient_sums<T, V, K>(vx, vd, nk, neg, r, pg, cstep, s, dg, db);
+        gradient_sums<T, V, K, false>(vx, vd, nk, neg, r, pg, cstep, s, dg, db);
         forget<T, V, K>(vx);
         forget<T, V, K>(vd);
         tile_sum<V, 2>(s, sm, q, w.l, buf);
-        if (STR || nv) gradient<T, V, K, STR>(vx, vd, nk, neg, r, pg, cstep, s, inv_C, dx + at, step, w.stride, nv);
+        if (STR || nv) gradient<T, V, K, STR, false>(vx, vd, nk, neg, r, pg, cstep, s, inv_C, dx + at, step, w.stride, nv);
     }
     if (q.cl > 1) cluster_sync();       // nobody leaves while a neighbour reads
     pdl_launch();
@@ -525,7 +526,7 @@ __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.com
 template <int LEFT> __device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(LEFT) : "memory"); }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
-template <typename T, int V, int K, bool BWD>
+template <typename T, int V, int K, bool BWD, bool FULL_K>
 __global__ void __launch_bounds__(32 * MAX_WARPS, 1) ln_ring(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmd,
                                                              const __grid_constant__ CUtensorMap tmo, const float* __restrict__ gamma,
                                                              const float* __restrict__ beta, float* __restrict__ mean, float* __restrict__ rstd,
@@ -586,7 +587,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 1) ln_ring(const __grid_consta
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             v[k].zero();
-            if (k < nk) v[k].load(tile + k * step);
+            if (FULL_K || k < nk) v[k].load(tile + k * step);
         }
         if constexpr (BWD) {
             Vec<T, V> vd[K];
@@ -594,23 +595,23 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 1) ln_ring(const __grid_consta
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 vd[k].zero();
-                if (k < nk) vd[k].load(td + k * step);
+                if (FULL_K || k < nk) vd[k].load(td + k * step);
             }
             F<V> s[2];
             const F<V> neg = -m;
             const float* pg = par + g;
-            gradient_sums<T, V, K>(v, vd, nk, neg, r, pg, cstep, s, dg, db);
+            gradient_sums<T, V, K, FULL_K>(v, vd, nk, neg, r, pg, cstep, s, dg, db);
             forget<T, V, K>(v);
             forget<T, V, K>(vd);
             tile_sum<V, 2>(s, sm, q, l, i & 1);
-            gradient<T, V, K, false>(v, vd, nk, neg, r, pg, cstep, s, inv_C, tile, step, 0, V);
+            gradient<T, V, K, false, FULL_K>(v, vd, nk, neg, r, pg, cstep, s, inv_C, tile, step, 0, V);
         } else {
-            statistics<T, V, K>(v, nk, eps, sm, q, l, m, r);
+            statistics<T, V, K, FULL_K>(v, nk, eps, sm, q, l, m, r);
             if (g == 0 && in) {
                 if (mean) store_floats<V>(mean + at, m.f);
                 if (rstd) store_floats<V>(rstd + at, r.f);
             }
-            normalise<T, V, K, false>(v, nk, m, r, par + g, par + q.C + g, cstep, tile, step, 0, V);
+            normalise<T, V, K, false, FULL_K>(v, nk, m, r, par + g, par + q.C + g, cstep, tile, step, 0, V);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
@@ -1216,7 +1217,7 @@ inline bool ring_map(CUtensorMap* tm, const void* ptr, int es, const Plan& p, in
     return fn(tm, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, const_cast<void*>(ptr), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-template <typename T, int V, int K, bool BWD>
+template <typename T, int V, int K, bool BWD, bool FULL_K>
 static wcc_status run_ring(const Plan& p, const void* x, const void* dy, void* out, const float* gamma, const float* beta, float* mean, float* rstd,
                            const Partials& part, int N, float eps, cudaStream_t st)
 {
@@ -1225,8 +1226,8 @@ static wcc_status run_ring(const Plan& p, const void* x, const void* dy, void* o
     DeviceInfo di;
     wcc_status s = device_info(di);
     if (s != WCC_OK) return s;
-    if ((s = allow_smem<ln_ring<T, V, K, BWD>>(di.dev, (int)p.smem)) != WCC_OK) return s;
-    return launch_overlapped(ln_ring<T, V, K, BWD>, dim3((unsigned)p.ctas), dim3((unsigned)(32 * p.q.warps)), p.smem, st, false, 1, tx, td, to, gamma, beta,
+    if ((s = allow_smem<ln_ring<T, V, K, BWD, FULL_K>>(di.dev, (int)p.smem)) != WCC_OK) return s;
+    return launch_overlapped(ln_ring<T, V, K, BWD, FULL_K>, dim3((unsigned)p.ctas), dim3((unsigned)(32 * p.q.warps)), p.smem, st, false, 1, tx, td, to, gamma, beta,
                              mean, rstd, part, p.h, eps, di.status);
 }
 template <typename T, bool BWD>
@@ -1235,7 +1236,9 @@ static wcc_status ring(const Plan& p, const void* x, const void* dy, void* out, 
 {
     constexpr int V4 = 4 / (int)sizeof(T);
 #define WCC_LN_RING(V_, K_) \
-    if (p.V == (V_) && p.K == (K_)) return run_ring<T, V_, K_, BWD>(p, x, dy, out, gamma, beta, mean, rstd, part, N, eps, st);
+    if (p.V == (V_) && p.K == (K_))                                                                                              \
+        return p.q.C == (K_) << p.q.groups_log2 ? run_ring<T, V_, K_, BWD, true>(p, x, dy, out, gamma, beta, mean, rstd, part, N, eps, st) \
+                                                : run_ring<T, V_, K_, BWD, false>(p, x, dy, out, gamma, beta, mean, rstd, part, N, eps, st);
     WCC_LN_RING(2 * V4, 2) WCC_LN_RING(2 * V4, 4) WCC_LN_RING(2 * V4, 8) WCC_LN_RING(4 * V4, 2) WCC_LN_RING(4 * V4, 4)
     if constexpr (!BWD) { WCC_LN_RING(2 * V4, 16) WCC_LN_RING(4 * V4, 8) }
 #undef WCC_LN_RING
