@@ -30,7 +30,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [nvcc, "-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-fmad=false", "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"),
+           "-fmad=false", "--split-compile=0", "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(_ROOT, "include"),
            "-I", os.path.join(_HERE, "csrc"), "-o", tmp, SRC]
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
