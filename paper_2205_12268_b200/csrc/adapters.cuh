@@ -4,14 +4,17 @@
 //     backward   V = t_a B_a^T dy_n, dx_n = base_n + A_a^T V,   dA_a = sum_n V x_n^T,   dB_a = t_a sum_n dy_n U^T
 // The rank is at most 64 and the maps are long, so both products together do about r / 2 operations a byte: the maps are the bound, not the
 // tensor pipes, and everything is arranged around reading and writing them once in whole lines.  A warp keeps the product of the first
-// factor in registers as the operand of the second: nothing of rank r goes to memory in the forward pass.
+// factor in registers as the operand of the second: nothing of rank r goes to memory in the forward pass.  (With accumulators in tensor memory it
+// would go through there and shared memory between the two; the warp-level instructions reach 20 to 40 % of their rate when the maps come at 5 TB/s.)
 //
 // The products are warp-level matrix instructions on registers.  Their rows, columns and summation index can be any permutation of
 // positions, ranks and channels that both operands agree on, and that freedom replaces every shuffle and transposition through shared memory:
-//  - first product, D[position][rank]: lane (g, t) = (lane / 4, lane % 4) loads 16 bytes of a channel, NP positions from p0 + NP g on; its b-th
+//  - first product, D[position][rank]: lane (g, t) = (lane / 4, lane % 4) takes 16 bytes of a channel, NP positions from p0 + NP g on; its b-th
 //    position is row g of row block b / 2 (upper half for odd b), its channels of a group are the CL from CL t on;
 //  - second product, D[channel][position]: the accumulators of position b are its operand as they stand, one instruction column block per b,
 //    and lane t ends up with 2 NP positions in a row of memory, 32 bytes, of the two channels g and g + 8.
+// The factors are laid out in the order of the instructions, by each CTA in shared memory or, where they are large, once by prep_kernel.  The maps
+// come through a ring of asynchronous copies that belongs to one warp (Feed).
 // bf16 maps: the factors are bf16, U is split into two bf16 parts (relative error 2^-17), sums are fp32.  fp32 maps: every operand is split into
 // two parts of 11 bits, three products of them are summed in fp32 (relative error about 2^-21 a term, beside 2^-24 of each fp32 addition).
 #pragma once
@@ -25,21 +28,19 @@ namespace ad {
 
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int MAX_RANK = 64;
-#ifndef AD_HALF
-#define AD_HALF 8
-#define AD_FILL 12LL
-#define AD_FUSED 296
-#define AD_STAGES 3
-#define AD_CTAS 3
-#define AD_RUNS 3LL
-#endif
+// What the sizes of a call decide against (us, bf16 project = 144 -> 24 on 4 x 128 x 256, fp32 headline = 64 -> 64 on 12 x 96 x 320, both rank 16):
+constexpr int HALF_FROM = 8;            // blocks of 8 ranks from which a lane takes half as many positions (from 8 / 4 / 1: headline 66 / 65 / 73)
+constexpr long long FILL = 12;          // warps an SM below which the warps of a CTA share tiles (12 / 24: 826 -> 899 on 14 x 18 x 72 59 / 72)
+constexpr int STAGES = 3;               // of a warp's feed (3 / 4: headline 57 / 62); rows that start anywhere: 2 (58 -> 70 on 3 x 129 x 257: 3 32, 2 27)
+constexpr int WAVES = 3;                // CTAs for each that fits at once, since images without an adapter are done early (1 / 3 / 6: headline 70 / 62 / 65,
+                                        // backward project 58 / 51 / -)
 
 template <typename T> struct Geo;
 template <> struct Geo<__nv_bfloat16> { static constexpr int NP = 8, TP = 64, CL = 8, GC = 32, PARTS = 1; };
 template <> struct Geo<float> { static constexpr int NP = 4, TP = 32, CL = 4, GC = 16, PARTS = 2; };
 // NP positions of a lane (16 bytes) and TP of a warp's tile in the widest form, CL channels of a lane in a group of GC, PARTS parts of a factor's
 // element.  For the largest ranks a lane takes half as many positions, which halves the sums it has to hold.
-template <typename T> __host__ __device__ constexpr int lane_positions(int rb) { return rb >= AD_HALF ? Geo<T>::NP / 2 : Geo<T>::NP; }
+template <typename T> __host__ __device__ constexpr int lane_positions(int rb) { return rb >= HALF_FROM ? Geo<T>::NP / 2 : Geo<T>::NP; }
 
 // steps of the second product's summation index, ranks in blocks of 8
 template <typename T> __host__ __device__ constexpr int steps2(int rb) { return sizeof(T) == 2 ? (rb + 1) / 2 : rb; }
@@ -78,13 +79,12 @@ __device__ __forceinline__ void split_bf16(float u0, float u1, uint32_t& hi, uin
 
 // NP positions of a channel's row from p on as they lie in memory, those at P and beyond as zeros.  VEC: rows start on multiples of NP positions.
 // Otherwise the two aligned pieces around them are loaded and shifted into place (`end`: behind the tensor's last element, nothing is read from
-// there on): single loads of 2 bytes cost eight times the instructions, a layer's odd map 76 us instead of the figure below.
+// there on).
 template <int WORDS> struct Words { uint32_t w[WORDS]; };
 template <int W> __device__ __forceinline__ Words<W> load_words(const void* p)
 {
     Words<W> r;
     if constexpr (W == 8) {
-        // volatile, so that it stays ahead of the products it is issued before
         asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
             : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
             : "l"(p));
@@ -401,7 +401,7 @@ __device__ __forceinline__ void first_step(Tile<T, RB, NP>& tile, const Words<NP
 // made of them.  With plain loads into registers the maps came no faster than 4.9 TB/s (headline batch, 57 us without those of the base).
 template <typename T, int NP, bool AL>
 struct Feed {
-    static constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), S = AL ? AD_STAGES : 2, W = PIECE / 4;
+    static constexpr int GC = Geo<T>::GC, CL = Geo<T>::CL, PIECE = NP * (int)sizeof(T), S = AL ? STAGES : 2, W = PIECE / 4;
     static constexpr int ROW = 8 * PIECE, PITCH = ROW + (AL ? 0 : 16), CH = PITCH / 16, STAGE = GC * PITCH;
     uint32_t base, fill, use;           // shared address, offsets of the stages to fill and to use next
     size_t off;                         // AL: this lane's first row and piece of a stage, from the stage's first channel at position 0; else p0
@@ -1066,7 +1066,7 @@ __global__ void __launch_bounds__(256) grad_reduce(const float* __restrict__ par
 // Shared memory of a warp for its feed, and for its tiles on their way out where rows start anywhere.
 template <typename T> static size_t feed_smem(int np, bool vec)
 {
-    return (size_t)(vec ? AD_STAGES : 2) * Geo<T>::GC * (8 * np * sizeof(T) + (vec ? 0 : 16)) + (vec ? 0 : (size_t)16 * (8 * np + 4) * 4);
+    return (size_t)(vec ? STAGES : 2) * Geo<T>::GC * (8 * np * sizeof(T) + (vec ? 0 : 16)) + (vec ? 0 : (size_t)16 * (8 * np + 4) * 4);
 }
 
 // ---- the whole backward pass in one kernel --------------------------------------------------------
@@ -1316,10 +1316,10 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
     f.nb = all <= 2 * BW ? 2 : all <= 4 * BW ? 4 : 8;
     f.units = (int)((P + unit - 1) / unit);
     const long long total = (long long)N * f.units;
-    if (rb > 2 || all > 8 * BW || N > 4096 || total < AD_FUSED) return f;
+    if (rb > 2 || all > 8 * BW || N > 4096 || total < 2 * B200_SMS) return f;
     const size_t smem = bwd_smem<T>(rb, Cin, Cout, true, P % Geo<T>::NP == 0);
     if (smem > 113 * 1024) return f;                                      // two CTAs an SM
-    f.runs = (int)std::min(total, AD_RUNS * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
+    f.runs = (int)std::min(total, (long long)WAVES * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
     f.share = (int)((total + f.runs - 1) / f.runs);
     f.runs = (int)((total + f.share - 1) / f.share);
     f.ok = true;
@@ -1386,7 +1386,7 @@ static void plan_apply(ApplyArgs<T>& q, int np, int most_ks, int& warps)
     const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
     const int most = std::max(ceil_div(q.K, Geo<T>::GC), q.f2.p ? ceil_div(q.M, 16) : 1);
     q.ks = 1;
-    while (q.ks < most_ks && q.ks * 2 <= most && (long long)q.N * tiles * q.ks < AD_FILL * B200_SMS) q.ks *= 2;
+    while (q.ks < most_ks && q.ks * 2 <= most && (long long)q.N * tiles * q.ks < FILL * B200_SMS) q.ks *= 2;
     if (!warps) warps = q.ks == 8 ? 8 : 4;
     if (q.ks == 8) warps = 8;
 }
@@ -1397,7 +1397,7 @@ static void plan_parts(ApplyArgs<T>& q, int np, int warps, bool sm)
     const long long tiles = (long long)(((q.tap ? q.Pp : q.P) + tp - 1) / tp);
     q.groups = (int)((tiles + per - 1) / per);
     // a CTA that lays out its factors takes as many groups as leave four CTAs an SM (eight warps: two)
-    const int ctas = AD_CTAS * B200_SMS * (warps == 8 ? 2 : 4);
+    const int ctas = WAVES * B200_SMS * (warps == 8 ? 2 : 4);
     q.per_part = sm ? (int)std::max(1LL, std::min((long long)q.groups, (long long)q.N * q.groups / ctas)) : 1;
     q.parts = ceil_div(q.groups, q.per_part);
 }

@@ -2,14 +2,15 @@
 //     mu = 1/C sum_c x,   v = 1/C sum_c (x - mu)^2,   r = (v + eps)^-1/2,   xh = (x - mu) r
 //     y  = xh gamma + beta
 //     g  = dy gamma,  dx = r (g - 1/C sum_c g - xh 1/C sum_c g xh),  dgamma = sum dy xh,  dbeta = sum dy  (over images, positions).
-// Both directions are bound by memory: every element is read once, kept in registers until the statistics of its position are
-// known, and written once.
+// Both directions are bound by memory: every element is read once, kept on the SM until the statistics of its position are known, and
+// written once.
 //
-// Maps: a CTA takes all channels of a tile of positions.  `segl` lanes cover the tile's positions in vectors of V elements, the
-// CTA's threads form 256 / segl groups, and group g holds channels g, g + G, ...: K vectors a thread.  Wide segments load whole lines,
-// narrow ones leave registers for more channels and make more tiles; ln_plan weighs them.  Channels beyond one CTA's registers go
-// to a cluster whose CTAs exchange their statistics through distributed shared memory.
-// Rows (one position an image): the channels are contiguous, 8, 32 or 256 threads take a row.
+// Maps: a CTA takes all channels of a tile of positions.  `segl` lanes cover 16 to 512 bytes of a channel's row in vectors of V elements; the
+// groups of lanes hold channels g, g + G, ...: K vectors a thread.  Large maps whose rows start on 16 bytes go through a ring of TMA tiles
+// (ln_ring), the others load straight into registers (ln_fwd_map, ln_bwd_map); channels beyond one CTA's registers go to a cluster whose
+// CTAs exchange their sums through distributed shared memory.
+// Rows (one position an image): the channels are contiguous.  Many rows: a warp a row, fed by copies of its own (ln_fwd_feed, ln_bwd_feed);
+// few, wide or odd ones: 8, 32 or 256 threads a row.
 // Statistics are fp32 sums over registers in two rounds, the mean and then the deviations from it, so that a large common offset of the
 // channels costs no digits of the variance.
 #pragma once
@@ -47,27 +48,41 @@ struct Vec {
         else if (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     }
-    // Element i from p[i * stride]; only the first n.
+    // Element i from p[i * stride]; only the first n.  (All of them but at the end of an image: without a test of each.)
     __device__ __forceinline__ void load(const T* p, int stride, int n)
     {
+        if (n == V) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (sizeof(T) == 4) { if (i < n) w[i % WORDS] = *reinterpret_cast<const uint32_t*>(p + i * stride); }
-            else {
-                uint32_t u = 0u;
-                if (i < n) u = *reinterpret_cast<const uint16_t*>(p + i * stride);
-                w[(i >> 1) % WORDS] |= u << (16 * (i & 1));
-            }
+            for (int i = 0; i < V; ++i, p += stride) put(i, p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i, p += stride)
+                if (i < n) put(i, p);
+        }
+    }
+    __device__ __forceinline__ void put(int i, const T* p)
+    {
+        if (sizeof(T) == 4) w[i % WORDS] = *reinterpret_cast<const uint32_t*>(p);
+        else {
+            const uint32_t u = *reinterpret_cast<const uint16_t*>(p);
+            w[(i >> 1) % WORDS] = i & 1 ? w[(i >> 1) % WORDS] | u << 16 : u;
         }
     }
     __device__ __forceinline__ void store(T* p, int stride, int n) const
     {
+        if (n == V) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) {
-                if (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p + i * stride) = w[i % WORDS];
-                else *reinterpret_cast<uint16_t*>(p + i * stride) = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
-            }
+            for (int i = 0; i < V; ++i, p += stride) take(i, p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i, p += stride)
+                if (i < n) take(i, p);
+        }
+    }
+    __device__ __forceinline__ void take(int i, T* p) const
+    {
+        if (sizeof(T) == 4) *reinterpret_cast<uint32_t*>(p) = w[i % WORDS];
+        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[(i >> 1) % WORDS] >> (16 * (i & 1)));
     }
     __device__ __forceinline__ void zero()
     {
@@ -637,6 +652,18 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 1) ln_ring(const __grid_consta
     }
 }
 
+// The gradients of the parameters from the sums of a CTA's warps, [warp][2][C] in shared memory: a thread a column, the warps in order.
+__device__ __forceinline__ void add_warps(const float* acc, int warps, int C, const Partials& out, int row)
+{
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * C; i += NT) {
+        float a = acc[i];
+        for (int w = 1; w < warps; ++w) a += acc[(size_t)w * 2 * C + i];
+        float* o = i < C ? out.g : out.b;
+        if (o) o[row * out.pitch + (i < C ? i : i - C)] = a;
+    }
+}
+
 // ---- rows (one position an image) -------------------------------------------------------------
 // TR threads take a row of C contiguous channels, vector j of thread t holds channels (t + j TR) V and on.
 template <int TR>
@@ -719,7 +746,7 @@ template <typename T, int V, int K, int TR>
 __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                   const float* __restrict__ rstd, T* dx, Partials out, int N, int C)
 {
-    extern __shared__ float acc_sm[];   // TR < 256: [2][C], the sums of the CTA's warps
+    extern __shared__ __align__(16) float acc_sm[];      // TR < 256: [warp][2][C], the sums of the CTA's warps
     __shared__ float2 sm[WARPS];
     const int t = threadIdx.x % TR, sub = threadIdx.x / TR;
     constexpr int R = NT / TR;
@@ -785,7 +812,7 @@ __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const
     }
     pdl_launch();
     if (!out.g && !out.b) return;
-    // the row groups of a warp add up, then the warps one after the other: a fixed order
+    // the row groups of a warp add up, then the warps: a fixed order
 #pragma unroll
     for (int o = TR; o < 32; o <<= 1)
 #pragma unroll
@@ -795,28 +822,31 @@ __global__ void __launch_bounds__(NT) ln_bwd_rows(const T* dy, const T* x, const
                 dg[k][i] += __shfl_xor_sync(FULL, dg[k][i], o);
                 db[k][i] += __shfl_xor_sync(FULL, db[k][i], o);
             }
-    constexpr int TURNS = TR < NT ? WARPS : 1;
-    const size_t row = blockIdx.x * out.pitch;
-    for (int w = 0; w < TURNS; ++w) {
-        if (TURNS == 1 || ((int)(threadIdx.x >> 5) == w && (int)(threadIdx.x & 31) < TR)) {
+    if constexpr (TR < NT) {
+        const int per = 32 / TR, warp = (int)threadIdx.x >> 5;         // rows of a warp at once
+        const long long left = N - (long long)blockIdx.x * R;
+        const int warps = (int)min((long long)WARPS, (left + per - 1) / per);      // those that had one
+        if ((int)(threadIdx.x & 31) < TR && warp < warps) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 const int c = (t + k * TR) * V;
                 if (c < C) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        float a = dg[k][i], b = db[k][i];
-                        if (w > 0) { a += acc_sm[c + i]; b += acc_sm[C + c + i]; }
-                        if (w + 1 < TURNS) { acc_sm[c + i] = a; acc_sm[C + c + i] = b; }
-                        else {
-                            if (out.g) out.g[row + c + i] = a;
-                            if (out.b) out.b[row + c + i] = b;
-                        }
-                    }
+                    store_floats<V>(acc_sm + (size_t)warp * 2 * C + c, dg[k]);
+                    store_floats<V>(acc_sm + (size_t)warp * 2 * C + C + c, db[k]);
                 }
             }
         }
-        if (TURNS > 1) __syncthreads();
+        add_warps(acc_sm, warps, C, out, blockIdx.x);
+    } else {
+        const size_t row = blockIdx.x * out.pitch;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (t + k * TR) * V;
+            if (c < C) {
+                if (out.g) store_floats<V>(out.g + row + c, dg[k]);
+                if (out.b) store_floats<V>(out.b + row + c, db[k]);
+            }
+        }
     }
 }
 
@@ -999,33 +1029,18 @@ __global__ void __launch_bounds__(NT, 2) ln_bwd_feed(const T* dy, const T* x, co
     RowFeed<T, K>::drain();
     pdl_launch();
     if (!out.g && !out.b) return;
-    // the warps add up one after the other, in the room of the rows: a fixed order
+    // the warps' sums, in the room of the rows
     float* acc = feed_sm + C;
     __syncthreads();
-    const size_t at = blockIdx.x * out.pitch;
-    for (int w = 0; w < WARPS; ++w) {
-        if (warp == w) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int c = (lane + 32 * k) * V;
-                if (c < C) {
-                    if (w > 0) {
-                        F<V> a, b;
-                        load_floats<V>(acc + c, a.f);
-                        load_floats<V>(acc + C + c, b.f);
-                        dg[k] = dg[k] + a;
-                        db[k] = db[k] + b;
-                    }
-                    if (w + 1 < WARPS) { store_floats<V>(acc + c, dg[k].f); store_floats<V>(acc + C + c, db[k].f); }
-                    else {
-                        if (out.g) store_floats<V>(out.g + at + c, dg[k].f);
-                        if (out.b) store_floats<V>(out.b + at + c, db[k].f);
-                    }
-                }
-            }
+    for (int k = 0; k < K; ++k) {
+        const int c = (lane + 32 * k) * V;
+        if (c < C) {
+            store_floats<V>(acc + (size_t)warp * 2 * C + c, dg[k].f);
+            store_floats<V>(acc + (size_t)warp * 2 * C + C + c, db[k].f);
         }
-        __syncthreads();
     }
+    add_warps(acc, WARPS, C, out, blockIdx.x);
 }
 
 // dgamma and dbeta from the partial rows: 32 columns a CTA, 32 threads a column, added in a fixed order.
@@ -1060,10 +1075,6 @@ struct Plan {
     size_t smem;
 };
 
-#ifndef LN_KF
-#define LN_KF 16
-#define LN_KB 8
-#endif
 // Elements of a vector
 inline int vec_elems(size_t len, int es)
 {
@@ -1072,17 +1083,14 @@ inline int vec_elems(size_t len, int es)
     return v;
 }
 
-#ifndef LN_RING_TILE
-#define LN_RING_TILE 32768
-#define LN_RING_VB 8
-#define LN_RING_MIN 2
-#endif
-// The ring, where rows start on 16 bytes and there are tiles enough to keep it busy.
+// The ring, where rows start on 16 bytes and there are two tiles or more for every CTA that fits at once.  Tiles of 32 KB (x and dy together), twice
+// that where rows of 64 bytes would be cut otherwise; 8 bytes a lane (forward on 4 x 1024 x 128 x 128 bf16, us: 4 bytes -, 8 65, 16 72; backward
+// on 12 x 64 x 96 x 320 fp32 8 54, 16 53).  Without the ring these take 114 and 74.
 inline bool ring_plan(Plan& p, int N, int C, size_t P, int es, bool bwd)
 {
     if (P * es % 16 != 0 || P * es < 64 || C < 8) return false;
     int row = 512;                                                       // bytes of a tile's row
-    const int most = LN_RING_TILE >> (bwd ? 1 : 0);
+    const int most = 32768 >> (bwd ? 1 : 0);
     while (row > 64 && (long long)row * C > most) row /= 2;
     while (row > 64 && (size_t)row > P * es) row /= 2;
     RingGeom& h = p.h;
@@ -1093,7 +1101,7 @@ inline bool ring_plan(Plan& p, int N, int C, size_t P, int es, bool bwd)
     if (h.half > 65536u >> (bwd ? 1 : 0)) return false;
     const size_t tiles = (P + h.tp - 1) / h.tp;
     if (tiles * N > 0x7FFFFFFFull) return false;
-    const int vb = std::min(row / 4, LN_RING_VB);
+    const int vb = std::min(row / 4, 8);
     p.V = vb / es;
     int lg = 0;
     while ((vb << lg) < row && lg < 5) ++lg;
@@ -1113,12 +1121,13 @@ inline bool ring_plan(Plan& p, int N, int C, size_t P, int es, bool bwd)
     p.smem = 128 + (size_t)STAGES * h.half * (bwd ? 2 : 1) + (size_t)tile_floats(q, h.tp) * 4 + (size_t)(bwd ? 1 : 2) * C * 4;
     const int per_sm = std::max(1, std::min((int)(225 * 1024 / (p.smem + 1200)), 512 / (32 * warps)));
     p.ctas = std::min(q.items, per_sm * B200_SMS);
-    if (q.items < LN_RING_MIN * p.ctas) return false;
+    if (q.items < 2 * p.ctas) return false;
     p.ring = true;
     return true;
 }
 
-// Registers: a thread of the forward pass holds K vectors, one of the backward pass 2 K (and 2 K sums).
+// Registers: a thread of the forward pass holds K vectors, one of the backward pass 2 K (and 2 K sums): at most 32 and 16 words of a map, and
+// half of that while more warps can share the channels.
 inline Plan plan_of(int N, int C, size_t P, int es, bool bwd)
 {
     Plan p{};
@@ -1129,27 +1138,28 @@ inline Plan plan_of(int N, int C, size_t P, int es, bool bwd)
         const int caps[5][2] = {{8, 8}, {8, 32}, {32, 32}, {256, 8}, {256, 32}};      // threads a row, channels a thread
         int i = 0;
         while (caps[i][0] * caps[i][1] < C) ++i;                                         // 256 x 32 = WCC_MAX_CHANNELS
+        // a warp a row: forward from four rows a warp on, where gamma and beta have been paid for
         const int v16 = 16 / es, k = ceil_div(C, 32 * v16);
         if (C % v16 == 0 && k <= (es == 2 ? 4 : 8) && N >= (bwd ? 1 : 4) * WARPS * B200_SMS) {
             p.feed = true;
             p.K = k <= 1 ? 1 : k <= 2 ? 2 : k <= 4 ? 4 : 8;
             p.smem = (size_t)(bwd ? 1 : 2) * C * 4 + (size_t)WARPS * ROW_STAGES * p.K * 512 * (bwd ? 2 : 1);
-            if (bwd && p.smem < (size_t)3 * C * 4) p.smem = (size_t)3 * C * 4;
+            if (bwd) p.smem = std::max(p.smem, (size_t)(1 + 2 * WARPS) * C * 4);
             const int per_sm = bwd ? 2 : 4;
             p.ctas = std::min(ceil_div(N, WARPS), B200_SMS * std::min(per_sm, (int)(228 * 1024 / (p.smem + 1024))));
             return p;
         }
         p.TR = caps[i][0];
         p.K = caps[i][1] / p.V;
-        p.smem = bwd && p.TR < NT ? (size_t)2 * C * 4 : 0;
+        p.smem = bwd && p.TR < NT ? (size_t)WARPS * 2 * C * 4 : 0;
         return p;
     }
     if (ring_plan(p, N, C, P, es, bwd)) return p;
     // single loads where rows start on no vector (a vector of two bf16 is hardly better)
     p.V = vec_elems(P, es);
     p.strided = p.V * es < (es == 2 ? 4 : 8);
-    if (p.strided) p.V = 16 / es;
-    const int words = p.V * es / 4, kmax = (bwd ? 16 : 32) / words, kgood = (bwd ? LN_KB : LN_KF) / words;
+    if (p.strided) p.V = 8 / es;
+    const int words = p.V * es / 4, kmax = (bwd ? 16 : 32) / words, kgood = (bwd ? 8 : 16) / words;
     int lg = 0;
     while (lg < 5 && ((size_t)p.V << lg) < P) ++lg;
     auto tiles_of = [&](int s) { return (P + ((size_t)p.V << s) - 1) / ((size_t)p.V << s); };
@@ -1202,6 +1212,9 @@ template <typename T, int V, int K, int TR>
 static wcc_status bwd_rows(const Plan& p, int ctas, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
                            const Partials& part, int N, int C, cudaStream_t st)
 {
+    DeviceInfo di;
+    wcc_status s = device_info(di);
+    if (s != WCC_OK || (s = allow_smem<ln_bwd_rows<T, V, K, TR>>(di.dev, (int)p.smem)) != WCC_OK) return s;
     return launch_overlapped(ln_bwd_rows<T, V, K, TR>, dim3((unsigned)ctas), dim3(NT), p.smem, st, false, 1, static_cast<const T*>(dy),
                              static_cast<const T*>(x), gamma, mean, rstd, static_cast<T*>(dx), part, N, C);
 }
@@ -1307,7 +1320,7 @@ static wcc_status forward(const Plan& p, const void* x, const float* gamma, cons
     constexpr int V4 = 4 / (int)sizeof(T);
     WCC_LN_MAP(4 * V4, 2, false) WCC_LN_MAP(4 * V4, 4, false) WCC_LN_MAP(4 * V4, 8, false)
     WCC_LN_MAP(2 * V4, 2, false) WCC_LN_MAP(2 * V4, 4, false) WCC_LN_MAP(2 * V4, 8, false) WCC_LN_MAP(2 * V4, 16, false)
-    WCC_LN_MAP(4 * V4, 2, true) WCC_LN_MAP(4 * V4, 4, true) WCC_LN_MAP(4 * V4, 8, true)
+    WCC_LN_MAP(2 * V4, 2, true) WCC_LN_MAP(2 * V4, 4, true) WCC_LN_MAP(2 * V4, 8, true) WCC_LN_MAP(2 * V4, 16, true)
     if constexpr (V4 == 2) { WCC_LN_MAP(V4, 2, false) WCC_LN_MAP(V4, 4, false) WCC_LN_MAP(V4, 8, false) WCC_LN_MAP(V4, 16, false) WCC_LN_MAP(V4, 32, false) }
 #undef WCC_LN_MAP
     return WCC_ERR_SHAPE;
@@ -1340,7 +1353,7 @@ static wcc_status backward(const Plan& p, const void* dy, const void* x, const f
     constexpr int V4 = 4 / (int)sizeof(T);
     WCC_LN_MAP(4 * V4, 2, false) WCC_LN_MAP(4 * V4, 4, false)
     WCC_LN_MAP(2 * V4, 2, false) WCC_LN_MAP(2 * V4, 4, false) WCC_LN_MAP(2 * V4, 8, false)
-    WCC_LN_MAP(4 * V4, 2, true) WCC_LN_MAP(4 * V4, 4, true)
+    WCC_LN_MAP(2 * V4, 2, true) WCC_LN_MAP(2 * V4, 4, true) WCC_LN_MAP(2 * V4, 8, true)
     if constexpr (V4 == 2) { WCC_LN_MAP(V4, 2, false) WCC_LN_MAP(V4, 4, false) WCC_LN_MAP(V4, 8, false) WCC_LN_MAP(V4, 16, false) }
 #undef WCC_LN_MAP
     return WCC_ERR_SHAPE;
