@@ -303,3 +303,59 @@ def test_binding_refusals(wcc):      # noqa: F811
     with pytest.raises(wcc.WccError) as e:
         ad.backward(dy, x, ids, ws=wcc.Workspace(256, x.device))
     assert e.value.code == 7
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(3, 24, 40, 1, 1, 2, 4), (3, 24, 40, 9, 7, 2, 4), (4, 24, 40, 128, 160, 2, 12), (3, 40, 24, 65, 129, 2, 5),
+                                  (2, 200, 300, 24, 24, 2, 20)])
+def test_the_factors_gradients_alone(wcc, size, dtype):      # noqa: F811
+    """No dx (the first layer of a network), through the C entry point: the gradients of the factors are those of the whole call."""
+    N, Cin, Cout, H, W, R, r = size
+    d = _data(size, dtype, 12)
+    ad = wcc.Adapters(d["A"], d["B"], d["scale"])
+    _, dA, dB = ad.backward(d["dy"], d["x"], d["ids"])
+    a, b, ws = torch.empty_like(dA), torch.empty_like(dB), ad.workspace(d["x"])
+    code = wcc.lib().wcc_adapters_bwd(d["dy"].data_ptr(), d["x"].data_ptr(), d["A"].data_ptr(), d["B"].data_ptr(), d["scale"].data_ptr(),
+                                      d["ids"].data_ptr(), None, N, Cin, Cout, H, W, R, r, ad.dt, None, a.data_ptr(), b.data_ptr(), ws.buf.data_ptr(),
+                                      ws.nbytes, wcc._stream())
+    assert code == 0 and torch.equal(a, dA) and torch.equal(b, dB)
+    _check_backward(d, None, ad.backward(d["dy"], d["x"], d["ids"], params=False)[0], None, None)
+    assert wcc.last_status() == 0
+
+
+@pytest.mark.parametrize("width", [1 << 15, (1 << 15) - 1])
+def test_more_than_two_to_the_31_elements(wcc, width):      # noqa: F811
+    """Offsets beyond 32 bits, aligned rows and others: maps that are constant over their positions but for the last one."""
+    C, H, r = 5, 1 << 14, 3
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x = torch.empty((1, C, H, width), dtype=torch.bfloat16, device="cuda")
+    for c in range(C):
+        x[:, c].fill_(float(c) - 1.5)
+    x[0, :, -1, -1] = torch.tensor([1.0, -2.0, 4.0, 0.5, 8.0])
+    A = torch.randn((1, r, C), device="cuda", generator=g).bfloat16()
+    B = torch.randn((1, C, r), device="cuda", generator=g).bfloat16()
+    ids = torch.zeros((1,), dtype=torch.int32, device="cuda")
+    ad = wcc.Adapters(A, B)
+    y = ad(x, ids)
+    for where in ((0, 0), (H - 1, width - 1), (H // 2, 7)):
+        v = x[0, :, where[0], where[1]].double()
+        want = B[0].double() @ (A[0].double() @ v)
+        tol = 2.0 ** -7 * (B[0].double().abs() @ (A[0].double().abs() @ v.abs()))
+        assert ((y[0, :, where[0], where[1]].double() - want).abs() <= tol).all()
+    assert torch.equal(y[0, :, 0], y[0, :, 0, :1].expand(C, width)) and torch.equal(y[0, :, -1, :-1], y[0, :, 0, 1:])
+    del y
+    dy = x
+    dx, dA, dB = ad.backward(dy, x.clone(), ids)
+    first, last, n = x[0, :, 0, 0].double(), x[0, :, -1, -1].double(), H * width - 1
+    for v, where in ((first, (0, 0)), (last, (H - 1, width - 1))):
+        V = B[0].double().t() @ v
+        want = A[0].double().t() @ V
+        tol = 2.0 ** -7 * (A[0].double().abs().t() @ (B[0].double().abs().t() @ v.abs()))
+        assert ((dx[0, :, where[0], where[1]].double() - want).abs() <= tol).all()
+    wA = n * torch.outer(B[0].double().t() @ first, first) + torch.outer(B[0].double().t() @ last, last)
+    wB = n * torch.outer(first, A[0].double() @ first) + torch.outer(last, A[0].double() @ last)
+    # equal terms, n of them, added in chains: n u relative bounds them with room, the chains are far shorter
+    mA = n * torch.outer(B[0].double().abs().t() @ first.abs(), first.abs())
+    mB = n * torch.outer(first.abs(), A[0].double().abs() @ first.abs())
+    assert ((dA[0].double() - wA).abs() <= 1e-3 * mA + 1).all() and ((dB[0].double() - wB).abs() <= 1e-3 * mB + 1).all()
+    assert wcc.last_status() == 0

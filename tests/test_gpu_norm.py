@@ -241,3 +241,48 @@ def test_binding_refusals(wcc):      # noqa: F811
     with pytest.raises(wcc.WccError) as e:
         wcc.layernorm_backward(dy, x, mean, rstd, ws=wcc.Workspace(16, x.device))
     assert e.value.code == 7
+
+
+@pytest.mark.parametrize("size", [(3, 40, 1, 1), (2, 24, 9, 8), (2, 64, 96, 128), (2, 30, 7, 9)])
+def test_one_affine_parameter_without_the_other(wcc, size):      # noqa: F811
+    x, dy, gamma, beta = _data(size, torch.float32, 12)
+    _check_forward(x, gamma, None, 1e-5, *wcc.layernorm(x, gamma, None, stats=True))
+    _check_forward(x, None, beta, 1e-5, *wcc.layernorm(x, None, beta, stats=True))
+    # and one gradient without the other, through the C entry point
+    N, C, H, W = size
+    _, mean, rstd = wcc.layernorm(x, stats=True)
+    dx, dgamma, dbeta = wcc.layernorm_backward(dy, x, mean, rstd)
+    ws = wcc.Workspace.for_layernorm_backward(x)
+    for g, b in ((True, False), (False, True)):
+        out, par = torch.empty_like(x), torch.empty((C,), device="cuda")
+        code = wcc.lib().wcc_layernorm_bwd(dy.data_ptr(), x.data_ptr(), None, mean.data_ptr(), rstd.data_ptr(), N, C, H, W, 0, out.data_ptr(),
+                                           par.data_ptr() if g else None, par.data_ptr() if b else None, ws.buf.data_ptr(), ws.nbytes, wcc._stream())
+        assert code == 0 and torch.equal(out, dx) and torch.equal(par, dgamma if g else dbeta)
+
+
+@pytest.mark.parametrize("width", [1 << 15, (1 << 15) - 1])
+def test_more_than_two_to_the_31_elements(wcc, width):      # noqa: F811
+    """Offsets beyond 32 bits: the last positions of the last channels, and the sums over everything."""
+    C, H = 5, 1 << 14
+    x = torch.empty((1, C, H, width), dtype=torch.bfloat16, device="cuda")
+    for c in range(C):
+        x[:, c].fill_(float(c))
+    x[0, :, -1, -1] = torch.tensor([1.0, -2.0, 4.0, 0.5, 8.0])
+    assert x.numel() > 1 << 31 or width % 2
+    y, mean, rstd = wcc.layernorm(x, eps=1e-5, stats=True)
+    for where in ((0, 0), (H - 1, width - 1), (H // 2, 7)):
+        v = x[0, :, where[0], where[1]].double()
+        want = (v - v.mean()) * (v.var(unbiased=False) + 1e-5) ** -0.5
+        assert ((y[0, :, where[0], where[1]].double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5).all()
+        assert abs(float(mean[0, where[0] * width + where[1]]) - float(v.mean())) <= 1e-6 * 8
+    assert torch.equal(y[0, :, 0], y[0, :, 0, :1].expand(C, width))
+    del y
+    dx, dgamma, dbeta = wcc.layernorm_backward(x, x, mean, rstd, dx=None)
+    # dy = x: sum over positions of channel c, H width - 1 times c and once the last position's value
+    want = torch.tensor([float(c) * (H * width - 1) for c in range(C)], dtype=torch.float64, device="cuda") + x[0, :, -1, -1].double()
+    assert ((dbeta.double() - want).abs() <= 2.0 ** -24 * (96 + H * width / 32) * want.abs() + 10).all()
+    v, r = x[0, :, -1, -1].double(), float(rstd[0, -1])
+    xh = (v - float(mean[0, -1])) * r
+    ref = r * (v - v.mean() - xh * (v * xh).mean())
+    assert ((dx[0, :, -1, -1].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-4).all()
+    assert wcc.last_status() == 0
