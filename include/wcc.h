@@ -322,7 +322,7 @@ wcc_status wcc_layernorm_fwd(const void* x, const float* gamma, const float* bet
  *     dx = rstd * (g - 1/C sum_c g - xh * 1/C sum_c g xh),   dgamma[c] = sum_{n,p} dy xh,   dbeta[c] = sum_{n,p} dy
  *   dy, x in: [N][C][H][Wd] of dt           mean, rstd in: what the forward pass returned
  *   dx   out: as x; may be dy or x itself   dgamma, dbeta out: fp32 [C], each may be NULL (both NULL: ws is not used and may be NULL)
- *   ws      : scratch of at least wcc_layernorm_bwd_workspace_bytes(...) bytes, 16-byte aligned
+ *   ws      : scratch of at least wcc_layernorm_bwd_workspace_bytes(...) bytes of this call's sizes (smaller ones may need more), 16-byte aligned
  * The sums over images and positions are fp32, in an order that depends on the sizes alone: the same call gives the same bits.
  */
 size_t wcc_layernorm_bwd_workspace_bytes(int N, int C, int H, int Wd, wcc_dtype dt);
@@ -354,7 +354,7 @@ wcc_status wcc_adapters_fwd(const void* x, const void* A, const void* B, const f
  *   dy   in : [N][Cout][H][Wd] of dt                 base in: [N][Cin][H][Wd] of dt, what dx is added to (the shared projection's own gradient), or NULL
  *   dx   out: [N][Cin][H][Wd] of dt, may be base, must not overlap x or dy; NULL: not wanted
  *   dA, dB out: fp32 [R][rank][Cin] and [R][Cout][rank], zeros for adapters without an image; both NULL: not wanted (x may then be NULL)
- *   ws      : scratch of at least wcc_adapters_workspace_bytes(..., 1) bytes, 16-byte aligned
+ *   ws      : scratch of at least wcc_adapters_workspace_bytes(..., 1) bytes of this call's sizes (smaller ones may need more), 16-byte aligned
  * The sums over images and positions are fp32, in an order that depends on the sizes and the ids alone: the same call gives the same bits.
  */
 wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const void* B, const float* scale, const int32_t* ids,

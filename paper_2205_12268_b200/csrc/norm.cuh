@@ -334,7 +334,7 @@ __device__ __forceinline__ void forget(Vec<T, V> (&v)[K])
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k].forget();
 }
-// FULL: every thread has all K channels; tests of each left there cost the large maps half of their speed (block's expanded map 73 -> 110 us).
+// FULL: every thread has all K channels; tests of each slowed the large maps (4 x 1024 x 128 x 128 bf16 110 us instead of 65).
 // A position's mean and reciprocal deviation from the channels that the tile's threads hold.  A first mean, then the sums of the deviations
 // from it and of their squares: they correct it, and what it was off by enters the variance in second order only.
 template <typename T, int V, int K, bool FULL>
