@@ -342,7 +342,8 @@ wcc_status wcc_layernorm_bwd(const void* dy, const void* x, const float* gamma, 
  * rank is 1 .. WCC_MAX_RANK; adapters of smaller rank are padded with zero rows of A and columns of B.  H and Wd are any positive numbers,
  * H = Wd = 1 is a batch of single tokens.  N * H * Wd <= 2^30, R <= 65535.  An id of R or more counts as none, and wcc_last_status then
  * reports WCC_ERR_INDEX.  Sums are fp32; the products of rank size keep at least 16 bits (bf16 maps) or 21 bits (fp32 maps) of a factor.
- * A position with a NaN or an infinity among its channels gives NaN or infinity at that position alone.
+ * A position with a NaN or an infinity among its channels gives NaN or infinity at that position alone (fp32 maps: so does a value within 2^-12 of
+ * the largest).
  */
 #define WCC_MAX_RANK 64
 size_t wcc_adapters_workspace_bytes(int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, int backward);

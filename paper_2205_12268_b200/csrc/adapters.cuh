@@ -32,8 +32,8 @@ constexpr int MAX_RANK = 64;
 constexpr int HALF_FROM = 8;            // blocks of 8 ranks from which a lane takes half as many positions (from 8 / 4 / 1: headline 66 / 65 / 73)
 constexpr long long FILL = 12;          // warps an SM below which the warps of a CTA share tiles (12 / 24: 826 -> 899 on 14 x 18 x 72 59 / 72)
 constexpr int STAGES = 3;               // of a warp's feed (3 / 4: headline 57 / 62); rows that start anywhere: 2 (58 -> 70 on 3 x 129 x 257: 3 32, 2 27)
-constexpr int WAVES = 3;                // CTAs for each that fits at once, since images without an adapter are done early (1 / 3 / 6: headline 70 / 62 / 65,
-                                        // backward project 58 / 51 / -)
+constexpr int WAVES = 3;                // CTAs for each that fits at once, since images without an adapter are done early (1 / 3 / 6: headline 70 / 62 / 65;
+                                        // its backward pass, 1 / 2 / 3: 120 / 117 / 112)
 
 template <typename T> struct Geo;
 template <> struct Geo<__nv_bfloat16> { static constexpr int NP = 8, TP = 64, CL = 8, GC = 32, PARTS = 1; };
@@ -1320,7 +1320,8 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
     const size_t smem = bwd_smem<T>(rb, Cin, Cout, true, P % Geo<T>::NP == 0);
     if (smem > 113 * 1024) return f;                                      // two CTAs an SM
     f.runs = (int)std::min(total, (long long)WAVES * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
-    f.share = (int)((total + f.runs - 1) / f.runs);
+    // two units at least: factors laid out and a feed filled for a single one are not paid for (512 units in runs of 1 / 2: project 65 / 46)
+    f.share = (int)std::max(2LL, (total + f.runs - 1) / f.runs);
     f.runs = (int)((total + f.share - 1) / f.share);
     f.ok = true;
     return f;
