@@ -397,6 +397,21 @@ wcc_status wcc_debug_select(const float* nrm2, int P, int k, const unsigned* his
                             int* rank, int* idx, void* stream);
 
 /*
+ * Test hooks: which kernels a call of these sizes runs (host arithmetic alone: no device needed, nothing is launched); 0: the sizes are refused.
+ *   out: the address of y or dx (forms of stores go by its alignment)      backward: 0 the forward pass, 1 the whole backward pass
+ * wcc_debug_adapters_path: one of WCC_PATH_ADAPTERS_*, WCC_PATH_FORM times how rows are stored (2: 32 bytes at once where a lane has that much, 1: 16, 0: from
+ * anywhere), and with WCC_PATH_ADAPTERS_ONE_KERNEL WCC_PATH_BLOCKS times the blocks of 16 channels that a warp has room for.
+ * wcc_debug_layernorm_path: one of WCC_PATH_NORM_*, and WCC_PATH_ALL_CHANNELS where every thread of the ring has all of its channels.
+ */
+enum {
+    WCC_PATH_ADAPTERS_TOKEN = 1, WCC_PATH_ADAPTERS_MAP = 2, WCC_PATH_ADAPTERS_MAP_PREPARED = 3, WCC_PATH_ADAPTERS_ONE_KERNEL = 4,
+    WCC_PATH_NORM_ROWS = 1, WCC_PATH_NORM_ROW_FEED = 2, WCC_PATH_NORM_MAP = 3, WCC_PATH_NORM_MAP_ANYWHERE = 4, WCC_PATH_NORM_RING = 5,
+    WCC_PATH_ALL_CHANNELS = 8, WCC_PATH_FORM = 16, WCC_PATH_BLOCKS = 64
+};
+int wcc_debug_adapters_path(int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, const void* out, int backward);
+int wcc_debug_layernorm_path(int N, int C, int H, int Wd, wcc_dtype dt, int backward);
+
+/*
  * Measurement helpers (no counterpart in the paper).  With profiling on, wcc_forward records CUDA events on its
  * stream around each stage; wcc_profile_read waits for the last recorded call and writes, to the HOST array ms, the
  * milliseconds of, for wcc_forward_staged: 0 Haar transform + norms, 1 top-k select + compaction, 2 weight

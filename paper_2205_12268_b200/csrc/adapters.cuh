@@ -517,8 +517,8 @@ struct Feed {
 };
 
 // dst = base + second product, of the blocks kw, kw + ks, ... of 16 channels of an image (base, dst: its first channel; base may be NULL).
-// next_base(x): this lane's part of the next block's base from the feed (VEC 0: the stage's address).  VEC 2: rows also start on 2 NP positions.  out: this warp's
-// 16 x (TP + 4) floats, VEC 0 only.
+// next_base(x): this lane's part of the next block's base from the feed (VEC 0: the stage's address).  VEC: see row_form; with 2 a lane stores its 2 NP
+// positions at once.  out: this warp's 16 x (TP + 4) floats, VEC 0 only.
 template <typename T, int RB, int VEC, bool SM, int NP, typename Next>
 __device__ __forceinline__ void second_product(const Tile<T, RB, NP>& tile, const T* base, T* dst, int M, size_t P, size_t p0, const uint4* w2, int kw, int ks,
                                                float* out, Next next_base)
@@ -1379,6 +1379,14 @@ static Ws carve(void* ws, int N, int Cin, int Cout, size_t P, int R, int rank, b
     return w;
 }
 
+// How rows start: 2 on 2 NP positions, which are stored at once, 1 on NP, 0 anywhere.  With all of a lane's positions the former are 32 bytes in one
+// store, and such a store needs an address on 32 bytes, where every map is only promised to start on 16: the output's own address decides too.
+template <typename T>
+static int row_form(size_t P, const void* dst, int np)
+{
+    if (P % (2 * np) == 0 && reinterpret_cast<uintptr_t>(dst) % (2 * np * sizeof(T)) == 0) return 2;
+    return P % np == 0 ? 1 : 0;
+}
 // Warps that share a tile: more only while the tiles alone do not fill the GPU.
 template <typename T>
 static void plan_apply(ApplyArgs<T>& q, int np, int most_ks, int& warps)
@@ -1443,7 +1451,7 @@ static wcc_status launch_apply(const ApplyArgs<T>& q0, ApplyArgs<T>* q1, int rb,
 {
     constexpr int FULL_NP = Geo<T>::NP;
     const bool sm = !q0.w1;
-    const int np = lane_positions<T>(rb), vec = q0.P % (2 * np) == 0 ? 2 : q0.P % np == 0 ? 1 : 0;
+    const int np = lane_positions<T>(rb), vec = row_form<T>(q0.P, q0.dst, np);
 #define WCC_AD_APPLY(RB_, NP_, SM_)                                                                                                      \
     if (rb == (RB_) && np == (NP_) && sm == (SM_))                                                                                       \
         return vec == 2 ? run_apply<T, RB_, NP_, 2, SM_>(q0, q1, dev, overlap, st)                                                        \
@@ -1512,7 +1520,7 @@ static wcc_status backward(const void* dy, const void* x, const void* A, const v
         q.dy = static_cast<const T*>(dy); q.x = static_cast<const T*>(x); q.base = static_cast<const T*>(base); q.dx = static_cast<T*>(dx);
         q.fB = fB; q.fAt = fAt; q.fA = fA; q.scale = scale; q.ids = ids; q.part = w.part; q.P = P; q.N = N; q.Cin = Cin; q.Cout = Cout; q.R = R;
         q.r = rank; q.units = f.units; q.share = f.share; q.status = di.status;
-        const int v = P % (2 * Geo<T>::NP) == 0 ? 2 : vec ? 1 : 0;
+        const int v = row_form<T>(P, dx, lane_positions<T>(rb));
         const size_t smem = bwd_smem<T>(rb, Cin, Cout, dx != nullptr, v > 0);
         const dim3 rgrid((unsigned)(all * 4 * rb), (unsigned)R);
 #define WCC_AD_BWD(RB_, VEC_, NB_)                                                                                                                \
@@ -1570,6 +1578,18 @@ static wcc_status backward(const void* dy, const void* x, const void* A, const v
     WCC_AD_GRAD(1) WCC_AD_GRAD(2) WCC_AD_GRAD(4) WCC_AD_GRAD(8)
 #undef WCC_AD_GRAD
     return WCC_ERR_SHAPE;
+}
+
+// What wcc_debug_adapters_path answers.
+template <typename T>
+static int path_of(int N, int Cin, int Cout, size_t P, int rank, const void* dst, bool bwd)
+{
+    if (!bwd && P == 1) return WCC_PATH_ADAPTERS_TOKEN;
+    const int rb = blocks_of(rank), form = WCC_PATH_FORM * row_form<T>(P, dst, lane_positions<T>(rb));
+    const Fused<T> f = fused_of<T>(N, Cin, Cout, P, rank);
+    if (bwd && f.ok) return WCC_PATH_ADAPTERS_ONE_KERNEL + form + WCC_PATH_BLOCKS * f.nb;
+    const bool sm = bwd ? staged<T>(rb, Cout, Cin) && staged<T>(rb, Cin, 0) : staged<T>(rb, Cin, Cout);
+    return (sm ? WCC_PATH_ADAPTERS_MAP : WCC_PATH_ADAPTERS_MAP_PREPARED) + form;
 }
 
 }  // namespace ad

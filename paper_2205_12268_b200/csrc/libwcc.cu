@@ -1212,6 +1212,21 @@ wcc_status wcc_debug_select(const float* nrm2, int P, int k, const unsigned* his
                              static_cast<cudaStream_t>(stream), true, cs, nrm2, P, k, idx, nullptr, rank, nullptr, nullptr, hist11, hist16, thr, want_rank);
 }
 
+int wcc_debug_adapters_path(int N, int Cin, int Cout, int H, int Wd, int R, int rank, wcc_dtype dt, const void* out, int backward)
+{
+    if (check_adapter_args(N, Cin, Cout, H, Wd, R, rank, dt) != WCC_OK) return 0;
+    const size_t P = (size_t)H * Wd;
+    return dt == WCC_BF16 ? ad::path_of<__nv_bfloat16>(N, Cin, Cout, P, rank, out, backward != 0) : ad::path_of<float>(N, Cin, Cout, P, rank, out, backward != 0);
+}
+
+int wcc_debug_layernorm_path(int N, int C, int H, int Wd, wcc_dtype dt, int backward)
+{
+    if (check_norm_args(N, C, H, Wd, dt) != WCC_OK) return 0;
+    const ln::Plan p = ln::plan_of(N, C, (size_t)H * Wd, dt == WCC_BF16 ? 2 : 4, backward != 0);
+    if (p.ring) return WCC_PATH_NORM_RING + (p.q.C == p.K << p.q.groups_log2 ? WCC_PATH_ALL_CHANNELS : 0);
+    return p.feed ? WCC_PATH_NORM_ROW_FEED : p.rows ? WCC_PATH_NORM_ROWS : p.strided ? WCC_PATH_NORM_MAP_ANYWHERE : WCC_PATH_NORM_MAP;
+}
+
 wcc_status wcc_profile_enable(int on)
 {
     g_profile = on != 0;

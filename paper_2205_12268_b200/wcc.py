@@ -27,7 +27,7 @@ EXPORTS = ("wcc_staged_workspace_bytes", "wcc_forward_staged", "wcc_workspace_by
            "wcc_padded_workspace_bytes", "wcc_forward_padded", "wcc_dwconv_haar_fwd", "wcc_block_workspace_bytes",
            "wcc_block_forward", "wcc_dwt_fwd", "wcc_dwt_inv", "wcc_wavelet_workspace_bytes", "wcc_forward_wavelet",
            "wcc_layernorm_fwd", "wcc_layernorm_bwd_workspace_bytes", "wcc_layernorm_bwd", "wcc_adapters_workspace_bytes",
-           "wcc_adapters_fwd", "wcc_adapters_bwd")
+           "wcc_adapters_fwd", "wcc_adapters_bwd", "wcc_debug_adapters_path", "wcc_debug_layernorm_path")
 STATIC_SCRATCH_BYTES = 512 * 1024
 STAGES = ("haar_fwd_norms", "select_topk", "weight_quant", "gather_quant", "contract", "scatter_inv")   # wcc_forward_staged
 FUSED_STAGES = ("clear", "haar_norms", "select_topk", "fused_pass2")                                      # wcc_forward
@@ -150,6 +150,10 @@ def _operator_prototypes(L):
     L.wcc_adapters_fwd.argtypes = [vp] * 6 + [i] * 8 + [vp, vp, sz, vp]
     L.wcc_adapters_bwd.restype = i
     L.wcc_adapters_bwd.argtypes = [vp] * 7 + [i] * 8 + [vp, vp, vp, vp, sz, vp]
+    L.wcc_debug_adapters_path.restype = i
+    L.wcc_debug_adapters_path.argtypes = [i] * 8 + [vp, i]
+    L.wcc_debug_layernorm_path.restype = i
+    L.wcc_debug_layernorm_path.argtypes = [i] * 6
     L.wcc_last_status.restype = i
     L.wcc_last_status.argtypes = [vp]
 
