@@ -13,7 +13,7 @@ SRC = os.path.join(_HERE, "csrc", "libwcc.cu")
 
 
 def _sources():
-    return [SRC] + sorted(glob.glob(os.path.join(_HERE, "csrc", "*.cuh"))) + [os.path.join(_ROOT, "include", "wcc.h")]
+    return [SRC] + sorted(glob.glob(os.path.join(_HERE, "csrc", "*.cuh")) + glob.glob(os.path.join(_HERE, "csrc", "*.h"))) + [os.path.join(_ROOT, "include", "wcc.h")]
 
 
 def is_stale() -> bool:

@@ -9,6 +9,7 @@
 
 #include <atomic>
 
+#include "grow.h"
 #include "wcc.h"
 
 namespace wcc {
@@ -75,15 +76,14 @@ static wcc_status device_info(DeviceInfo& d)
     }
     return WCC_OK;
 }
-// Allows kernel K up to `smem` bytes of dynamic shared memory, once per device.
+// Allows kernel K up to `smem` bytes of dynamic shared memory on device `dev`, from any thread.
 template <auto K>
 static wcc_status allow_smem(int dev, int smem)
 {
-    static std::atomic<int> allowed[MAX_DEVICES];
-    if (allowed[dev].load(std::memory_order_relaxed) >= smem) return WCC_OK;
-    WCC_CUDA_TRY(cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    allowed[dev].store(smem, std::memory_order_relaxed);
-    return WCC_OK;
+    static GrowingLimit allowed[MAX_DEVICES];
+    const bool ok = allowed[dev].raise(smem, [](int n) { return cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, n) == cudaSuccess; });
+    if (!ok) (void)cudaGetLastError();                 // this call's error, not the next one's
+    return ok ? WCC_OK : WCC_ERR_CUDA;
 }
 
 // `overlap` false: an ordinary launch.  cluster > 1: cluster size along x.
