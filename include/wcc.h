@@ -365,7 +365,7 @@ wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const 
 /*
  * Synchronises `stream` and returns the device-side status word of the calling thread's current device:
  * WCC_OK, or WCC_ERR_TIMEOUT if a bounded wait inside a kernel gave up (the output of that call is then
- * undefined), or WCC_ERR_INDEX if an adapter index was out of range.  Reading clears the word.
+ * undefined), or WCC_ERR_INDEX if an adapter index was out of range and no wait gave up.  Reading clears the word.
  */
 wcc_status wcc_last_status(void* stream);
 

@@ -244,12 +244,13 @@ __device__ __forceinline__ void lay_second(const Factor<T>& f, int a, int r, int
     }
 }
 
-// The ids of a call as the kernels take them: anything but 0 .. R - 1 is no adapter, and one at R or beyond is an error.
+// The ids of a call as the kernels take them: anything but 0 .. R - 1 is no adapter, and one at R or beyond is an error.  It enters a clear status word
+// only: a wait that ran out leaves an output undefined, and nobody may miss that for an index.
 __device__ __forceinline__ int adapter_of(const int32_t* ids, int n, int R, int* status)
 {
     const int a = ids[n];
     if (a < R) return a < 0 ? -1 : a;
-    if (status) atomicExch(status, (int)WCC_ERR_INDEX);
+    if (status) atomicCAS(status, (int)WCC_OK, (int)WCC_ERR_INDEX);
     return -1;
 }
 
