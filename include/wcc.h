@@ -223,6 +223,10 @@ typedef struct wcc_options {
 wcc_status wcc_forward_ex(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int Wd,
                           int levels, int k, int bits, void* y, wcc_dtype dt,
                           void* ws, size_t ws_bytes, void* stream, const wcc_options* opt, const wcc_taps* taps);
+/* What wcc_forward_ex would refuse these arguments for, WCC_OK if nothing: host arithmetic alone, nothing is launched.  For callers that write into
+ * y (or what the options point at) before the layer runs. */
+wcc_status wcc_forward_check(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int Wd, int levels, int k, int bits, const void* y,
+                             wcc_dtype dt, const void* ws, size_t ws_bytes, const wcc_options* opt, const wcc_taps* taps);
 
 /*
  * Other wavelets than Haar (App. F compares db2, db3, coif1, bior1.3, bior2.2, sym4 under the same layer): a generic
@@ -334,7 +338,8 @@ wcc_status wcc_layernorm_bwd(const void* dy, const void* x, const float* gamma, 
  * is a request with adapter a = ids[n], any negative id for none,
  *     y_n = base_n + scale[a] * B_a (A_a x_n)            (a < 0: y_n = base_n)
  * over the channels at every position.  Added to a layer: wcc_adapters_fwd writes into y (with the layer's own residual, if it has one, as base),
- * then wcc_forward_ex runs with residual = y into the same y; the layer's ReLU then comes after the sum.
+ * then wcc_forward_ex runs with residual = y into the same y; the layer's ReLU then comes after the sum (wcc_forward_check first, if y is to stay as it
+ * is where the layer would be refused).
  *   x     in : [N][Cin][H][Wd] of dt                A in: [R][rank][Cin] of dt          B in: [R][Cout][rank] of dt
  *   scale in : fp32 [R], or NULL for 1              ids in: int32 [N] on the DEVICE     base in: [N][Cout][H][Wd] of dt, or NULL for 0
  *   y     out: [N][Cout][H][Wd] of dt; may be base, must not overlap x

@@ -420,9 +420,9 @@ static wcc_status wide_impl(const void* x, const float* Wt, int N, int Cin, int 
     return WCC_OK;
 }
 
-static wcc_status forward_impl(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int W,
-                               int L, int k, int bits, void* y, wcc_dtype dt, void* ws, size_t ws_bytes,
-                               cudaStream_t st, const wcc_taps* taps, const wcc_options* opt = nullptr)
+// Everything that wcc_forward_ex refuses a call for, and the pipeline that it will run otherwise; decided before anything is launched.
+static wcc_status check_forward_call(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int W, int L, int k, int bits, const void* y,
+                                     wcc_dtype dt, const void* ws, size_t ws_bytes, const wcc_taps* taps, const wcc_options* opt, Path& path)
 {
     const bool own_codes = opt && opt->Wq;             // weights arrive quantized: Wt is not read
     if (!x || (!Wt && !own_codes) || !y || !ws) return WCC_ERR_NULL;
@@ -433,13 +433,28 @@ static wcc_status forward_impl(const void* x, const float* Wt, int N, int Cin, i
     if (taps && (!aligned16(taps->coef) || !aligned16(taps->Xq) || !aligned16(taps->Xb) || !aligned16(taps->acc)))
         return WCC_ERR_ALIGN;
     if (own_codes && !p2_plan_of(4, Cout, wcc_kpad(Cin, bits), true, L).ok) return WCC_ERR_SHAPE;
-    switch (layer_path(N, Cin, Cout, H, W, L, k, bits, own_codes, taps && taps->coef, ws_bytes)) {      // decided before anything is launched
+    path = layer_path(N, Cin, Cout, H, W, L, k, bits, own_codes, taps && taps->coef, ws_bytes);
+    if (path == Path::STAGED && !staged_fits(Cin, Cout, bits)) return WCC_ERR_SHAPE;
+    const size_t need = path == Path::FUSED ? carve_fused_ws(nullptr, N, Cin, Cout, H, W, k, bits).total
+                        : path == Path::WIDE ? carve_wide_ws(nullptr, N, Cin, Cout, H, W, k, bits).total
+                                             : carve_forward_ws(nullptr, N, Cin, Cout, H, W, k, bits).total;
+    return ws_bytes < need ? WCC_ERR_WORKSPACE : WCC_OK;
+}
+
+static wcc_status forward_impl(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int W,
+                               int L, int k, int bits, void* y, wcc_dtype dt, void* ws, size_t ws_bytes,
+                               cudaStream_t st, const wcc_taps* taps, const wcc_options* opt = nullptr)
+{
+    Path path = Path::FUSED;
+    wcc_status s = check_forward_call(x, Wt, N, Cin, Cout, H, W, L, k, bits, y, dt, ws, ws_bytes, taps, opt, path);
+    if (s != WCC_OK) return s;
+    switch (path) {
         case Path::WIDE: return wide_impl(x, Wt, N, Cin, Cout, H, W, L, k, bits, y, dt, ws, ws_bytes, st, taps, opt);
         case Path::STAGED: return staged_impl(x, Wt, N, Cin, Cout, H, W, L, k, bits, y, dt, ws, ws_bytes, st, taps, opt);
         case Path::FUSED: break;
     }
+    const bool own_codes = opt && opt->Wq;
     const FusedWs f = carve_fused_ws(ws, N, Cin, Cout, H, W, k, bits);
-    if (ws_bytes < f.total) return WCC_ERR_WORKSPACE;
     const int P = H * W, M = N * k;
 
     if ((s = profile_mark(0, st)) != WCC_OK) return s;
@@ -828,6 +843,13 @@ wcc_status wcc_forward_ex(const void* x, const float* Wt, int N, int Cin, int Co
 {
     return forward_impl(x, Wt, N, Cin, Cout, H, Wd, levels, k, bits, y, dt, ws, ws_bytes,
                         static_cast<cudaStream_t>(stream), taps, opt);
+}
+
+wcc_status wcc_forward_check(const void* x, const float* Wt, int N, int Cin, int Cout, int H, int Wd, int levels, int k, int bits, const void* y,
+                             wcc_dtype dt, const void* ws, size_t ws_bytes, const wcc_options* opt, const wcc_taps* taps)
+{
+    Path path = Path::FUSED;
+    return check_forward_call(x, Wt, N, Cin, Cout, H, Wd, levels, k, bits, y, dt, ws, ws_bytes, taps, opt, path);
 }
 
 wcc_status wcc_dwconv_haar_fwd(const void* u, const float* Wdw, int N, int C, int H, int Wd, int levels, wcc_dtype dt,

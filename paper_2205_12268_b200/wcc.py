@@ -27,7 +27,7 @@ EXPORTS = ("wcc_staged_workspace_bytes", "wcc_forward_staged", "wcc_workspace_by
            "wcc_padded_workspace_bytes", "wcc_forward_padded", "wcc_dwconv_haar_fwd", "wcc_block_workspace_bytes",
            "wcc_block_forward", "wcc_dwt_fwd", "wcc_dwt_inv", "wcc_wavelet_workspace_bytes", "wcc_forward_wavelet",
            "wcc_layernorm_fwd", "wcc_layernorm_bwd_workspace_bytes", "wcc_layernorm_bwd", "wcc_adapters_workspace_bytes",
-           "wcc_adapters_fwd", "wcc_adapters_bwd", "wcc_debug_adapters_path", "wcc_debug_layernorm_path")
+           "wcc_adapters_fwd", "wcc_adapters_bwd", "wcc_forward_check", "wcc_debug_adapters_path", "wcc_debug_layernorm_path")
 STATIC_SCRATCH_BYTES = 512 * 1024
 STAGES = ("haar_fwd_norms", "select_topk", "weight_quant", "gather_quant", "contract", "scatter_inv")   # wcc_forward_staged
 FUSED_STAGES = ("clear", "haar_norms", "select_topk", "fused_pass2")                                      # wcc_forward
@@ -150,6 +150,8 @@ def _operator_prototypes(L):
     L.wcc_adapters_fwd.argtypes = [vp] * 6 + [i] * 8 + [vp, vp, sz, vp]
     L.wcc_adapters_bwd.restype = i
     L.wcc_adapters_bwd.argtypes = [vp] * 7 + [i] * 8 + [vp, vp, vp, vp, sz, vp]
+    L.wcc_forward_check.restype = i
+    L.wcc_forward_check.argtypes = [vp, vp] + [i] * 8 + [vp, i, vp, sz, C.POINTER(Options), C.POINTER(Taps)]
     L.wcc_debug_adapters_path.restype = i
     L.wcc_debug_adapters_path.argtypes = [i] * 8 + [vp, i]
     L.wcc_debug_layernorm_path.restype = i
@@ -592,7 +594,8 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
     ``alpha``, ``wbits``, ``relu``, ``residual``, ``Wq`` + ``scale_w``: the options of wcc_forward_ex (see wcc.h);
     with pre-quantized weights ``Wt`` may be None.
     ``adapters`` with ``ids`` (int32 [N], negative: none): low-rank adapters beside the layer's projection.  Their sum (and ``residual``) is written to y
-    in the map's type and enters the layer as its residual, so the ReLU comes after it."""
+    in the map's type and enters the layer as its residual, so the ReLU comes after it.  They run in ``ws`` where it is large enough, else in scratch of
+    their own.  A call that is refused leaves y as it is.  Without ``adapters``, ``ids`` are not read."""
     _dev(x, "x")
     N, Cin, H, W = x.shape
     if adapters is not None:
@@ -600,10 +603,7 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
             raise ValueError("adapters need ids")
         if staged:
             raise ValueError("options are only available on the fused path")
-        if adapters.Cin != Cin or adapters.Cout != (Wt if Wq is None else Wq).shape[0]:
-            raise ValueError("the adapters must have the layer's channels")
-        y = residual = adapters(x, ids, base=residual, y=y)
-    use_ex = bool(alpha > 0.0 or wbits or relu or residual is not None or Wq is not None)
+    use_ex = bool(alpha > 0.0 or wbits or relu or residual is not None or Wq is not None or adapters is not None)
     if Wq is not None:
         _dev(Wq, "Wq")
         if scale_w is not None:
@@ -616,6 +616,8 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
         Cout = Wt.shape[0]
         if Wt.shape[1] != Cin:
             raise ValueError("Wt must be [Cout][Cin]")
+    if adapters is not None and (adapters.Cin != Cin or adapters.Cout != Cout):
+        raise ValueError("the adapters must have the layer's channels")
     if use_ex and staged:
         raise ValueError("options are only available on the fused path")
     if residual is not None:
@@ -629,6 +631,12 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
     args = (x.data_ptr(), _ptr(Wt), N, Cin, Cout, H, W, levels, k, bits, y.data_ptr(), _dt(x),
             ws.buf.data_ptr(), ws.nbytes, _stream())
     opt = Options(float(alpha), int(wbits), int(bool(relu)), _ptr(residual), _ptr(Wq), _ptr(scale_w)) if use_ex else None
+    t, s = _tap_tensors(x, Cout, k, bits, taps) if taps else (None, None)
+    if adapters is not None:
+        # the layer's residual is what the adapters leave in y: their launch comes after all that could refuse the layer
+        opt.residual = y.data_ptr()
+        _check(lib().wcc_forward_check(*args[:-1], C.byref(opt), C.byref(s) if taps else None), "wcc_forward_check")
+        adapters(x, ids, base=residual, y=y, ws=ws if ws.nbytes >= adapters._bytes(N, H, W, False) else None)
     if not taps:
         if staged:
             _check(lib().wcc_forward_staged(*args, None), "wcc_forward_staged")
@@ -637,6 +645,18 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
         else:
             _check(lib().wcc_forward(*args), "wcc_forward")
         return y
+    if staged:
+        _check(lib().wcc_forward_staged(*args, C.byref(s)), "wcc_forward_staged")
+    elif use_ex:
+        _check(lib().wcc_forward_ex(*args, C.byref(opt), C.byref(s)), "wcc_forward_ex")
+    else:
+        _check(lib().wcc_forward_debug(*args, C.byref(s)), "wcc_forward_debug")
+    return y, t
+
+
+def _tap_tensors(x: torch.Tensor, Cout: int, k: int, bits: int, taps):
+    """Tensors for the intermediates of a layer that ``taps`` names (True: all), and the Taps that point at them."""
+    N, Cin, H, W = x.shape
     P, M, kp = H * W, N * k, kpad(Cin, bits)
     dev = x.device
     t = dict(coef=torch.empty((N, Cin, P), dtype=torch.float32, device=dev),
@@ -653,14 +673,7 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
     for name in ("Xq", "Xb", "acc"):          # every row is a kept position and gets written; start from zeros anyway
         if name in t:
             t[name].zero_()
-    s = Taps(**{name: _ptr(t.get(name)) for name, _ in Taps._fields_})
-    if staged:
-        _check(lib().wcc_forward_staged(*args, C.byref(s)), "wcc_forward_staged")
-    elif use_ex:
-        _check(lib().wcc_forward_ex(*args, C.byref(opt), C.byref(s)), "wcc_forward_ex")
-    else:
-        _check(lib().wcc_forward_debug(*args, C.byref(s)), "wcc_forward_debug")
-    return y, t
+    return t, Taps(**{name: _ptr(t.get(name)) for name, _ in Taps._fields_})
 
 
 class Chain:
@@ -733,10 +746,8 @@ class Chain:
                 gamma, beta, eps = self.norms[i]
                 x = layernorm(x, gamma, beta, eps, y=self.normed[:x.numel()].view(shape))
             out = y if i + 1 == n else self.between[i % len(self.between)][:self.N * layer.Cout * self.H * self.W].view(self.N, layer.Cout, self.H, self.W)
-            residual = None
-            if self.adapters[i] is not None:
-                residual = self.adapters[i](x, ids, y=out, ws=self.ws)
-            x = forward(x, self.weights[i], self.levels, self.k, self.bits, y=out, ws=self.ws, alpha=layer.alpha, relu=bool(layer.relu), residual=residual)
+            x = forward(x, self.weights[i], self.levels, self.k, self.bits, y=out, ws=self.ws, alpha=layer.alpha, relu=bool(layer.relu),
+                        adapters=self.adapters[i], ids=ids)
         return x
 
     def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None, ids: torch.Tensor | None = None) -> torch.Tensor:
