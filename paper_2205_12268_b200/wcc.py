@@ -192,6 +192,12 @@ def _dev(t: torch.Tensor, name: str):
         raise ValueError("%s must be a contiguous CUDA tensor" % name)
 
 
+def _room(t: torch.Tensor, n: int, like: torch.Tensor, name: str):
+    """t holds at least n elements of `like`'s type, one after the other on `like`'s device: the kernels go by the sizes of the call, not by t's."""
+    if not (t.is_cuda and t.is_contiguous() and t.dtype == like.dtype and t.device == like.device and t.numel() >= n):
+        raise ValueError("%s must be contiguous, of at least %d elements of %s on %s" % (name, n, like.dtype, like.device))
+
+
 def workspace_bytes(N, Cin, Cout, H, W, levels, k, bits, dt) -> int:
     return int(lib().wcc_workspace_bytes(N, Cin, Cout, H, W, levels, k, bits, dt))
 
@@ -307,8 +313,14 @@ class Block:
 
     def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None) -> torch.Tensor:
         _dev(x, "x")
+        if _dt(x) != self.dt:
+            raise ValueError("x must have the type the block was made for")
+        n = self.N * self.C * self.H * self.W
+        _room(x, n, x, "x")
         if y is None:
             y = torch.empty_like(x)
+        else:
+            _room(y, n, x, "y")
         _check(lib().wcc_block_forward(x.data_ptr(), self.W1.data_ptr(), self.Wdw.data_ptr(), self.W3.data_ptr(), self.N,
                                        self.C, self.E, self.H, self.W, self.levels, self.k, self.bits, y.data_ptr(), self.dt,
                                        self.ws.buf.data_ptr(), self.ws.nbytes, _stream()), "wcc_block_forward")
@@ -626,6 +638,8 @@ def forward(x: torch.Tensor, Wt: torch.Tensor | None, levels: int, k: int, bits:
             raise ValueError("residual must have the output's shape and type")
     if y is None:
         y = torch.empty((N, Cout, H, W), dtype=x.dtype, device=x.device)
+    else:
+        _room(y, N * Cout * H * W, x, "y")
     if ws is None:
         ws = Workspace.for_problem(x, Cout, levels, k, bits, staged=staged)
     args = (x.data_ptr(), _ptr(Wt), N, Cin, Cout, H, W, levels, k, bits, y.data_ptr(), _dt(x),
@@ -752,11 +766,14 @@ class Chain:
 
     def __call__(self, x: torch.Tensor, y: torch.Tensor | None = None, ids: torch.Tensor | None = None) -> torch.Tensor:
         _dev(x, "x")
+        if _dt(x) != self.dt or (not self.plain and tuple(x.shape) != (self.N, self.layers[0].Cin, self.H, self.W)):
+            raise ValueError("x must have the shape and type the chain was made for")
+        _room(x, self.N * self.layers[0].Cin * self.H * self.W, x, "x")
         if y is None:
             y = torch.empty((self.N, self.Cout, self.H, self.W), dtype=x.dtype, device=x.device)
+        else:
+            _room(y, self.N * self.Cout * self.H * self.W, x, "y")
         if not self.plain:
-            if tuple(x.shape) != (self.N, self.layers[0].Cin, self.H, self.W) or _dt(x) != self.dt:
-                raise ValueError("x must have the shape and type the chain was made for")
             return self._run(x, y, ids)
         _check(lib().wcc_chain_forward(x.data_ptr(), self.layers, len(self.weights), self.N, self.H, self.W, self.levels,
                                        self.k, self.bits, y.data_ptr(), self.dt, self.ws.buf.data_ptr(), self.ws.nbytes,
