@@ -84,11 +84,7 @@ template <int WORDS> struct Words { uint32_t w[WORDS]; };
 template <int W> __device__ __forceinline__ Words<W> load_words(const void* p)
 {
     Words<W> r;
-    if constexpr (W == 8) {
-        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-            : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
-            : "l"(p));
-    } else if constexpr (W == 4) {
+    if constexpr (W == 4) {
         const uint4 u = *static_cast<const uint4*>(p);
         r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w;
     } else {
@@ -344,52 +340,52 @@ template <typename T, int RB, bool SM, int NP>
 __device__ __forceinline__ void first_step(Tile<T, RB, NP>& tile, const Words<NP * (int)sizeof(T) / 4> (&x)[Geo<T>::CL], const uint4* wg)
 {
     constexpr int MB = NP / 2, CL = Geo<T>::CL;
-            if constexpr (sizeof(T) == 2) {
-                uint32_t fa[2][MB][4];
-    #pragma unroll
-                for (int s = 0; s < 2; ++s)
-    #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) {
-                        fa[s][mb][0] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x5410);
-                        fa[s][mb][1] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x7632);
-                        fa[s][mb][2] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x5410);
-                        fa[s][mb][3] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x7632);
-                    }
-    #pragma unroll
-                for (int jb = 0; jb < RB; ++jb) {
-                    const uint4 w = load_factor<SM>(wg + jb * 32);
-    #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) {
-                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_bf16(d, fa[0][mb], w.x, w.y);
-                        mma_bf16(d, fa[1][mb], w.z, w.w);
-                        add(tile.acc[mb][jb], d);
-                    }
-                }
-            } else {
-                uint32_t hi[2][MB][4], lo[2][MB][4];
-    #pragma unroll
-                for (int s = 0; s < 2; ++s)
-    #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb)
-    #pragma unroll
-                        for (int i = 0; i < 4; ++i) split_tf32(x[2 * s + (i >> 1)].w[2 * mb + (i & 1)], hi[s][mb][i], lo[s][mb][i]);
-    #pragma unroll
-                for (int jb = 0; jb < RB; ++jb) {
-                    const uint4 wh = load_factor<SM>(wg + (jb * 2) * 32), wl = load_factor<SM>(wg + (jb * 2 + 1) * 32);
-    #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) {
-                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                        mma_tf32(d, lo[0][mb], wh.x, wh.y);
-                        mma_tf32(d, lo[1][mb], wh.z, wh.w);
-                        mma_tf32(d, hi[0][mb], wl.x, wl.y);
-                        mma_tf32(d, hi[1][mb], wl.z, wl.w);
-                        mma_tf32(d, hi[0][mb], wh.x, wh.y);
-                        mma_tf32(d, hi[1][mb], wh.z, wh.w);
-                        add(tile.acc[mb][jb], d);
-                    }
-                }
+    if constexpr (sizeof(T) == 2) {
+        uint32_t fa[2][MB][4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                fa[s][mb][0] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x5410);
+                fa[s][mb][1] = __byte_perm(x[4 * s].w[mb], x[4 * s + 1].w[mb], 0x7632);
+                fa[s][mb][2] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x5410);
+                fa[s][mb][3] = __byte_perm(x[(4 * s + 2) % CL].w[mb], x[(4 * s + 3) % CL].w[mb], 0x7632);
             }
+#pragma unroll
+        for (int jb = 0; jb < RB; ++jb) {
+            const uint4 w = load_factor<SM>(wg + jb * 32);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                mma_bf16(d, fa[0][mb], w.x, w.y);
+                mma_bf16(d, fa[1][mb], w.z, w.w);
+                add(tile.acc[mb][jb], d);
+            }
+        }
+    } else {
+        uint32_t hi[2][MB][4], lo[2][MB][4];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split_tf32(x[2 * s + (i >> 1)].w[2 * mb + (i & 1)], hi[s][mb][i], lo[s][mb][i]);
+#pragma unroll
+        for (int jb = 0; jb < RB; ++jb) {
+            const uint4 wh = load_factor<SM>(wg + (jb * 2) * 32), wl = load_factor<SM>(wg + (jb * 2 + 1) * 32);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                mma_tf32(d, lo[0][mb], wh.x, wh.y);
+                mma_tf32(d, lo[1][mb], wh.z, wh.w);
+                mma_tf32(d, hi[0][mb], wl.x, wl.y);
+                mma_tf32(d, hi[1][mb], wl.z, wl.w);
+                mma_tf32(d, hi[0][mb], wh.x, wh.y);
+                mma_tf32(d, hi[1][mb], wh.z, wh.w);
+                add(tile.acc[mb][jb], d);
+            }
+        }
+    }
 }
 
 // The maps of first products and the bases of second ones on their way through shared memory: a warp copies the groups of channels ahead of
@@ -1321,7 +1317,8 @@ static Fused<T> fused_of(int N, int Cin, int Cout, size_t P, int rank)
     const size_t smem = bwd_smem<T>(rb, Cin, Cout, true, P % Geo<T>::NP == 0);
     if (smem > 113 * 1024) return f;                                      // two CTAs an SM
     f.runs = (int)std::min(total, (long long)WAVES * B200_SMS * std::min<int>(3, (int)(228 * 1024 / (smem + 1024))));
-    // two units at least: factors laid out and a feed filled for a single one are not paid for (512 units in runs of 1 / 2: project 65 / 46)
+    // two units at least: factors laid out and a feed filled for a single one are not paid for.  512 units in runs of 1 / 2, 144 -> 24 on 4 x 128 x 256
+    // with adapters 0 1 2 3: 64 / 62, 0 - 2 3: 63 / 60; but - - 1 2: 46 / 58, where half of the runs have nothing to do.
     f.share = (int)std::max(2LL, (total + f.runs - 1) / f.runs);
     f.runs = (int)((total + f.share - 1) / f.share);
     f.ok = true;
