@@ -361,6 +361,9 @@ wcc_status wcc_adapters_fwd(const void* x, const void* A, const void* B, const f
  *   dx   out: [N][Cin][H][Wd] of dt, may be base, must not overlap x or dy; NULL: not wanted
  *   dA, dB out: fp32 [R][rank][Cin] and [R][Cout][rank], zeros for adapters without an image; both NULL: not wanted (x may then be NULL)
  *   ws      : scratch of at least wcc_adapters_workspace_bytes(..., 1) bytes of this call's sizes (smaller ones may need more), 16-byte aligned
+ * Where V and U go through ws (ranks above 16, more than 512 channels or 4096 images, few positions in all) they take 12 bytes (bf16 maps) or 8 (fp32) for each rank,
+ * in multiples of 8, 16, 32 or 64, and position, and each image's positions count as a multiple of 64 (bf16) or 32: images of few positions, rows of single
+ * tokens above all, take up to 64 times the scratch and the products of what they hold (8192 rows of rank 16: 100 MB bf16, 34 MB fp32).
  * The sums over images and positions are fp32, in an order that depends on the sizes and the ids alone: the same call gives the same bits.
  */
 wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const void* B, const float* scale, const int32_t* ids,

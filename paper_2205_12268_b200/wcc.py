@@ -696,8 +696,8 @@ class Chain:
     The workspace (intermediate maps included) is allocated once, here.
 
     ``norms[i]`` = (gamma, beta, eps): layer i's input is normalised over its channels first (``layernorm``; gamma and beta may be None);
-    ``adapters[i]``: ``Adapters`` beside layer i, taken by the ``ids`` of the call.  Either list may hold None for layers without.  Such a chain runs
-    layer by layer."""
+    ``adapters[i]``: ``Adapters`` beside layer i, taken by the ``ids`` of the call (not read where no layer has any).  Either list may hold None for layers
+    without.  Such a chain runs layer by layer."""
 
     def __init__(self, x: torch.Tensor, weights, levels: int, k: int, bits: int = 8, relu_last: bool = False, alphas=None, norms=None,
                  adapters=None):
