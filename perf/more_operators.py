@@ -115,8 +115,10 @@ def _put_away(x):
     top = v.abs().amax(2, keepdim=True)
     some = top >= SMALLEST
     top = torch.where(some, top, torch.ones_like(top))
-    codes = torch.where(some, torch.round(v * (127.0 / top)), torch.zeros_like(v)).to(torch.int8)
-    scales = torch.where(some, top / 127.0, torch.zeros_like(top)).reshape(-1, blocks)
+    # a tensor of 127: with a plain number torch multiplies by a reciprocal, which rounds twice
+    full = torch.full_like(top, 127.0)
+    codes = torch.where(some, torch.round(v * (full / top)), torch.zeros_like(v)).to(torch.int8)
+    scales = torch.where(some, top / full, torch.zeros_like(top)).reshape(-1, blocks)
     return codes.reshape(-1, blocks * BLOCK)[:, :L].reshape(x.shape).contiguous(), scales
 
 
@@ -342,8 +344,9 @@ def _kept64(x):
         top = part.abs().amax(-1, keepdim=True)
         some = (top >= SMALLEST).double()
         top = top + (1 - some)
-        scale = (top / 127).float().double() * some
-        back[..., b:b + BLOCK] = torch.round((part * (127 / top).float().double()).float().double()) * scale
+        full = torch.full_like(top, 127)
+        scale = (top / full).float().double() * some
+        back[..., b:b + BLOCK] = torch.round((part * (full / top).float().double()).float().double()) * scale
         scales.append(scale.reshape(-1))
     return back, torch.stack(scales, 1)
 
