@@ -371,6 +371,77 @@ wcc_status wcc_adapters_bwd(const void* dy, const void* x, const void* A, const 
                             float* dB, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Operators for training around the layer, on channels-last tensors: [N][P][C] dense, P = the positions of an image (H * Wd in any number of
+ * dimensions; 1 for rows of tokens), channels innermost.
+ */
+typedef enum { WCC_ACT_NONE = 0, WCC_ACT_RELU = 1, WCC_ACT_SILU = 2, WCC_ACT_GELU = 3 } wcc_act;
+
+/*
+ * Activation checkpoints in 8 bits: what a backward pass needs of a map, kept at half or a quarter of its size.  A tensor is [rows][L]; a block is
+ * WCC_CKPT_BLOCK consecutive values of a row (the last one of a row may be shorter).  With top = the largest magnitude of a block, in fp32 arithmetic,
+ *     code = round(x * (127 / top)) (to nearest, ties to even),   scale = top / 127,   restored value = code * scale, rounded to the type
+ * A block with top < 2^-100 is kept as zeros.  A block with a NaN or an infinity has the scale NaN and comes back as NaN, all of it.
+ *   x      in : [rows][L] of dt                codes out: int8 [rows][L]
+ *   scales out: fp32 [rows][ceil(L / WCC_CKPT_BLOCK)]
+ * rows >= 1 and L >= 1 are any numbers with rows * L <= 2^40.
+ */
+#define WCC_CKPT_BLOCK 128
+wcc_status wcc_checkpoint(const void* x, long long rows, int L, wcc_dtype dt, int8_t* codes, float* scales, void* stream);
+/* out [rows][L] of dt (any dt, not only the one it was made from). */
+wcc_status wcc_checkpoint_restore(const int8_t* codes, const float* scales, long long rows, int L, wcc_dtype dt, void* out, void* stream);
+
+/*
+ * Group norm with an activation: the channels of an image in `groups` groups of D = C / groups, each normalised over its D channels at all P positions,
+ *     mean = 1/(P D) sum x,  rstd = (1/(P D) sum (x - mean)^2 + eps)^-1/2,  z = (x - mean) * rstd * gamma[c] + beta[c],  y = act(z)
+ * (of each image and group).  act: WCC_ACT_NONE, WCC_ACT_RELU or WCC_ACT_SILU (z / (1 + exp(-z))).
+ *   x     in : [N][P][C] of dt             gamma, beta in: fp32 [C], each may be NULL (1 and 0)
+ *   y     out: as x; may be x itself       mean, rstd out: fp32 [N][groups], each may be NULL; the backward pass reads them
+ *   codes, scales out: the checkpoint of x as wcc_checkpoint(x, N * P, C, ...) writes it; both NULL: not wanted
+ *   eps      : >= 0 and finite.  With eps = 0 a group whose values are all equal gives NaN, as the formula does.
+ *   ws       : scratch of at least wcc_groupnorm_workspace_bytes(..., 0) bytes of this call's sizes, 16-byte aligned
+ * groups divides C, C <= WCC_MAX_CHANNELS, N * P <= 2^30, N * P * C <= 2^40.  fp32 arithmetic; the variance is put together from squared deviations from a value of the
+ * data or a mean, so a large common offset costs it no digits.  The order of the sums depends on the sizes alone: the same call gives the same bits.
+ */
+size_t wcc_groupnorm_workspace_bytes(int N, int P, int C, int groups, wcc_dtype dt, int backward);
+wcc_status wcc_groupnorm_fwd(const void* x, const float* gamma, const float* beta, int N, int P, int C, int groups, float eps, wcc_act act,
+                             wcc_dtype dt, void* y, float* mean, float* rstd, int8_t* codes, float* scales, void* ws, size_t ws_bytes, void* stream);
+/*
+ * Its backward pass.  With xh = (x - mean) * rstd, t = dy * act'(xh gamma + beta) and g = t * gamma[c]:
+ *     dx = rstd * (g - 1/(P D) sum g - xh * 1/(P D) sum g xh),   dgamma[c] = sum_{n,p} t xh,   dbeta[c] = sum_{n,p} t
+ * (relu: act'(z) = 1 for z > 0, else 0).
+ *   dy    in : [N][P][C] of dt             x in: as the forward pass had it, or NULL: then codes and scales are its checkpoint
+ *   gamma, beta in: as in the forward pass (beta is read only with an activation)
+ *   mean, rstd  in: what the forward pass returned
+ *   dx    out: as dy; may be dy or x       dgamma, dbeta out: fp32 [C], each may be NULL
+ *   ws       : scratch of at least wcc_groupnorm_workspace_bytes(..., 1) bytes of this call's sizes, 16-byte aligned; it also serves the forward pass
+ */
+wcc_status wcc_groupnorm_bwd(const void* dy, const void* x, const int8_t* codes, const float* scales, const float* gamma, const float* beta,
+                             const float* mean, const float* rstd, int N, int P, int C, int groups, wcc_act act, wcc_dtype dt, void* dx, float* dgamma,
+                             float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The gated pointwise block on rows of channels (positions of a channels-last map, tokens): both projections, the activation and the product,
+ *     g = x Wg^T,  u = x Wu^T,  y = act(g) * u
+ * act: any wcc_act (gelu: g * Phi(g) with the normal distribution function).  bf16 only, sums in fp32 on the tensor cores; y is rounded once.
+ *   x  in : bf16 [rows][Cin]          Wg, Wu in: bf16 [F][Cin]          y out: bf16 [rows][F], must not overlap the inputs
+ * Cin and F are multiples of 8, at most WCC_MAX_GATED; 1 <= rows <= 2^30.
+ */
+#define WCC_MAX_GATED 65536
+wcc_status wcc_gated_fwd(const void* x, const void* Wg, const void* Wu, int rows, int Cin, int F, wcc_act act, void* y, void* stream);
+/*
+ * Its backward pass.  Nothing is kept of the forward pass but x: g and u are computed again.
+ *     dG = dy * u * act'(g),  dU = dy * act(g),   dx = dG Wg + dU Wu,   dWg = dG^T x,   dWu = dU^T x
+ * dG and dU are rounded to bf16, as operands of the products (2^-9 of a term at most, on top of the results' own rounding).
+ *   dy in : bf16 [rows][F]            dx out: bf16 [rows][Cin], must not overlap the inputs; NULL: not wanted
+ *   dWg, dWu out: bf16 [F][Cin], both NULL: not wanted
+ *   ws    : scratch of at least wcc_gated_bwd_workspace_bytes(...) bytes of this call's sizes, 16-byte aligned
+ * The order of the sums depends on the sizes alone: the same call gives the same bits.
+ */
+size_t wcc_gated_bwd_workspace_bytes(int rows, int Cin, int F);
+wcc_status wcc_gated_bwd(const void* dy, const void* x, const void* Wg, const void* Wu, int rows, int Cin, int F, wcc_act act, void* dx, void* dWg,
+                         void* dWu, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Synchronises `stream` and returns the device-side status word of the calling thread's current device:
  * WCC_OK, or WCC_ERR_TIMEOUT if a bounded wait inside a kernel gave up (the output of that call is then
  * undefined), or WCC_ERR_INDEX if an adapter index was out of range and no wait gave up.  Reading clears the word.

@@ -1,5 +1,6 @@
 // Shared declarations of the WCC CUDA library (sm_100a).  Internal: not part of the C ABI.
-// The library is one translation unit (libwcc.cu includes every *.cuh), so device globals are defined here.
+// The library is two translation units, compiled side by side: libwcc.cu (the layer, layer norm, adapters) and training.cu (group norm,
+// checkpoints, the gated block).  Device globals belong to libwcc.cu; each unit has its own copy of the wait limit.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -14,8 +15,12 @@
 
 namespace wcc {
 
-// Device status word: WCC_OK, or WCC_ERR_TIMEOUT once a bounded wait inside a kernel gave up.
+// Device status word: WCC_OK, or WCC_ERR_TIMEOUT once a bounded wait inside a kernel gave up.  Kernels of the other unit get its address.
+#ifndef WCC_TRAINING_UNIT
 __device__ int g_status = 0;
+#endif
+wcc_status status_address(int** status);               // on the current device (libwcc.cu)
+wcc_status set_training_wait_limit(uint32_t polls);    // of the other unit's copy (training.cu)
 
 inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -27,7 +32,7 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
     } while (0)
 
 // host-side count of kernel launches (reported by wcc_kernel_launches)
-static unsigned long long g_launches = 0;
+inline unsigned long long g_launches = 0;
 
 #define WCC_LAUNCH_CHECK()                                   \
     do {                                                     \
@@ -70,7 +75,8 @@ static wcc_status device_info(DeviceInfo& d)
     d.status = status[d.dev].load(std::memory_order_relaxed);
     if (!d.sms || !d.status) {
         WCC_CUDA_TRY(cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, d.dev));
-        WCC_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void**>(&d.status), g_status));
+        const wcc_status s = status_address(&d.status);
+        if (s != WCC_OK) return s;
         sms[d.dev].store(d.sms, std::memory_order_relaxed);
         status[d.dev].store(d.status, std::memory_order_relaxed);
     }
@@ -115,7 +121,7 @@ static wcc_status launch_overlapped(void (*kern)(KArgs...), dim3 grid, dim3 bloc
 }
 
 // Zeroes `n16` 16-byte words (the selection's histograms and counters of one call).
-__global__ void __launch_bounds__(256) clear_kernel(uint4* __restrict__ p, size_t n16)
+static __global__ void __launch_bounds__(256) clear_kernel(uint4* __restrict__ p, size_t n16)
 {
     pdl_wait();
     pdl_launch();

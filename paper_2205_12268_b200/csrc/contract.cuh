@@ -13,6 +13,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "tcgen05.cuh"
 #include "tma.cuh"
 
 namespace wcc {
@@ -27,41 +28,6 @@ constexpr int B_ATOM_BYTES = TILE_N * ATOM_BYTES;
 constexpr int STAGE_BYTES = A_ATOM_BYTES + B_ATOM_BYTES;      // 48 KB, a multiple of 1024 (swizzle alignment)
 constexpr int TMEM_COLS = 2 * TILE_N;           // two accumulator buffers
 
-// K-major operand tile, 128-byte swizzle: rows of 128 bytes, groups of 8 rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t addr)
-{
-    const uint32_t lo = ((addr & 0x3FFFFu) >> 4) | (1u << 16);                 // start, leading offset (unused)
-    const uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);                // stride 1024 B, version 1, SWIZZLE_128B
-    return ((uint64_t)hi << 32) | lo;
-}
-
-template <bool I8>
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
-{
-    if (I8)
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n"
-                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-    else
-        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                     ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void mma_commit(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void tmem_ld8_nowait(uint32_t taddr, uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr));
-}
 // Eight words to one 32-byte sector.  A lane's row of accumulators is far from its neighbours', so every store instruction goes to 32
 // lines: in stores of 16 bytes the row tiles of a wide layer cost twice the cycles and twice the (partial) sectors.  Block of 256 -> 1024
 // -> 256 channels bf16 on 4 x 128 x 128, two contractions of 67 and 17 MB: 367 -> 350 us; layer 384 -> 512 of 2 x 64 x 128 44.2 -> 42.2.
@@ -70,9 +36,6 @@ __device__ __forceinline__ void st_sector(int32_t* p, const uint32_t (&r)[8])
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
 struct SmemCtl {
     uint64_t full[STAGES];
     uint64_t empty[STAGES];

@@ -1,0 +1,833 @@
+// Group norm with an activation on channels-last maps [N][P][C], forward and backward.
+//
+// Statistics run over the positions and the D channels of a group, so every map is gone through twice: once for sums, once to apply them.  The
+// bytes bound it: x and y (forward), x, dy and dx (backward), each once, if the second time finds the map in L2.  So an image is cut into tiles
+// of whole positions, and one launch works through a list of tiles in the order
+//     sums of image 0 .. lag-1 | sums of image lag, apply image 0 (tile by tile in turn) | sums of image lag+1, apply image 1 | ...
+// with a lag of about 24 MB: far enough that the last of the sums is ready when the first CTA asks for it, near enough that the map is still in L2.
+// CTAs take tiles by a ticket, in order.  A tile only ever waits for tiles in front of it, so whichever CTAs are resident finish: the lowest
+// unfinished tile waits for nobody.  The last CTA to bring a tile's sums (by a count of arrivals) adds them all up in the tiles' order, so results
+// do not depend on the schedule, and raises the image's flag.
+// Images of one tile need none of that: a CTA does sums and result of an image, and goes on to its next.
+//
+// A thread meets the same channels all along: its vectors (of V values) are a multiple of the period p = C / gcd(C, V) vectors apart, so its
+// constants and sums sit in registers.  Periods longer than the CTA are gone through in slots of one vector a thread.
+#pragma once
+
+#include "checkpoint.cuh"
+#include "tma.cuh"
+#include "vec.cuh"
+
+namespace wcc {
+namespace gn {
+
+using namespace tr;
+
+constexpr int T = 256;                     // threads of a CTA
+constexpr int FAN = 16;                    // tiles whose channel sums are added up in one step
+constexpr int CTAS_FWD = 4, CTAS_BWD = 3;  // CTAs of an SM
+constexpr size_t LAG_BYTES = (size_t)24 << 20;
+
+struct Plan {
+    int V, p, lanes, reps, slots;          // period of p vectors; `reps` periods side by side, or one in `slots` turns of the CTA
+    bool aligned;                          // all of a vector's channels are in one group
+    int tile, nt, supers;                  // positions of a tile, tiles of an image, steps of FAN tiles
+    int lag;                               // images between sums and result
+    int ctl;                               // words of control an image: arrivals of each step, of the steps, flag
+    bool solo;
+};
+
+struct Args {
+    const void *x, *dy;
+    const int8_t* codes;                   // checkpoint of x, read (backward) ...
+    const float* scales;
+    const float *gamma, *beta, *mean, *rstd;
+    void* out;
+    float *mean_out, *rstd_out;
+    float *part, *sup, *img;               // partial sums of tiles, of steps, of images (or the parameters' gradients themselves)
+    long long img_beta, img_gamma, img_row;  // img + row * img_row + {img_beta, img_gamma}
+    float2* coef;
+    unsigned* ctl;                         // ticket, then Plan::ctl words an image
+    int N, P, C, G, D, nb, act;
+    float eps, inv_count;
+    bool params;
+    Plan q;
+    int* status;
+};
+
+inline int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
+
+inline Plan plan_of(int N, int P, int C, int G, int es, bool backward, bool whole_rows)
+{
+    Plan q{};
+    const long long E = (long long)P * C;
+    // Vectors of 16 bytes where every image starts on one and the period fits the CTA; else as wide as the rows' own alignment.  (A checkpoint's
+    // scale is that of a row, so a vector must not go over a row's end.)
+    q.V = 16 / es;
+    while (q.V > 1 && !(E % q.V == 0 && (C % q.V == 0 || (!whole_rows && C / gcd(C, q.V) <= T)))) q.V /= 2;
+    q.p = C / gcd(C, q.V);
+    q.lanes = q.p < T ? q.p : T;
+    q.reps = q.p < T ? T / q.p : 1;
+    q.slots = (q.p + T - 1) / T;
+    const int D = C / G;
+    q.aligned = C % q.V == 0 && D % q.V == 0;
+    // Tiles: eight for each SM, of 8 to 64 KB, and of 64 positions at least where there are enough (the backward pass stores two sums a channel and tile).
+    const int unit = q.p * q.V / C;        // positions of a period
+    const long long row = (long long)C * es;
+    long long hi = 65536 / row, lo = 8192 / row;
+    if (hi < 64) hi = 64;
+    if (lo < 1) lo = 1;
+    long long t = (long long)N * P / (B200_SMS * 8);
+    t = t < lo ? lo : t > hi ? hi : t;
+    if (t < (P + 1023) / 1024) t = (P + 1023) / 1024;
+    t = (t + unit - 1) / unit * unit;
+    q.tile = (int)(t < P ? t : P);
+    q.nt = (P + q.tile - 1) / q.tile;
+    q.supers = (q.nt + FAN - 1) / FAN;
+    q.solo = q.nt == 1;
+    const size_t bytes = (size_t)E * es * (backward ? 2 : 1);
+    const long long lag = (long long)((LAG_BYTES + bytes - 1) / bytes);
+    q.lag = (int)(lag < N ? lag : N);
+    q.ctl = q.supers + 2;
+    return q;
+}
+
+inline int grid_of(const Plan& q, int N, int sms, bool backward)
+{
+    const long long items = q.solo ? (long long)N : 2LL * N * q.nt, most = (long long)sms * (backward ? CTAS_BWD : CTAS_FWD);
+    return (int)(items < most ? items : most);
+}
+
+struct Layout { size_t ctl, part, sup, img, coef, total; };
+inline Layout layout_of(const Plan& q, int N, int C, int G, bool backward)
+{
+    Layout l{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 256); return a; };
+    if (!q.solo) {
+        l.ctl = take((1 + (size_t)N * q.ctl) * 4);
+        l.part = take((size_t)N * q.nt * (backward ? 2 * C : 2 * G) * 4);
+        if (backward) l.sup = take((size_t)N * q.supers * 2 * C * 4);
+        l.coef = take((size_t)N * G * 8);
+    }
+    if (backward) l.img = take((size_t)(q.solo ? grid_of(q, N, B200_SMS, true) : N) * 2 * C * 4);
+    l.total = at < 256 ? 256 : at;
+    return l;
+}
+
+// ---- pieces ----------------------------------------------------------------------------------------
+struct Stat { float n, mean, m2; };
+__device__ __forceinline__ Stat merge(Stat a, Stat b)
+{
+    const float n = a.n + b.n;
+    if (n == 0.0f) return a;
+    const float d = b.mean - a.mean, f = __fdividef(b.n, n);
+    return {n, __fmaf_rn(d, f, a.mean), a.m2 + b.m2 + d * d * a.n * f};
+}
+__device__ __forceinline__ Stat warp_merge(Stat s)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        Stat b{__shfl_xor_sync(0xFFFFFFFFu, s.n, o), __shfl_xor_sync(0xFFFFFFFFu, s.mean, o), __shfl_xor_sync(0xFFFFFFFFu, s.m2, o)};
+        // the lower lane's part first on both sides: the same bits on all lanes
+        s = (threadIdx.x & o) ? merge(b, s) : merge(s, b);
+    }
+    return s;
+}
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Channel of value e of vector q of a period.
+template <int V> __device__ __forceinline__ int channel(const Args& a, int q, int e)
+{
+    const int f = q * V + e;
+    return f < a.C ? f : f % a.C;
+}
+
+// ---- forward ---------------------------------------------------------------------------------------
+// Sums of a tile.  Deviations are taken from the thread's first value (of the channel, or of its group), so a common offset costs nothing: a
+// thread's sum of squares holds the pivot's own distance squared, and loses at most (values of the thread) * 2^-24 of itself.  Threads and tiles
+// are then put together as (count, mean, sum of squared deviations).
+template <typename X, int V, bool ALIGNED>
+__device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, Stat* entries)
+{
+    const Plan& q = a.q;
+    const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
+    const int step = q.reps * q.p;
+    for (int j = 0; j < q.slots; ++j) {
+        const int vq = j * T + lane;
+        if (sub >= q.reps || vq >= q.p) continue;
+        const int v0 = sub * q.p + vq;
+        if constexpr (ALIGNED) {
+            float2 s = both(0.0f), ss = both(0.0f);
+            float s1 = 0.0f, ss1 = 0.0f, pivot = 0.0f;
+            int k = 0;
+            if (v0 < nvec) {
+                pivot = (float)x[(size_t)v0 * V];
+                const float2 neg = both(-pivot);
+#pragma unroll 4
+                for (int v = v0; v < nvec; v += step, ++k) {
+                    Vec<X, V> r;
+                    r.load(x + (size_t)v * V);
+                    float f[V];
+                    unpack(r, f);
+                    if constexpr (V == 1) {
+                        const float d = f[0] - pivot;
+                        s1 += d;
+                        ss1 = __fmaf_rn(d, d, ss1);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; e += 2) {
+                            const float2 d = add2(make_float2(f[e], f[e + 1]), neg);
+                            s = add2(s, d);
+                            ss = fma2(d, d, ss);
+                        }
+                    }
+                }
+            }
+            const float n = (float)(k * V), sum = s.x + s.y + s1, sq = ss.x + ss.y + ss1, m = k ? __fdividef(sum, n) : 0.0f;
+            entries[v0] = {n, pivot + m, fmaxf(sq - sum * m, 0.0f)};
+        } else {
+            float s[V], ss[V], pivot[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e] = ss[e] = pivot[e] = 0.0f;
+            int k = 0;
+            if (v0 < nvec) {
+                Vec<X, V> r;
+                r.load(x + (size_t)v0 * V);
+                unpack(r, pivot);
+#pragma unroll 2
+                for (int v = v0; v < nvec; v += step, ++k) {
+                    r.load(x + (size_t)v * V);
+                    float f[V];
+                    unpack(r, f);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float d = f[e] - pivot[e];
+                        s[e] += d;
+                        ss[e] = __fmaf_rn(d, d, ss[e]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float n = (float)k, m = k ? __fdividef(s[e], n) : 0.0f;
+                entries[v0 * V + e] = {n, pivot[e] + m, fmaxf(ss[e] - s[e] * m, 0.0f)};
+            }
+        }
+    }
+}
+
+// Group g of the CTA's entries; the whole warp calls it.
+template <int V, bool ALIGNED>
+__device__ __forceinline__ Stat group_of(const Args& a, int g, const Stat* entries)
+{
+    const Plan& q = a.q;
+    constexpr int W = ALIGNED ? V : 1;
+    const int period = q.p * V / W, Cw = a.C / W, Dw = a.D / W, copies = period / Cw, each = copies * Dw, total = q.reps * each;
+    Stat s{0.0f, 0.0f, 0.0f};
+    for (int m = threadIdx.x & 31; m < total; m += 32) {
+        const int sub = m / each, rest = m - sub * each, i = rest / Dw;
+        s = merge(s, entries[sub * period + i * Cw + g * Dw + (rest - i * Dw)]);
+    }
+    return warp_merge(s);
+}
+
+template <int V, int ACT> __device__ __forceinline__ void activate(float (&z)[V])
+{
+    if constexpr (ACT == WCC_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = z[e] < 0.0f ? 0.0f : z[e];       // (a NaN stays one)
+    } else if constexpr (ACT == WCC_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[e] = z[e] * sigmoid(z[e]);
+    }
+}
+
+template <typename X, int V, int ACT>
+__device__ __forceinline__ void apply_tile(const Args& a, const X* x, X* y, int nvec, const float2* coef)
+{
+    const Plan& q = a.q;
+    const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
+    const int step = q.reps * q.p;
+    constexpr int U = 4;
+    for (int j = 0; j < q.slots; ++j) {
+        const int vq = j * T + lane;
+        if (sub >= q.reps || vq >= q.p) continue;
+        float m[V], k[V], b[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int c = channel<V>(a, vq, e);
+            const float2 st = coef[c / a.D];
+            m[e] = -st.x;
+            k[e] = st.y * (a.gamma ? __ldg(a.gamma + c) : 1.0f);
+            b[e] = a.beta ? __ldg(a.beta + c) : 0.0f;
+        }
+        for (int v = sub * q.p + vq; v < nvec; v += U * step) {
+            Vec<X, V> r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (v + u * step < nvec) r[u].load(x + (size_t)(v + u * step) * V);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * step >= nvec) break;
+                float f[V];
+                unpack(r[u], f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[e] = __fmaf_rn(f[e] + m[e], k[e], b[e]);
+                activate<V, ACT>(f);
+                pack(r[u], f);
+                r[u].store(y + (size_t)(v + u * step) * V);
+            }
+        }
+    }
+}
+template <typename X, int V>
+__device__ __forceinline__ void apply(const Args& a, const X* x, X* y, int nvec, const float2* coef)
+{
+    if (a.act == WCC_ACT_SILU) apply_tile<X, V, WCC_ACT_SILU>(a, x, y, nvec, coef);
+    else if (a.act == WCC_ACT_RELU) apply_tile<X, V, WCC_ACT_RELU>(a, x, y, nvec, coef);
+    else apply_tile<X, V, WCC_ACT_NONE>(a, x, y, nvec, coef);
+}
+
+// ---- the list of tiles -----------------------------------------------------------------------------
+struct Item { bool sums; int n, tile; };
+__device__ __forceinline__ Item item_of(const Args& a, long long i)
+{
+    const int nt = a.q.nt, lag = a.q.lag;
+    const long long head = (long long)lag * nt, mid = 2LL * (a.N - lag) * nt;
+    if (i < head) return {true, (int)(i / nt), (int)(i % nt)};
+    i -= head;
+    if (i < mid) {
+        const long long round = i / (2 * nt);
+        const int k = (int)(i - round * 2 * nt);
+        return (k & 1) ? Item{false, (int)round, k >> 1} : Item{true, (int)round + lag, k >> 1};
+    }
+    i -= mid;
+    return {false, a.N - lag + (int)(i / nt), (int)(i % nt)};
+}
+
+__device__ __forceinline__ unsigned load_acquire(const unsigned* p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store_release(unsigned* p, unsigned v)
+{
+    asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+// True on every thread if this CTA is the last of `of` to arrive; then what the others wrote before is visible.
+__device__ __forceinline__ bool arrive_last(unsigned* count, unsigned of, int* flag)
+{
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *flag = atomicAdd(count, 1u) == of - 1;
+    __syncthreads();
+    const bool last = *flag != 0;
+    if (last) __threadfence();
+    return last;
+}
+// Bounded wait of the whole CTA for an image's flag.
+__device__ __forceinline__ bool wait_flag(const unsigned* f, int* status, int* flag)
+{
+    if (threadIdx.x == 0) {
+        bool ok = false;
+        const uint32_t limit = tc::c_wait_limit;
+        for (uint32_t i = 0; i < limit && !ok; ++i) {
+            ok = load_acquire(f) != 0u;
+            if (!ok) __nanosleep(100);
+        }
+        if (!ok) atomicExch(status, (int)WCC_ERR_TIMEOUT);
+        *flag = ok;
+    }
+    __syncthreads();
+    return *flag != 0;
+}
+
+template <typename X, int V, bool ALIGNED>
+__global__ void __launch_bounds__(T, CTAS_FWD) forward_kernel(const __grid_constant__ Args a)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ long long s_item;
+    __shared__ int s_flag;
+    Stat* entries = reinterpret_cast<Stat*>(smem);
+    const Plan& q = a.q;
+    const int warp = threadIdx.x >> 5;
+    const X* x = static_cast<const X*>(a.x);
+    X* y = static_cast<X*>(a.out);
+    const long long E = (long long)a.P * a.C;
+    pdl_wait();
+    pdl_launch();
+    if (q.solo) {
+        const int words = q.slots > 1 ? q.p * V / (ALIGNED ? V : 1) : q.reps * q.p * (ALIGNED ? 1 : V);
+        float2* coef = reinterpret_cast<float2*>(entries + words + (words & 1));
+        const int nvec = (int)(E / V);
+        for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
+            stats_tile<X, V, ALIGNED>(a, x + n * E, nvec, entries);
+            __syncthreads();
+            for (int g = warp; g < a.G; g += T / 32) {
+                const Stat s = group_of<V, ALIGNED>(a, g, entries);
+                if ((threadIdx.x & 31) == 0) {
+                    const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps));
+                    coef[g] = make_float2(s.mean, r);
+                    if (a.mean_out) a.mean_out[(size_t)n * a.G + g] = s.mean;
+                    if (a.rstd_out) a.rstd_out[(size_t)n * a.G + g] = r;
+                }
+            }
+            __syncthreads();
+            apply<X, V>(a, x + n * E, y + n * E, nvec, coef);
+        }
+        return;
+    }
+    const long long items = 2LL * a.N * q.nt;
+    long long next = threadIdx.x == 0 ? (long long)atomicAdd(a.ctl, 1u) : 0;
+    for (;;) {
+        if (threadIdx.x == 0) s_item = next;
+        __syncthreads();
+        const long long i = s_item;
+        if (i >= items) return;
+        if (threadIdx.x == 0) next = (long long)atomicAdd(a.ctl, 1u);
+        const Item it = item_of(a, i);
+        const int p0 = it.tile * q.tile, positions = min(q.tile, a.P - p0);
+        const long long at = it.n * E + (long long)p0 * a.C;
+        const int nvec = (int)((long long)positions * a.C / V);
+        unsigned* ctl = a.ctl + 1 + (size_t)it.n * q.ctl;
+        float2* coef = a.coef + (size_t)it.n * a.G;
+        if (it.sums) {
+            float2* part = reinterpret_cast<float2*>(a.part) + (size_t)it.n * q.nt * a.G;
+            stats_tile<X, V, ALIGNED>(a, x + at, nvec, entries);
+            __syncthreads();
+            for (int g = warp; g < a.G; g += T / 32) {
+                const Stat s = group_of<V, ALIGNED>(a, g, entries);
+                if ((threadIdx.x & 31) == 0) part[(size_t)it.tile * a.G + g] = make_float2(s.mean, s.m2);
+            }
+            if (arrive_last(ctl, (unsigned)q.nt, &s_flag)) {
+                for (int g = warp; g < a.G; g += T / 32) {
+                    Stat s{0.0f, 0.0f, 0.0f};
+                    for (int t = threadIdx.x & 31; t < q.nt; t += 32) {
+                        const float2 v = __ldcg(part + (size_t)t * a.G + g);
+                        s = merge(s, {(float)((long long)min(q.tile, a.P - t * q.tile) * a.D), v.x, v.y});
+                    }
+                    s = warp_merge(s);
+                    if ((threadIdx.x & 31) == 0) {
+                        const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps));
+                        coef[g] = make_float2(s.mean, r);
+                        if (a.mean_out) a.mean_out[(size_t)it.n * a.G + g] = s.mean;
+                        if (a.rstd_out) a.rstd_out[(size_t)it.n * a.G + g] = r;
+                    }
+                }
+                __threadfence();
+                __syncthreads();
+                if (threadIdx.x == 0) store_release(ctl + q.ctl - 1, 1u);
+            }
+        } else {
+            if (!wait_flag(ctl + q.ctl - 1, a.status, &s_flag)) return;
+            // through shared memory: written during this launch, so not to be read by the path of constant data
+            float2* c = reinterpret_cast<float2*>(entries);
+            for (int g = threadIdx.x; g < a.G; g += T) c[g] = __ldcg(coef + g);
+            __syncthreads();
+            apply<X, V>(a, x + at, y + at, nvec, c);
+        }
+        __syncthreads();
+    }
+}
+
+// ---- backward --------------------------------------------------------------------------------------
+template <int V, int ACT> __device__ __forceinline__ void slope_times(const float (&z)[V], float (&t)[V])
+{
+    if constexpr (ACT == WCC_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[e] = z[e] > 0.0f ? t[e] : 0.0f;
+    } else if constexpr (ACT == WCC_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float s = sigmoid(z[e]);
+            t[e] *= __fmaf_rn(z[e] * s, 1.0f - s, s);
+        }
+    }
+}
+
+// What a thread's channels need: -mean, rstd * gamma, beta.
+template <int V> struct Channels {
+    float m[V], k[V], b[V];
+    __device__ __forceinline__ void load(const Args& a, int n, int vq)
+    {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int c = channel<V>(a, vq, e);
+            const size_t g = (size_t)n * a.G + c / a.D;
+            m[e] = -__ldg(a.mean + g);
+            k[e] = __ldg(a.rstd + g) * (a.gamma ? __ldg(a.gamma + c) : 1.0f);
+            b[e] = a.beta ? __ldg(a.beta + c) : 0.0f;
+        }
+    }
+};
+
+// One vector of x: as it is, or from its checkpoint.
+template <typename X, int V, bool KEPT> struct Source {
+    const X* x;
+    const int8_t* codes;
+    const float* scales;                   // of the tile's first row
+    Vec<X, V> r;
+    Vec<int8_t, V> c;
+    float s;
+    __device__ __forceinline__ void load(int v, int row, int nb, int block)
+    {
+        if constexpr (KEPT) {
+            c.load(codes + (size_t)v * V);
+            s = __ldg(scales + (size_t)row * nb + block);
+        } else {
+            r.load(x + (size_t)v * V);
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[V]) const
+    {
+        if constexpr (KEPT) {
+            unpack(c, f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] *= s;
+        } else {
+            unpack(r, f);
+        }
+    }
+};
+
+// Sums over the tile's positions of t and t * (x - mean) for each channel, to dst[0 .. C) and dst[C .. 2C).
+template <typename X, int V, bool KEPT, int ACT>
+__device__ __forceinline__ void sums_tile(const Args& a, int n, long long at, int nvec, float* sums, float* dst)
+{
+    const Plan& q = a.q;
+    const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
+    const int step = q.reps * q.p, width = q.p * V;
+    const X* dy = static_cast<const X*>(a.dy) + at;
+    constexpr int U = 2;
+    for (int j = 0; j < q.slots; ++j) {
+        const int vq = j * T + lane;
+        if (sub >= q.reps || vq >= q.p) continue;
+        Channels<V> ch;
+        ch.load(a, n, vq);
+        float s0[V], s1[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) s0[e] = s1[e] = 0.0f;
+        const int block = vq * V / ck::BLOCK;
+        int row = sub;
+        for (int v = sub * q.p + vq; v < nvec; v += U * step, row += U * q.reps) {
+            Source<X, V, KEPT> src[U];
+            Vec<X, V> d[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * step >= nvec) break;
+                src[u].x = static_cast<const X*>(a.x) + at;
+                src[u].codes = a.codes + at;
+                src[u].scales = a.scales + at / a.C * a.nb;
+                src[u].load(v + u * step, row + u * q.reps, a.nb, block);
+                d[u].load(dy + (size_t)(v + u * step) * V);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * step >= nvec) break;
+                float xc[V], t[V], z[V];
+                src[u].get(xc);
+                unpack(d[u], t);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    xc[e] += ch.m[e];
+                    z[e] = __fmaf_rn(xc[e], ch.k[e], ch.b[e]);
+                }
+                slope_times<V, ACT>(z, t);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    s0[e] += t[e];
+                    s1[e] = __fmaf_rn(t[e], xc[e], s1[e]);
+                }
+            }
+        }
+        if (q.slots > 1) {                 // a channel is one thread's
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                dst[vq * V + e] = s0[e];
+                dst[a.C + vq * V + e] = s1[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                sums[sub * width + vq * V + e] = s0[e];
+                sums[(q.reps + sub) * width + vq * V + e] = s1[e];
+            }
+        }
+    }
+    __syncthreads();
+    if (q.slots == 1) {
+        const int copies = width / a.C;
+        for (int c = threadIdx.x; c < a.C; c += T) {
+            float s0 = 0.0f, s1 = 0.0f;
+            for (int k = 0; k < q.reps; ++k)
+                for (int i = 0; i < copies; ++i) {
+                    s0 += sums[k * width + i * a.C + c];
+                    s1 += sums[(q.reps + k) * width + i * a.C + c];
+                }
+            dst[c] = s0;
+            dst[a.C + c] = s1;
+        }
+    }
+}
+
+template <typename X, int V, bool KEPT, int ACT>
+__device__ __forceinline__ void dx_tile(const Args& a, int n, long long at, int nvec, const float2* coef)
+{
+    const Plan& q = a.q;
+    const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
+    const int step = q.reps * q.p;
+    const X* dy = static_cast<const X*>(a.dy) + at;
+    X* out = static_cast<X*>(a.out) + at;
+    constexpr int U = 2;
+    for (int j = 0; j < q.slots; ++j) {
+        const int vq = j * T + lane;
+        if (sub >= q.reps || vq >= q.p) continue;
+        Channels<V> ch;
+        ch.load(a, n, vq);
+        float k0[V], k1[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float2 c = coef[channel<V>(a, vq, e) / a.D];
+            k0[e] = c.x;
+            k1[e] = c.y;
+        }
+        const int block = vq * V / ck::BLOCK;
+        int row = sub;
+        for (int v = sub * q.p + vq; v < nvec; v += U * step, row += U * q.reps) {
+            Source<X, V, KEPT> src[U];
+            Vec<X, V> d[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * step >= nvec) break;
+                src[u].x = static_cast<const X*>(a.x) + at;
+                src[u].codes = a.codes + at;
+                src[u].scales = a.scales + at / a.C * a.nb;
+                src[u].load(v + u * step, row + u * q.reps, a.nb, block);
+                d[u].load(dy + (size_t)(v + u * step) * V);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (v + u * step >= nvec) break;
+                float xc[V], t[V], z[V];
+                src[u].get(xc);
+                unpack(d[u], t);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    xc[e] += ch.m[e];
+                    z[e] = __fmaf_rn(xc[e], ch.k[e], ch.b[e]);
+                }
+                slope_times<V, ACT>(z, t);
+#pragma unroll
+                for (int e = 0; e < V; ++e) t[e] = __fmaf_rn(t[e], ch.k[e], __fmaf_rn(xc[e], k1[e], k0[e]));
+                pack(d[u], t);
+                d[u].store(out + (size_t)(v + u * step) * V);
+            }
+        }
+    }
+}
+template <typename X, int V, bool KEPT>
+__device__ __forceinline__ void sums_of(const Args& a, int n, long long at, int nvec, float* sums, float* dst)
+{
+    if (a.act == WCC_ACT_SILU) sums_tile<X, V, KEPT, WCC_ACT_SILU>(a, n, at, nvec, sums, dst);
+    else if (a.act == WCC_ACT_RELU) sums_tile<X, V, KEPT, WCC_ACT_RELU>(a, n, at, nvec, sums, dst);
+    else sums_tile<X, V, KEPT, WCC_ACT_NONE>(a, n, at, nvec, sums, dst);
+}
+template <typename X, int V, bool KEPT>
+__device__ __forceinline__ void dx_of(const Args& a, int n, long long at, int nvec, const float2* coef)
+{
+    if (a.act == WCC_ACT_SILU) dx_tile<X, V, KEPT, WCC_ACT_SILU>(a, n, at, nvec, coef);
+    else if (a.act == WCC_ACT_RELU) dx_tile<X, V, KEPT, WCC_ACT_RELU>(a, n, at, nvec, coef);
+    else dx_tile<X, V, KEPT, WCC_ACT_NONE>(a, n, at, nvec, coef);
+}
+
+// From the channel sums of image n: dx = rstd gamma t + k1 (x - mean) + k0 with k0 = -rstd mean(g), k1 = -rstd^2 mean(g xh).
+__device__ __forceinline__ void group_terms(const Args& a, int n, const float* chan, float2* coef)
+{
+    for (int g = threadIdx.x >> 5; g < a.G; g += T / 32) {
+        float c1 = 0.0f, c2 = 0.0f;
+        for (int d = threadIdx.x & 31; d < a.D; d += 32) {
+            const int c = g * a.D + d;
+            const float w = a.gamma ? __ldg(a.gamma + c) : 1.0f;
+            c1 = __fmaf_rn(w, chan[c], c1);
+            c2 = __fmaf_rn(w, chan[a.C + c], c2);
+        }
+        c1 = warp_sum(c1);
+        c2 = warp_sum(c2);
+        if ((threadIdx.x & 31) == 0) {
+            const float r = __ldg(a.rstd + (size_t)n * a.G + g);
+            coef[g] = make_float2(-r * c1 * a.inv_count, -r * r * r * c2 * a.inv_count);
+        }
+    }
+}
+
+template <typename X, int V, bool KEPT>
+__global__ void __launch_bounds__(T, CTAS_BWD) backward_kernel(const __grid_constant__ Args a)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ long long s_item;
+    __shared__ int s_flag;
+    const Plan& q = a.q;
+    const long long E = (long long)a.P * a.C;
+    float* chan = reinterpret_cast<float*>(smem);                      // [2][C]
+    float2* coef_s = reinterpret_cast<float2*>(chan + 2 * a.C);        // [G]
+    float* acc = reinterpret_cast<float*>(coef_s + a.G);               // [2][C], solo
+    float* sums = acc + (q.solo ? 2 * a.C : 0);                        // [2][reps][p V] where slots == 1
+    pdl_wait();
+    pdl_launch();
+    if (q.solo) {
+        const int nvec = (int)(E / V);
+        for (int c = threadIdx.x; c < 2 * a.C; c += T) acc[c] = 0.0f;
+        for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
+            sums_of<X, V, KEPT>(a, n, n * E, nvec, sums, chan);
+            __syncthreads();
+            group_terms(a, n, chan, coef_s);
+            for (int c = threadIdx.x; c < a.C; c += T) {
+                acc[c] += chan[c];
+                acc[a.C + c] = __fmaf_rn(__ldg(a.rstd + (size_t)n * a.G + c / a.D), chan[a.C + c], acc[a.C + c]);
+            }
+            __syncthreads();
+            dx_of<X, V, KEPT>(a, n, n * E, nvec, coef_s);
+        }
+        if (a.params) {
+            __syncthreads();
+            float* row = a.img + (long long)blockIdx.x * a.img_row;
+            for (int c = threadIdx.x; c < a.C; c += T) {
+                row[a.img_beta + c] = acc[c];
+                row[a.img_gamma + c] = acc[a.C + c];
+            }
+        }
+        return;
+    }
+    const long long items = 2LL * a.N * q.nt;
+    long long next = threadIdx.x == 0 ? (long long)atomicAdd(a.ctl, 1u) : 0;
+    for (;;) {
+        if (threadIdx.x == 0) s_item = next;
+        __syncthreads();
+        const long long i = s_item;
+        if (i >= items) return;
+        if (threadIdx.x == 0) next = (long long)atomicAdd(a.ctl, 1u);
+        const Item it = item_of(a, i);
+        const int p0 = it.tile * q.tile, positions = min(q.tile, a.P - p0);
+        const long long at = it.n * E + (long long)p0 * a.C;
+        const int nvec = (int)((long long)positions * a.C / V);
+        unsigned* ctl = a.ctl + 1 + (size_t)it.n * q.ctl;
+        float2* coef = a.coef + (size_t)it.n * a.G;
+        if (it.sums) {
+            const int s = it.tile / FAN, t0 = s * FAN, tn = min(FAN, q.nt - t0);
+            float* part = a.part + (size_t)it.n * q.nt * 2 * a.C;
+            float* sup = a.sup + (size_t)it.n * q.supers * 2 * a.C;
+            sums_of<X, V, KEPT>(a, it.n, at, nvec, sums, part + (size_t)it.tile * 2 * a.C);
+            if (arrive_last(ctl + s, (unsigned)tn, &s_flag)) {
+                for (int c = threadIdx.x; c < 2 * a.C; c += T) {
+                    float v = 0.0f;
+#pragma unroll 8
+                    for (int k = 0; k < tn; ++k) v += __ldcg(part + (size_t)(t0 + k) * 2 * a.C + c);
+                    sup[(size_t)s * 2 * a.C + c] = v;
+                }
+                if (arrive_last(ctl + q.supers, (unsigned)q.supers, &s_flag)) {
+                    for (int c = threadIdx.x; c < 2 * a.C; c += T) {
+                        float v = 0.0f;
+#pragma unroll 8
+                        for (int k = 0; k < q.supers; ++k) v += __ldcg(sup + (size_t)k * 2 * a.C + c);
+                        chan[c] = v;
+                    }
+                    __syncthreads();
+                    group_terms(a, it.n, chan, coef);
+                    if (a.params) {
+                        float* row = a.img + it.n * a.img_row;
+                        for (int c = threadIdx.x; c < a.C; c += T) {
+                            row[a.img_beta + c] = chan[c];
+                            row[a.img_gamma + c] = __ldg(a.rstd + (size_t)it.n * a.G + c / a.D) * chan[a.C + c];
+                        }
+                    }
+                    __threadfence();
+                    __syncthreads();
+                    if (threadIdx.x == 0) store_release(ctl + q.ctl - 1, 1u);
+                }
+            }
+        } else {
+            if (!wait_flag(ctl + q.ctl - 1, a.status, &s_flag)) return;
+            for (int g = threadIdx.x; g < a.G; g += T) coef_s[g] = __ldcg(coef + g);
+            __syncthreads();
+            dx_of<X, V, KEPT>(a, it.n, at, nvec, coef_s);
+        }
+        __syncthreads();
+    }
+}
+
+// dbeta and dgamma from the rows of partial sums, 32 columns a block, rows in order of a warp's number.
+static __global__ void __launch_bounds__(256) reduce_kernel(const float* __restrict__ img, int rows, int C, float* __restrict__ dgamma, float* __restrict__ dbeta)
+{
+    __shared__ float s[8][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    pdl_wait();
+    pdl_launch();
+    float v = 0.0f;
+    if (c < 2 * C)
+#pragma unroll 4
+        for (int r = warp; r < rows; r += 8) v += __ldcg(img + (size_t)r * 2 * C + c);
+    s[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && c < 2 * C) {
+        for (int k = 1; k < 8; ++k) v += s[k][lane];
+        float* dst = c < C ? dbeta : dgamma;
+        if (dst) dst[c < C ? c : c - C] = v;
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+template <typename X, int V, bool ALIGNED>
+wcc_status launch_forward(const Args& a, const DeviceInfo& di, cudaStream_t st)
+{
+    const Plan& q = a.q;
+    const int words = (q.slots > 1 ? q.p : q.reps * q.p) * (ALIGNED ? 1 : V);
+    size_t smem = (size_t)(words + (words & 1)) * sizeof(Stat) + (q.solo ? (size_t)a.G * 8 : 0);
+    if (smem < (size_t)a.G * 8) smem = (size_t)a.G * 8;
+    if (smem > 48 * 1024) {
+        const wcc_status s = allow_smem<forward_kernel<X, V, ALIGNED>>(di.dev, (int)smem);
+        if (s != WCC_OK) return s;
+    }
+    return launch_overlapped(forward_kernel<X, V, ALIGNED>, dim3((unsigned)grid_of(q, a.N, di.sms, false)), dim3(T), smem, st, true, 1, a);
+}
+template <typename X>
+wcc_status forward(const Args& a, const DeviceInfo& di, cudaStream_t st)
+{
+    const Plan& q = a.q;
+    if constexpr (sizeof(X) == 2)
+        if (q.V == 8) return q.aligned ? launch_forward<X, 8, true>(a, di, st) : launch_forward<X, 8, false>(a, di, st);
+    if (q.V == 4) return q.aligned ? launch_forward<X, 4, true>(a, di, st) : launch_forward<X, 4, false>(a, di, st);
+    if (q.V == 2) return q.aligned ? launch_forward<X, 2, true>(a, di, st) : launch_forward<X, 2, false>(a, di, st);
+    return launch_forward<X, 1, true>(a, di, st);
+}
+template <typename X, int V, bool KEPT>
+wcc_status launch_backward(const Args& a, const DeviceInfo& di, int grid, cudaStream_t st)
+{
+    const Plan& q = a.q;
+    const size_t smem = (size_t)(2 * a.C + 2 * a.G + (q.solo ? 2 * a.C : 0) + (q.slots == 1 ? 2 * q.reps * q.p * V : 0)) * 4;
+    if (smem > 48 * 1024) {
+        const wcc_status s = allow_smem<backward_kernel<X, V, KEPT>>(di.dev, (int)smem);
+        if (s != WCC_OK) return s;
+    }
+    return launch_overlapped(backward_kernel<X, V, KEPT>, dim3((unsigned)grid), dim3(T), smem, st, true, 1, a);
+}
+template <typename X>
+wcc_status backward(const Args& a, const DeviceInfo& di, int grid, cudaStream_t st)
+{
+    const Plan& q = a.q;
+    const bool kept = a.x == nullptr;
+    if constexpr (sizeof(X) == 2)
+        if (q.V == 8) return kept ? launch_backward<X, 8, true>(a, di, grid, st) : launch_backward<X, 8, false>(a, di, grid, st);
+    if (q.V == 4) return kept ? launch_backward<X, 4, true>(a, di, grid, st) : launch_backward<X, 4, false>(a, di, grid, st);
+    if (q.V == 2) return kept ? launch_backward<X, 2, true>(a, di, grid, st) : launch_backward<X, 2, false>(a, di, grid, st);
+    return kept ? launch_backward<X, 1, true>(a, di, grid, st) : launch_backward<X, 1, false>(a, di, grid, st);
+}
+
+}  // namespace gn
+}  // namespace wcc

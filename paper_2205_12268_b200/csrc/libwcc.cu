@@ -1,4 +1,5 @@
-// libwcc: C-ABI entry points (see include/wcc.h).  One translation unit: the kernels live in the *.cuh files.
+// libwcc: C-ABI entry points (see include/wcc.h) of the layer and of what stands in front of and beside it; the kernels live in the *.cuh files.
+// Group norm, checkpoints and the gated block: training.cu.
 #include <algorithm>
 #include <type_traits>
 
@@ -16,6 +17,12 @@
 #include "wavelet.cuh"
 
 namespace wcc {
+
+wcc_status status_address(int** status)
+{
+    WCC_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void**>(status), g_status));
+    return WCC_OK;
+}
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -1209,7 +1216,7 @@ wcc_status wcc_debug_set_wait_limit(unsigned polls)
 {
     const uint32_t v = polls ? (uint32_t)polls : tc::WAIT_LIMIT_DEFAULT;
     if (cudaMemcpyToSymbol(tc::c_wait_limit, &v, sizeof(v)) != cudaSuccess) return WCC_ERR_CUDA;
-    return WCC_OK;
+    return set_training_wait_limit(v);
 }
 
 wcc_status wcc_debug_wait_selftest(void* stream)

@@ -13,7 +13,7 @@ namespace tc {
 // kernel reports WCC_ERR_TIMEOUT.  A constant-bank word so that reading it costs nothing on the fast path; the host
 // can lower it (wcc_debug_set_wait_limit) to exercise the timeout path in a millisecond.
 constexpr uint32_t WAIT_LIMIT_DEFAULT = 2000000u;
-__constant__ uint32_t c_wait_limit = WAIT_LIMIT_DEFAULT;
+static __constant__ uint32_t c_wait_limit = WAIT_LIMIT_DEFAULT;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

@@ -27,7 +27,11 @@ EXPORTS = ("wcc_staged_workspace_bytes", "wcc_forward_staged", "wcc_workspace_by
            "wcc_padded_workspace_bytes", "wcc_forward_padded", "wcc_dwconv_haar_fwd", "wcc_block_workspace_bytes",
            "wcc_block_forward", "wcc_dwt_fwd", "wcc_dwt_inv", "wcc_wavelet_workspace_bytes", "wcc_forward_wavelet",
            "wcc_layernorm_fwd", "wcc_layernorm_bwd_workspace_bytes", "wcc_layernorm_bwd", "wcc_adapters_workspace_bytes",
-           "wcc_adapters_fwd", "wcc_adapters_bwd", "wcc_forward_check", "wcc_debug_adapters_path", "wcc_debug_layernorm_path")
+           "wcc_adapters_fwd", "wcc_adapters_bwd", "wcc_forward_check", "wcc_debug_adapters_path", "wcc_debug_layernorm_path",
+           "wcc_checkpoint", "wcc_checkpoint_restore", "wcc_groupnorm_workspace_bytes", "wcc_groupnorm_fwd", "wcc_groupnorm_bwd", "wcc_gated_fwd",
+           "wcc_gated_bwd_workspace_bytes", "wcc_gated_bwd")
+CKPT_BLOCK = 128
+ACTS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 STATIC_SCRATCH_BYTES = 512 * 1024
 STAGES = ("haar_fwd_norms", "select_topk", "weight_quant", "gather_quant", "contract", "scatter_inv")   # wcc_forward_staged
 FUSED_STAGES = ("clear", "haar_norms", "select_topk", "fused_pass2")                                      # wcc_forward
@@ -158,6 +162,23 @@ def _operator_prototypes(L):
     L.wcc_debug_layernorm_path.argtypes = [i] * 6
     L.wcc_last_status.restype = i
     L.wcc_last_status.argtypes = [vp]
+    ll = C.c_longlong
+    L.wcc_checkpoint.restype = i
+    L.wcc_checkpoint.argtypes = [vp, ll, i, i, vp, vp, vp]
+    L.wcc_checkpoint_restore.restype = i
+    L.wcc_checkpoint_restore.argtypes = [vp, vp, ll, i, i, vp, vp]
+    L.wcc_groupnorm_workspace_bytes.restype = sz
+    L.wcc_groupnorm_workspace_bytes.argtypes = [i] * 6
+    L.wcc_groupnorm_fwd.restype = i
+    L.wcc_groupnorm_fwd.argtypes = [vp, vp, vp, i, i, i, i, f, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.wcc_groupnorm_bwd.restype = i
+    L.wcc_groupnorm_bwd.argtypes = [vp] * 8 + [i] * 6 + [vp, vp, vp, vp, sz, vp]
+    L.wcc_gated_fwd.restype = i
+    L.wcc_gated_fwd.argtypes = [vp, vp, vp, i, i, i, i, vp, vp]
+    L.wcc_gated_bwd_workspace_bytes.restype = sz
+    L.wcc_gated_bwd_workspace_bytes.argtypes = [i] * 3
+    L.wcc_gated_bwd.restype = i
+    L.wcc_gated_bwd.argtypes = [vp] * 4 + [i] * 4 + [vp, vp, vp, vp, sz, vp]
 
 
 def _check(code: int, where: str):
@@ -165,7 +186,7 @@ def _check(code: int, where: str):
         raise WccError(code, where)
 
 
-def _dt(t: torch.Tensor) -> int:
+def _dt(t) -> int:
     if t.dtype == torch.float32:
         return F32
     if t.dtype == torch.bfloat16:
@@ -417,6 +438,20 @@ class Workspace:
             raise WccError(2, "wcc_layernorm_bwd_workspace_bytes")
         return cls(n, x.device)
 
+    @classmethod
+    def for_groupnorm(cls, x, groups: int, backward: bool = True):
+        """For ``groupnorm`` and (unless ``backward`` is False) ``groupnorm_backward`` of x, a tensor or a ``Checkpoint``."""
+        t = x.codes if isinstance(x, Checkpoint) else x
+        return cls(_groupnorm_bytes(*_last_shape(t, "x"), groups, _dt(x), backward), t.device)
+
+    @classmethod
+    def for_gated_backward(cls, x, Wg: torch.Tensor):
+        t = x.codes if isinstance(x, Checkpoint) else x
+        n = int(lib().wcc_gated_bwd_workspace_bytes(t.numel() // t.shape[-1], t.shape[-1], Wg.shape[0]))
+        if n == 0:
+            raise WccError(2, "wcc_gated_bwd_workspace_bytes")
+        return cls(n, t.device)
+
 
 def _map_shape(x: torch.Tensor, name: str):
     """(N, C, H, W) of a map [N][C][H][W] or of rows [N][C], which are maps of one position."""
@@ -475,7 +510,10 @@ def layernorm(x: torch.Tensor, gamma: torch.Tensor | None = None, beta: torch.Te
 def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: torch.Tensor | None = None,
                        dx: torch.Tensor | None = None, params: bool = True, ws: Workspace | None = None):
     """The gradients of ``layernorm``: (dx, dgamma, dbeta), the last two fp32 [C] and None without ``params``.
-    ``dx`` may be dy or x.  ``ws`` is a ``Workspace.for_layernorm_backward``, allocated here if it is not given."""
+    ``dx`` may be dy or x.  ``ws`` is a ``Workspace.for_layernorm_backward``, allocated here if it is not given.
+    ``x`` may be a ``Checkpoint`` of the map; its values are brought back first."""
+    if isinstance(x, Checkpoint):
+        x = x.restore()
     N, Cc, H, W = _map_shape(x, "x")
     dt, dev = _dt(x), _here(x)
     pdy, pg = _same(dy, x, dev, "dy", "x"), _floats(gamma, Cc, dev, "gamma")
@@ -494,6 +532,209 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
         pdg, pdb, pw, nw = dgamma.data_ptr(), dbeta.data_ptr(), ws.buf.data_ptr(), ws.nbytes
     _check(lib().wcc_layernorm_bwd(pdy, x.data_ptr(), pg, pm, pr, N, Cc, H, W, dt, pdx, pdg, pdb, pw, nw, _stream()), "wcc_layernorm_bwd")
     return dx, dgamma, dbeta
+
+
+class Checkpoint:
+    """A tensor kept in 8 bits for the backward pass: ``codes`` int8 in its shape and ``scales`` fp32 [rows][blocks], a scale for each block of
+    ``CKPT_BLOCK`` values of a row (the last dimension); ``dtype`` is the type it comes back in.  ``checkpoint`` makes one; ``groupnorm`` fills one
+    (``keep=``); ``groupnorm_backward``, ``gated_backward``, ``layernorm_backward`` and ``Adapters.backward`` take one for x.  See wcc_checkpoint."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype):
+        _dev(codes, "codes")
+        _dev(scales, "scales")
+        if codes.dtype != torch.int8 or codes.dim() < 1 or codes.numel() == 0:
+            raise ValueError("codes must be int8 and hold a value")
+        self.L = codes.shape[-1]
+        self.rows = codes.numel() // self.L
+        if scales.dtype != torch.float32 or scales.device != codes.device or tuple(scales.shape) != (self.rows, -(-self.L // CKPT_BLOCK)):
+            raise ValueError("scales must be float32 [rows][blocks of %d values] on the device of the codes" % CKPT_BLOCK)
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("a checkpoint comes back as float32 or bfloat16, got %s" % dtype)
+        self.codes, self.scales, self.dtype = codes, scales, dtype
+
+    @classmethod
+    def like(cls, x: torch.Tensor) -> "Checkpoint":
+        """Room for a checkpoint of x, nothing written."""
+        _dev(x, "x")
+        if x.dim() < 1 or x.numel() == 0:
+            raise ValueError("x must hold a value")
+        L = x.shape[-1]
+        return cls(x.new_empty(x.shape, dtype=torch.int8), x.new_empty((x.numel() // L, -(-L // CKPT_BLOCK)), dtype=torch.float32), x.dtype)
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def _fits(self, x: torch.Tensor):
+        if self.codes.shape != x.shape or self.codes.device != x.device or self.dtype != x.dtype:
+            raise ValueError("the checkpoint must have x's shape, type and device")
+
+    def restore(self, out: torch.Tensor | None = None) -> torch.Tensor:
+        dev = _here(self.codes)
+        if out is None:
+            out = self.codes.new_empty(self.codes.shape, dtype=self.dtype)
+        elif not (out.get_device() == dev and out.is_contiguous() and out.dtype == self.dtype and out.shape == self.codes.shape):
+            raise ValueError("out must be contiguous, of the checkpoint's shape, type and device")
+        _check(lib().wcc_checkpoint_restore(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.L, _dt(out), out.data_ptr(), _stream()),
+               "wcc_checkpoint_restore")
+        return out
+
+
+def checkpoint(x: torch.Tensor, into: Checkpoint | None = None) -> Checkpoint:
+    """x (float32 or bfloat16, any shape) in 8 bits, a scale for each block of 128 values of its last dimension; ``into``: a checkpoint to write over."""
+    _dev(x, "x")
+    dt, _ = _dt(x), _here(x)
+    if into is None:
+        into = Checkpoint.like(x)
+    else:
+        into._fits(x)
+    _check(lib().wcc_checkpoint(x.data_ptr(), into.rows, into.L, dt, into.codes.data_ptr(), into.scales.data_ptr(), _stream()), "wcc_checkpoint")
+    return into
+
+
+def _act(act) -> int:
+    if act not in ACTS:
+        raise ValueError("act must be one of %s" % ", ".join(str(a) for a in ACTS))
+    return ACTS[act]
+
+
+def _last_shape(x: torch.Tensor, name: str):
+    """(N, positions, C) of a channels-last tensor [N]...[C]."""
+    _dev(x, name)
+    if x.dim() < 2 or x.numel() == 0:
+        raise ValueError("%s must be [N]...[C], channels last, and hold a value" % name)
+    N, Cc = x.shape[0], x.shape[-1]
+    return N, x.numel() // (N * Cc), Cc
+
+
+_gn_bytes = {}
+
+
+def _groupnorm_bytes(N, P, Cc, groups, dt, backward) -> int:
+    key = (N, P, Cc, groups, dt, bool(backward))
+    n = _gn_bytes.get(key)
+    if n is None:
+        n = int(lib().wcc_groupnorm_workspace_bytes(N, P, Cc, groups, dt, int(bool(backward))))
+        if n == 0:
+            raise WccError(2, "wcc_groupnorm_workspace_bytes")
+        if len(_gn_bytes) >= 256:              # sizes that change from call to call
+            _gn_bytes.clear()
+        _gn_bytes[key] = n
+    return n
+
+
+def groupnorm(x: torch.Tensor, groups: int, gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None, eps: float = 1e-5, act=None,
+              y: torch.Tensor | None = None, stats: bool = False, keep: Checkpoint | None = None, ws: Workspace | None = None):
+    """Group norm of a channels-last tensor [N]...[C] (a map [N][H][W][C], rows [N][C]) with an activation (None, "relu" or "silu") behind it; fp32
+    ``gamma`` and ``beta`` [C] or None.  Returns y (``y`` may be x), or with ``stats`` (y, mean, rstd), the statistics fp32 [N][groups] as the backward
+    pass reads them.  ``keep``: a ``Checkpoint.like(x)`` that x is written to as well, for the backward pass.  ``ws``: a ``Workspace.for_groupnorm``,
+    allocated here if it is not given.  A map in torch's channels_last format goes in as x.permute(0, 2, 3, 1)."""
+    N, P, Cc = _last_shape(x, "x")
+    dt, dev = _dt(x), _here(x)
+    pg, pb = _floats(gamma, Cc, dev, "gamma"), _floats(beta, Cc, dev, "beta")
+    if y is None:
+        y = torch.empty_like(x)
+        py = y.data_ptr()
+    else:
+        py = _same(y, x, dev, "y", "x")
+    pc = ps = mean = rstd = pm = pr = None
+    if keep is not None:
+        keep._fits(x)
+        pc, ps = keep.codes.data_ptr(), keep.scales.data_ptr()
+    if stats:
+        mean, rstd = x.new_empty((N, groups), dtype=torch.float32), x.new_empty((N, groups), dtype=torch.float32)
+        pm, pr = mean.data_ptr(), rstd.data_ptr()
+    if ws is None:
+        ws = Workspace(_groupnorm_bytes(N, P, Cc, groups, dt, False), x.device)
+    _check(lib().wcc_groupnorm_fwd(x.data_ptr(), pg, pb, N, P, Cc, groups, eps, _act(act), dt, py, pm, pr, pc, ps, ws.buf.data_ptr(), ws.nbytes,
+                                   _stream()), "wcc_groupnorm_fwd")
+    return (y, mean, rstd) if stats else y
+
+
+def groupnorm_backward(dy: torch.Tensor, x, mean: torch.Tensor, rstd: torch.Tensor, groups: int, gamma: torch.Tensor | None = None,
+                       beta: torch.Tensor | None = None, act=None, dx: torch.Tensor | None = None, params: bool = True, ws: Workspace | None = None):
+    """The gradients of ``groupnorm``: (dx, dgamma, dbeta), the last two fp32 [C] and None without ``params``.  ``x`` is the map or its ``Checkpoint``
+    (read as it is, 8 bits a value); ``act`` and ``beta`` are the forward pass's.  ``dx`` may be dy or x.  ``ws`` as for ``groupnorm``."""
+    N, P, Cc = _last_shape(dy, "dy")
+    dt, dev = _dt(dy), _here(dy)
+    pc = ps = px = None
+    if isinstance(x, Checkpoint):
+        x._fits(dy)
+        pc, ps = x.codes.data_ptr(), x.scales.data_ptr()
+    else:
+        px = _same(x, dy, dev, "x", "dy")
+    pg, pb = _floats(gamma, Cc, dev, "gamma"), _floats(beta, Cc, dev, "beta")
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd are those of the forward pass")
+    pm, pr = _floats(mean, groups, dev, "mean", N), _floats(rstd, groups, dev, "rstd", N)
+    if dx is None:
+        dx = torch.empty_like(dy)
+        pdx = dx.data_ptr()
+    else:
+        pdx = _same(dx, dy, dev, "dx", "dy")
+    dgamma = dbeta = pdg = pdb = None
+    if params:
+        dgamma, dbeta = dy.new_empty((Cc,), dtype=torch.float32), dy.new_empty((Cc,), dtype=torch.float32)
+        pdg, pdb = dgamma.data_ptr(), dbeta.data_ptr()
+    if ws is None:
+        ws = Workspace(_groupnorm_bytes(N, P, Cc, groups, dt, True), dy.device)
+    _check(lib().wcc_groupnorm_bwd(dy.data_ptr(), px, pc, ps, pg, pb, pm, pr, N, P, Cc, groups, _act(act), dt, pdx, pdg, pdb, ws.buf.data_ptr(),
+                                   ws.nbytes, _stream()), "wcc_groupnorm_bwd")
+    return dx, dgamma, dbeta
+
+
+def _gated_shape(x: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor):
+    """(rows, Cin, F, device) of the gated block's arguments."""
+    _dev(x, "x")
+    if x.dim() < 1 or x.numel() == 0 or x.dtype != torch.bfloat16:
+        raise TypeError("the gated block takes bfloat16 rows of channels")
+    dev, Cin = _here(x), x.shape[-1]
+    for t, name in ((Wg, "Wg"), (Wu, "Wu")):
+        if not (t.get_device() == dev and t.is_contiguous() and t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[1] == Cin and t.shape == Wg.shape):
+            raise ValueError("%s must be contiguous bfloat16 [F][Cin] on the device of x" % name)
+    return x.numel() // Cin, Cin, Wg.shape[0], dev
+
+
+def gated(x: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, act="silu", y: torch.Tensor | None = None) -> torch.Tensor:
+    """The gated pointwise block act(x Wg^T) * (x Wu^T) on bfloat16 rows of channels [...][Cin] (positions of a channels-last map, tokens); ``Wg`` and
+    ``Wu`` [F][Cin], Cin and F multiples of 8; ``act`` None, "relu", "silu" or "gelu".  Returns y [...][F]."""
+    rows, Cin, F, dev = _gated_shape(x, Wg, Wu)
+    shape = tuple(x.shape[:-1]) + (F,)
+    if y is None:
+        y = x.new_empty(shape)
+    elif not (y.get_device() == dev and y.is_contiguous() and y.dtype == x.dtype and tuple(y.shape) == shape):
+        raise ValueError("y must be contiguous bfloat16 %s on the device of x" % (list(shape),))
+    py = y.data_ptr()
+    if py in (x.data_ptr(), Wg.data_ptr(), Wu.data_ptr()):
+        raise ValueError("y must not be an input")
+    _check(lib().wcc_gated_fwd(x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), rows, Cin, F, _act(act), py, _stream()), "wcc_gated_fwd")
+    return y
+
+
+def gated_backward(dy: torch.Tensor, x, Wg: torch.Tensor, Wu: torch.Tensor, act="silu", dx: torch.Tensor | None = None, params: bool = True,
+                   ws: Workspace | None = None):
+    """The gradients of ``gated``: (dx, dWg, dWu), all bfloat16, the last two None without ``params``.  Nothing is needed of the forward pass but x, which
+    may be a ``Checkpoint`` (its values are brought back first).  ``ws``: a ``Workspace.for_gated_backward``, allocated here if it is not given."""
+    if isinstance(x, Checkpoint):
+        x = x.restore()
+    rows, Cin, F, dev = _gated_shape(x, Wg, Wu)
+    if not (dy.get_device() == dev and dy.is_contiguous() and dy.dtype == x.dtype and dy.shape == tuple(x.shape[:-1]) + (F,)):
+        raise ValueError("dy must be contiguous bfloat16 [...][F] with x's rows on its device")
+    if dx is None:
+        dx = torch.empty_like(x)
+        pdx = dx.data_ptr()
+    else:
+        pdx = _same(dx, x, dev, "dx", "x")
+        if pdx in (x.data_ptr(), dy.data_ptr()):
+            raise ValueError("dx must not be x or dy")
+    dWg = dWu = None
+    if params:
+        dWg, dWu = torch.empty_like(Wg), torch.empty_like(Wu)
+    if ws is None:
+        ws = Workspace.for_gated_backward(x, Wg)
+    _check(lib().wcc_gated_bwd(dy.data_ptr(), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), rows, Cin, F, _act(act), pdx, _ptr(dWg), _ptr(dWu),
+                               ws.buf.data_ptr(), ws.nbytes, _stream()), "wcc_gated_bwd")
+    return dx, dWg, dWu
 
 
 class Adapters:
@@ -579,7 +820,10 @@ class Adapters:
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None, dx: torch.Tensor | None = None,
                  params: bool = True, ws: Workspace | None = None):
-        """(dx, dA, dB): dx = base + the adapters' part of the map's gradient, dA and dB fp32 in the factors' shapes (None without ``params``)."""
+        """(dx, dA, dB): dx = base + the adapters' part of the map's gradient, dA and dB fp32 in the factors' shapes (None without ``params``).
+        ``x`` may be a ``Checkpoint`` of the map; its values are brought back first."""
+        if isinstance(x, Checkpoint):
+            x = x.restore()
         N, _, H, W = self._shape(x)
         dev, px = _here(x), x.data_ptr()
         pi, pdy, pb = self._ids(ids, N, dev), self._map(dy, x, self.Cout, dev, "dy"), self._map(base, x, self.Cin, dev, "base")
