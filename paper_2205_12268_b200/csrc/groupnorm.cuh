@@ -25,17 +25,35 @@ using namespace tr;
 
 constexpr int T = 256;                     // threads of a CTA
 constexpr int FAN = 16;                    // tiles whose channel sums are added up in one step
-constexpr int CTAS_FWD = 4, CTAS_BWD = 3;  // CTAs of an SM
+constexpr int CTAS_FWD = 3, CTAS_BWD = 2;  // CTAs of an SM
 constexpr size_t LAG_BYTES = (size_t)24 << 20;
+constexpr int RING_GAP = B200_SMS * 3 / 2;         // ring: tiles of sums in flight, about half of the CTAs'
 
 struct Plan {
     int V, p, lanes, reps, slots;          // period of p vectors; `reps` periods side by side, or one in `slots` turns of the CTA
     bool aligned;                          // all of a vector's channels are in one group
-    int tile, nt, supers;                  // positions of a tile, tiles of an image, steps of FAN tiles
+    bool ring;                             // groupnorm_ring.cuh; else the kernels of this file
+    int tile, nt, supers;                  // positions (ring: vectors) of a tile, tiles of an image, steps of FAN tiles
     int lag;                               // images between sums and result
-    int ctl;                               // words of control an image: arrivals of each step, of the steps, flag
+    // ring: a tile's result comes `delay` tiles behind its sums, an image's sums are finished by `fin` steps, `gap` tiles behind its last
+    int delay, gap, fin;
+    int copies;                            // ring: rows of C in a period
+    int ctl;                               // words of control an image: arrivals of each step, of the steps, flag (ring: arrivals of warps)
     bool solo;
 };
+
+// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(32 + s) / d) < 2^32 with 2^s < d <= 2^(s + 1)
+struct Divisor {
+    unsigned m, s, d;
+    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((unsigned)n, m) >> s); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+inline Divisor divisor_of(unsigned d)
+{
+    unsigned s = 0;
+    while ((2u << s) < d) ++s;             // 2^(s + 1) >= d
+    return {d == 1 ? 0u : (unsigned)(((1ull << (32 + s)) + d - 1) / d), s, d};
+}
 
 struct Args {
     const void *x, *dy;
@@ -51,6 +69,7 @@ struct Args {
     int N, P, C, G, D, nb, act;
     float eps, inv_count;
     bool params;
+    Divisor dC, dD, dW;                    // by C, D and the vectors (or values) of a group in a row
     Plan q;
     int* status;
 };
@@ -61,6 +80,38 @@ inline Plan plan_of(int N, int P, int C, int G, int es, bool backward, bool whol
 {
     Plan q{};
     const long long E = (long long)P * C;
+    const size_t bytes = (size_t)E * es * (backward ? 2 : 1);
+    const long long lag = (long long)((LAG_BYTES + bytes - 1) / bytes);
+    q.lag = (int)(lag < N ? lag : N);
+    // The ring takes whole 16-byte vectors whatever the channels, if the period fits the CTA and the image has tiles enough; a checkpoint's where rows
+    // start on 16 bytes of codes.
+    q.V = 16 / es;
+    q.p = C / gcd(C, q.V);
+    if (q.p <= T && (!whole_rows || C % 16 == 0) && E / q.V < (1LL << 30)) {
+        q.lanes = q.p;
+        q.reps = T / q.p;
+        q.slots = 1;
+        q.aligned = C % q.V == 0 && (C / G) % q.V == 0;
+        const long long nv = E / q.V, step = (long long)q.reps * q.p;
+        long long hi = 4096, lo = 512;
+        if (!backward) hi = 8192;
+        if (hi < 64LL * C / q.V) hi = 64LL * C / q.V;
+        long long t = N * nv / (B200_SMS * 8);
+        t = t < lo ? lo : t > hi ? hi : t;
+        if (t < (nv + 4095) / 4096) t = (nv + 4095) / 4096;
+        q.tile = (int)((t + step - 1) / step * step);
+        q.nt = (int)((nv + q.tile - 1) / q.tile);
+        q.ctl = 1;
+        q.copies = q.p * q.V / C;
+        q.ring = q.nt > 1;
+        const long long all = (long long)N * q.nt, gap = RING_GAP < all - q.nt ? RING_GAP : all - q.nt, delay = q.nt + gap + RING_GAP / 2;
+        q.gap = (int)gap;
+        q.delay = (int)(delay < all ? delay : all);
+        // an item's threads have all of their loads on the way at once: 4096 channels' sums, or 512 groups' statistics
+        const long long fin = backward ? (2LL * C * q.nt + 4095) / 4096 : ((long long)G * q.nt + 511) / 512;
+        q.fin = (int)(fin < G ? fin : G);
+        if (q.ring) return q;
+    }
     // Vectors of 16 bytes where every image starts on one and the period fits the CTA; else as wide as the rows' own alignment.  (A checkpoint's
     // scale is that of a row, so a vector must not go over a row's end.)
     q.V = 16 / es;
@@ -85,9 +136,6 @@ inline Plan plan_of(int N, int P, int C, int G, int es, bool backward, bool whol
     q.nt = (P + q.tile - 1) / q.tile;
     q.supers = (q.nt + FAN - 1) / FAN;
     q.solo = q.nt == 1;
-    const size_t bytes = (size_t)E * es * (backward ? 2 : 1);
-    const long long lag = (long long)((LAG_BYTES + bytes - 1) / bytes);
-    q.lag = (int)(lag < N ? lag : N);
     q.ctl = q.supers + 2;
     return q;
 }
@@ -105,10 +153,11 @@ inline Layout layout_of(const Plan& q, int N, int C, int G, bool backward)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 256); return a; };
     if (!q.solo) {
+        // (the words of control and the ring's coefficients start as zeros)
         l.ctl = take((1 + (size_t)N * q.ctl) * 4);
-        l.part = take((size_t)N * q.nt * (backward ? 2 * C : 2 * G) * 4);
-        if (backward) l.sup = take((size_t)N * q.supers * 2 * C * 4);
         l.coef = take((size_t)N * G * 8);
+        l.part = take((size_t)N * q.nt * (backward ? 2 * C : 3 * G) * 4);
+        if (backward && !q.ring) l.sup = take((size_t)N * q.supers * 2 * C * 4);
     }
     if (backward) l.img = take((size_t)(q.solo ? grid_of(q, N, B200_SMS, true) : N) * 2 * C * 4);
     l.total = at < 256 ? 256 : at;
@@ -163,12 +212,12 @@ __device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, 
         if (sub >= q.reps || vq >= q.p) continue;
         const int v0 = sub * q.p + vq;
         if constexpr (ALIGNED) {
-            float2 s = both(0.0f), ss = both(0.0f);
+            f2 s = both(0.0f), ss = both(0.0f);
             float s1 = 0.0f, ss1 = 0.0f, pivot = 0.0f;
             int k = 0;
             if (v0 < nvec) {
                 pivot = (float)x[(size_t)v0 * V];
-                const float2 neg = both(-pivot);
+                const f2 neg = both(-pivot);
 #pragma unroll 4
                 for (int v = v0; v < nvec; v += step, ++k) {
                     Vec<X, V> r;
@@ -182,14 +231,14 @@ __device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, 
                     } else {
 #pragma unroll
                         for (int e = 0; e < V; e += 2) {
-                            const float2 d = add2(make_float2(f[e], f[e + 1]), neg);
+                            const f2 d = add2(pair(f[e], f[e + 1]), neg);
                             s = add2(s, d);
                             ss = fma2(d, d, ss);
                         }
                     }
                 }
             }
-            const float n = (float)(k * V), sum = s.x + s.y + s1, sq = ss.x + ss.y + ss1, m = k ? __fdividef(sum, n) : 0.0f;
+            const float n = (float)(k * V), sum = s.x() + s.y() + s1, sq = ss.x() + ss.y() + ss1, m = k ? __fdividef(sum, n) : 0.0f;
             entries[v0] = {n, pivot + m, fmaxf(sq - sum * m, 0.0f)};
         } else {
             float s[V], ss[V], pivot[V];

@@ -5,6 +5,7 @@
 #include "common.cuh"
 #include "gated.cuh"
 #include "groupnorm.cuh"
+#include "groupnorm_ring.cuh"
 
 namespace wcc {
 
@@ -32,6 +33,9 @@ static gn::Args groupnorm_args(int N, int P, int C, int G, int act, const gn::Pl
     a.N = N; a.P = P; a.C = C; a.G = G; a.D = C / G; a.nb = ceil_div(C, ck::BLOCK); a.act = act;
     a.inv_count = (float)(1.0 / ((double)P * a.D));
     a.q = q;
+    a.dC = gn::divisor_of((unsigned)C);
+    a.dD = gn::divisor_of((unsigned)a.D);
+    a.dW = gn::divisor_of((unsigned)(q.aligned ? a.D / q.V : a.D));
     a.ctl = reinterpret_cast<unsigned*>(w + l.ctl);
     a.part = reinterpret_cast<float*>(w + l.part);
     a.sup = reinterpret_cast<float*>(w + l.sup);
@@ -105,6 +109,7 @@ wcc_status wcc_groupnorm_fwd(const void* x, const float* gamma, const float* bet
     a.x = x; a.out = y; a.gamma = gamma; a.beta = beta; a.mean_out = mean; a.rstd_out = rstd; a.eps = eps;
     if (codes && (s = wcc_checkpoint(x, (long long)N * P, C, dt, codes, scales, stream)) != WCC_OK) return s;
     if (!q.solo && (s = launch_clear(a.ctl, l.part - l.ctl, st)) != WCC_OK) return s;
+    if (q.ring) return dt == WCC_BF16 ? gn::ring_forward<__nv_bfloat16>(a, di, st) : gn::ring_forward<float>(a, di, st);
     return dt == WCC_BF16 ? gn::forward<__nv_bfloat16>(a, di, st) : gn::forward<float>(a, di, st);
 }
 
@@ -128,7 +133,8 @@ wcc_status wcc_groupnorm_bwd(const void* dy, const void* x, const int8_t* codes,
     const int grid = gn::grid_of(q, N, di.sms < B200_SMS ? di.sms : B200_SMS, true);
     a.img_beta = 0; a.img_gamma = C; a.img_row = 2LL * C;
     if (!q.solo && (s = launch_clear(a.ctl, l.part - l.ctl, st)) != WCC_OK) return s;
-    s = dt == WCC_BF16 ? gn::backward<__nv_bfloat16>(a, di, grid, st) : gn::backward<float>(a, di, grid, st);
+    if (q.ring) s = dt == WCC_BF16 ? gn::ring_backward<__nv_bfloat16>(a, di, st) : gn::ring_backward<float>(a, di, st);
+    else s = dt == WCC_BF16 ? gn::backward<__nv_bfloat16>(a, di, grid, st) : gn::backward<float>(a, di, grid, st);
     if (s != WCC_OK || !a.params) return s;
     return launch_overlapped(gn::reduce_kernel, dim3((unsigned)ceil_div(2 * C, 32)), dim3(256), 0, st, true, 1, a.img, q.solo ? grid : N, C, dgamma, dbeta);
 }

@@ -7,28 +7,37 @@ namespace wcc {
 namespace tr {
 
 // ---- two fp32 operations in one instruction ------------------------------------------------------
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
+// The pair is a 64-bit value throughout, so that it stays in neighbouring registers.
+struct f2 {
+    unsigned long long w;
+    __device__ __forceinline__ float x() const { return __uint_as_float((unsigned)w); }
+    __device__ __forceinline__ float y() const { return __uint_as_float((unsigned)(w >> 32)); }
+};
+__device__ __forceinline__ f2 pair(float x, float y)
 {
-    float2 r;
-    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.w) : "f"(x), "f"(y));
     return r;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
 {
-    float2 r;
-    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w));
     return r;
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
 {
-    float2 r;
-    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}"
-        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w));
     return r;
 }
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+    return r;
+}
 
 __device__ __forceinline__ float exp2_approx(float v)
 {
@@ -103,6 +112,48 @@ template <int V> __device__ __forceinline__ void pack(Vec<__nv_bfloat16, V>& v, 
 // ---- activations ---------------------------------------------------------------------------------
 // 1 / (1 + e^-z).  e^-z overflows to infinity below z = -88 and the result is 0, as it should be to fp32.
 __device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.0f + exp2_approx(-1.4426950408889634f * z)); }
+
+// Two at once with one reciprocal, 1/a = b / (a b): the unit of 2^x and of reciprocals gives 16 results a clock and SM and bounds the backward pass of
+// group norm with its four a value (three this way).  Below z = -43 the result stays e^-43 = 2e-19, so that a b does not overflow.
+__device__ __forceinline__ f2 sigmoid2(f2 z)
+{
+    const f2 v = mul2(pair(fmaxf(z.x(), -43.0f), fmaxf(z.y(), -43.0f)), both(-1.4426950408889634f));
+    const f2 a = add2(pair(exp2_approx(v.x()), exp2_approx(v.y())), both(1.0f));
+    return mul2(both(rcp_approx(a.x() * a.y())), pair(a.y(), a.x()));
+}
+
+// Values of a vector as pairs.
+template <int V> struct Pairs { f2 v[V / 2]; };
+
+__device__ __forceinline__ void unpack2(const uint4& w, Pairs<4>& f, float)
+{
+    f.v[0] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
+    f.v[1] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
+}
+__device__ __forceinline__ void unpack2(const uint4& w, Pairs<8>& f, __nv_bfloat16)
+{
+    f.v[0] = pair(bf16lo(w.x), bf16hi(w.x));
+    f.v[1] = pair(bf16lo(w.y), bf16hi(w.y));
+    f.v[2] = pair(bf16lo(w.z), bf16hi(w.z));
+    f.v[3] = pair(bf16lo(w.w), bf16hi(w.w));
+}
+__device__ __forceinline__ uint4 pack2(const Pairs<4>& f, float)
+{
+    return make_uint4((unsigned)f.v[0].w, (unsigned)(f.v[0].w >> 32), (unsigned)f.v[1].w, (unsigned)(f.v[1].w >> 32));
+}
+__device__ __forceinline__ uint4 pack2(const Pairs<8>& f, __nv_bfloat16)
+{
+    return make_uint4(pack_bf16x2(f.v[0].x(), f.v[0].y()), pack_bf16x2(f.v[1].x(), f.v[1].y()), pack_bf16x2(f.v[2].x(), f.v[2].y()),
+                      pack_bf16x2(f.v[3].x(), f.v[3].y()));
+}
+// Four int8 codes to fp32: with their sign bit flipped they are code + 128 in the low byte of 2^23, exact.
+__device__ __forceinline__ void codes4(uint32_t w, f2& a, f2& b)
+{
+    w ^= 0x80808080u;
+    const f2 off = both(-8388736.0f);
+    a = add2(pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540)), __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7541))), off);
+    b = add2(pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7542)), __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7543))), off);
+}
 
 }  // namespace tr
 }  // namespace wcc
