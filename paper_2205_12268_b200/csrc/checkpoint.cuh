@@ -26,93 +26,208 @@ __device__ __forceinline__ Scale scale_of(float top, bool bad)
 __device__ __forceinline__ int code_of(float x, float inv) { return __float2int_rn(x * inv); }
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u; }
 
-// One warp a block, lanes on neighbouring values: rows may start anywhere.
-template <typename T>
-__global__ void __launch_bounds__(256) pack_kernel(const T* __restrict__ x, long long rows, int L, int nb, int8_t* __restrict__ codes, float* __restrict__ scales)
+// Where block b lies: its row and its first column.  SMALL: rows * L < 2^31.
+template <bool SMALL> __device__ __forceinline__ void place(long long b, int nb, Divisor by_nb, long long& row, int& c0)
 {
+    row = SMALL ? (long long)by_nb.div((int)b) : b / nb;
+    c0 = (int)(b - row * nb) * BLOCK;
+}
+
+// Rows that start on 16 bytes: 16 bytes a lane, 16 (bf16) or 32 (fp32) lanes a block, fewer (LANES) where rows are shorter than a block, U blocks on the way at once.
+template <typename T, int LANES, bool SMALL>
+__global__ void __launch_bounds__(256, 5) pack_vectors(const T* __restrict__ x, long long blocks, int L, int nb, Divisor by_nb, int8_t* __restrict__ codes,
+                                                    float* __restrict__ scales)
+{
+    constexpr int V = 16 / (int)sizeof(T), EACH = 256 / LANES, U = 4;
+    pdl_wait();
+    pdl_launch();
+    const int lane = threadIdx.x % LANES, col = lane * V;
+    for (long long b0 = (long long)blockIdx.x * EACH * U + threadIdx.x / LANES; b0 - threadIdx.x / LANES < blocks; b0 += (long long)gridDim.x * EACH * U) {
+        Vec<T, V> r[U];
+        long long at[U];
+        bool on[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long b = b0 + u * EACH;
+            long long row = 0;
+            int c0 = 0;
+            if (b < blocks) place<SMALL>(b, nb, by_nb, row, c0);
+            on[u] = b < blocks && c0 + col < L;
+            at[u] = row * L + c0 + col;
+            if (on[u]) r[u].load(x + at[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[V], top = 0.0f;
+            if (on[u]) unpack(r[u], v);
+            unsigned bad = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (!on[u]) v[i] = 0.0f;
+                top = fmaxf(top, fabsf(v[i]));
+                bad |= not_finite(v[i]);
+            }
+            // a NaN among the values would be left out of the maximum: an infinity stands for it
+            if (bad) top = __int_as_float(0x7F800000);
+#pragma unroll
+            for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const Scale s = scale_of(top, not_finite(top));
+            if (on[u]) {
+                uint32_t q[V / 4];
+#pragma unroll
+                for (int i = 0; i < V; i += 4)
+                    q[i / 4] = __byte_perm(__byte_perm((uint32_t)code_of(v[i], s.inv), (uint32_t)code_of(v[i + 1], s.inv), 0x0040),
+                                           __byte_perm((uint32_t)code_of(v[i + 2], s.inv), (uint32_t)code_of(v[i + 3], s.inv), 0x0040), 0x5410);
+                if constexpr (V == 8) *reinterpret_cast<uint2*>(codes + at[u]) = make_uint2(q[0], q[1]);
+                else *reinterpret_cast<uint32_t*>(codes + at[u]) = q[0];
+                if (lane == 0) scales[b0 + u * EACH] = s.scale;
+            }
+        }
+    }
+}
+
+// Rows that start anywhere: a warp a block, lanes on neighbouring values, U blocks on the way at once.
+template <typename T, bool SMALL>
+__global__ void __launch_bounds__(256) pack_anywhere(const T* __restrict__ x, long long blocks, int L, int nb, Divisor by_nb, int8_t* __restrict__ codes,
+                                                     float* __restrict__ scales)
+{
+    constexpr int U = 3;
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x & 31;
-    const long long blocks = rows * nb, step = (long long)gridDim.x * 8;
-    for (long long b = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); b < blocks; b += step) {
-        const long long row = b / nb;
-        const int c0 = (int)(b - row * nb) * BLOCK, n = min(BLOCK, L - c0);
-        const T* p = x + row * L + c0;
-        float v[4], top = 0.0f;
-        bool bad = false;
+    for (long long b0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * U; b0 < blocks; b0 += (long long)gridDim.x * 8 * U) {
+        float v[U][4];
+        long long at[U];
+        int n[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = 0.0f;
-            if (lane + 32 * i < n) v[i] = (float)p[lane + 32 * i];
-            top = fmaxf(top, fabsf(v[i]));
-            bad |= not_finite(v[i]);
+        for (int u = 0; u < U; ++u) {
+            long long row = 0;
+            int c0 = 0;
+            n[u] = 0;
+            if (b0 + u < blocks) {
+                place<SMALL>(b0 + u, nb, by_nb, row, c0);
+                n[u] = min(BLOCK, L - c0);
+            }
+            at[u] = row * L + c0 + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] = lane + 32 * i < n[u] ? (float)x[at[u] + 32 * i] : 0.0f;
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        bad = __any_sync(0xFFFFFFFFu, bad);
-        const Scale s = scale_of(top, bad);
-        int8_t* q = codes + row * L + c0;
+        for (int u = 0; u < U; ++u) {
+            if (n[u] == 0) break;
+            float top = 0.0f;
+            bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < n) q[lane + 32 * i] = (int8_t)code_of(v[i], s.inv);
-        if (lane == 0) scales[b] = s.scale;
+            for (int i = 0; i < 4; ++i) {
+                top = fmaxf(top, fabsf(v[u][i]));
+                bad |= not_finite(v[u][i]);
+            }
+            if (bad) top = __int_as_float(0x7F800000);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const Scale s = scale_of(top, not_finite(top));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (lane + 32 * i < n[u]) codes[at[u] + 32 * i] = (int8_t)code_of(v[u][i], s.inv);
+            if (lane == 0) scales[b0 + u] = s.scale;
+        }
     }
 }
 
-// Sixteen neighbouring codes a thread, whatever the rows: codes and output are dense.
-template <typename T>
+// 16 bytes of output a thread, whatever the rows: codes and output are dense.  ROUND: a vector's values are of one block (L a multiple of V); else most often.
+template <typename T, bool SMALL, bool ROUND>
 __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales, long long total, int L, int nb,
-                                                      T* __restrict__ out)
+                                                      Divisor by_L, T* __restrict__ out)
 {
+    constexpr int V = 16 / (int)sizeof(T), U = 4;
     pdl_wait();
     pdl_launch();
-    constexpr int V = 16 / (int)sizeof(T);
-    const long long step = (long long)gridDim.x * 256 * 16;
-    for (long long f = ((long long)blockIdx.x * 256 + threadIdx.x) * 16; f < total; f += step) {
-        long long row = f / L;
-        int col = (int)(f - row * L);
-        if (f + 16 <= total) {
-            Vec<int8_t, 16> q;
-            q.load(codes + f);
-            float v[16];
-            unpack(q, v);
-            float s = __ldg(scales + row * nb + col / BLOCK);
+    const long long step = 256 * V;
+    for (long long f0 = (long long)blockIdx.x * step * U + threadIdx.x * V; f0 < total; f0 += (long long)gridDim.x * step * U) {
+        Vec<int8_t, V> q[U];
+        long long row[U];
+        int col[U];
+        float s[U];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] *= s;
-                ++col;
-                if (col == L) { col = 0; ++row; if (i < 15) s = __ldg(scales + row * nb); }
-                else if (col % BLOCK == 0 && i < 15) s = __ldg(scales + row * nb + col / BLOCK);
+        for (int u = 0; u < U; ++u) {
+            const long long f = f0 + u * step;
+            if (f < total) {
+                row[u] = SMALL ? (long long)by_L.div((int)f) : f / L;
+                col[u] = (int)(f - row[u] * L);
+                s[u] = __ldg(scales + row[u] * nb + col[u] / BLOCK);
+                if (f + V <= total) q[u].load(codes + f);
             }
+        }
 #pragma unroll
-            for (int i = 0; i < 16; i += V) {
-                float w[V];
+        for (int u = 0; u < U; ++u) {
+            const long long f = f0 + u * step;
+            if (f >= total) break;
+            if (f + V > total) {                           // the tensor's last few
+                for (int i = 0; i < (int)(total - f); ++i) {
+                    const long long r = (f + i) / L;
+                    out[f + i] = (T)((float)codes[f + i] * __ldg(scales + r * nb + (int)(f + i - r * L) / BLOCK));
+                }
+                break;
+            }
+            float v[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) w[j] = v[i + j];
-                Vec<T, V> o;
-                pack(o, w);
-                o.store(out + f + i);
+            for (int i = 0; i < V; i += 4) {
+                f2 a, b;
+                codes4(reinterpret_cast<const uint32_t*>(&q[u].r.w)[i / 4], a, b);
+                v[i] = a.x(); v[i + 1] = a.y(); v[i + 2] = b.x(); v[i + 3] = b.y();
             }
-        } else {
-            for (; f < total; ++f) {
-                row = f / L;
-                col = (int)(f - row * L);
-                out[f] = (T)((float)codes[f] * __ldg(scales + row * nb + col / BLOCK));
+            const int here = min(L - col[u], BLOCK - col[u] % BLOCK);      // values left of this block
+            if (ROUND || here >= V) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] *= s[u];
+            } else {
+                long long r = row[u];
+                int c = col[u], left = here;
+                float w = s[u];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    v[i] *= w;
+                    ++c;
+                    if (--left == 0 && i < V - 1) {
+                        if (c == L) { c = 0; ++r; }
+                        left = min(L - c, BLOCK);
+                        w = __ldg(scales + r * nb + c / BLOCK);
+                    }
+                }
             }
+            Vec<T, V> o;
+            pack(o, v);
+            o.store(out + f);
         }
     }
 }
 
+template <typename T, int LANES>
+wcc_status launch_pack(const T* x, long long blocks, int L, int nb, bool small, int8_t* codes, float* scales, const DeviceInfo& di, cudaStream_t st)
+{
+    const long long each = 4 * (256 / LANES), want = (blocks + each - 1) / each, most = (long long)di.sms * 10;
+    return launch_overlapped(small ? pack_vectors<T, LANES, true> : pack_vectors<T, LANES, false>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0,
+                             st, true, 1, x, blocks, L, nb, divisor_of((unsigned)nb), codes, scales);
+}
 template <typename T>
-wcc_status pack(const void* x, long long rows, int L, int8_t* codes, float* scales, cudaStream_t st)
+wcc_status pack(const void* in, long long rows, int L, int8_t* codes, float* scales, cudaStream_t st)
 {
     DeviceInfo di;
     const wcc_status s = device_info(di);
     if (s != WCC_OK) return s;
+    constexpr int FULL = BLOCK * (int)sizeof(T) / 16;
+    const T* x = static_cast<const T*>(in);
     const int nb = ceil_div(L, BLOCK);
-    const long long want = (rows * nb + 7) / 8, most = (long long)di.sms * 8;
-    return launch_overlapped(pack_kernel<T>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1, static_cast<const T*>(x), rows, L, nb,
-                             codes, scales);
+    const long long blocks = rows * nb;
+    const bool small = rows * L < (1LL << 31);
+    if ((long long)L * sizeof(T) % 16 == 0) {
+        if (L <= BLOCK / 4) return launch_pack<T, FULL / 4>(x, blocks, L, nb, small, codes, scales, di, st);
+        if (L <= BLOCK / 2) return launch_pack<T, FULL / 2>(x, blocks, L, nb, small, codes, scales, di, st);
+        return launch_pack<T, FULL>(x, blocks, L, nb, small, codes, scales, di, st);
+    }
+    const long long want = (blocks + 23) / 24, most = (long long)di.sms * 8;
+    return launch_overlapped(small ? pack_anywhere<T, true> : pack_anywhere<T, false>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1,
+                             x, blocks, L, nb, divisor_of((unsigned)nb), codes, scales);
 }
 template <typename T>
 wcc_status restore(const int8_t* codes, const float* scales, long long rows, int L, void* out, cudaStream_t st)
@@ -120,10 +235,13 @@ wcc_status restore(const int8_t* codes, const float* scales, long long rows, int
     DeviceInfo di;
     const wcc_status s = device_info(di);
     if (s != WCC_OK) return s;
+    constexpr int V = 16 / (int)sizeof(T);
     const int nb = ceil_div(L, BLOCK);
-    const long long total = rows * L, want = (total + 4095) / 4096, most = (long long)di.sms * 8;
-    return launch_overlapped(restore_kernel<T>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1, codes, scales, total, L, nb,
-                             static_cast<T*>(out));
+    const long long total = rows * L, want = (total + 1024 * V - 1) / (1024 * V), most = (long long)di.sms * 16;
+    const bool small = total < (1LL << 31), round = L % V == 0;
+    auto kernel = round ? (small ? restore_kernel<T, true, true> : restore_kernel<T, false, true>) : (small ? restore_kernel<T, true, false> : restore_kernel<T, false, false>);
+    return launch_overlapped(kernel, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1, codes, scales, total, L, nb,
+                             divisor_of((unsigned)L), static_cast<T*>(out));
 }
 
 }  // namespace ck

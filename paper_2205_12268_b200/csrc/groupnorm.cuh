@@ -42,19 +42,6 @@ struct Plan {
     bool solo;
 };
 
-// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(32 + s) / d) < 2^32 with 2^s < d <= 2^(s + 1)
-struct Divisor {
-    unsigned m, s, d;
-    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((unsigned)n, m) >> s); }
-    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
-};
-inline Divisor divisor_of(unsigned d)
-{
-    unsigned s = 0;
-    while ((2u << s) < d) ++s;             // 2^(s + 1) >= d
-    return {d == 1 ? 0u : (unsigned)(((1ull << (32 + s)) + d - 1) / d), s, d};
-}
-
 struct Args {
     const void *x, *dy;
     const int8_t* codes;                   // checkpoint of x, read (backward) ...

@@ -6,6 +6,20 @@
 namespace wcc {
 namespace tr {
 
+// ---- whole numbers -------------------------------------------------------------------------------
+// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(32 + s) / d) < 2^32 with 2^s < d <= 2^(s + 1)
+struct Divisor {
+    unsigned m, s, d;
+    __device__ __forceinline__ int div(int n) const { return d == 1 ? n : (int)(__umulhi((unsigned)n, m) >> s); }
+    __device__ __forceinline__ int mod(int n) const { return n - div(n) * (int)d; }
+};
+inline Divisor divisor_of(unsigned d)
+{
+    unsigned s = 0;
+    while ((2u << s) < d) ++s;             // 2^(s + 1) >= d
+    return {d == 1 ? 0u : (unsigned)(((1ull << (32 + s)) + d - 1) / d), s, d};
+}
+
 // ---- two fp32 operations in one instruction ------------------------------------------------------
 // The pair is a 64-bit value throughout, so that it stays in neighbouring registers.
 struct f2 {
