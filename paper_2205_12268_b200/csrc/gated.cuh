@@ -19,9 +19,7 @@ namespace wcc {
 namespace gt {
 
 using namespace tc;
-using tr::exp2_approx;
-using tr::rcp_approx;
-using tr::sigmoid;
+using namespace tr;
 
 enum Use { FORWARD, PARTS, DX, DW };
 
@@ -56,79 +54,91 @@ __device__ __forceinline__ uint64_t smem_desc_outer(uint32_t addr)
     return ((uint64_t)hi << 32) | lo;
 }
 
-// Value and derivative of the activation.
-// gelu: Phi by Abramowitz and Stegun 7.1.26 (erf to 1.5e-7 absolute: far below the result's rounding).
-struct Act { float a, d; };
-template <int ACT> __device__ __forceinline__ Act act_of(float z)
+// Value and derivative of the activation, two at a time.
+// gelu: Phi by Abramowitz and Stegun 7.1.26 (erf to 1.5e-7 absolute: far below the result's rounding), with one reciprocal for two; |z| beyond 42 is taken
+// as 42 in it (the exponential is 0 there), so that their product does not overflow.
+struct Act2 { f2 a, d; };
+template <int ACT, bool SLOPE> __device__ __forceinline__ Act2 act_of(f2 z)
 {
-    if constexpr (ACT == WCC_ACT_RELU) return {z < 0.0f ? 0.0f : z, z > 0.0f ? 1.0f : 0.0f};
+    const f2 one = both(1.0f);
+    if constexpr (ACT == WCC_ACT_RELU)
+        return {pair(z.x() < 0.0f ? 0.0f : z.x(), z.y() < 0.0f ? 0.0f : z.y()), pair(z.x() > 0.0f ? 1.0f : 0.0f, z.y() > 0.0f ? 1.0f : 0.0f)};
     if constexpr (ACT == WCC_ACT_SILU) {
-        const float s = sigmoid(z), a = z * s;
-        return {a, __fmaf_rn(a, 1.0f - s, s)};
+        const f2 s = sigmoid2(z), a = mul2(z, s);
+        return {a, SLOPE ? fma2(a, fma2(s, both(-1.0f), one), s) : one};
     }
     if constexpr (ACT == WCC_ACT_GELU) {
-        const float x = fabsf(z) * 0.70710678118654752f;
-        const float t = rcp_approx(__fmaf_rn(0.3275911f, x, 1.0f));
-        const float e = exp2_approx(z * z * -0.72134752044448170f);                // e^(-z^2 / 2)
-        float p = __fmaf_rn(1.061405429f, t, -1.453152027f);
-        p = __fmaf_rn(p, t, 1.421413741f);
-        p = __fmaf_rn(p, t, -0.284496736f);
-        p = __fmaf_rn(p, t, 0.254829592f);
-        const float h = 0.5f * p * t * e, phi = z < 0.0f ? h : 1.0f - h;
-        return {z * phi, __fmaf_rn(z * 0.39894228040143268f, e, phi)};
+        const f2 x = pair(fminf(fabsf(z.x()), 42.0f), fminf(fabsf(z.y()), 42.0f));
+        const f2 q = fma2(x, both(0.3275911f * 0.70710678118654752f), one);
+        const f2 t = mul2(both(rcp_approx(q.x() * q.y())), pair(q.y(), q.x()));
+        const f2 w = mul2(mul2(z, z), both(-0.72134752044448170f));                // e^(-z^2 / 2)
+        const f2 e = pair(exp2_approx(w.x()), exp2_approx(w.y()));
+        f2 p = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+        p = fma2(p, t, both(0.5f * 1.421413741f));
+        p = fma2(p, t, both(0.5f * -0.284496736f));
+        p = fma2(p, t, both(0.5f * 0.254829592f));
+        const f2 h = mul2(mul2(p, t), e), far = fma2(h, both(-1.0f), one);
+        const f2 phi = pair(z.x() < 0.0f ? h.x() : far.x(), z.y() < 0.0f ? h.y() : far.y());
+        return {mul2(z, phi), SLOPE ? fma2(mul2(z, both(0.39894228040143268f)), e, phi) : one};
     }
-    return {z, 1.0f};
+    return {z, one};
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&r)[16])
+// N columns of this warp's lanes; what is read is there after tmem_wait.
+template <int N> __device__ __forceinline__ void tmem_read(uint32_t taddr, uint32_t (&u)[N])
 {
-    uint32_t u[16];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
-                   "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-                 : "r"(taddr));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = __uint_as_float(u[i]);
+    if constexpr (N == 16)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+                       "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+                     : "r"(taddr));
+    else
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+                     "%28,%29,%30,%31}, [%32];"
+                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+                       "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]),
+                       "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+                     : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* f)
+// 16 bf16 values, those of the first `cols` columns (a multiple of 8).  A lane's row is far from its neighbours', so a store goes to 32 lines: a whole
+// 32-byte sector at once where the rows start on one.
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* w, int cols, bool sectors)
 {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float* f)
-{
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-    f[0] = bf16lo(w.x); f[1] = bf16hi(w.x); f[2] = bf16lo(w.y); f[3] = bf16hi(w.y);
-    f[4] = bf16lo(w.z); f[5] = bf16hi(w.z); f[6] = bf16lo(w.w); f[7] = bf16hi(w.w);
+    if (sectors && cols >= 16) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        if (cols > 0) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (cols > 8) *reinterpret_cast<uint4*>(p + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
 }
 
-// 16 columns of a gate and its partner: to y, or with dy to dG and dU.  `cols`: those inside the matrix (a multiple of 8).
-template <int USE, int ACT>
-__device__ __forceinline__ void gate16(const Args& a, const float (&g)[16], const float (&u)[16], size_t at, int cols)
+// N columns of gates and their partners: to y, or with dy (`d`, bf16 pairs) to dG and dU.
+template <int USE, int ACT, int N>
+__device__ __forceinline__ void gates_out(const Args& a, const uint32_t (&g)[N], const uint32_t (&u)[N], const uint32_t* d, size_t at, int cols, bool sectors)
 {
-    float o[16], o2[16], d[16];
-    if constexpr (USE == PARTS) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 8)
-            if (i < cols) load8(a.dy + at + i, d + i);
-    }
+    for (int c = 0; c < N; c += 16) {
+        uint32_t o[8], o2[8];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const Act v = act_of<ACT>(g[i]);
-        if constexpr (USE == FORWARD) {
-            o[i] = v.a * u[i];
-        } else {
-            o[i] = d[i] * u[i] * v.d;
-            o2[i] = d[i] * v.a;
+        for (int i = 0; i < 8; ++i) {
+            const int k = c + 2 * i;
+            const f2 z = pair(__uint_as_float(g[k]), __uint_as_float(g[k + 1])), w = pair(__uint_as_float(u[k]), __uint_as_float(u[k + 1]));
+            const Act2 v = act_of<ACT, USE == PARTS>(z);
+            if constexpr (USE == FORWARD) {
+                const f2 r = mul2(v.a, w);
+                o[i] = pack_bf16x2(r.x(), r.y());
+            } else {
+                const f2 t = pair(bf16lo(d[k / 2]), bf16hi(d[k / 2])), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
+                o[i] = pack_bf16x2(r.x(), r.y());
+                o2[i] = pack_bf16x2(r2.x(), r2.y());
+            }
         }
+        store16(a.y + at + c, o, cols - c, sectors);
+        if constexpr (USE == PARTS) store16(a.y2 + at + c, o2, cols - c, sectors);
     }
-#pragma unroll
-    for (int i = 0; i < 16; i += 8)
-        if (i < cols) {
-            store8(a.y + at + i, o + i);
-            if constexpr (USE == PARTS) store8(a.y2 + at + i, o2 + i);
-        }
 }
 
 template <int USE, int BN>
@@ -235,60 +245,66 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         __syncwarp();
     } else {
         const int q = warp & 3, half = (warp - 2) >> 2;        // lanes of tensor memory that the warp may read; its half of the columns
+        constexpr bool GATES = USE == FORWARD || USE == PARTS;
+        constexpr int MINE = GATES ? BN / 4 : BN / 2, N = MINE < 32 ? MINE : 32;   // columns of the warp, and those at once
+        const int width = GATES ? a.F : a.Cin, mhalf = a.m_tiles / 2;
+        const bool sectors = width % 16 == 0 && ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.y2)) & 31u) == 0;
         int item = 0;
         for (int w = blockIdx.x; w < items; w += gridDim.x, ++item) {
             const int nt = w % a.n_tiles, ms = w / a.n_tiles, mt = ms % a.m_tiles, sp = ms / a.m_tiles;
+            const bool up = USE == DW && mt >= mhalf;
+            const int row = (up ? mt - mhalf : mt) * BM + q * 32 + lane, col0 = nt * (GATES ? BN / 2 : BN) + half * MINE;
+            const bool on = row < (USE == DW ? a.F : a.rows);
+            const size_t at0 = (size_t)row * width + col0;
+            // dy does not wait for the products
+            uint32_t d[USE == PARTS ? MINE / 2 : 1];
+            if constexpr (USE == PARTS) {
+#pragma unroll
+                for (int i = 0; i < MINE; i += 8) {
+                    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                    if (on && col0 + i < width) v = __ldg(reinterpret_cast<const uint4*>(a.dy + at0 + i));
+                    d[i / 2] = v.x; d[i / 2 + 1] = v.y; d[i / 2 + 2] = v.z; d[i / 2 + 3] = v.w;
+                }
+            }
             const int buf = item & 1;
             const uint32_t bph = (uint32_t)(item >> 1) & 1u;
             int ok = mbar_wait(smem_u32(&ctl->tfull[buf]), bph, abort_flag) ? 1 : 0;
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) { failed = true; break; }
             fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN);
-            if constexpr (USE == FORWARD || USE == PARTS) {
-                const int row = mt * BM + q * 32 + lane;
-                for (int c = half * (BN / 4); c < (half + 1) * (BN / 4); c += 16) {
-                    const int col = nt * (BN / 2) + c;
-                    if (col >= a.F) break;                      // (the whole warp)
-                    float g[16], u[16];
-                    tmem_ld16(taddr + (uint32_t)c, g);
-                    tmem_ld16(taddr + (uint32_t)(BN / 2 + c), u);
-                    tmem_wait();
-                    if (row < a.rows) {
-                        const size_t at = (size_t)row * a.F + col;
-                        const int cols = a.F - col;
-                        if (a.act == WCC_ACT_SILU) gate16<USE, WCC_ACT_SILU>(a, g, u, at, cols);
-                        else if (a.act == WCC_ACT_GELU) gate16<USE, WCC_ACT_GELU>(a, g, u, at, cols);
-                        else if (a.act == WCC_ACT_RELU) gate16<USE, WCC_ACT_RELU>(a, g, u, at, cols);
-                        else gate16<USE, WCC_ACT_NONE>(a, g, u, at, cols);
-                    }
-                    __syncwarp();
-                }
-            } else {
-                const int mhalf = a.m_tiles / 2;
-                const bool up = USE == DW && mt >= mhalf;
-                const int row = (up ? mt - mhalf : mt) * BM + q * 32 + lane, limit = USE == DW ? a.F : a.rows;
-                for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 16) {
-                    const int col = nt * BN + c;
-                    if (col >= a.Cin) break;
-                    float v[16];
-                    tmem_ld16(taddr + (uint32_t)c, v);
-                    tmem_wait();
-                    if (row < limit) {
-                        if (USE == DW && a.splits > 1) {
-                            float* p = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col;
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * MINE);
 #pragma unroll
-                            for (int i = 0; i < 16; i += 4)
-                                if (col + i < a.Cin) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                        } else {
-                            __nv_bfloat16* p = (up ? a.y2 : a.y) + (size_t)row * a.Cin + col;
+            for (int c = 0; c < MINE; c += N) {
+                const int cols = width - col0 - c;
+                if (cols <= 0) break;                           // (the whole warp)
+                uint32_t v[N], p[GATES ? N : 1];
+                tmem_read<N>(taddr + (uint32_t)c, v);
+                if constexpr (GATES) tmem_read<N>(taddr + (uint32_t)(BN / 2 + c), p);
+                tmem_wait();
+                if (on) {
+                    const size_t at = at0 + c;
+                    if constexpr (GATES) {
+                        const uint32_t* dc = USE == PARTS ? d + c / 2 : d;
+                        if (a.act == WCC_ACT_SILU) gates_out<USE, WCC_ACT_SILU, N>(a, v, p, dc, at, cols, sectors);
+                        else if (a.act == WCC_ACT_GELU) gates_out<USE, WCC_ACT_GELU, N>(a, v, p, dc, at, cols, sectors);
+                        else if (a.act == WCC_ACT_RELU) gates_out<USE, WCC_ACT_RELU, N>(a, v, p, dc, at, cols, sectors);
+                        else gates_out<USE, WCC_ACT_NONE, N>(a, v, p, dc, at, cols, sectors);
+                    } else if (USE == DW && a.splits > 1) {
+                        float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c;
 #pragma unroll
-                            for (int i = 0; i < 16; i += 8)
-                                if (col + i < a.Cin) store8(p + i, v + i);
+                        for (int i = 0; i < N; i += 4)
+                            if (i < cols) *reinterpret_cast<uint4*>(o + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < N; i += 16) {
+                            uint32_t o[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) o[k] = pack_bf16x2(__uint_as_float(v[i + 2 * k]), __uint_as_float(v[i + 2 * k + 1]));
+                            store16((up ? a.y2 : a.y) + at + i, o, cols - i, sectors);
                         }
                     }
-                    __syncwarp();
                 }
+                __syncwarp();
             }
             fence_before();
             __syncwarp();
@@ -313,22 +329,24 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     }
 }
 
-// Partial sums of the weights' gradients, added in order, four values a thread.
-static __global__ void __launch_bounds__(256) add_parts(const float* __restrict__ part, int splits, size_t each, __nv_bfloat16* __restrict__ dWg,
+// Partial sums of the weights' gradients, added in order, two values a thread, sixteen parts on their way at once.
+static __global__ void __launch_bounds__(128) add_parts(const float* __restrict__ part, int splits, size_t each, __nv_bfloat16* __restrict__ dWg,
                                                         __nv_bfloat16* __restrict__ dWu)
 {
     pdl_wait();
     pdl_launch();
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    const size_t i = ((size_t)blockIdx.x * 128 + threadIdx.x) * 2;
     if (i >= 2 * each) return;
-    float4 v = __ldcg(reinterpret_cast<const float4*>(part + i));
-#pragma unroll 4
-    for (int s = 1; s < splits; ++s) {
-        const float4 p = __ldcg(reinterpret_cast<const float4*>(part + (size_t)s * 2 * each + i));
-        v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+    float2 v = make_float2(0.0f, 0.0f);
+    for (int s0 = 0; s0 < splits; s0 += 16) {
+        float2 p[16];
+#pragma unroll
+        for (int s = 0; s < 16; ++s) p[s] = s0 + s < splits ? __ldcg(reinterpret_cast<const float2*>(part + (size_t)(s0 + s) * 2 * each + i)) : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int s = 0; s < 16; ++s) { v.x += p[s].x; v.y += p[s].y; }
     }
     __nv_bfloat16* dst = i < each ? dWg + i : dWu + (i - each);
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+    *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(v.x, v.y);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -416,7 +434,7 @@ inline wcc_status dw(const void* dG, const void* dU, const void* x, Args a, cons
     else s = launch<DW, 64>(A0, A1, B, B, a, di, st);
     if (s != WCC_OK || p.splits == 1) return s;
     const size_t each = (size_t)a.F * a.Cin;
-    return launch_overlapped(add_parts, dim3((unsigned)((2 * each / 4 + 255) / 256)), dim3(256), 0, st, true, 1, a.part, p.splits, each, a.y, a.y2);
+    return launch_overlapped(add_parts, dim3((unsigned)((each + 127) / 128)), dim3(128), 0, st, true, 1, a.part, p.splits, each, a.y, a.y2);
 }
 
 struct Layout { size_t dG, dU, part, total; };
