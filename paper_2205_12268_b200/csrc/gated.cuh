@@ -9,6 +9,9 @@
 //            next to maps) are cut along the rows, partial sums in fp32 are added in order by a kernel of their own.
 // TMA (128-byte swizzle, no multicast) feeds a ring of stages, one thread issues the instructions, the accumulator is double-buffered, so the
 // epilogue of a tile runs under the products of the next one.  Sizes that are no multiples of a tile arrive as zeros from TMA.
+//
+// Tiles of 256 columns are the work of two CTAs on neighbouring SMs (cta_group::2): 128 rows each, and each brings in half of B for both, 32 KB a
+// step instead of 48.  What bounds the loop is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2): six steps instead of four.
 #pragma once
 
 #include "tcgen05.cuh"
@@ -23,11 +26,17 @@ using namespace tr;
 
 enum Use { FORWARD, PARTS, DX, DW };
 
-constexpr int BM = 128, KSTEP = 64, THREADS = 320;
+constexpr int BM = 128, KSTEP = 64;
 constexpr int A_BYTES = BM * KSTEP * 2;
 
-template <int BN> constexpr int STAGES_OF = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-template <int BN> constexpr int STAGE_BYTES_OF = A_BYTES + BN * KSTEP * 2;
+// Warps of the epilogue, four for each share of a tile's columns.  Its arithmetic depends on results of a few units with long ways, so two warps on an SM's quarter
+// issue in 42 of 100 cycles; four fill it (65536 x 256 -> 1024 with gelu: 88 us with eight warps).
+template <int BN> constexpr int SHARES = BN == 64 ? 2 : 4;
+template <int BN> constexpr int THREADS_OF = 64 + 128 * SHARES<BN>;
+template <int BN> constexpr bool PAIR = BN == 256;                     // two CTAs a tile
+template <int BN> constexpr int STAGES_OF = BN == 64 ? 8 : 6;
+template <int BN> constexpr int B_COLS = PAIR<BN> ? BN / 2 : BN;        // columns of B that a CTA brings in
+template <int BN> constexpr int STAGE_BYTES_OF = A_BYTES + B_COLS<BN> * KSTEP * 2;
 
 struct Ctl {
     uint64_t full[8], empty[8], tfull[2], tempty[2];
@@ -44,6 +53,62 @@ struct Args {
     float* part;                           // DW with splits > 1: [splits][2 F][Cin]
     int* status;
 };
+
+__device__ __forceinline__ uint32_t cta_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// Address of the pair's first CTA's copy of something in shared memory.
+__device__ __forceinline__ uint32_t of_first(uint32_t addr)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Bounded wait for a barrier that another CTA of the pair arrives at.
+__device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+{
+    const uint32_t limit = c_wait_limit;
+    for (uint32_t it = 0; it < limit; ++it) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+        if (ok) return true;
+        if (*abort_flag) return false;
+    }
+    return false;
+}
+// PAIR: bytes count at the first CTA's barrier.
+template <bool PR> __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar)
+{
+    if constexpr (PR)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(c0), "r"(c1), "r"(bar) : "memory");
+    else
+        tma_load_2d(dst, tm, c0, c1, bar);
+}
+template <bool PR> __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (PR)
+        asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        mma_ss<false>(d, a, b, idesc, accumulate);
+}
+// All products issued so far are done: arrive at this barrier (PAIR: of both CTAs).
+template <bool PR> __device__ __forceinline__ void commit(uint32_t bar)
+{
+    if constexpr (PR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        mma_commit(bar);
+}
 
 // Operand with the contraction outside: rows of 64 columns (128 bytes, swizzled), groups of 8 of the contraction 1024 bytes apart, the next 64 columns
 // KSTEP rows further on.
@@ -87,18 +152,11 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ Act2 act_of(f2 z)
 // N columns of this warp's lanes; what is read is there after tmem_wait.
 template <int N> __device__ __forceinline__ void tmem_read(uint32_t taddr, uint32_t (&u)[N])
 {
-    if constexpr (N == 16)
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
-                       "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
-                     : "r"(taddr));
-    else
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
-                     "%28,%29,%30,%31}, [%32];"
-                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
-                       "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]),
-                       "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
-                     : "r"(taddr));
+    static_assert(N == 16, "");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]),
+                   "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15])
+                 : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -142,11 +200,12 @@ __device__ __forceinline__ void gates_out(const Args& a, const uint32_t (&g)[N],
 }
 
 template <int USE, int BN>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(THREADS_OF<BN>, 1)
 contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtensorMap tA1, const __grid_constant__ CUtensorMap tB0,
          const __grid_constant__ CUtensorMap tB1, const __grid_constant__ Args a)
 {
-    constexpr int ST = STAGES_OF<BN>, SB = STAGE_BYTES_OF<BN>, COLS = 2 * BN;
+    constexpr int ST = STAGES_OF<BN>, SB = STAGE_BYTES_OF<BN>, COLS = 2 * BN, BC = B_COLS<BN>;
+    constexpr bool PR = PAIR<BN>;
     constexpr bool A_OUTER = USE == DW, B_OUTER = USE == DX || USE == DW;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -154,22 +213,31 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     volatile int* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int items = a.m_tiles * a.n_tiles * a.splits;
+    // PAIR: both CTAs go through the same items, each with its half of the rows and of B
+    const int rank = PR ? (int)cta_rank() : 0, worker = PR ? blockIdx.x / 2 : blockIdx.x, workers = PR ? gridDim.x / 2 : gridDim.x;
+    constexpr int TM = PR ? 2 * BM : BM;                       // rows of a tile
     // steps of the ring for an item: along the channels, along F twice, along the rows
     const int f_steps = (a.F + KSTEP - 1) / KSTEP, row_steps = (a.rows + KSTEP - 1) / KSTEP;
     const int all_steps = USE == DX ? 2 * f_steps : USE == DW ? row_steps : (a.Cin + KSTEP - 1) / KSTEP;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < ST; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tfull[b]), 1); mbar_init(smem_u32(&ctl->tempty[b]), 8); }
+        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tfull[b]), 1); mbar_init(smem_u32(&ctl->tempty[b]), (PR ? 8 : 4) * SHARES<BN>); }
         ctl->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"((uint32_t)COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (PR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"((uint32_t)COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"((uint32_t)COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     fence_before();
     __syncthreads();
+    if constexpr (PR) cluster_sync();                          // the other CTA's barriers are ready
     fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
     bool failed = false;
@@ -180,80 +248,84 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     if (warp == 0) {
         if (lane == 0) {
             int it = 0;
-            for (int w = blockIdx.x; w < items && !failed; w += gridDim.x) {
+            for (int w = worker; w < items && !failed; w += workers) {
                 const int nt = w % a.n_tiles, ms = w / a.n_tiles, mt = ms % a.m_tiles, sp = ms / a.m_tiles;
                 const int k0 = (int)((long long)all_steps * sp / a.splits), k1 = (int)((long long)all_steps * (sp + 1) / a.splits);
                 for (int k = k0; k < k1; ++k, ++it) {
                     const int s = it % ST;
                     const uint32_t ph = (uint32_t)(it / ST) & 1u;
                     if (!mbar_wait(smem_u32(&ctl->empty[s]), ph ^ 1u, abort_flag)) { failed = true; break; }
-                    const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES, bar = smem_u32(&ctl->full[s]);
-                    mbar_expect_tx(bar, (uint32_t)SB);
+                    const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES, own = smem_u32(&ctl->full[s]), bar = PR ? of_first(own) : own;
+                    if (rank == 0) mbar_expect_tx(own, (uint32_t)(PR ? 2 * SB : SB));
                     if constexpr (USE == FORWARD || USE == PARTS) {
-                        tma_load_2d(sA, &tA0, k * KSTEP, mt * BM, bar);
-                        tma_load_2d(sB, &tB0, k * KSTEP, nt * (BN / 2), bar);
-                        tma_load_2d(sB + BN / 2 * 128, &tB1, k * KSTEP, nt * (BN / 2), bar);
+                        load_tile<PR>(sA, &tA0, k * KSTEP, mt * TM + rank * BM, bar);
+                        if constexpr (PR) {                    // one CTA the gates' columns, the other their partners'
+                            load_tile<PR>(sB, rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
+                        } else {
+                            load_tile<PR>(sB, &tB0, k * KSTEP, nt * (BN / 2), bar);
+                            load_tile<PR>(sB + BN / 2 * 128, &tB1, k * KSTEP, nt * (BN / 2), bar);
+                        }
                     } else if constexpr (USE == DX) {
                         const bool up = k >= f_steps;
                         const int f0 = (up ? k - f_steps : k) * KSTEP;
-                        tma_load_2d(sA, up ? &tA1 : &tA0, f0, mt * BM, bar);
-                        for (int i = 0; i < BN / 64; ++i) tma_load_2d(sB + i * KSTEP * 128, up ? &tB1 : &tB0, nt * BN + 64 * i, f0, bar);
+                        load_tile<PR>(sA, up ? &tA1 : &tA0, f0, mt * TM + rank * BM, bar);
+                        for (int i = 0; i < BC / 64; ++i) load_tile<PR>(sB + i * KSTEP * 128, up ? &tB1 : &tB0, nt * BN + rank * BC + 64 * i, f0, bar);
                     } else {
-                        const int half = a.m_tiles / 2;
-                        const bool up = mt >= half;
-                        const int f0 = (up ? mt - half : mt) * BM;
-                        for (int i = 0; i < 2; ++i) tma_load_2d(sA + i * KSTEP * 128, up ? &tA1 : &tA0, f0 + 64 * i, k * KSTEP, bar);
-                        for (int i = 0; i < BN / 64; ++i) tma_load_2d(sB + i * KSTEP * 128, &tB0, nt * BN + 64 * i, k * KSTEP, bar);
+                        const int mhalf = a.m_tiles / 2;
+                        const bool up = mt >= mhalf;
+                        const int f0 = (up ? mt - mhalf : mt) * TM + rank * BM;
+                        for (int i = 0; i < 2; ++i) load_tile<PR>(sA + i * KSTEP * 128, up ? &tA1 : &tA0, f0 + 64 * i, k * KSTEP, bar);
+                        for (int i = 0; i < BC / 64; ++i) load_tile<PR>(sB + i * KSTEP * 128, &tB0, nt * BN + rank * BC + 64 * i, k * KSTEP, bar);
                     }
                 }
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             // D fp32, A and B bf16; bits 15 and 16: the contraction lies outside
             constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_OUTER ? 1u : 0u) << 15) | ((B_OUTER ? 1u : 0u) << 16) |
-                                       ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+                                       ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
             int it = 0, item = 0;
-            for (int w = blockIdx.x; w < items && !failed; w += gridDim.x, ++item) {
+            for (int w = worker; w < items && !failed; w += workers, ++item) {
                 const int sp = w / a.n_tiles / a.m_tiles;
                 const int k0 = (int)((long long)all_steps * sp / a.splits), k1 = (int)((long long)all_steps * (sp + 1) / a.splits);
                 const int buf = item & 1;
                 const uint32_t bph = (uint32_t)(item >> 1) & 1u;
-                if (!mbar_wait(smem_u32(&ctl->tempty[buf]), bph ^ 1u, abort_flag)) { failed = true; break; }
+                if (!(PR ? wait_cluster(smem_u32(&ctl->tempty[buf]), bph ^ 1u, abort_flag) : mbar_wait(smem_u32(&ctl->tempty[buf]), bph ^ 1u, abort_flag))) { failed = true; break; }
                 fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(buf * BN);
                 uint32_t accumulate = 0;
                 for (int k = k0; k < k1; ++k, ++it) {
                     const int s = it % ST;
                     const uint32_t ph = (uint32_t)(it / ST) & 1u;
-                    if (!mbar_wait(smem_u32(&ctl->full[s]), ph, abort_flag)) { failed = true; break; }
+                    if (!(PR ? wait_cluster(smem_u32(&ctl->full[s]), ph, abort_flag) : mbar_wait(smem_u32(&ctl->full[s]), ph, abort_flag))) { failed = true; break; }
                     fence_after();
                     const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES;
                     const uint64_t ad = A_OUTER ? smem_desc_outer(sA) : smem_desc_sw128(sA), bd = B_OUTER ? smem_desc_outer(sB) : smem_desc_sw128(sB);
 #pragma unroll
                     for (int kk = 0; kk < KSTEP / 16; ++kk) {      // 16 of the contraction: 32 bytes of a row, or 16 rows of 128 bytes
-                        mma_ss<false>(d, ad + (uint64_t)((A_OUTER ? 128 : 2) * kk), bd + (uint64_t)((B_OUTER ? 128 : 2) * kk), idesc, accumulate);
+                        multiply<PR>(d, ad + (uint64_t)((A_OUTER ? 128 : 2) * kk), bd + (uint64_t)((B_OUTER ? 128 : 2) * kk), idesc, accumulate);
                         accumulate = 1;
                     }
-                    mma_commit(smem_u32(&ctl->empty[s]));
+                    commit<PR>(smem_u32(&ctl->empty[s]));
                 }
                 if (failed) break;
-                mma_commit(smem_u32(&ctl->tfull[buf]));
+                commit<PR>(smem_u32(&ctl->tfull[buf]));
             }
         }
         __syncwarp();
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;        // lanes of tensor memory that the warp may read; its half of the columns
+        const int q = warp & 3, share = (warp - 2) >> 2;       // lanes of tensor memory that the warp may read; its share of the columns
         constexpr bool GATES = USE == FORWARD || USE == PARTS;
-        constexpr int MINE = GATES ? BN / 4 : BN / 2, N = MINE < 32 ? MINE : 32;   // columns of the warp, and those at once
+        constexpr int MINE = (GATES ? BN / 2 : BN) / SHARES<BN>, N = 16;         // columns of the warp, and those at once
         const int width = GATES ? a.F : a.Cin, mhalf = a.m_tiles / 2;
         const bool sectors = width % 16 == 0 && ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.y2)) & 31u) == 0;
         int item = 0;
-        for (int w = blockIdx.x; w < items; w += gridDim.x, ++item) {
+        for (int w = worker; w < items; w += workers, ++item) {
             const int nt = w % a.n_tiles, ms = w / a.n_tiles, mt = ms % a.m_tiles, sp = ms / a.m_tiles;
             const bool up = USE == DW && mt >= mhalf;
-            const int row = (up ? mt - mhalf : mt) * BM + q * 32 + lane, col0 = nt * (GATES ? BN / 2 : BN) + half * MINE;
+            const int row = (up ? mt - mhalf : mt) * TM + rank * BM + q * 32 + lane, col0 = nt * (GATES ? BN / 2 : BN) + share * MINE;
             const bool on = row < (USE == DW ? a.F : a.rows);
             const size_t at0 = (size_t)row * width + col0;
             // dy does not wait for the products
@@ -272,7 +344,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) { failed = true; break; }
             fence_after();
-            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * MINE);
+            const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + share * MINE);
 #pragma unroll
             for (int c = 0; c < MINE; c += N) {
                 const int cols = width - col0 - c;
@@ -308,7 +380,10 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl->tempty[buf]));
+            if (lane == 0) {
+                if constexpr (PR) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(of_first(smem_u32(&ctl->tempty[buf]))) : "memory");
+                else mbar_arrive(smem_u32(&ctl->tempty[buf]));
+            }
         }
     }
 
@@ -323,9 +398,11 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);
         __syncthreads();
     }
+    if constexpr (PR) cluster_sync();                          // the other CTA arrives at this one's barriers no more
     if (warp == 1) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)COLS) : "memory");
+        if constexpr (PR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)COLS) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)COLS) : "memory");
     }
 }
 
@@ -368,7 +445,8 @@ wcc_status launch(const CUtensorMap& A0, const CUtensorMap& A1, const CUtensorMa
     const wcc_status s = allow_smem<contract<USE, BN>>(di.dev, smem);
     if (s != WCC_OK) return s;
     const int items = a.m_tiles * a.n_tiles * a.splits;
-    return launch_overlapped(contract<USE, BN>, dim3((unsigned)(items < di.sms ? items : di.sms)), dim3(THREADS), smem, st, true, 1, A0, A1, B0, B1, a);
+    const int workers = PAIR<BN> ? di.sms / 2 : di.sms, grid = (items < workers ? items : workers) * (PAIR<BN> ? 2 : 1);
+    return launch_overlapped(contract<USE, BN>, dim3((unsigned)grid), dim3(THREADS_OF<BN>), smem, st, true, PAIR<BN> ? 2 : 1, A0, A1, B0, B1, a);
 }
 
 // Columns of a tile: as many as fill the SMs, 64 at least.  `cols` columns in all (FORWARD: gates and partners).
@@ -382,8 +460,8 @@ inline int tile_of(int m_tiles, long long cols, int sms)
 template <int USE>
 wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const DeviceInfo& di, cudaStream_t st)
 {
-    a.m_tiles = ceil_div(a.rows, BM);
-    const int bn = tile_of(a.m_tiles, 2LL * a.F, di.sms);
+    const int bn = tile_of(ceil_div(a.rows, BM), 2LL * a.F, di.sms);
+    a.m_tiles = ceil_div(a.rows, bn == 256 ? 2 * BM : BM);
     a.n_tiles = ceil_div(a.F, bn / 2);
     a.splits = 1;
     CUtensorMap A, G, U;
@@ -395,8 +473,8 @@ wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const De
 
 inline wcc_status dx(const void* dG, const void* dU, const void* Wg, const void* Wu, Args a, const DeviceInfo& di, cudaStream_t st)
 {
-    a.m_tiles = ceil_div(a.rows, BM);
-    const int bn = tile_of(a.m_tiles, a.Cin, di.sms);
+    const int bn = tile_of(ceil_div(a.rows, BM), a.Cin, di.sms);
+    a.m_tiles = ceil_div(a.rows, bn == 256 ? 2 * BM : BM);
     a.n_tiles = ceil_div(a.Cin, bn);
     a.splits = 1;
     CUtensorMap A0, A1, B0, B1;
@@ -412,7 +490,9 @@ inline DwPlan dw_plan(int rows, int Cin, int F, int sms)
 {
     DwPlan p;
     p.bn = Cin > 128 ? 256 : Cin > 64 ? 128 : 64;
-    p.m_tiles = 2 * ceil_div(F, BM);
+    if (p.bn == 256 && F <= BM) p.bn = 128;                    // half a tile of two CTAs would be empty
+    if (p.bn == 256) sms /= 2;
+    p.m_tiles = 2 * ceil_div(F, p.bn == 256 ? 2 * BM : BM);
     p.n_tiles = ceil_div(Cin, p.bn);
     const long long tiles = (long long)p.m_tiles * p.n_tiles;
     const int steps = ceil_div(rows, KSTEP);
