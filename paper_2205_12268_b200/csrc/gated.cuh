@@ -12,6 +12,7 @@
 //
 // Tiles of 256 columns are the work of two CTAs on neighbouring SMs (cta_group::2): 128 rows each, and each brings in half of B for both, 32 KB a
 // step instead of 48.  What bounds the loop is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2): six steps instead of four.
+// With up to 256 channels the weights of a column tile stay in shared memory (HOLD) while a pair goes through the row tiles, and the ring holds rows alone.
 #pragma once
 
 #include "tcgen05.cuh"
@@ -37,9 +38,10 @@ template <int BN> constexpr bool PAIR = BN == 256;                     // two CT
 template <int BN> constexpr int STAGES_OF = BN == 64 ? 8 : 6;
 template <int BN> constexpr int B_COLS = PAIR<BN> ? BN / 2 : BN;        // columns of B that a CTA brings in
 template <int BN> constexpr int STAGE_BYTES_OF = A_BYTES + B_COLS<BN> * KSTEP * 2;
+constexpr int HOLD_STEPS = 4, HOLD_STAGES = 8;                          // HOLD: steps of weights that stay, stages of rows
 
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2];
+    uint64_t full[8], empty[8], tfull[2], tempty[2], bfull, bempty;
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -199,23 +201,40 @@ __device__ __forceinline__ void gates_out(const Args& a, const uint32_t (&g)[N],
     }
 }
 
-template <int USE, int BN>
+template <int USE, int BN, bool HOLD>
 __global__ void __launch_bounds__(THREADS_OF<BN>, 1)
 contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtensorMap tA1, const __grid_constant__ CUtensorMap tB0,
          const __grid_constant__ CUtensorMap tB1, const __grid_constant__ Args a)
 {
-    constexpr int ST = STAGES_OF<BN>, SB = STAGE_BYTES_OF<BN>, COLS = 2 * BN, BC = B_COLS<BN>;
+    constexpr int ST = HOLD ? HOLD_STAGES : STAGES_OF<BN>, SB = HOLD ? A_BYTES : STAGE_BYTES_OF<BN>, COLS = 2 * BN, BC = B_COLS<BN>;
+    constexpr int HELD = HOLD ? HOLD_STEPS * BC * KSTEP * 2 : 0;
+    static_assert(!HOLD || (BN == 256 && (USE == FORWARD || USE == PARTS)), "");
     constexpr bool PR = PAIR<BN>;
     constexpr bool A_OUTER = USE == DW, B_OUTER = USE == DX || USE == DW;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + (size_t)ST * SB);
+    Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + (size_t)ST * SB + HELD);
     volatile int* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int items = a.m_tiles * a.n_tiles * a.splits;
     // PAIR: both CTAs go through the same items, each with its half of the rows and of B
     const int rank = PR ? (int)cta_rank() : 0, worker = PR ? blockIdx.x / 2 : blockIdx.x, workers = PR ? gridDim.x / 2 : gridDim.x;
     constexpr int TM = PR ? 2 * BM : BM;                       // rows of a tile
+    // Items: HOLD: a stretch of them, row tiles within a column tile; else every workers'th, column tiles within a row tile within a part of the rows.
+    const int w_first = HOLD ? (int)((long long)items * worker / workers) : worker, w_end = HOLD ? (int)((long long)items * (worker + 1) / workers) : items;
+    const int w_step = HOLD ? 1 : workers;
+    auto place = [&](int w, int& nt, int& mt, int& sp) {
+        if constexpr (HOLD) {
+            nt = w / a.m_tiles;
+            mt = w - nt * a.m_tiles;
+            sp = 0;
+        } else {
+            const int ms = w / a.n_tiles;
+            nt = w - ms * a.n_tiles;
+            sp = ms / a.m_tiles;
+            mt = ms - sp * a.m_tiles;
+        }
+    };
     // steps of the ring for an item: along the channels, along F twice, along the rows
     const int f_steps = (a.F + KSTEP - 1) / KSTEP, row_steps = (a.rows + KSTEP - 1) / KSTEP;
     const int all_steps = USE == DX ? 2 * f_steps : USE == DW ? row_steps : (a.Cin + KSTEP - 1) / KSTEP;
@@ -223,6 +242,8 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     if (threadIdx.x == 0) {
         for (int s = 0; s < ST; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tfull[b]), 1); mbar_init(smem_u32(&ctl->tempty[b]), (PR ? 8 : 4) * SHARES<BN>); }
+        mbar_init(smem_u32(&ctl->bfull), 1);
+        mbar_init(smem_u32(&ctl->bempty), 1);
         ctl->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -244,22 +265,31 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     pdl_wait();
     pdl_launch();
 
-    // item = (split * m_tiles + m) * n_tiles + n
     if (warp == 0) {
         if (lane == 0) {
-            int it = 0;
-            for (int w = worker; w < items && !failed; w += workers) {
-                const int nt = w % a.n_tiles, ms = w / a.n_tiles, mt = ms % a.m_tiles, sp = ms / a.m_tiles;
+            int s = 0, held = -1, swaps = 0;                   // column tile whose weights are here, times that they were brought in
+            uint32_t ph = 1;
+            for (int w = w_first; w < w_end && !failed; w += w_step) {
+                int nt, mt, sp;
+                place(w, nt, mt, sp);
+                if (HOLD && nt != held) {
+                    if (!mbar_wait(smem_u32(&ctl->bempty), (uint32_t)(swaps & 1) ^ 1u, abort_flag)) { failed = true; break; }
+                    const uint32_t bar = of_first(smem_u32(&ctl->bfull));
+                    if (rank == 0) mbar_expect_tx(smem_u32(&ctl->bfull), (uint32_t)(2 * all_steps * BC * KSTEP * 2));
+                    for (int k = 0; k < all_steps; ++k)
+                        load_tile<PR>(base + ST * SB + k * (BC * KSTEP * 2), rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
+                    held = nt;
+                    ++swaps;
+                }
                 const int k0 = (int)((long long)all_steps * sp / a.splits), k1 = (int)((long long)all_steps * (sp + 1) / a.splits);
-                for (int k = k0; k < k1; ++k, ++it) {
-                    const int s = it % ST;
-                    const uint32_t ph = (uint32_t)(it / ST) & 1u;
-                    if (!mbar_wait(smem_u32(&ctl->empty[s]), ph ^ 1u, abort_flag)) { failed = true; break; }
+                for (int k = k0; k < k1; ++k) {
+                    if (!mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag)) { failed = true; break; }
                     const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES, own = smem_u32(&ctl->full[s]), bar = PR ? of_first(own) : own;
                     if (rank == 0) mbar_expect_tx(own, (uint32_t)(PR ? 2 * SB : SB));
                     if constexpr (USE == FORWARD || USE == PARTS) {
                         load_tile<PR>(sA, &tA0, k * KSTEP, mt * TM + rank * BM, bar);
-                        if constexpr (PR) {                    // one CTA the gates' columns, the other their partners'
+                        if constexpr (HOLD) {
+                        } else if constexpr (PR) {             // one CTA the gates' columns, the other their partners'
                             load_tile<PR>(sB, rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
                         } else {
                             load_tile<PR>(sB, &tB0, k * KSTEP, nt * (BN / 2), bar);
@@ -277,6 +307,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                         for (int i = 0; i < 2; ++i) load_tile<PR>(sA + i * KSTEP * 128, up ? &tA1 : &tA0, f0 + 64 * i, k * KSTEP, bar);
                         for (int i = 0; i < BC / 64; ++i) load_tile<PR>(sB + i * KSTEP * 128, &tB0, nt * BN + rank * BC + 64 * i, k * KSTEP, bar);
                     }
+                    if (++s == ST) { s = 0; ph ^= 1u; }
                 }
             }
         }
@@ -286,9 +317,21 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
             // D fp32, A and B bf16; bits 15 and 16: the contraction lies outside
             constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_OUTER ? 1u : 0u) << 15) | ((B_OUTER ? 1u : 0u) << 16) |
                                        ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
-            int it = 0, item = 0;
-            for (int w = worker; w < items && !failed; w += workers, ++item) {
-                const int sp = w / a.n_tiles / a.m_tiles;
+            // (this thread issues next to the epilogue's warps: little more than the instructions themselves stands in its loop)
+            int s = 0, item = 0, held = -1, swaps = 0;
+            uint32_t ph = 0;
+            const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
+            const uint64_t a0 = A_OUTER ? smem_desc_outer(base) : smem_desc_sw128(base);
+            const uint64_t b0 = HOLD ? smem_desc_sw128(base + ST * SB) : B_OUTER ? smem_desc_outer(base + A_BYTES) : smem_desc_sw128(base + A_BYTES);
+            for (int w = w_first; w < w_end && !failed; w += w_step, ++item) {
+                int nt, mt, sp;
+                place(w, nt, mt, sp);
+                if (HOLD && nt != held) {
+                    if (held >= 0) commit<PR>(smem_u32(&ctl->bempty));         // the products with the old weights are done: they may go
+                    if (!wait_cluster(smem_u32(&ctl->bfull), (uint32_t)(swaps & 1), abort_flag)) { failed = true; break; }
+                    held = nt;
+                    ++swaps;
+                }
                 const int k0 = (int)((long long)all_steps * sp / a.splits), k1 = (int)((long long)all_steps * (sp + 1) / a.splits);
                 const int buf = item & 1;
                 const uint32_t bph = (uint32_t)(item >> 1) & 1u;
@@ -296,19 +339,21 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(buf * BN);
                 uint32_t accumulate = 0;
-                for (int k = k0; k < k1; ++k, ++it) {
-                    const int s = it % ST;
-                    const uint32_t ph = (uint32_t)(it / ST) & 1u;
-                    if (!(PR ? wait_cluster(smem_u32(&ctl->full[s]), ph, abort_flag) : mbar_wait(smem_u32(&ctl->full[s]), ph, abort_flag))) { failed = true; break; }
+                uint64_t bd = b0;
+#pragma unroll 2
+                for (int k = k0; k < k1; ++k) {
+                    if (!(PR ? wait_cluster(full0 + 8 * s, ph, abort_flag) : mbar_wait(full0 + 8 * s, ph, abort_flag))) { failed = true; break; }
                     fence_after();
-                    const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES;
-                    const uint64_t ad = A_OUTER ? smem_desc_outer(sA) : smem_desc_sw128(sA), bd = B_OUTER ? smem_desc_outer(sB) : smem_desc_sw128(sB);
+                    const uint64_t ad = a0 + (uint64_t)(s * (SB >> 4));
+                    if constexpr (!HOLD) bd = b0 + (uint64_t)(s * (SB >> 4));
 #pragma unroll
                     for (int kk = 0; kk < KSTEP / 16; ++kk) {      // 16 of the contraction: 32 bytes of a row, or 16 rows of 128 bytes
                         multiply<PR>(d, ad + (uint64_t)((A_OUTER ? 128 : 2) * kk), bd + (uint64_t)((B_OUTER ? 128 : 2) * kk), idesc, accumulate);
                         accumulate = 1;
                     }
-                    commit<PR>(smem_u32(&ctl->empty[s]));
+                    commit<PR>(empty0 + 8 * s);
+                    if constexpr (HOLD) bd += (uint64_t)(BC * KSTEP * 2 >> 4);
+                    if (++s == ST) { s = 0; ph ^= 1u; }
                 }
                 if (failed) break;
                 commit<PR>(smem_u32(&ctl->tfull[buf]));
@@ -322,8 +367,9 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         const int width = GATES ? a.F : a.Cin, mhalf = a.m_tiles / 2;
         const bool sectors = width % 16 == 0 && ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.y2)) & 31u) == 0;
         int item = 0;
-        for (int w = worker; w < items; w += workers, ++item) {
-            const int nt = w % a.n_tiles, ms = w / a.n_tiles, mt = ms % a.m_tiles, sp = ms / a.m_tiles;
+        for (int w = w_first; w < w_end; w += w_step, ++item) {
+            int nt, mt, sp;
+            place(w, nt, mt, sp);
             const bool up = USE == DW && mt >= mhalf;
             const int row = (up ? mt - mhalf : mt) * TM + rank * BM + q * 32 + lane, col0 = nt * (GATES ? BN / 2 : BN) + share * MINE;
             const bool on = row < (USE == DW ? a.F : a.rows);
@@ -345,46 +391,46 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
             if (!ok) { failed = true; break; }
             fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + share * MINE);
+            // The accumulator is free as soon as it is in registers: with few steps a tile, what the next product but one waits for is this warp.
+            uint32_t v[MINE / N][N], p[GATES ? MINE / N : 1][N];
 #pragma unroll
-            for (int c = 0; c < MINE; c += N) {
-                const int cols = width - col0 - c;
-                if (cols <= 0) break;                           // (the whole warp)
-                uint32_t v[N], p[GATES ? N : 1];
-                tmem_read<N>(taddr + (uint32_t)c, v);
-                if constexpr (GATES) tmem_read<N>(taddr + (uint32_t)(BN / 2 + c), p);
-                tmem_wait();
-                if (on) {
-                    const size_t at = at0 + c;
-                    if constexpr (GATES) {
-                        const uint32_t* dc = USE == PARTS ? d + c / 2 : d;
-                        if (a.act == WCC_ACT_SILU) gates_out<USE, WCC_ACT_SILU, N>(a, v, p, dc, at, cols, sectors);
-                        else if (a.act == WCC_ACT_GELU) gates_out<USE, WCC_ACT_GELU, N>(a, v, p, dc, at, cols, sectors);
-                        else if (a.act == WCC_ACT_RELU) gates_out<USE, WCC_ACT_RELU, N>(a, v, p, dc, at, cols, sectors);
-                        else gates_out<USE, WCC_ACT_NONE, N>(a, v, p, dc, at, cols, sectors);
-                    } else if (USE == DW && a.splits > 1) {
-                        float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c;
-#pragma unroll
-                        for (int i = 0; i < N; i += 4)
-                            if (i < cols) *reinterpret_cast<uint4*>(o + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < N; i += 16) {
-                            uint32_t o[8];
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) o[k] = pack_bf16x2(__uint_as_float(v[i + 2 * k]), __uint_as_float(v[i + 2 * k + 1]));
-                            store16((up ? a.y2 : a.y) + at + i, o, cols - i, sectors);
-                        }
-                    }
-                }
-                __syncwarp();
+            for (int c = 0; c < MINE / N; ++c) {
+                tmem_read<N>(taddr + (uint32_t)(c * N), v[c]);
+                if constexpr (GATES) tmem_read<N>(taddr + (uint32_t)(BN / 2 + c * N), p[c]);
             }
+            tmem_wait();
             fence_before();
             __syncwarp();
             if (lane == 0) {
                 if constexpr (PR) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(of_first(smem_u32(&ctl->tempty[buf]))) : "memory");
                 else mbar_arrive(smem_u32(&ctl->tempty[buf]));
             }
+            if (!on) continue;
+#pragma unroll
+            for (int c = 0; c < MINE / N; ++c) {
+                const int cols = width - col0 - c * N;
+                if (cols <= 0) break;
+                const size_t at = at0 + c * N;
+                if constexpr (GATES) {
+                    const uint32_t* dc = USE == PARTS ? d + c * N / 2 : d;
+                    if (a.act == WCC_ACT_SILU) gates_out<USE, WCC_ACT_SILU, N>(a, v[c], p[c], dc, at, cols, sectors);
+                    else if (a.act == WCC_ACT_GELU) gates_out<USE, WCC_ACT_GELU, N>(a, v[c], p[c], dc, at, cols, sectors);
+                    else if (a.act == WCC_ACT_RELU) gates_out<USE, WCC_ACT_RELU, N>(a, v[c], p[c], dc, at, cols, sectors);
+                    else gates_out<USE, WCC_ACT_NONE, N>(a, v[c], p[c], dc, at, cols, sectors);
+                } else if (USE == DW && a.splits > 1) {
+                    float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c * N;
+#pragma unroll
+                    for (int i = 0; i < N; i += 4)
+                        if (i < cols) *reinterpret_cast<uint4*>(o + i) = make_uint4(v[c][i], v[c][i + 1], v[c][i + 2], v[c][i + 3]);
+                } else {
+                    uint32_t o[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = pack_bf16x2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1]));
+                    store16((up ? a.y2 : a.y) + at, o, cols, sectors);
+                }
+            }
         }
+        __syncwarp();
     }
 
     if (failed) {
@@ -438,15 +484,16 @@ inline bool map_of(CUtensorMap* tm, const void* p, int inner, int outer, int box
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int USE, int BN>
+template <int USE, int BN, bool HOLD = false>
 wcc_status launch(const CUtensorMap& A0, const CUtensorMap& A1, const CUtensorMap& B0, const CUtensorMap& B1, const Args& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr int smem = 1024 + STAGES_OF<BN> * STAGE_BYTES_OF<BN> + (int)sizeof(Ctl) + 16;
-    const wcc_status s = allow_smem<contract<USE, BN>>(di.dev, smem);
+    constexpr int ring = HOLD ? HOLD_STAGES * A_BYTES + HOLD_STEPS * B_COLS<BN> * KSTEP * 2 : STAGES_OF<BN> * STAGE_BYTES_OF<BN>;
+    constexpr int smem = 1024 + ring + (int)sizeof(Ctl) + 16;
+    const wcc_status s = allow_smem<contract<USE, BN, HOLD>>(di.dev, smem);
     if (s != WCC_OK) return s;
     const int items = a.m_tiles * a.n_tiles * a.splits;
     const int workers = PAIR<BN> ? di.sms / 2 : di.sms, grid = (items < workers ? items : workers) * (PAIR<BN> ? 2 : 1);
-    return launch_overlapped(contract<USE, BN>, dim3((unsigned)grid), dim3(THREADS_OF<BN>), smem, st, true, PAIR<BN> ? 2 : 1, A0, A1, B0, B1, a);
+    return launch_overlapped(contract<USE, BN, HOLD>, dim3((unsigned)grid), dim3(THREADS_OF<BN>), smem, st, true, PAIR<BN> ? 2 : 1, A0, A1, B0, B1, a);
 }
 
 // Columns of a tile: as many as fill the SMs, 64 at least.  `cols` columns in all (FORWARD: gates and partners).
@@ -466,6 +513,7 @@ wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const De
     a.splits = 1;
     CUtensorMap A, G, U;
     if (!map_of(&A, x, a.Cin, a.rows, BM) || !map_of(&G, Wg, a.Cin, a.F, bn / 2) || !map_of(&U, Wu, a.Cin, a.F, bn / 2)) return WCC_ERR_CUDA;
+    if (bn == 256 && a.Cin <= HOLD_STEPS * KSTEP) return launch<USE, 256, true>(A, A, G, U, a, di, st);
     if (bn == 256) return launch<USE, 256>(A, A, G, U, a, di, st);
     if (bn == 128) return launch<USE, 128>(A, A, G, U, a, di, st);
     return launch<USE, 64>(A, A, G, U, a, di, st);
