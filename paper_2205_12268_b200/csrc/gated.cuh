@@ -10,10 +10,13 @@
 // TMA (128-byte swizzle, no multicast) feeds a ring of stages, one thread issues the instructions, the accumulator is double-buffered, so the
 // epilogue of a tile runs under the products of the next one.  Sizes that are no multiples of a tile arrive as zeros from TMA.
 //
-// Tiles of 256 columns are the work of two CTAs on neighbouring SMs (cta_group::2): 128 rows each, and each brings in half of B for both, 32 KB a
-// step instead of 48.  What bounds the loop is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2): six steps instead of four.
-// With up to 256 channels the weights of a column tile stay in shared memory (HOLD) while a pair goes through the row tiles, and the ring holds rows alone.
+// Where the contraction is long, tiles of 256 columns are the work of two CTAs on neighbouring SMs (PAIR, cta_group::2): 128 rows each, and each brings in half
+// of B for both, 32 KB a step instead of 48.  What bounds the loop then is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2):
+// seven steps instead of four.  Forward with up to 256 channels, the weights of a column tile stay in shared memory (HOLD) while a CTA goes through the row
+// tiles, and the ring holds rows alone.
 #pragma once
+
+#include <type_traits>
 
 #include "tcgen05.cuh"
 #include "tma.cuh"
@@ -30,15 +33,27 @@ enum Use { FORWARD, PARTS, DX, DW };
 constexpr int BM = 128, KSTEP = 64;
 constexpr int A_BYTES = BM * KSTEP * 2;
 
-// Warps of the epilogue, four for each share of a tile's columns.  Its arithmetic depends on results of a few units with long ways, so two warps on an SM's quarter
-// issue in 42 of 100 cycles; four fill it (65536 x 256 -> 1024 with gelu: 88 us with eight warps).
-template <int BN> constexpr int SHARES = BN == 64 ? 2 : 4;
-template <int BN> constexpr int THREADS_OF = 64 + 128 * SHARES<BN>;
-template <int BN> constexpr bool PAIR = BN == 256;                     // two CTAs a tile
-template <int BN> constexpr int STAGES_OF = BN == 64 ? 8 : 6;
-template <int BN> constexpr int B_COLS = PAIR<BN> ? BN / 2 : BN;        // columns of B that a CTA brings in
-template <int BN> constexpr int STAGE_BYTES_OF = A_BYTES + B_COLS<BN> * KSTEP * 2;
-constexpr int HOLD_STEPS = 4, HOLD_STAGES = 8;                          // HOLD: steps of weights that stay, stages of rows
+constexpr int HOLD_STEPS = 4;                  // HOLD: steps of weights that fit
+
+// A variant of the kernel: its use, columns of a tile, whether two CTAs share a tile (PAIR), whether the weights of a column tile stay in shared memory
+// (HOLD).
+template <int USE_, int BN_, bool PAIR_, bool HOLD_> struct Form {
+    static constexpr int USE = USE_, BN = BN_;
+    static constexpr bool PAIR = PAIR_, HOLD = HOLD_;
+    static constexpr bool GATES = USE == FORWARD || USE == PARTS;
+    static_assert(GATES || !HOLD, "");
+    static constexpr int B_COLS = PAIR ? BN / 2 : BN;                   // columns of B that a CTA brings in
+    static constexpr int B_BYTES = B_COLS * KSTEP * 2;
+    static constexpr int STAGE_BYTES = HOLD ? A_BYTES : A_BYTES + B_BYTES;
+    static constexpr int HELD_BYTES = HOLD ? HOLD_STEPS * B_BYTES : 0;
+    static constexpr int ROOM = 224 * 1024;
+    static constexpr int FIT = (ROOM - HELD_BYTES) / STAGE_BYTES;
+    static constexpr int STAGES = FIT < 8 ? FIT : 8;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + HELD_BYTES;   // and Ctl
+    static constexpr int SHARES = BN == 64 ? 2 : 4;                     // warps of the epilogue: four for each share of a tile's columns
+    static constexpr int THREADS = 64 + 128 * SHARES;
+    static constexpr int ROWS = PAIR ? 2 * BM : BM;                     // of a tile
+};
 
 struct Ctl {
     uint64_t full[8], empty[8], tfull[2], tempty[2], bfull, bempty;
@@ -175,51 +190,41 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* w, int
     }
 }
 
-// N columns of gates and their partners: to y, or with dy (`d`, bf16 pairs) to dG and dU.
-template <int USE, int ACT, int N>
-__device__ __forceinline__ void gates_out(const Args& a, const uint32_t (&g)[N], const uint32_t (&u)[N], const uint32_t* d, size_t at, int cols, bool sectors)
+// 16 columns of gates and their partners: y, or with dy (`d`, bf16 pairs) dG and dU.
+template <int USE, int ACT>
+__device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t (&u)[16], const uint32_t* d, uint32_t* o, uint32_t* o2)
 {
 #pragma unroll
-    for (int c = 0; c < N; c += 16) {
-        uint32_t o[8], o2[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int k = c + 2 * i;
-            const f2 z = pair(__uint_as_float(g[k]), __uint_as_float(g[k + 1])), w = pair(__uint_as_float(u[k]), __uint_as_float(u[k + 1]));
-            const Act2 v = act_of<ACT, USE == PARTS>(z);
-            if constexpr (USE == FORWARD) {
-                const f2 r = mul2(v.a, w);
-                o[i] = pack_bf16x2(r.x(), r.y());
-            } else {
-                const f2 t = pair(bf16lo(d[k / 2]), bf16hi(d[k / 2])), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
-                o[i] = pack_bf16x2(r.x(), r.y());
-                o2[i] = pack_bf16x2(r2.x(), r2.y());
-            }
+    for (int i = 0; i < 8; ++i) {
+        const f2 z = pair(__uint_as_float(g[2 * i]), __uint_as_float(g[2 * i + 1])), w = pair(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+        const Act2 v = act_of<ACT, USE == PARTS>(z);
+        if constexpr (USE == FORWARD) {
+            const f2 r = mul2(v.a, w);
+            o[i] = pack_bf16x2(r.x(), r.y());
+        } else {
+            const f2 t = pair(bf16lo(d[i]), bf16hi(d[i])), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
+            o[i] = pack_bf16x2(r.x(), r.y());
+            o2[i] = pack_bf16x2(r2.x(), r2.y());
         }
-        store16(a.y + at + c, o, cols - c, sectors);
-        if constexpr (USE == PARTS) store16(a.y2 + at + c, o2, cols - c, sectors);
     }
 }
 
-template <int USE, int BN, bool HOLD>
-__global__ void __launch_bounds__(THREADS_OF<BN>, 1)
+template <typename Fm>
+__global__ void __launch_bounds__(Fm::THREADS, 1)
 contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtensorMap tA1, const __grid_constant__ CUtensorMap tB0,
          const __grid_constant__ CUtensorMap tB1, const __grid_constant__ Args a)
 {
-    constexpr int ST = HOLD ? HOLD_STAGES : STAGES_OF<BN>, SB = HOLD ? A_BYTES : STAGE_BYTES_OF<BN>, COLS = 2 * BN, BC = B_COLS<BN>;
-    constexpr int HELD = HOLD ? HOLD_STEPS * BC * KSTEP * 2 : 0;
-    static_assert(!HOLD || (BN == 256 && (USE == FORWARD || USE == PARTS)), "");
-    constexpr bool PR = PAIR<BN>;
+    constexpr int USE = Fm::USE, BN = Fm::BN, ST = Fm::STAGES, SB = Fm::STAGE_BYTES, COLS = 2 * BN, BC = Fm::B_COLS, TM = Fm::ROWS;
+    constexpr bool PR = Fm::PAIR, HOLD = Fm::HOLD;
     constexpr bool A_OUTER = USE == DW, B_OUTER = USE == DX || USE == DW;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + (size_t)ST * SB + HELD);
+    Ctl* ctl = reinterpret_cast<Ctl*>(smem_raw + (base - raw) + Fm::SMEM - 1024);
     volatile int* abort_flag = &ctl->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int items = a.m_tiles * a.n_tiles * a.splits;
     // PAIR: both CTAs go through the same items, each with its half of the rows and of B
     const int rank = PR ? (int)cta_rank() : 0, worker = PR ? blockIdx.x / 2 : blockIdx.x, workers = PR ? gridDim.x / 2 : gridDim.x;
-    constexpr int TM = PR ? 2 * BM : BM;                       // rows of a tile
     // Items: HOLD: a stretch of them, row tiles within a column tile; else every workers'th, column tiles within a row tile within a part of the rows.
     const int w_first = HOLD ? (int)((long long)items * worker / workers) : worker, w_end = HOLD ? (int)((long long)items * (worker + 1) / workers) : items;
     const int w_step = HOLD ? 1 : workers;
@@ -241,7 +246,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < ST; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tfull[b]), 1); mbar_init(smem_u32(&ctl->tempty[b]), (PR ? 8 : 4) * SHARES<BN>); }
+        for (int b = 0; b < 2; ++b) { mbar_init(smem_u32(&ctl->tfull[b]), 1); mbar_init(smem_u32(&ctl->tempty[b]), (PR ? 8 : 4) * Fm::SHARES); }
         mbar_init(smem_u32(&ctl->bfull), 1);
         mbar_init(smem_u32(&ctl->bempty), 1);
         ctl->abort_flag = 0;
@@ -267,6 +272,15 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
 
     if (warp == 0) {
         if (lane == 0) {
+            // a step of weights: gates' columns, then their partners' (PAIR: one CTA has these, the other those)
+            [[maybe_unused]] auto weights = [&](uint32_t dst, int k, int nt, uint32_t bar) {
+                if constexpr (PR) {
+                    load_tile<PR>(dst, rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
+                } else {
+                    load_tile<PR>(dst, &tB0, k * KSTEP, nt * (BN / 2), bar);
+                    load_tile<PR>(dst + BN / 2 * 128, &tB1, k * KSTEP, nt * (BN / 2), bar);
+                }
+            };
             int s = 0, held = -1, swaps = 0;                   // column tile whose weights are here, times that they were brought in
             uint32_t ph = 1;
             for (int w = w_first; w < w_end && !failed; w += w_step) {
@@ -274,10 +288,9 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 place(w, nt, mt, sp);
                 if (HOLD && nt != held) {
                     if (!mbar_wait(smem_u32(&ctl->bempty), (uint32_t)(swaps & 1) ^ 1u, abort_flag)) { failed = true; break; }
-                    const uint32_t bar = of_first(smem_u32(&ctl->bfull));
-                    if (rank == 0) mbar_expect_tx(smem_u32(&ctl->bfull), (uint32_t)(2 * all_steps * BC * KSTEP * 2));
-                    for (int k = 0; k < all_steps; ++k)
-                        load_tile<PR>(base + ST * SB + k * (BC * KSTEP * 2), rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
+                    const uint32_t own = smem_u32(&ctl->bfull), bar = PR ? of_first(own) : own;
+                    if (rank == 0) mbar_expect_tx(own, (uint32_t)((PR ? 2 : 1) * all_steps * Fm::B_BYTES));
+                    for (int k = 0; k < all_steps; ++k) weights(base + ST * SB + k * Fm::B_BYTES, k, nt, bar);
                     held = nt;
                     ++swaps;
                 }
@@ -288,13 +301,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                     if (rank == 0) mbar_expect_tx(own, (uint32_t)(PR ? 2 * SB : SB));
                     if constexpr (USE == FORWARD || USE == PARTS) {
                         load_tile<PR>(sA, &tA0, k * KSTEP, mt * TM + rank * BM, bar);
-                        if constexpr (HOLD) {
-                        } else if constexpr (PR) {             // one CTA the gates' columns, the other their partners'
-                            load_tile<PR>(sB, rank == 0 ? &tB0 : &tB1, k * KSTEP, nt * (BN / 2), bar);
-                        } else {
-                            load_tile<PR>(sB, &tB0, k * KSTEP, nt * (BN / 2), bar);
-                            load_tile<PR>(sB + BN / 2 * 128, &tB1, k * KSTEP, nt * (BN / 2), bar);
-                        }
+                        if constexpr (!HOLD) weights(sB, k, nt, bar);
                     } else if constexpr (USE == DX) {
                         const bool up = k >= f_steps;
                         const int f0 = (up ? k - f_steps : k) * KSTEP;
@@ -328,7 +335,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 place(w, nt, mt, sp);
                 if (HOLD && nt != held) {
                     if (held >= 0) commit<PR>(smem_u32(&ctl->bempty));         // the products with the old weights are done: they may go
-                    if (!wait_cluster(smem_u32(&ctl->bfull), (uint32_t)(swaps & 1), abort_flag)) { failed = true; break; }
+                    if (!(PR ? wait_cluster(smem_u32(&ctl->bfull), (uint32_t)(swaps & 1), abort_flag) : mbar_wait(smem_u32(&ctl->bfull), (uint32_t)(swaps & 1), abort_flag))) { failed = true; break; }
                     held = nt;
                     ++swaps;
                 }
@@ -352,7 +359,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                         accumulate = 1;
                     }
                     commit<PR>(empty0 + 8 * s);
-                    if constexpr (HOLD) bd += (uint64_t)(BC * KSTEP * 2 >> 4);
+                    if constexpr (HOLD) bd += (uint64_t)(Fm::B_BYTES >> 4);
                     if (++s == ST) { s = 0; ph ^= 1u; }
                 }
                 if (failed) break;
@@ -362,8 +369,8 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         __syncwarp();
     } else {
         const int q = warp & 3, share = (warp - 2) >> 2;       // lanes of tensor memory that the warp may read; its share of the columns
-        constexpr bool GATES = USE == FORWARD || USE == PARTS;
-        constexpr int MINE = (GATES ? BN / 2 : BN) / SHARES<BN>, N = 16;         // columns of the warp, and those at once
+        constexpr bool GATES = Fm::GATES;
+        constexpr int MINE = (GATES ? BN / 2 : BN) / Fm::SHARES, N = 16;         // columns of the warp, and those at once
         const int width = GATES ? a.F : a.Cin, mhalf = a.m_tiles / 2;
         const bool sectors = width % 16 == 0 && ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.y2)) & 31u) == 0;
         int item = 0;
@@ -405,28 +412,42 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 if constexpr (PR) asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(of_first(smem_u32(&ctl->tempty[buf]))) : "memory");
                 else mbar_arrive(smem_u32(&ctl->tempty[buf]));
             }
-            if (!on) continue;
+            if constexpr (GATES) {
+                uint32_t o[MINE / 2], o2[USE == PARTS ? MINE / 2 : 1];
+                auto all = [&](auto act) {
 #pragma unroll
-            for (int c = 0; c < MINE / N; ++c) {
-                const int cols = width - col0 - c * N;
-                if (cols <= 0) break;
-                const size_t at = at0 + c * N;
-                if constexpr (GATES) {
-                    const uint32_t* dc = USE == PARTS ? d + c * N / 2 : d;
-                    if (a.act == WCC_ACT_SILU) gates_out<USE, WCC_ACT_SILU, N>(a, v[c], p[c], dc, at, cols, sectors);
-                    else if (a.act == WCC_ACT_GELU) gates_out<USE, WCC_ACT_GELU, N>(a, v[c], p[c], dc, at, cols, sectors);
-                    else if (a.act == WCC_ACT_RELU) gates_out<USE, WCC_ACT_RELU, N>(a, v[c], p[c], dc, at, cols, sectors);
-                    else gates_out<USE, WCC_ACT_NONE, N>(a, v[c], p[c], dc, at, cols, sectors);
-                } else if (USE == DW && a.splits > 1) {
-                    float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c * N;
+                    for (int c = 0; c < MINE / N; ++c)
+                        gates16<USE, decltype(act)::value>(v[c], p[c], USE == PARTS ? d + c * 8 : d, o + c * 8, USE == PARTS ? o2 + c * 8 : o2);
+                };
+                if (a.act == WCC_ACT_SILU) all(std::integral_constant<int, WCC_ACT_SILU>());
+                else if (a.act == WCC_ACT_GELU) all(std::integral_constant<int, WCC_ACT_GELU>());
+                else if (a.act == WCC_ACT_RELU) all(std::integral_constant<int, WCC_ACT_RELU>());
+                else all(std::integral_constant<int, WCC_ACT_NONE>());
+                if (on) {
 #pragma unroll
-                    for (int i = 0; i < N; i += 4)
-                        if (i < cols) *reinterpret_cast<uint4*>(o + i) = make_uint4(v[c][i], v[c][i + 1], v[c][i + 2], v[c][i + 3]);
-                } else {
-                    uint32_t o[8];
+                    for (int c = 0; c < MINE / N; ++c) {
+                        const int cols = width - col0 - c * N;
+                        if (cols <= 0) break;
+                        store16(a.y + at0 + c * N, o + c * 8, cols, sectors);
+                        if constexpr (USE == PARTS) store16(a.y2 + at0 + c * N, o2 + c * 8, cols, sectors);
+                    }
+                }
+            } else if (on) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) o[k] = pack_bf16x2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1]));
-                    store16((up ? a.y2 : a.y) + at, o, cols, sectors);
+                for (int c = 0; c < MINE / N; ++c) {
+                    const int cols = width - col0 - c * N;
+                    if (cols <= 0) break;
+                    if (USE == DW && a.splits > 1) {
+                        float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c * N;
+#pragma unroll
+                        for (int i = 0; i < N; i += 4)
+                            if (i < cols) *reinterpret_cast<uint4*>(o + i) = make_uint4(v[c][i], v[c][i + 1], v[c][i + 2], v[c][i + 3]);
+                    } else {
+                        uint32_t o[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) o[k] = pack_bf16x2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1]));
+                        store16((up ? a.y2 : a.y) + at0 + c * N, o, cols, sectors);
+                    }
                 }
             }
         }
@@ -484,16 +505,14 @@ inline bool map_of(CUtensorMap* tm, const void* p, int inner, int outer, int box
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int USE, int BN, bool HOLD = false>
+template <typename Fm>
 wcc_status launch(const CUtensorMap& A0, const CUtensorMap& A1, const CUtensorMap& B0, const CUtensorMap& B1, const Args& a, const DeviceInfo& di, cudaStream_t st)
 {
-    constexpr int ring = HOLD ? HOLD_STAGES * A_BYTES + HOLD_STEPS * B_COLS<BN> * KSTEP * 2 : STAGES_OF<BN> * STAGE_BYTES_OF<BN>;
-    constexpr int smem = 1024 + ring + (int)sizeof(Ctl) + 16;
-    const wcc_status s = allow_smem<contract<USE, BN, HOLD>>(di.dev, smem);
+    constexpr int smem = Fm::SMEM + (int)sizeof(Ctl) + 16;
+    const wcc_status s = allow_smem<contract<Fm>>(di.dev, smem);
     if (s != WCC_OK) return s;
-    const int items = a.m_tiles * a.n_tiles * a.splits;
-    const int workers = PAIR<BN> ? di.sms / 2 : di.sms, grid = (items < workers ? items : workers) * (PAIR<BN> ? 2 : 1);
-    return launch_overlapped(contract<USE, BN, HOLD>, dim3((unsigned)grid), dim3(THREADS_OF<BN>), smem, st, true, PAIR<BN> ? 2 : 1, A0, A1, B0, B1, a);
+    const int items = a.m_tiles * a.n_tiles * a.splits, workers = Fm::PAIR ? di.sms / 2 : di.sms, grid = (items < workers ? items : workers) * (Fm::PAIR ? 2 : 1);
+    return launch_overlapped(contract<Fm>, dim3((unsigned)grid), dim3(Fm::THREADS), smem, st, true, Fm::PAIR ? 2 : 1, A0, A1, B0, B1, a);
 }
 
 // Columns of a tile: as many as fill the SMs, 64 at least.  `cols` columns in all (FORWARD: gates and partners).
@@ -503,44 +522,61 @@ inline int tile_of(int m_tiles, long long cols, int sms)
     while (bn > 64 && (cols <= bn / 2 || (long long)m_tiles * ((cols + bn - 1) / bn) < sms)) bn /= 2;
     return bn;
 }
+// Two CTAs a tile from this length of the contraction on: their barriers cost 1.3 us a tile instead of half of that, their loads a third less.  Forward with
+// silu, 65536 rows to 1024 columns, one CTA / two: 256 channels 70 / 88 us, 512 119 / 112, 16384 x 1024 -> 4096 206 / 191.
+constexpr int PAIR_FROM = 512;
 
 template <int USE>
 wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const DeviceInfo& di, cudaStream_t st)
 {
     const int bn = tile_of(ceil_div(a.rows, BM), 2LL * a.F, di.sms);
-    a.m_tiles = ceil_div(a.rows, bn == 256 ? 2 * BM : BM);
+    const bool two = bn == 256 && a.Cin >= PAIR_FROM;
+    a.m_tiles = ceil_div(a.rows, two ? 2 * BM : BM);
     a.n_tiles = ceil_div(a.F, bn / 2);
     a.splits = 1;
     CUtensorMap A, G, U;
     if (!map_of(&A, x, a.Cin, a.rows, BM) || !map_of(&G, Wg, a.Cin, a.F, bn / 2) || !map_of(&U, Wu, a.Cin, a.F, bn / 2)) return WCC_ERR_CUDA;
-    if (bn == 256 && a.Cin <= HOLD_STEPS * KSTEP) return launch<USE, 256, true>(A, A, G, U, a, di, st);
-    if (bn == 256) return launch<USE, 256>(A, A, G, U, a, di, st);
-    if (bn == 128) return launch<USE, 128>(A, A, G, U, a, di, st);
-    return launch<USE, 64>(A, A, G, U, a, di, st);
+    if (two) return launch<Form<USE, 256, true, false>>(A, A, G, U, a, di, st);
+    // Few channels: the weights stay (forward, to 1024 columns: 65536 x 256 72 -> 69 us, 66306 x 64 -> 256 18.8 -> 17.2).  Not where dy is read: the column
+    // tiles of a row tile are then far apart in time, and its lines with them (gradients of the second 66 -> 70 us).
+    if constexpr (USE == FORWARD)
+        if (bn == 256 && a.Cin <= HOLD_STEPS * KSTEP) return launch<Form<USE, 256, false, true>>(A, A, G, U, a, di, st);
+    if (bn == 256) return launch<Form<USE, 256, false, false>>(A, A, G, U, a, di, st);
+    if (bn == 128) return launch<Form<USE, 128, false, false>>(A, A, G, U, a, di, st);
+    return launch<Form<USE, 64, false, false>>(A, A, G, U, a, di, st);
+}
+
+template <int USE>
+wcc_status products(int bn, bool two, const CUtensorMap& A0, const CUtensorMap& A1, const CUtensorMap& B0, const CUtensorMap& B1, const Args& a, const DeviceInfo& di,
+                    cudaStream_t st)
+{
+    if (two) return launch<Form<USE, 256, true, false>>(A0, A1, B0, B1, a, di, st);
+    if (bn == 256) return launch<Form<USE, 256, false, false>>(A0, A1, B0, B1, a, di, st);
+    if (bn == 128) return launch<Form<USE, 128, false, false>>(A0, A1, B0, B1, a, di, st);
+    return launch<Form<USE, 64, false, false>>(A0, A1, B0, B1, a, di, st);
 }
 
 inline wcc_status dx(const void* dG, const void* dU, const void* Wg, const void* Wu, Args a, const DeviceInfo& di, cudaStream_t st)
 {
     const int bn = tile_of(ceil_div(a.rows, BM), a.Cin, di.sms);
-    a.m_tiles = ceil_div(a.rows, bn == 256 ? 2 * BM : BM);
+    const bool two = bn == 256 && 2 * a.F >= PAIR_FROM;
+    a.m_tiles = ceil_div(a.rows, two ? 2 * BM : BM);
     a.n_tiles = ceil_div(a.Cin, bn);
     a.splits = 1;
     CUtensorMap A0, A1, B0, B1;
     if (!map_of(&A0, dG, a.F, a.rows, BM) || !map_of(&A1, dU, a.F, a.rows, BM) || !map_of(&B0, Wg, a.Cin, a.F, KSTEP) || !map_of(&B1, Wu, a.Cin, a.F, KSTEP))
         return WCC_ERR_CUDA;
-    if (bn == 256) return launch<DX, 256>(A0, A1, B0, B1, a, di, st);
-    if (bn == 128) return launch<DX, 128>(A0, A1, B0, B1, a, di, st);
-    return launch<DX, 64>(A0, A1, B0, B1, a, di, st);
+    return products<DX>(bn, two, A0, A1, B0, B1, a, di, st);
 }
 
-struct DwPlan { int bn, m_tiles, n_tiles, splits; };
+struct DwPlan { int bn; bool two; int m_tiles, n_tiles, splits; };
 inline DwPlan dw_plan(int rows, int Cin, int F, int sms)
 {
     DwPlan p;
     p.bn = Cin > 128 ? 256 : Cin > 64 ? 128 : 64;
-    if (p.bn == 256 && F <= BM) p.bn = 128;                    // half a tile of two CTAs would be empty
-    if (p.bn == 256) sms /= 2;
-    p.m_tiles = 2 * ceil_div(F, p.bn == 256 ? 2 * BM : BM);
+    p.two = p.bn == 256 && F > BM && rows >= PAIR_FROM;        // (F up to 128: half a tile of two CTAs would be empty)
+    if (p.two) sms /= 2;
+    p.m_tiles = 2 * ceil_div(F, p.two ? 2 * BM : BM);
     p.n_tiles = ceil_div(Cin, p.bn);
     const long long tiles = (long long)p.m_tiles * p.n_tiles;
     const int steps = ceil_div(rows, KSTEP);
@@ -556,10 +592,7 @@ inline wcc_status dw(const void* dG, const void* dU, const void* x, Args a, cons
     a.splits = p.splits;
     CUtensorMap A0, A1, B;
     if (!map_of(&A0, dG, a.F, a.rows, KSTEP) || !map_of(&A1, dU, a.F, a.rows, KSTEP) || !map_of(&B, x, a.Cin, a.rows, KSTEP)) return WCC_ERR_CUDA;
-    wcc_status s;
-    if (p.bn == 256) s = launch<DW, 256>(A0, A1, B, B, a, di, st);
-    else if (p.bn == 128) s = launch<DW, 128>(A0, A1, B, B, a, di, st);
-    else s = launch<DW, 64>(A0, A1, B, B, a, di, st);
+    const wcc_status s = products<DW>(p.bn, p.two, A0, A1, B, B, a, di, st);
     if (s != WCC_OK || p.splits == 1) return s;
     const size_t each = (size_t)a.F * a.Cin;
     return launch_overlapped(add_parts, dim3((unsigned)((each + 127) / 128)), dim3(128), 0, st, true, 1, a.part, p.splits, each, a.y, a.y2);
