@@ -31,32 +31,33 @@ using namespace tr;
 enum Use { FORWARD, PARTS, DX, DW };
 
 constexpr int BM = 128, KSTEP = 64;
-constexpr int A_BYTES = BM * KSTEP * 2;
+constexpr int FEW = 32;                        // rows of a call that a stage of its own size holds
 
 constexpr int HOLD_STEPS = 4;                  // HOLD: steps of weights that fit
 
 // A variant of the kernel: its use, columns of a tile, whether two CTAs share a tile (PAIR), whether the weights of a column tile stay in shared memory
-// (HOLD).
-template <int USE_, int BN_, bool PAIR_, bool HOLD_> struct Form {
+// (HOLD), rows of A that a step brings in (calls of few rows: the instruction then reads other steps' rows for the rest, whose results go nowhere).
+template <int USE_, int BN_, bool PAIR_, bool HOLD_, int A_ROWS_ = BM> struct Form {
     static constexpr int USE = USE_, BN = BN_;
     static constexpr bool PAIR = PAIR_, HOLD = HOLD_;
     static constexpr bool GATES = USE == FORWARD || USE == PARTS;
     static_assert(GATES || !HOLD, "");
     static constexpr int B_COLS = PAIR ? BN / 2 : BN;                   // columns of B that a CTA brings in
     static constexpr int B_BYTES = B_COLS * KSTEP * 2;
+    static constexpr int A_ROWS = A_ROWS_, A_BYTES = A_ROWS * KSTEP * 2;
     static constexpr int STAGE_BYTES = HOLD ? A_BYTES : A_BYTES + B_BYTES;
     static constexpr int HELD_BYTES = HOLD ? HOLD_STEPS * B_BYTES : 0;
-    static constexpr int ROOM = 224 * 1024;
+    static constexpr int ROOM = (A_ROWS < BM ? 208 : 224) * 1024, MOST_STAGES = A_ROWS < BM ? 17 : 8;
     static constexpr int FIT = (ROOM - HELD_BYTES) / STAGE_BYTES;
-    static constexpr int STAGES = FIT < 8 ? FIT : 8;
-    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + HELD_BYTES;   // and Ctl
+    static constexpr int STAGES = FIT < MOST_STAGES ? FIT : MOST_STAGES;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + HELD_BYTES + (A_ROWS < BM ? BM * KSTEP * 2 : 0);      // and Ctl
     static constexpr int SHARES = BN == 64 ? 2 : 4;                     // warps of the epilogue: four for each share of a tile's columns
     static constexpr int THREADS = 64 + 128 * SHARES;
     static constexpr int ROWS = PAIR ? 2 * BM : BM;                     // of a tile
 };
 
 struct Ctl {
-    uint64_t full[8], empty[8], tfull[2], tempty[2], bfull, bempty;
+    uint64_t full[17], empty[17], tfull[2], tempty[2], bfull, bempty;
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -297,7 +298,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 const int k0 = (int)((long long)all_steps * sp / a.splits), k1 = (int)((long long)all_steps * (sp + 1) / a.splits);
                 for (int k = k0; k < k1; ++k) {
                     if (!mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag)) { failed = true; break; }
-                    const uint32_t sA = base + (uint32_t)s * SB, sB = sA + A_BYTES, own = smem_u32(&ctl->full[s]), bar = PR ? of_first(own) : own;
+                    const uint32_t sA = base + (uint32_t)s * SB, sB = sA + Fm::A_BYTES, own = smem_u32(&ctl->full[s]), bar = PR ? of_first(own) : own;
                     if (rank == 0) mbar_expect_tx(own, (uint32_t)(PR ? 2 * SB : SB));
                     if constexpr (USE == FORWARD || USE == PARTS) {
                         load_tile<PR>(sA, &tA0, k * KSTEP, mt * TM + rank * BM, bar);
@@ -329,7 +330,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
             uint32_t ph = 0;
             const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]);
             const uint64_t a0 = A_OUTER ? smem_desc_outer(base) : smem_desc_sw128(base);
-            const uint64_t b0 = HOLD ? smem_desc_sw128(base + ST * SB) : B_OUTER ? smem_desc_outer(base + A_BYTES) : smem_desc_sw128(base + A_BYTES);
+            const uint64_t b0 = HOLD ? smem_desc_sw128(base + ST * SB) : B_OUTER ? smem_desc_outer(base + Fm::A_BYTES) : smem_desc_sw128(base + Fm::A_BYTES);
             for (int w = w_first; w < w_end && !failed; w += w_step, ++item) {
                 int nt, mt, sp;
                 place(w, nt, mt, sp);
@@ -529,13 +530,15 @@ constexpr int PAIR_FROM = 512;
 template <int USE>
 wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const DeviceInfo& di, cudaStream_t st)
 {
-    const int bn = tile_of(ceil_div(a.rows, BM), 2LL * a.F, di.sms);
+    // few rows: the weights are the traffic, so as many CTAs as there are, and the whole of their share on its way at once
+    const bool few = a.rows <= FEW;
+    const int bn = few ? 64 : tile_of(ceil_div(a.rows, BM), 2LL * a.F, di.sms);
     const bool two = bn == 256 && a.Cin >= PAIR_FROM;
     a.m_tiles = ceil_div(a.rows, two ? 2 * BM : BM);
     a.n_tiles = ceil_div(a.F, bn / 2);
     a.splits = 1;
     CUtensorMap A, G, U;
-    if (!map_of(&A, x, a.Cin, a.rows, BM) || !map_of(&G, Wg, a.Cin, a.F, bn / 2) || !map_of(&U, Wu, a.Cin, a.F, bn / 2)) return WCC_ERR_CUDA;
+    if (!map_of(&A, x, a.Cin, a.rows, few ? FEW : BM) || !map_of(&G, Wg, a.Cin, a.F, bn / 2) || !map_of(&U, Wu, a.Cin, a.F, bn / 2)) return WCC_ERR_CUDA;
     if (two) return launch<Form<USE, 256, true, false>>(A, A, G, U, a, di, st);
     // Few channels: the weights stay (forward, to 1024 columns: 65536 x 256 72 -> 69 us, 66306 x 64 -> 256 18.8 -> 17.2).  Not where dy is read: the column
     // tiles of a row tile are then far apart in time, and its lines with them (gradients of the second 66 -> 70 us).
@@ -543,6 +546,7 @@ wcc_status gates(const void* x, const void* Wg, const void* Wu, Args a, const De
         if (bn == 256 && a.Cin <= HOLD_STEPS * KSTEP) return launch<Form<USE, 256, false, true>>(A, A, G, U, a, di, st);
     if (bn == 256) return launch<Form<USE, 256, false, false>>(A, A, G, U, a, di, st);
     if (bn == 128) return launch<Form<USE, 128, false, false>>(A, A, G, U, a, di, st);
+    if (few) return launch<Form<USE, 64, false, false, FEW>>(A, A, G, U, a, di, st);
     return launch<Form<USE, 64, false, false>>(A, A, G, U, a, di, st);
 }
 
