@@ -14,17 +14,69 @@ constexpr int BLOCK = WCC_CKPT_BLOCK;
 constexpr float SMALLEST = 7.8886090522101181e-31f;    // 2^-100: 127 / top stays far from the end of fp32
 
 struct Scale { float inv, scale; };
-// top: the largest magnitude as fmaxf gives it (NaN values left out); bad: a NaN or an infinity is among the values
-__device__ __forceinline__ Scale scale_of(float top, bool bad)
+__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u; }
+// The larger magnitude; NaN if either is.
+__device__ __forceinline__ float larger(float a, float b)
 {
-    if (bad) return {0.0f, __int_as_float(0x7FC00000)};
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+// Of a block with the largest magnitude `top` (NaN if a NaN is among its values).
+__device__ __forceinline__ Scale scale_of(float top)
+{
+    if (not_finite(top)) return {0.0f, __int_as_float(0x7FC00000)};
     if (top < SMALLEST) return {0.0f, 0.0f};
     return {__fdiv_rn(127.0f, top), __fdiv_rn(top, 127.0f)};
 }
-// |x * inv| <= 127 (1 + 2^-23) rounds to 127 at most.  A block that is not finite has inv = 0: its codes are 0 or, for NaN, what the
-// conversion makes of NaN, which is 0 as well.
-__device__ __forceinline__ int code_of(float x, float inv) { return __float2int_rn(x * inv); }
-__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7F800000u) == 0x7F800000u; }
+// A value's code in the low byte: |x * inv| <= 127 (1 + 2^-23), and adding 1.5 * 2^23 rounds it to a whole number, ties to even.  (Two roundings: as a pair of
+// packed instructions they came back as one multiply-add, whose ties are others.)
+__device__ __forceinline__ uint32_t code_of(float x, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12582912.0f)); }
+__device__ __forceinline__ uint32_t pack_codes(f2 a, f2 b, float inv)
+{
+    return __byte_perm(__byte_perm(code_of(a.x(), inv), code_of(a.y(), inv), 0x0040), __byte_perm(code_of(b.x(), inv), code_of(b.y(), inv), 0x0040), 0x5410);
+}
+// The largest magnitude among 16 bytes of values and, by shuffles, among those of LANES lanes, for U such vectors; NaN if a NaN is among them.  bf16: by pairs.
+template <int LANES, int U> __device__ __forceinline__ void largest(const uint4 (&w)[U], float (&top)[U], float)
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        top[u] = larger(larger(fabsf(__uint_as_float(w[u].x)), __uint_as_float(w[u].y)), larger(fabsf(__uint_as_float(w[u].z)), __uint_as_float(w[u].w)));
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < U; ++u) top[u] = larger(top[u], __shfl_xor_sync(0xFFFFFFFFu, top[u], o));
+}
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int LANES, int U> __device__ __forceinline__ void largest(const uint4 (&w)[U], float (&top)[U], __nv_bfloat16)
+{
+    constexpr uint32_t ABS = 0x7FFF7FFFu;
+    uint32_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = larger2(larger2(w[u].x & ABS, w[u].y & ABS), larger2(w[u].z & ABS, w[u].w & ABS));
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1)
+#pragma unroll
+        for (int u = 0; u < U; ++u) m[u] = larger2(m[u], __shfl_xor_sync(0xFFFFFFFFu, m[u], o));
+#pragma unroll
+    for (int u = 0; u < U; ++u) top[u] = larger(bf16lo(m[u]), bf16hi(m[u]));
+}
+template <int V> __device__ __forceinline__ void put_codes(const Pairs<V>& f, float inv, int8_t* codes)
+{
+    uint32_t q[V / 4];
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        q[i] = pack_codes(f.v[2 * i], f.v[2 * i + 1], inv);
+        if (inv == 0.0f) q[i] = 0u;                        // (what is not finite times 0 is no number)
+    }
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(codes) = make_uint2(q[0], q[1]);
+    else *reinterpret_cast<uint32_t*>(codes) = q[0];
+}
 
 // Where block b lies: its row and its first column.  SMALL: rows * L < 2^31.
 template <bool SMALL> __device__ __forceinline__ void place(long long b, int nb, Divisor by_nb, long long& row, int& c0)
@@ -43,7 +95,7 @@ __global__ void __launch_bounds__(256, 5) pack_vectors(const T* __restrict__ x, 
     pdl_launch();
     const int lane = threadIdx.x % LANES, col = lane * V;
     for (long long b0 = (long long)blockIdx.x * EACH * U + threadIdx.x / LANES; b0 - threadIdx.x / LANES < blocks; b0 += (long long)gridDim.x * EACH * U) {
-        Vec<T, V> r[U];
+        uint4 w[U];
         long long at[U];
         bool on[U];
 #pragma unroll
@@ -54,35 +106,34 @@ __global__ void __launch_bounds__(256, 5) pack_vectors(const T* __restrict__ x, 
             if (b < blocks) place<SMALL>(b, nb, by_nb, row, c0);
             on[u] = b < blocks && c0 + col < L;
             at[u] = row * L + c0 + col;
-            if (on[u]) r[u].load(x + at[u]);
+            w[u] = on[u] ? *reinterpret_cast<const uint4*>(x + at[u]) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        float top[U];
+        largest<LANES, U>(w, top, T());
+        // each of four lanes divides for one of the four blocks
+        float inv[U];
+        const int j = lane & (U - 1);
+        Scale s{0.0f, 0.0f};
+        if constexpr (LANES >= U) {
+            s = scale_of(j == 1 ? top[1] : j == 2 ? top[2] : j == 3 ? top[3] : top[0]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) inv[u] = __shfl_sync(0xFFFFFFFFu, s.inv, u, LANES);
+            if (lane < U && b0 + j * EACH < blocks) scales[b0 + j * EACH] = s.scale;
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s = scale_of(top[u]);
+                inv[u] = s.inv;
+                if (lane == 0 && b0 + u * EACH < blocks) scales[b0 + u * EACH] = s.scale;
+            }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float v[V], top = 0.0f;
-            if (on[u]) unpack(r[u], v);
-            unsigned bad = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (!on[u]) v[i] = 0.0f;
-                top = fmaxf(top, fabsf(v[i]));
-                bad |= not_finite(v[i]);
-            }
-            // a NaN among the values would be left out of the maximum: an infinity stands for it
-            if (bad) top = __int_as_float(0x7F800000);
-#pragma unroll
-            for (int o = LANES / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const Scale s = scale_of(top, not_finite(top));
+        for (int u = 0; u < U; ++u)
             if (on[u]) {
-                uint32_t q[V / 4];
-#pragma unroll
-                for (int i = 0; i < V; i += 4)
-                    q[i / 4] = __byte_perm(__byte_perm((uint32_t)code_of(v[i], s.inv), (uint32_t)code_of(v[i + 1], s.inv), 0x0040),
-                                           __byte_perm((uint32_t)code_of(v[i + 2], s.inv), (uint32_t)code_of(v[i + 3], s.inv), 0x0040), 0x5410);
-                if constexpr (V == 8) *reinterpret_cast<uint2*>(codes + at[u]) = make_uint2(q[0], q[1]);
-                else *reinterpret_cast<uint32_t*>(codes + at[u]) = q[0];
-                if (lane == 0) scales[b0 + u * EACH] = s.scale;
+                Pairs<V> f;
+                unpack2(w[u], f, T());
+                put_codes(f, inv[u], codes + at[u]);
             }
-        }
     }
 }
 
@@ -116,19 +167,14 @@ __global__ void __launch_bounds__(256) pack_anywhere(const T* __restrict__ x, lo
         for (int u = 0; u < U; ++u) {
             if (n[u] == 0) break;
             float top = 0.0f;
-            bool bad = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                top = fmaxf(top, fabsf(v[u][i]));
-                bad |= not_finite(v[u][i]);
-            }
-            if (bad) top = __int_as_float(0x7F800000);
+            for (int i = 0; i < 4; ++i) top = larger(top, v[u][i]);
 #pragma unroll
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const Scale s = scale_of(top, not_finite(top));
+            for (int o = 16; o; o >>= 1) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const Scale s = scale_of(top);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (lane + 32 * i < n[u]) codes[at[u] + 32 * i] = (int8_t)code_of(v[u][i], s.inv);
+                if (lane + 32 * i < n[u]) codes[at[u] + 32 * i] = s.inv == 0.0f ? (int8_t)0 : (int8_t)__float2int_rn(v[u][i] * s.inv);
             if (lane == 0) scales[b0 + u] = s.scale;
         }
     }
