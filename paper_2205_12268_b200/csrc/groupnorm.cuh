@@ -83,7 +83,9 @@ inline Plan plan_of(int N, int P, int C, int G, int es, bool backward, bool whol
         long long hi = 4096, lo = 512;
         if (!backward) hi = 8192;
         if (hi < 64LL * C / q.V) hi = 64LL * C / q.V;
-        long long t = N * nv / (B200_SMS * 8);
+        // Small maps: two or three tiles of each kind for an SM, that the end of a tile is met once.  (us, forward / backward, with eight: 4 x 64 x 64 x 256
+        // bf16 44 / 44, now 25 / 26; 24 x 60 x 50 x 40 fp32 39 / 40, now 24 / 27.)
+        long long t = N * nv / (B200_SMS * (backward ? 2 : 3));
         t = t < lo ? lo : t > hi ? hi : t;
         if (t < (nv + 4095) / 4096) t = (nv + 4095) / 4096;
         q.tile = (int)((t + step - 1) / step * step);

@@ -35,13 +35,14 @@ __device__ __forceinline__ void put_coef(float2* p, float a, float b)
     const unsigned ua = (a != a ? 0x7FFFFFFFu : __float_as_uint(a)) ^ NONE, ub = (b != b ? 0x7FFFFFFFu : __float_as_uint(b)) ^ NONE;
     asm volatile("st.relaxed.gpu.global.v2.u32 [%0], {%1, %2};" ::"l"(p), "r"(ua), "r"(ub) : "memory");
 }
-__device__ __forceinline__ bool get_coef(const float2* p, float2& v)
+__device__ __forceinline__ unsigned long long load_coef(const float2* p)
 {
     unsigned long long w;
     asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(w) : "l"(p) : "memory");
-    v = make_float2(__uint_as_float((unsigned)w ^ NONE), __uint_as_float((unsigned)(w >> 32) ^ NONE));
-    return (unsigned)w != 0u && (unsigned)(w >> 32) != 0u;
+    return w;
 }
+__device__ __forceinline__ bool is_there(unsigned long long w) { return (unsigned)w != 0u && (unsigned)(w >> 32) != 0u; }
+__device__ __forceinline__ float2 decode(unsigned long long w) { return make_float2(__uint_as_float((unsigned)w ^ NONE), __uint_as_float((unsigned)(w >> 32) ^ NONE)); }
 
 // One chunk: where its image's whole vectors start, its first vector, its vectors; the image, the tile and its end; values at the image's ends; its first
 // row among all images' (checkpoints).
@@ -374,24 +375,29 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 // the image's sums are known: usually long since
                 bool all = false;
                 const uint32_t limit = tc::c_wait_limit;
-                for (uint32_t i = 0; i < limit; ++i) {
-                    bool ok = true;
-                    if (active) {
+                constexpr int NG = ALIGNED ? 1 : V;
+                const float2* where[NG];
 #pragma unroll
-                        for (int j = 0; j < (ALIGNED ? 1 : VP); ++j) {
-                            const int g0 = ALIGNED ? g_first : a.dD.div(channel_at(2 * j)), g1 = ALIGNED ? g0 : a.dD.div(channel_at(2 * j + 1));
-                            float2 p0, p1;
-                            ok = get_coef(coef + g0, p0) && ok;
-                            if (ALIGNED || g1 == g0) p1 = p0;
-                            else ok = get_coef(coef + g1, p1) && ok;
-                            k0[j] = pair(p0.x, p1.x);
-                            k1[j] = pair(p0.y, p1.y);
-                        }
-                    }
-                    if (!ALIGNED && lane < h.front + h.back) {     // those of the edges too
-                        const long long f = lane < h.front ? (long long)lane : (long long)a.P * a.C - h.back + (lane - h.front);
-                        float2 p;
-                        ok = get_coef(coef + (int)(f % a.C) / a.D, p) && ok;
+                for (int e = 0; e < NG; ++e) where[e] = coef + (ALIGNED ? g_first : a.dD.div(channel_at(e)));
+                const float2* where_edge = coef;
+                if (!ALIGNED && lane < h.front + h.back) {         // that of an edge too
+                    const long long f = lane < h.front ? (long long)lane : (long long)a.P * a.C - h.back + (lane - h.front);
+                    where_edge = coef + (int)(f % a.C) / a.D;
+                }
+                for (uint32_t i = 0; i < limit; ++i) {
+                    if (!ALIGNED && !__all_sync(0xFFFFFFFFu, is_there(load_coef(where[0]))) && !*abort_flag) { __nanosleep(256); continue; }
+                    unsigned long long w[NG], we = ~0ull;          // (all on their way at once)
+#pragma unroll
+                    for (int e = 0; e < NG; ++e) w[e] = load_coef(where[e]);
+                    if (!ALIGNED && h.front + h.back) we = load_coef(where_edge);
+                    bool ok = is_there(we);
+#pragma unroll
+                    for (int e = 0; e < NG; ++e) ok = ok && is_there(w[e]);
+#pragma unroll
+                    for (int j = 0; j < (ALIGNED ? 1 : VP); ++j) {
+                        const float2 p0 = decode(w[ALIGNED ? 0 : 2 * j]), p1 = ALIGNED ? p0 : decode(w[ALIGNED ? 0 : 2 * j + 1]);
+                        k0[j] = pair(p0.x, p1.x);
+                        k1[j] = pair(p0.y, p1.y);
                     }
                     all = __all_sync(0xFFFFFFFFu, ok);
                     if (all || *abort_flag) break;
@@ -573,8 +579,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
         if (applying) {
             if (!ALIGNED && warp == 0 && edge_ch >= 0 && !skip) {
                 const int g = edge_ch / a.D;
-                float2 cf;
-                get_coef(coef + g, cf);
+                const float2 cf = decode(load_coef(coef + g));
                 const float w = a.gamma ? __ldg(a.gamma + edge_ch) : 1.0f, be = a.beta ? __ldg(a.beta + edge_ch) : 0.0f;
                 float r[1];
                 if constexpr (BWD) {
