@@ -27,7 +27,7 @@ constexpr int T = 256;                     // threads of a CTA
 constexpr int FAN = 16;                    // tiles whose channel sums are added up in one step
 constexpr int CTAS_FWD = 3, CTAS_BWD = 2;  // CTAs of an SM
 constexpr size_t LAG_BYTES = (size_t)24 << 20;
-constexpr int RING_GAP = B200_SMS * 3 / 2;         // ring: tiles of sums in flight, about half of the CTAs'
+constexpr int RING_GAP = B200_SMS * 3 / 2;         // ring: tiles of sums in flight, and what they finish behind
 
 struct Plan {
     int V, p, lanes, reps, slots;          // period of p vectors; `reps` periods side by side, or one in `slots` turns of the CTA

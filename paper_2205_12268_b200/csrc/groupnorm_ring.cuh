@@ -75,9 +75,11 @@ __device__ __forceinline__ Work work_of(const Args& a, unsigned ticket)
 
 template <typename X, bool BWD, bool KEPT> struct Ring {
     static constexpr int V = 16 / (int)sizeof(X);
-    // vectors of a thread and chunk: waiting for a chunk, reading its head and letting it go cost as much as two vectors (backward, two a chunk / this
-    // many)
-    static constexpr int K = BWD && !KEPT ? 3 : 4;
+    // Vectors of a thread and chunk: waiting for a chunk, reading its head and letting it go cost as much as two vectors.  (us, backward, two a chunk / as
+    // many as here: 12 x 96 x 320 x 64 fp32 95 / 86, 4 x 128 x 128 x 1024 bf16 148 / 136, from the checkpoint 198 / 156.)
+    static constexpr int K = BWD ? 4 : 6;
+    // and those whose instructions stand one after the other (a checkpoint's scales have to: they sit in registers)
+    static constexpr int UNROLL = KEPT ? K : 2;
     static constexpr int X_BYTES = KEPT ? K * T * V : K * T * 16;
     static constexpr int BYTES = X_BYTES + (BWD ? K * T * 16 : 0);
 };
@@ -453,17 +455,10 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
 
         // one chunk: f(u, vector of the chunk) for each of this thread's vectors
         auto each = [&](auto f) {
-            if (h.nvec == chunk) {
-                if (active) {
-#pragma unroll
-                    for (int u = 0; u < K; ++u) f(u, u * step + v_mine);
-                }
-            } else {
-#pragma unroll
-                for (int u = 0; u < K; ++u) {
-                    const int v = u * step + v_mine;
-                    if (active && v < h.nvec) f(u, v);
-                }
+#pragma unroll R::UNROLL
+            for (int u = 0; u < K; ++u) {
+                const int v = u * step + v_mine;
+                if (active && v < h.nvec) f(u, v);
             }
         };
         auto centred = [&](int u, int v, Pairs<V>& xc) {           // x - mean
