@@ -3,12 +3,18 @@
 // Four uses of one contraction kernel, D[128 x BN] += A[128 x 64] B[64 x BN] per step of the ring:
 //   FORWARD  A = x (rows x channels), B = BN/2 rows of Wg and BN/2 of Wu: a gate and its partner are BN/2 columns apart in the same lane of
 //            tensor memory, so the epilogue has both and writes y, rounded once.
-//   PARTS    the same product again, its epilogue reads dy and writes dG and dU (bf16, operands of what follows)
+//   PARTS    the same product again, its epilogue reads dy and writes dG and dU, operands of what follows
 //   DX       A = dG then dU (rows x F), B = Wg then Wu as they lie: [F][Cin] has the contraction outside, an operand whose columns are contiguous
 //   DW       A = dG or dU with the rows as contraction, B = x the same way: both lie with the contraction outside.  Few tiles (weights are small
 //            next to maps) are cut along the rows, partial sums in fp32 are added in order by a kernel of their own.
 // TMA (128-byte swizzle, no multicast) feeds a ring of stages, one thread issues the instructions, the accumulator is double-buffered, so the
 // epilogue of a tile runs under the products of the next one.  Sizes that are no multiples of a tile arrive as zeros from TMA.
+//
+// dG and dU are fp16 with a power of two for each row, and so are x and the weights as operands of DX and DW.  Rounded to bf16, dG would add an error as large as
+// the results' own rounding (2.4e-3 instead of 1.7e-3 against 64 bits); fp16 has three more bits at the same rate of the tensor cores, and bf16 values fit it
+// exactly once the largest is near its end.  Row r's factor 2^k(r) comes from bounds, |dG|, |dU| < 1.13 Cin max|dy_r| max|x_r| max|W|, so nothing overflows,
+// and what lies 2^-25 and more below a row's bound loses bits.  Products of the rows' sums DW need one factor for all: x_r is scaled by 2^(c - k(r)), with
+// the c that brings the largest |dy_r| max|x_r|^2 to the end of fp16; rows that lose bits of x are those that the sum does not notice.
 //
 // Where the contraction is long, tiles of 256 columns are the work of two CTAs on neighbouring SMs (PAIR, cta_group::2): 128 rows each, and each brings in half
 // of B for both, 32 KB a step instead of 48.  What bounds the loop then is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2):
@@ -62,8 +68,15 @@ struct Ctl {
     int abort_flag;
 };
 
+// Exponents: |v| < 2^E.  of the weights and of what rows bring to DW, with 512 added; each row's |dy| |x|.
+struct Exps { unsigned weights, rows; };
+constexpr int BIAS = 512;
+
 struct Args {
     int rows, Cin, F;
+    const Exps* exps;
+    const short* row_exp;
+    int log_cin;                           // Cin <= 2^log_cin
     int m_tiles, n_tiles, splits;          // DW: m_tiles counts those of dG and dU
     int act;
     const __nv_bfloat16* dy;
@@ -126,6 +139,28 @@ template <bool PR> __device__ __forceinline__ void commit(uint32_t bar)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
     else
         mma_commit(bar);
+}
+
+// ---- powers of two
+__device__ __forceinline__ float power(int n) { return __int_as_float((min(max(n, -126), 127) + 127) << 23); }
+__device__ __forceinline__ float times_power(float v, int n) { return v * power(n / 2) * power(n - n / 2); }
+struct Scales {
+    int base = 0, weights = 0, all = 0;    // k(r) = base - E(r); of the weights; c
+    __device__ __forceinline__ Scales() {}
+    __device__ __forceinline__ Scales(const Exps* e, int log_cin)
+    {
+        const int ew = (int)__ldcg(&e->weights) - BIAS, er = (int)__ldcg(&e->rows) - BIAS;
+        base = 13 - log_cin - ew;
+        weights = 15 - ew;
+        all = min(base + 15 - er, 100);
+    }
+    __device__ __forceinline__ int row(int e) const { return min(max(base - e, -120), 120); }
+};
+__device__ __forceinline__ uint32_t pack_half2(float a, float b)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
 }
 
 // Operand with the contraction outside: rows of 64 columns (128 bytes, swizzled), groups of 8 of the contraction 1024 bytes apart, the next 64 columns
@@ -191,9 +226,9 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* w, int
     }
 }
 
-// 16 columns of gates and their partners: y, or with dy (`d`, bf16 pairs) dG and dU.
+// 16 columns of gates and their partners: y, or with dy (`d`, bf16 pairs) dG and dU times the row's factor.
 template <int USE, int ACT>
-__device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t (&u)[16], const uint32_t* d, uint32_t* o, uint32_t* o2)
+__device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t (&u)[16], const uint32_t* d, float factor, uint32_t* o, uint32_t* o2)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -203,9 +238,9 @@ __device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t 
             const f2 r = mul2(v.a, w);
             o[i] = pack_bf16x2(r.x(), r.y());
         } else {
-            const f2 t = pair(bf16lo(d[i]), bf16hi(d[i])), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
-            o[i] = pack_bf16x2(r.x(), r.y());
-            o2[i] = pack_bf16x2(r2.x(), r2.y());
+            const f2 t = mul2(pair(bf16lo(d[i]), bf16hi(d[i])), both(factor)), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
+            o[i] = pack_half2(r.x(), r.y());
+            o2[i] = pack_half2(r2.x(), r2.y());
         }
     }
 }
@@ -322,8 +357,8 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            // D fp32, A and B bf16; bits 15 and 16: the contraction lies outside
-            constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_OUTER ? 1u : 0u) << 15) | ((B_OUTER ? 1u : 0u) << 16) |
+            // D fp32, A and B bf16 (bits 7 and 10) or fp16; bits 15 and 16: the contraction lies outside
+            constexpr uint32_t idesc = (1u << 4) | (Fm::GATES ? (1u << 7) | (1u << 10) : 0u) | ((A_OUTER ? 1u : 0u) << 15) | ((B_OUTER ? 1u : 0u) << 16) |
                                        ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
             // (this thread issues next to the epilogue's warps: little more than the instructions themselves stands in its loop)
             int s = 0, item = 0, held = -1, swaps = 0;
@@ -374,6 +409,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
         constexpr int MINE = (GATES ? BN / 2 : BN) / Fm::SHARES, N = 16;         // columns of the warp, and those at once
         const int width = GATES ? a.F : a.Cin, mhalf = a.m_tiles / 2;
         const bool sectors = width % 16 == 0 && ((reinterpret_cast<uintptr_t>(a.y) | reinterpret_cast<uintptr_t>(a.y2)) & 31u) == 0;
+        const Scales scales = USE == FORWARD ? Scales{} : Scales(a.exps, a.log_cin);
         int item = 0;
         for (int w = w_first; w < w_end; w += w_step, ++item) {
             int nt, mt, sp;
@@ -392,6 +428,12 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                     d[i / 2] = v.x; d[i / 2 + 1] = v.y; d[i / 2 + 2] = v.z; d[i / 2 + 3] = v.w;
                 }
             }
+            // the row's factor: of dG and dU, or what takes it (and the other operand's) away again
+            int n = 0;
+            if constexpr (USE == PARTS || USE == DX) n = on ? scales.row(a.row_exp[row]) : 0;
+            if constexpr (USE == DX) n = -(n + scales.weights);
+            if constexpr (USE == DW) n = -scales.all;
+            const float factor = power(USE == PARTS ? n : n / 2), second = power(n - n / 2);
             const int buf = item & 1;
             const uint32_t bph = (uint32_t)(item >> 1) & 1u;
             int ok = mbar_wait(smem_u32(&ctl->tfull[buf]), bph, abort_flag) ? 1 : 0;
@@ -418,7 +460,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 auto all = [&](auto act) {
 #pragma unroll
                     for (int c = 0; c < MINE / N; ++c)
-                        gates16<USE, decltype(act)::value>(v[c], p[c], USE == PARTS ? d + c * 8 : d, o + c * 8, USE == PARTS ? o2 + c * 8 : o2);
+                        gates16<USE, decltype(act)::value>(v[c], p[c], USE == PARTS ? d + c * 8 : d, factor, o + c * 8, USE == PARTS ? o2 + c * 8 : o2);
                 };
                 if (a.act == WCC_ACT_SILU) all(std::integral_constant<int, WCC_ACT_SILU>());
                 else if (a.act == WCC_ACT_GELU) all(std::integral_constant<int, WCC_ACT_GELU>());
@@ -438,6 +480,8 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 for (int c = 0; c < MINE / N; ++c) {
                     const int cols = width - col0 - c * N;
                     if (cols <= 0) break;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[c][i] = __float_as_uint(__uint_as_float(v[c][i]) * factor * second);
                     if (USE == DW && a.splits > 1) {
                         float* o = a.part + (((size_t)sp * 2 + (up ? 1 : 0)) * a.F + row) * a.Cin + col0 + c * N;
 #pragma unroll
@@ -474,6 +518,88 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
     }
 }
 
+// ---- operands in fp16
+// Exponents of the rows, and of the weights (rows behind them): a warp a row.  What is not finite counts for nothing.
+__device__ __forceinline__ int exponent_of(const __nv_bfloat16* p, int n, int lane)
+{
+    unsigned m = 0;
+    for (int i = lane * 8; i < n; i += 256) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + i));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned lo = w[k] & 0x7FFFu, hi = (w[k] >> 16) & 0x7FFFu;
+            if (lo < 0x7F80u) m = max(m, lo);
+            if (hi < 0x7F80u) m = max(m, hi);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    return (int)(m >> 7) - 126;
+}
+static __global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg,
+                                                        const __nv_bfloat16* __restrict__ Wu, int rows, int Cin, int F, short* __restrict__ row_exp, Exps* exps)
+{
+    __shared__ unsigned most[2];
+    pdl_wait();
+    pdl_launch();
+    if (threadIdx.x < 2) most[threadIdx.x] = 0;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const long long all = (long long)rows + 2 * F;
+    for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < all; r += (long long)gridDim.x * 8) {
+        if (r < rows) {
+            const int ey = exponent_of(dy + r * F, F, lane), ex = exponent_of(x + r * Cin, Cin, lane);
+            if (lane == 0) {
+                row_exp[r] = (short)(ey + ex);
+                atomicMax(&most[1], (unsigned)(ey + 2 * ex + BIAS));
+            }
+        } else {
+            const long long f = r - rows;
+            const int e = exponent_of(f < F ? Wg + f * Cin : Wu + (f - F) * Cin, Cin, lane);
+            if (lane == 0) atomicMax(&most[0], (unsigned)(e + BIAS));
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && most[0]) atomicMax(&exps->weights, most[0]);
+    if (threadIdx.x == 1 && most[1]) atomicMax(&exps->rows, most[1]);
+}
+// x and the weights in fp16 with their factors; x16 or W16 NULL: not wanted.
+static __global__ void __launch_bounds__(256) to_half(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg, const __nv_bfloat16* __restrict__ Wu,
+                                                      int rows, int Cin, int F, const short* __restrict__ row_exp, const Exps* exps, int log_cin, Divisor by_row, uint4* x16, uint4* W16)
+{
+    pdl_wait();
+    pdl_launch();
+    const Scales s(exps, log_cin);
+    const int per = Cin / 8;
+    const long long nx = x16 ? (long long)rows * per : 0, nw = W16 ? (long long)F * per : 0;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < nx + 2 * nw; i += (long long)gridDim.x * 256) {
+        const uint4* from;
+        uint4* to;
+        int n = s.weights;
+        if (i < nx) {
+            const long long row = nx < (1LL << 31) ? (long long)by_row.div((int)i) : i / per;
+            n = s.all - s.row(row_exp[row]);
+            from = reinterpret_cast<const uint4*>(x) + i;
+            to = x16 + i;
+        } else {
+            const long long j = i - nx;
+            from = j < nw ? reinterpret_cast<const uint4*>(Wg) + j : reinterpret_cast<const uint4*>(Wu) + (j - nw);
+            to = W16 + j;
+        }
+        const uint4 v = __ldg(from);
+        const float f = power(n / 2), g = power(n - n / 2);
+        auto two = [&](uint32_t w) {
+            float a = bf16lo(w) * f * g, b = bf16hi(w) * f * g;
+            // (a finite value never becomes an infinity, whatever the exponents)
+            if (fabsf(a) > 65504.0f && (w & 0x7F80u) != 0x7F80u) a = copysignf(65504.0f, a);
+            if (fabsf(b) > 65504.0f && (w & 0x7F800000u) != 0x7F800000u) b = copysignf(65504.0f, b);
+            return pack_half2(a, b);
+        };
+        *to = make_uint4(two(v.x), two(v.y), two(v.z), two(v.w));
+    }
+}
+
 // Partial sums of the weights' gradients, added in order, two values a thread, sixteen parts on their way at once.
 static __global__ void __launch_bounds__(128) add_parts(const float* __restrict__ part, int splits, size_t each, __nv_bfloat16* __restrict__ dWg,
                                                         __nv_bfloat16* __restrict__ dWu)
@@ -495,14 +621,14 @@ static __global__ void __launch_bounds__(128) add_parts(const float* __restrict_
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// [outer][inner] bf16, boxes of 64 x `box` rows.
-inline bool map_of(CUtensorMap* tm, const void* p, int inner, int outer, int box)
+// [outer][inner] bf16 or fp16, boxes of 64 x `box` rows.
+inline bool map_of(CUtensorMap* tm, const void* p, int inner, int outer, int box, bool half = false)
 {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer}, strides[1] = {(cuuint64_t)inner * 2};
     cuuint32_t boxes[2] = {64, (cuuint32_t)box}, steps[2] = {1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn(tm, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -568,7 +694,8 @@ inline wcc_status dx(const void* dG, const void* dU, const void* Wg, const void*
     a.n_tiles = ceil_div(a.Cin, bn);
     a.splits = 1;
     CUtensorMap A0, A1, B0, B1;
-    if (!map_of(&A0, dG, a.F, a.rows, BM) || !map_of(&A1, dU, a.F, a.rows, BM) || !map_of(&B0, Wg, a.Cin, a.F, KSTEP) || !map_of(&B1, Wu, a.Cin, a.F, KSTEP))
+    if (!map_of(&A0, dG, a.F, a.rows, BM, true) || !map_of(&A1, dU, a.F, a.rows, BM, true) || !map_of(&B0, Wg, a.Cin, a.F, KSTEP, true) ||
+        !map_of(&B1, Wu, a.Cin, a.F, KSTEP, true))
         return WCC_ERR_CUDA;
     return products<DX>(bn, two, A0, A1, B0, B1, a, di, st);
 }
@@ -595,23 +722,44 @@ inline wcc_status dw(const void* dG, const void* dU, const void* x, Args a, cons
     a.n_tiles = p.n_tiles;
     a.splits = p.splits;
     CUtensorMap A0, A1, B;
-    if (!map_of(&A0, dG, a.F, a.rows, KSTEP) || !map_of(&A1, dU, a.F, a.rows, KSTEP) || !map_of(&B, x, a.Cin, a.rows, KSTEP)) return WCC_ERR_CUDA;
+    if (!map_of(&A0, dG, a.F, a.rows, KSTEP, true) || !map_of(&A1, dU, a.F, a.rows, KSTEP, true) || !map_of(&B, x, a.Cin, a.rows, KSTEP, true)) return WCC_ERR_CUDA;
     const wcc_status s = products<DW>(p.bn, p.two, A0, A1, B, B, a, di, st);
     if (s != WCC_OK || p.splits == 1) return s;
     const size_t each = (size_t)a.F * a.Cin;
     return launch_overlapped(add_parts, dim3((unsigned)((each + 127) / 128)), dim3(128), 0, st, true, 1, a.part, p.splits, each, a.y, a.y2);
 }
 
-struct Layout { size_t dG, dU, part, total; };
+struct Layout { size_t exps, row_exp, dG, dU, x16, W16, part, total; };
 inline Layout layout_of(int rows, int Cin, int F)
 {
     Layout l;
-    l.dG = 0;
-    l.dU = align_up((size_t)rows * F * 2, 256);
-    l.part = 2 * l.dU;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t a = at; at = align_up(at + bytes, 256); return a; };
+    l.exps = take(sizeof(Exps));
+    l.row_exp = take((size_t)rows * 2);
+    l.dG = take((size_t)rows * F * 2);
+    l.dU = take((size_t)rows * F * 2);
+    l.x16 = take((size_t)rows * Cin * 2);
+    l.W16 = take((size_t)2 * F * Cin * 2);
     const DwPlan p = dw_plan(rows, Cin, F, B200_SMS);
-    l.total = l.part + (p.splits > 1 ? align_up((size_t)p.splits * 2 * F * Cin * 4, 256) : 0);
+    l.part = take(p.splits > 1 ? (size_t)p.splits * 2 * F * Cin * 4 : 0);
+    l.total = at;
     return l;
+}
+
+inline wcc_status operands(const void* dy, const void* x, const void* Wg, const void* Wu, const Args& a, Exps* exps, short* row_exp, void* x16, void* W16,
+                           const DeviceInfo& di, cudaStream_t st)
+{
+    const __nv_bfloat16 *px = static_cast<const __nv_bfloat16*>(x), *pg = static_cast<const __nv_bfloat16*>(Wg), *pu = static_cast<const __nv_bfloat16*>(Wu);
+    wcc_status s = launch_clear(exps, 256, st);
+    if (s != WCC_OK) return s;
+    const long long all = ((long long)a.rows + 2LL * a.F + 7) / 8, most = (long long)di.sms * 8;
+    s = launch_overlapped(exponents, dim3((unsigned)(all < most ? all : most)), dim3(256), 0, st, true, 1, static_cast<const __nv_bfloat16*>(dy), px, pg, pu, a.rows, a.Cin, a.F,
+                          row_exp, exps);
+    if (s != WCC_OK) return s;
+    const long long n = ((x16 ? (long long)a.rows : 0) + (W16 ? 2LL * a.F : 0)) * (a.Cin / 8), want = (n + 255) / 256;
+    return launch_overlapped(to_half, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1, px, pg, pu, a.rows, a.Cin, a.F, row_exp, exps, a.log_cin,
+                             divisor_of((unsigned)(a.Cin / 8)), static_cast<uint4*>(x16), static_cast<uint4*>(W16));
 }
 
 }  // namespace gt

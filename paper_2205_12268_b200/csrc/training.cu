@@ -177,18 +177,25 @@ wcc_status wcc_gated_bwd(const void* dy, const void* x, const void* Wg, const vo
     a.dy = static_cast<const __nv_bfloat16*>(dy);
     a.y = reinterpret_cast<__nv_bfloat16*>(w + l.dG);
     a.y2 = reinterpret_cast<__nv_bfloat16*>(w + l.dU);
+    while ((1 << a.log_cin) < Cin) ++a.log_cin;
+    gt::Exps* exps = reinterpret_cast<gt::Exps*>(w + l.exps);
+    short* row_exp = reinterpret_cast<short*>(w + l.row_exp);
+    a.exps = exps;
+    a.row_exp = row_exp;
+    char *x16 = w + l.x16, *W16 = w + l.W16;
+    if ((s = gt::operands(dy, x, Wg, Wu, a, exps, row_exp, dWg ? x16 : nullptr, dx ? W16 : nullptr, di, st)) != WCC_OK) return s;
     if ((s = gt::gates<gt::PARTS>(x, Wg, Wu, a, di, st)) != WCC_OK) return s;
     if (dWg) {
         gt::Args b = a;
         b.y = static_cast<__nv_bfloat16*>(dWg);
         b.y2 = static_cast<__nv_bfloat16*>(dWu);
         b.part = reinterpret_cast<float*>(w + l.part);
-        if ((s = gt::dw(a.y, a.y2, x, b, gt::dw_plan(rows, Cin, F, B200_SMS), di, st)) != WCC_OK) return s;
+        if ((s = gt::dw(a.y, a.y2, x16, b, gt::dw_plan(rows, Cin, F, B200_SMS), di, st)) != WCC_OK) return s;
     }
     if (dx) {
         gt::Args b = a;
         b.y = static_cast<__nv_bfloat16*>(dx);
-        if ((s = gt::dx(a.y, a.y2, Wg, Wu, b, di, st)) != WCC_OK) return s;
+        if ((s = gt::dx(a.y, a.y2, W16, W16 + (size_t)F * Cin * 2, b, di, st)) != WCC_OK) return s;
     }
     return WCC_OK;
 }
