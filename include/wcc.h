@@ -431,7 +431,9 @@ wcc_status wcc_gated_fwd(const void* x, const void* Wg, const void* Wu, int rows
 /*
  * Its backward pass.  Nothing is kept of the forward pass but x: g and u are computed again.
  *     dG = dy * u * act'(g),  dU = dy * act(g),   dx = dG Wg + dU Wu,   dWg = dG^T x,   dWu = dU^T x
- * dG and dU are rounded to bf16, as operands of the products (2^-9 of a term at most, on top of the results' own rounding).
+ * dG, dU, x and the weights enter the products as fp16 with a power of two for each row (of x, dy) and for the weights, from bounds, so that nothing
+ * overflows: a rounding of 2^-12 of a term at most, of what is at least 2^-28 of its row's bound 1.13 Cin max|dy_r| max|x_r| max|W|, on top of the results' own.
+ * A row with a NaN or an infinity gives such in its own row of dx and in the weights' gradients.
  *   dy in : bf16 [rows][F]            dx out: bf16 [rows][Cin], must not overlap the inputs; NULL: not wanted
  *   dWg, dWu out: bf16 [F][Cin], both NULL: not wanted
  *   ws    : scratch of at least wcc_gated_bwd_workspace_bytes(...) bytes of this call's sizes, 16-byte aligned

@@ -519,21 +519,22 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
 }
 
 // ---- operands in fp16
-// Exponents of the rows, and of the weights (rows behind them): eight lanes a row, 128 bytes of it a load.  What is not finite counts for nothing.
-__device__ __forceinline__ int exponent_of(const __nv_bfloat16* p, int n, int lane)
+// Exponents of the rows, and of the weights (rows behind them): eight lanes a row, or a warp where rows are long.  What is not finite counts for nothing.
+// (66306 rows of 64 and 256 values, a warp / eight lanes a row: 26 / 11 us; 8192 of 1024 and 4096 22 / 29.)
+template <int LANES> __device__ __forceinline__ int exponent_of(const __nv_bfloat16* p, int n, int lane)
 {
     const uint4* q = reinterpret_cast<const uint4*>(p);
     const int vectors = n / 8;
     unsigned m = 0;
 #pragma unroll 8
-    for (int i = lane; i < vectors; i += 8) {
+    for (int i = lane; i < vectors; i += LANES) {
         const uint4 v = __ldg(q + i);
         m = __vmaxu2(m, __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu)));
     }
     unsigned top = max(m & 0xFFFFu, m >> 16);
     if (top >= 0x7F80u) {                                   // once more without what is not finite
         top = 0;
-        for (int i = lane * 8; i < n; i += 64)
+        for (int i = lane * 8; i < n; i += LANES * 8)
             for (int k = 0; k < 8; ++k) {
                 const unsigned h = __bfloat16_as_ushort(p[i + k]) & 0x7FFFu;
                 if (h < 0x7F80u) top = max(top, h);
@@ -541,10 +542,11 @@ __device__ __forceinline__ int exponent_of(const __nv_bfloat16* p, int n, int la
     }
     __syncwarp();
 #pragma unroll
-    for (int o = 4; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    for (int o = LANES / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     return (int)(top >> 7) - 126;
 }
-static __global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg,
+template <int LANES>
+__global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg,
                                                         const __nv_bfloat16* __restrict__ Wu, int rows, int Cin, int F, short* __restrict__ row_exp, Exps* exps)
 {
     __shared__ unsigned most[2];
@@ -552,15 +554,16 @@ static __global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __r
     pdl_launch();
     if (threadIdx.x < 2) most[threadIdx.x] = 0;
     __syncthreads();
-    const int lane = threadIdx.x & 7;
-    const long long all = (long long)rows + 2 * F, step = (long long)gridDim.x * 32;
+    constexpr int EACH = 256 / LANES;
+    const int lane = threadIdx.x & (LANES - 1);
+    const long long all = (long long)rows + 2 * F, step = (long long)gridDim.x * EACH;
     unsigned top_w = 0, top_r = 0;
-    for (long long r0 = (long long)blockIdx.x * 32; r0 < all; r0 += step) {
+    for (long long r0 = (long long)blockIdx.x * EACH; r0 < all; r0 += step) {
         // (lanes without a row go along with the last one)
-        const long long r = min(r0 + (threadIdx.x >> 3), all - 1), f = r - rows;
+        const long long r = min(r0 + threadIdx.x / LANES, all - 1), f = r - rows;
         const bool row = r < rows;
-        const int ex = exponent_of(row ? x + r * Cin : f < F ? Wg + f * Cin : Wu + (f - F) * Cin, Cin, lane);
-        const int ey = exponent_of(row ? dy + r * F : dy, row ? F : 0, lane);
+        const int ex = exponent_of<LANES>(row ? x + r * Cin : f < F ? Wg + f * Cin : Wu + (f - F) * Cin, Cin, lane);
+        const int ey = exponent_of<LANES>(row ? dy + r * F : dy, row ? F : 0, lane);
         if (row) {
             if (lane == 0) row_exp[r] = (short)(ey + ex);
             top_r = max(top_r, (unsigned)(ey + 2 * ex + BIAS));
@@ -765,8 +768,10 @@ inline wcc_status operands(const void* dy, const void* x, const void* Wg, const 
     const __nv_bfloat16 *px = static_cast<const __nv_bfloat16*>(x), *pg = static_cast<const __nv_bfloat16*>(Wg), *pu = static_cast<const __nv_bfloat16*>(Wu);
     wcc_status s = launch_clear(exps, 256, st);
     if (s != WCC_OK) return s;
-    const long long all = ((long long)a.rows + 2LL * a.F + 31) / 32, most = (long long)di.sms * 8;
-    s = launch_overlapped(exponents, dim3((unsigned)(all < most ? all : most)), dim3(256), 0, st, true, 1, static_cast<const __nv_bfloat16*>(dy), px, pg, pu, a.rows, a.Cin, a.F,
+    const bool wide = a.F >= 2048 || a.Cin >= 2048;
+    const int each = wide ? 8 : 32;
+    const long long all = ((long long)a.rows + 2LL * a.F + each - 1) / each, most = (long long)di.sms * 8;
+    s = launch_overlapped(wide ? exponents<32> : exponents<8>, dim3((unsigned)(all < most ? all : most)), dim3(256), 0, st, true, 1, static_cast<const __nv_bfloat16*>(dy), px, pg, pu, a.rows, a.Cin, a.F,
                           row_exp, exps);
     if (s != WCC_OK) return s;
     const long long n = ((x16 ? (long long)a.rows : 0) + (W16 ? 2LL * a.F : 0)) * (a.Cin / 8), want = (n + 255) / 256;

@@ -2,8 +2,11 @@
 
 Tolerances.  Products of bf16 numbers are exact in fp32; a sum of n of them goes through at most n additions that round or cut off, so it is off by at
 most 2 n U times the sum of magnitudes (U = 2^-24).  Activations: sigmoid to 2^-20 + 4 U |z| of its value (2^x, a reciprocal); gelu's Phi to 2^-22 absolute
-(the approximation's 1.5e-7 of erf, halved, and its roundings), its derivative to 2^-21 (1 + |z|).  dG and dU are rounded to bf16 (2^-8 of
-their value: half a step), and so is every result."""
+(the approximation's 1.5e-7 of erf, halved, and its roundings), its derivative to 2^-21 (1 + |z|).  dG and dU are rounded to fp16 times a power of two
+for their row: half a step is 2^-11 of a value, and where fp16 ends 2^-25, at a scale at which the row's bound B = 1.13 Cin max|dy| max|x| max|W| is at least 2^9
+(2^13 but for the rounding up of Cin and of three maxima to powers of two): 2^-34 B.  x and the weights are exact but for what lies 2^-25 below a scale at which
+the largest is 2^14: 2^-39 of it.  In the weights' gradients the scale is that of the row with the largest B max|x|: 2^-25 of x at a factor of at most 2^14 and a
+scale of 2^23 and more for that product, 2^-34 of it for each row.  Every result is rounded to bf16 (2^-8 of its value: half a step)."""
 import pytest
 import torch
 
@@ -63,18 +66,22 @@ def _check_backward(dy, x, Wg, Wu, act, dx, dWg, dWu):
     ds = es + (dg if act != "relu" else 0) * 1.13 + ((g.abs() <= dg).double() if act == "relu" else 0)
     d = dy.double()
     G, Um = d * u * s, d * a
-    eG = _rounded(d.abs() * (du * s.abs() + (u.abs() + du) * ds) + 4 * U * G.abs(), G)
-    eU = _rounded(d.abs() * (1.13 * dg + ea) + 4 * U * Um.abs(), Um)
     F, rows = Wg.shape[0], x.shape[0]
     xd, wg, wu = x.double(), Wg.double(), Wu.double()
+    most = lambda t: torch.nan_to_num(t.abs(), posinf=0, neginf=0).amax(1, keepdim=True)
+    B = 1.13 * x.shape[1] * most(d) * most(xd) * max(wg.abs().max(), wu.abs().max())
+    half = lambda tol, want: tol + 2.0 ** -11 * (want.abs() + tol) + 2.0 ** -34 * B
+    eG = half(d.abs() * (du * s.abs() + (u.abs() + du) * ds) + 4 * U * G.abs(), G)
+    eU = half(d.abs() * (1.13 * dg + ea) + 4 * U * Um.abs(), Um)
     if dx is not None:
         want = G @ wg + Um @ wu
         tol = eG @ wg.abs() + eU @ wu.abs() + 2 * (2 * F) * U * ((G.abs() + eG) @ wg.abs() + (Um.abs() + eU) @ wu.abs())
+        tol = tol + 2.0 ** -39 * ((G.abs() + Um.abs()).sum(1, keepdim=True) * max(wg.abs().max(), wu.abs().max()))
         assert ((dx.double() - want).abs() <= _rounded(tol, want)).all()
     if dWg is not None:
         for got, M, e in ((dWg, G, eG), (dWu, Um, eU)):
             want = M.t() @ xd
-            tol = e.t() @ xd.abs() + 2 * (rows + 64) * U * ((M.abs() + e).t() @ xd.abs())
+            tol = e.t() @ xd.abs() + 2 * (rows + 64) * U * ((M.abs() + e).t() @ xd.abs()) + rows * 2.0 ** -34 * (B * most(xd)).max()
             assert ((got.double() - want).abs() <= _rounded(tol, want)).all()
 
 
@@ -125,6 +132,27 @@ def test_formula_against_differences(wcc):      # noqa: F811
             # h^2 = 1e-10 of third derivatives, 2^-53 / h = 1e-11 of the loss's terms, both times sums of some thousand terms
             assert abs((loss(*up) - loss(*down)) / 2e-5 - (grads[i] * v).sum()) <= 1e-6 * (grads[i].abs() * v.abs()).sum()
         _check_backward(dy, x, Wg, Wu, act, *wcc.gated_backward(dy, x, Wg, Wu, act=act))
+
+
+@pytest.mark.parametrize("dy_exp, x_exp, w_exp", [(-60, 0, 0), (40, 10, -20), (-100, 30, 20), (0, -40, 30), (20, 20, 20)])
+def test_scales_of_all_sizes(wcc, dy_exp, x_exp, w_exp):      # noqa: F811
+    """Powers of two in front of everything: fp16 alone would overflow or lose all."""
+    x, Wg, Wu, dy = _data(700, 136, 264, seed=12)
+    x, Wg, Wu, dy = x * 2.0 ** x_exp, Wg * 2.0 ** w_exp, Wu * 2.0 ** w_exp, dy * 2.0 ** dy_exp
+    for act in (None, "silu"):
+        _check_backward(dy, x, Wg, Wu, act, *wcc.gated_backward(dy, x, Wg, Wu, act=act))
+
+
+def test_rows_of_all_sizes(wcc):      # noqa: F811
+    """Rows whose gradients and inputs differ by many powers of two, rows of zeros among them: each row of dx is as good as alone."""
+    x, Wg, Wu, dy = _data(600, 72, 136, seed=13)
+    step = torch.arange(600, device="cuda")
+    x = x * torch.exp2(((step * 7) % 21 - 10).float())[:, None].bfloat16()
+    dy = dy * torch.exp2(-((step * 5) % 41).float())[:, None].bfloat16()
+    x[17], dy[18], x[19], dy[19] = 0, 0, 0, 0
+    out = wcc.gated_backward(dy, x, Wg, Wu)
+    _check_backward(dy, x, Wg, Wu, "silu", *out)
+    assert not out[0][18:20].any()
 
 
 def test_parts_of_the_result(wcc):      # noqa: F811
