@@ -180,6 +180,36 @@ __global__ void __launch_bounds__(256) pack_anywhere(const T* __restrict__ x, lo
     }
 }
 
+// Rows of up to 32 values that start anywhere: LANES lanes a row, U rows on the way at once.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256) pack_short(const T* __restrict__ x, long long rows, int L, int8_t* __restrict__ codes, float* __restrict__ scales)
+{
+    constexpr int EACH = 256 / LANES, U = 4;
+    pdl_wait();
+    pdl_launch();
+    const int lane = threadIdx.x % LANES;
+    for (long long r0 = (long long)blockIdx.x * EACH * U + threadIdx.x / LANES; r0 - threadIdx.x / LANES < rows; r0 += (long long)gridDim.x * EACH * U) {
+        float v[U], top[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * EACH;
+            v[u] = r < rows && lane < L ? (float)x[r * L + lane] : 0.0f;
+            top[u] = larger(0.0f, v[u]);
+        }
+#pragma unroll
+        for (int o = LANES / 2; o; o >>= 1)
+#pragma unroll
+            for (int u = 0; u < U; ++u) top[u] = larger(top[u], __shfl_xor_sync(0xFFFFFFFFu, top[u], o));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long r = r0 + u * EACH;
+            const Scale s = scale_of(top[u]);
+            if (r < rows && lane < L) codes[r * L + lane] = s.inv == 0.0f ? (int8_t)0 : (int8_t)__float2int_rn(v[u] * s.inv);
+            if (r < rows && lane == 0) scales[r] = s.scale;
+        }
+    }
+}
+
 // 16 bytes of output a thread, whatever the rows: codes and output are dense.  ROUND: a vector's values are of one block (L a multiple of V); else most often.
 template <typename T, bool SMALL, bool ROUND>
 __global__ void __launch_bounds__(256) restore_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales, long long total, int L, int nb,
@@ -271,7 +301,14 @@ wcc_status pack(const void* in, long long rows, int L, int8_t* codes, float* sca
         if (L <= BLOCK / 2) return launch_pack<T, FULL / 2>(x, blocks, L, nb, small, codes, scales, di, st);
         return launch_pack<T, FULL>(x, blocks, L, nb, small, codes, scales, di, st);
     }
-    const long long want = (blocks + 23) / 24, most = (long long)di.sms * 8;
+    const long long most = (long long)di.sms * 8;
+    if (L <= 32) {
+        const int lanes = L <= 2 ? 2 : L <= 4 ? 4 : L <= 8 ? 8 : L <= 16 ? 16 : 32;
+        const long long each = 4 * (256 / lanes), ctas = (rows + each - 1) / each;
+        auto kernel = lanes == 2 ? pack_short<T, 2> : lanes == 4 ? pack_short<T, 4> : lanes == 8 ? pack_short<T, 8> : lanes == 16 ? pack_short<T, 16> : pack_short<T, 32>;
+        return launch_overlapped(kernel, dim3((unsigned)(ctas < most ? ctas : most)), dim3(256), 0, st, true, 1, x, rows, L, codes, scales);
+    }
+    const long long want = (blocks + 23) / 24;
     return launch_overlapped(small ? pack_anywhere<T, true> : pack_anywhere<T, false>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, true, 1,
                              x, blocks, L, nb, divisor_of((unsigned)nb), codes, scales);
 }

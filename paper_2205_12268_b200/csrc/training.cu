@@ -136,7 +136,8 @@ wcc_status wcc_groupnorm_bwd(const void* dy, const void* x, const int8_t* codes,
     if (q.ring) s = dt == WCC_BF16 ? gn::ring_backward<__nv_bfloat16>(a, di, st) : gn::ring_backward<float>(a, di, st);
     else s = dt == WCC_BF16 ? gn::backward<__nv_bfloat16>(a, di, grid, st) : gn::backward<float>(a, di, grid, st);
     if (s != WCC_OK || !a.params) return s;
-    return launch_overlapped(gn::reduce_kernel, dim3((unsigned)ceil_div(2 * C, 32)), dim3(256), 0, st, true, 1, a.img, q.solo ? grid : N, C, dgamma, dbeta);
+    const int es = dt == WCC_BF16 ? 2 : 4, rows = gn::rows_path(P, C, groups, es, x == nullptr) ? gn::rows_grid(N, C, es, di.sms, true).blocks : q.solo ? grid : N;
+    return launch_overlapped(gn::reduce_kernel, dim3((unsigned)ceil_div(2 * C, 32)), dim3(256), 0, st, true, 1, a.img, rows, C, dgamma, dbeta);
 }
 
 wcc_status wcc_gated_fwd(const void* x, const void* Wg, const void* Wu, int rows, int Cin, int F, wcc_act act, void* y, void* stream)

@@ -7,7 +7,7 @@ from test_gpu_layer import wcc      # noqa: F401  (fixture)
 pytestmark = pytest.mark.gpu
 
 SHAPES = [(1,), (5,), (1, 1), (3, 127), (3, 128), (3, 129), (7, 257), (2, 3, 5, 16), (9, 64), (5, 70), (33, 320), (1000, 1), (17, 8192), (4, 1000), (301, 96),
-          (4096, 256), (3, 100003)]
+          (4096, 256), (3, 100003), (50000, 3), (777, 31), (5, 7), (100, 17), (64, 33)]
 DTYPES = [torch.float32, torch.bfloat16]
 
 

@@ -17,7 +17,8 @@ U, D = 2.0 ** -24, 1024
 # N, H, W, C, groups: one position, one channel a group, one group, odd channels and images off 16 bytes, periods beyond a CTA, one tile and many
 SIZES = [(1, 1, 1, 1, 1), (3, 1, 1, 8, 2), (9, 1, 1, 64, 64), (300, 1, 1, 1024, 32), (5, 1, 1, 2047, 89), (2, 3, 3, 7, 7), (1, 1, 17, 33, 11), (3, 6, 2, 6, 1),
          (2, 8, 12, 64, 16), (1, 5, 7, 130, 10), (2, 4, 6, 513, 27), (1, 3, 2, 8192, 1), (1, 3, 11, 8191, 1), (2, 40, 50, 70, 10), (3, 33, 65, 24, 3), (2, 31, 129, 58, 29),
-         (1, 64, 64, 32, 8), (5, 64, 48, 128, 4), (1, 200, 300, 3, 3), (2, 130, 120, 12, 4), (1, 60, 60, 1026, 2), (40, 20, 20, 96, 8), (1, 48, 48, 4096, 64)]
+         (1, 64, 64, 32, 8), (5, 64, 48, 128, 4), (1, 200, 300, 3, 3), (2, 130, 120, 12, 4), (1, 60, 60, 1026, 2), (40, 20, 20, 96, 8), (1, 48, 48, 4096, 64), (2000, 1, 1, 2048, 8), (70, 1, 1, 4096, 64),
+         (5000, 1, 1, 24, 3), (3, 1, 1, 144, 3)]
 DTYPES = [torch.float32, torch.bfloat16]
 
 
