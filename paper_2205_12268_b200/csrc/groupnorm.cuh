@@ -1,14 +1,15 @@
 // Group norm with an activation on channels-last maps [N][P][C], forward and backward.
 //
 // Statistics run over the positions and the D channels of a group, so every map is gone through twice: once for sums, once to apply them.  The
-// bytes bound it: x and y (forward), x, dy and dx (backward), each once, if the second time finds the map in L2.  So an image is cut into tiles
-// of whole positions, and one launch works through a list of tiles in the order
+// bytes bound it: x and y (forward), x, dy and dx (backward), each once, if the second time finds the map in L2.  Four ways:
+//  - images of one position whose groups are 2^k lanes of a warp (token rows): rows_forward, rows_backward, nothing is read twice;
+//  - other images of one tile: a CTA does sums and result of an image, and goes on to its next;
+//  - images of many tiles whose channels repeat within a CTA's vectors: groupnorm_ring.cuh;
+//  - images of many tiles and more channels than that (beyond 2048 bf16 or 1024 fp32, odd numbers beyond 256): one launch works through a list of tiles,
 //     sums of image 0 .. lag-1 | sums of image lag, apply image 0 (tile by tile in turn) | sums of image lag+1, apply image 1 | ...
-// with a lag of about 24 MB: far enough that the last of the sums is ready when the first CTA asks for it, near enough that the map is still in L2.
-// CTAs take tiles by a ticket, in order.  A tile only ever waits for tiles in front of it, so whichever CTAs are resident finish: the lowest
-// unfinished tile waits for nobody.  The last CTA to bring a tile's sums (by a count of arrivals) adds them all up in the tiles' order, so results
-// do not depend on the schedule, and raises the image's flag.
-// Images of one tile need none of that: a CTA does sums and result of an image, and goes on to its next.
+//    with a lag of about 24 MB.  CTAs take tiles by a ticket, in order.  A tile only ever waits for tiles in front of it, so whichever CTAs are resident finish:
+//    the lowest unfinished tile waits for nobody.  The last CTA to bring a tile's sums (by a count of arrivals) adds them all up in the tiles' order, so
+//    results do not depend on the schedule, and raises the image's flag.
 //
 // A thread meets the same channels all along: its vectors (of V values) are a multiple of the period p = C / gcd(C, V) vectors apart, so its
 // constants and sums sit in registers.  Periods longer than the CTA are gone through in slots of one vector a thread.

@@ -1,7 +1,7 @@
 // Group norm of images of many tiles, fed by a ring in shared memory.
 //
 // One thread of a CTA takes tickets and brings the tiles' vectors in by bulk copies, chunk by chunk, as far ahead as the ring has room: across the ends of
-// tiles, where the other 256 threads add up sums and hand them on.  So the memory stays busy meanwhile (some 80 KB in flight a CTA, two CTAs an SM),
+// tiles, where the other 256 threads add up sums and hand them on.  So the memory stays busy meanwhile (48 to 96 KB in flight a CTA, two CTAs an SM),
 // and the threads' registers hold constants and sums, not loads.
 //
 // The list of tiles has three kinds of items.  Step i of it: the sums of tile i; the result of tile i - delay; and, `gap` tiles behind the last sums of

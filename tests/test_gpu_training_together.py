@@ -47,7 +47,7 @@ def _off(a, b):
 def test_block_and_its_gradients(wcc):      # noqa: F811
     p = _setup()
     want = _autograd(p, 8)
-    # four roundings to bf16 in a row (h, dG and dU, dh, the result), each at most 2^-8 of a value and so of the norm; a factor of 2 for what the
+    # at most four roundings to bf16 in a row, each at most 2^-8 of a value and so of the norm; a factor of 2 for what the
     # gates' and the norm's derivatives make of one
     for got, w in zip(_step(wcc, p, 8, False), want):
         assert _off(got, w) <= 8 * 2.0 ** -8
@@ -94,7 +94,7 @@ def test_training_step_in_a_graph(wcc):      # noqa: F811
 
 
 def test_through_torch_autograd(wcc):      # noqa: F811
-    """The operators as the two halves of a torch function: an eager graph of the same leaves lives while the backward pass is captured."""
+    """The operators as the two halves of a torch function, which keeps a checkpoint between them."""
     p = _setup(seed=6)
 
     class Block(torch.autograd.Function):
@@ -113,10 +113,10 @@ def test_through_torch_autograd(wcc):      # noqa: F811
 
     leaves = [p[k].clone().requires_grad_() for k in ("x", "gamma", "beta")]
     dy = torch.randn_like(p["x"])
-    eager = torch.autograd.grad(Block.apply(*leaves), leaves, dy)
+    got = torch.autograd.grad(Block.apply(*leaves), leaves, dy)
     ck = wcc.checkpoint(p["x"])
     _, mean, rstd = wcc.groupnorm(p["x"], 8, p["gamma"], p["beta"], act="silu", stats=True)
-    for a, b in zip(eager, wcc.groupnorm_backward(dy, ck, mean, rstd, 8, p["gamma"], p["beta"], act="silu")):
+    for a, b in zip(got, wcc.groupnorm_backward(dy, ck, mean, rstd, 8, p["gamma"], p["beta"], act="silu")):
         assert torch.equal(a, b)
 
 
