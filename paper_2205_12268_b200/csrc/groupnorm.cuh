@@ -154,6 +154,10 @@ inline Layout layout_of(const Plan& q, int N, int C, int G, bool backward)
     return l;
 }
 
+// Vectors that a thread has on their way at once (backward: of either map): the narrower, the more, as far as registers go.
+template <int V> constexpr int LOADS_FWD = V == 1 ? 8 : 4;
+template <int V> constexpr int LOADS_BWD = V >= 4 ? 2 : 8 / V;
+
 // ---- pieces ----------------------------------------------------------------------------------------
 struct Stat { float n, mean, m2; };
 __device__ __forceinline__ Stat merge(Stat a, Stat b)
@@ -293,7 +297,7 @@ __device__ __forceinline__ void apply_tile(const Args& a, const X* x, X* y, int 
     const Plan& q = a.q;
     const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
     const int step = q.reps * q.p;
-    constexpr int U = 4;
+    constexpr int U = LOADS_FWD<V>;
     for (int j = 0; j < q.slots; ++j) {
         const int vq = j * T + lane;
         if (sub >= q.reps || vq >= q.p) continue;
@@ -544,7 +548,7 @@ __device__ __forceinline__ void sums_tile(const Args& a, int n, long long at, in
     const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
     const int step = q.reps * q.p, width = q.p * V;
     const X* dy = static_cast<const X*>(a.dy) + at;
-    constexpr int U = 2;
+    constexpr int U = LOADS_BWD<V>;
     for (int j = 0; j < q.slots; ++j) {
         const int vq = j * T + lane;
         if (sub >= q.reps || vq >= q.p) continue;
@@ -624,7 +628,7 @@ __device__ __forceinline__ void dx_tile(const Args& a, int n, long long at, int 
     const int step = q.reps * q.p;
     const X* dy = static_cast<const X*>(a.dy) + at;
     X* out = static_cast<X*>(a.out) + at;
-    constexpr int U = 2;
+    constexpr int U = LOADS_BWD<V>;
     for (int j = 0; j < q.slots; ++j) {
         const int vq = j * T + lane;
         if (sub >= q.reps || vq >= q.p) continue;
