@@ -38,7 +38,7 @@ enum Use { FORWARD, PARTS, DX, DW };
 
 constexpr int BM = 128, KSTEP = 64;
 constexpr int FEW = 32;                        // rows of a call that a stage of its own size holds
-
+constexpr int FEW_STAGES = 17;
 constexpr int HOLD_STEPS = 4;                  // HOLD: steps of weights that fit
 
 // A variant of the kernel: its use, columns of a tile, whether two CTAs share a tile (PAIR), whether the weights of a column tile stay in shared memory
@@ -53,7 +53,7 @@ template <int USE_, int BN_, bool PAIR_, bool HOLD_, int A_ROWS_ = BM> struct Fo
     static constexpr int A_ROWS = A_ROWS_, A_BYTES = A_ROWS * KSTEP * 2;
     static constexpr int STAGE_BYTES = HOLD ? A_BYTES : A_BYTES + B_BYTES;
     static constexpr int HELD_BYTES = HOLD ? HOLD_STEPS * B_BYTES : 0;
-    static constexpr int ROOM = (A_ROWS < BM ? 208 : 224) * 1024, MOST_STAGES = A_ROWS < BM ? 17 : 8;
+    static constexpr int ROOM = (A_ROWS < BM ? 208 : 224) * 1024, MOST_STAGES = A_ROWS < BM ? FEW_STAGES : 8;
     static constexpr int FIT = (ROOM - HELD_BYTES) / STAGE_BYTES;
     static constexpr int STAGES = FIT < MOST_STAGES ? FIT : MOST_STAGES;
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + HELD_BYTES + (A_ROWS < BM ? BM * KSTEP * 2 : 0);      // and Ctl
@@ -63,12 +63,13 @@ template <int USE_, int BN_, bool PAIR_, bool HOLD_, int A_ROWS_ = BM> struct Fo
 };
 
 struct Ctl {
-    uint64_t full[17], empty[17], tfull[2], tempty[2], bfull, bempty;
+    uint64_t full[FEW_STAGES], empty[FEW_STAGES], tfull[2], tempty[2], bfull, bempty;
     uint32_t tmem_base;
     int abort_flag;
 };
 
-// Exponents: |v| < 2^E.  of the weights and of what rows bring to DW, with 512 added; each row's |dy| |x|.
+// Exponents E, |v| < 2^E, with BIAS added: of the weights, and the largest over the rows of what they bring to DW, |dy_r| |x_r|^2.  (A row's own, of |dy_r| |x_r|,
+// are a list.)
 struct Exps { unsigned weights, rows; };
 constexpr int BIAS = 512;
 
@@ -143,7 +144,6 @@ template <bool PR> __device__ __forceinline__ void commit(uint32_t bar)
 
 // ---- powers of two
 __device__ __forceinline__ float power(int n) { return __int_as_float((min(max(n, -126), 127) + 127) << 23); }
-__device__ __forceinline__ float times_power(float v, int n) { return v * power(n / 2) * power(n - n / 2); }
 struct Scales {
     int base = 0, weights = 0, all = 0;    // k(r) = base - E(r); of the weights; c
     __device__ __forceinline__ Scales() {}
@@ -238,7 +238,8 @@ __device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t 
             const f2 r = mul2(v.a, w);
             o[i] = pack_bf16x2(r.x(), r.y());
         } else {
-            const f2 t = mul2(pair(bf16lo(d[i]), bf16hi(d[i])), both(factor)), r = mul2(mul2(t, w), v.d), r2 = mul2(t, v.a);
+            // (the factor last: dy alone times it might be too large)
+            const f2 t = pair(bf16lo(d[i]), bf16hi(d[i])), r = mul2(mul2(mul2(t, w), v.d), both(factor)), r2 = mul2(mul2(t, v.a), both(factor));
             o[i] = pack_half2(r.x(), r.y());
             o2[i] = pack_half2(r2.x(), r2.y());
         }

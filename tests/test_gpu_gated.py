@@ -134,7 +134,7 @@ def test_formula_against_differences(wcc):      # noqa: F811
         _check_backward(dy, x, Wg, Wu, act, *wcc.gated_backward(dy, x, Wg, Wu, act=act))
 
 
-@pytest.mark.parametrize("dy_exp, x_exp, w_exp", [(-60, 0, 0), (40, 10, -20), (-100, 30, 20), (0, -40, 30), (20, 20, 20)])
+@pytest.mark.parametrize("dy_exp, x_exp, w_exp", [(-60, 0, 0), (40, 10, -20), (-100, 30, 20), (0, -40, 30), (20, 20, 20), (60, -50, -60)])
 def test_scales_of_all_sizes(wcc, dy_exp, x_exp, w_exp):      # noqa: F811
     """Powers of two in front of everything: fp16 alone would overflow or lose all."""
     x, Wg, Wu, dy = _data(700, 136, 264, seed=12)
