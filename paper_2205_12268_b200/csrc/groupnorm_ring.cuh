@@ -17,6 +17,7 @@
 
 #include <type_traits>
 
+#include "feed.h"
 #include "groupnorm.cuh"
 
 namespace wcc {
@@ -83,8 +84,6 @@ template <typename X, bool BWD, bool KEPT> struct Ring {
     static constexpr int X_BYTES = KEPT ? K * T * V : K * T * 16;
     static constexpr int BYTES = X_BYTES + (BWD ? K * T * 16 : 0);
 };
-
-constexpr int AHEAD = 3;
 
 constexpr int POSTS = 4;               // tiles whose sums are stored and not yet counted
 
@@ -265,10 +264,8 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 v += n;
             }
             if (end) return;
-            // The next ticket is taken when AHEAD chunks of this tile are left, the first at the latest used up: early enough to bring the next tile in on time,
-            // and no earlier, so that no tile waits behind another while a CTA has nothing to do.
-            const int w = sent - 1 - AHEAD > first ? sent - 1 - AHEAD : first;
-            if (!tc::mbar_wait(tc::smem_u32(&c.empty[w % stages]), (uint32_t)(w / stages) & 1u)) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); return; }
+            const int w = awaited_chunk(first, sent, stages);
+            if (w >= 0 && !tc::mbar_wait(tc::smem_u32(&c.empty[w % stages]), (uint32_t)(w / stages) & 1u)) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); return; }
         }
     }
 
