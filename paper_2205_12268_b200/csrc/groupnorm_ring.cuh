@@ -11,6 +11,10 @@
 // A tile of sums ends with one barrier (the threads' sums are in shared memory), then each of the eight warps stores those of its share of the groups and
 // counts itself done.  What the last kind of item needs of a group is one word of 64 bits, which is zero until it is there (coded so that no result is zero).
 //
+// Every wait has a limit, the meetings of the 256 threads among them (an mbarrier, not bar.sync): a warp whose wait ran out says so, and the others give up at
+// their next wait, wherever they are.  What the threads of a warp do next goes by a vote, what the 256 do by a word that one of them wrote before they meet.
+// Whoever leaves early stays until copies that are on their way have landed.
+//
 // Vectors are the aligned 16 bytes of the whole tensor.  An image that starts or ends inside one has up to V - 1 values at either end that
 // belong to no vector of its own; they are the first and the last tile's edges, gone through one by one.
 #pragma once
@@ -27,7 +31,26 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void consumers() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// The T threads that compute meet: false if this or another wait of the CTA ran out (the same on all lanes of a warp, not on all warps).
+struct Meeting {
+    uint32_t bar, parity;
+    volatile int* abort_flag;
+    __device__ __forceinline__ bool operator()()
+    {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) tc::mbar_arrive(bar);
+        const bool ok = tc::mbar_wait(bar, parity, abort_flag);
+        parity ^= 1u;
+        return __all_sync(0xFFFFFFFFu, ok);
+    }
+};
+// A wait of this thread ran out, or another one's: the CTA stays until copies that are on their way have landed.
+__device__ __noinline__ void give_up(volatile int* abort_flag, int* status)
+{
+    *abort_flag = 1;
+    atomicExch(status, (int)WCC_ERR_TIMEOUT);
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+}
 
 // A group's two numbers as a word that is never zero: arithmetic gives no NaN of this pattern.
 constexpr unsigned NONE = 0xFFE5A5A5u;
@@ -88,15 +111,15 @@ template <typename X, bool BWD, bool KEPT> struct Ring {
 constexpr int POSTS = 4;               // tiles whose sums are stored and not yet counted
 
 struct RingCtl {
-    uint64_t full[8], empty[8], stored[POSTS];
+    uint64_t full[8], empty[8], stored[POSTS], meeting;
     int post[POSTS], posted;           // images of those tiles (-1: no more), tiles counted so far
     Head head[8];
-    int abort;
+    int abort, go;                     // a wait ran out; the sums to be finished are all there
     float partial[T];
 };
 
-// Finishes share `part_of` of image n's groups: all 256 threads.  scratch: room for the sums of a share's channels.
-template <bool BWD> __device__ __forceinline__ void finish(const Args& a, int n, int part_of, float* scratch, float* partial)
+// Finishes share `part_of` of image n's groups: all 256 threads.  scratch: room for the sums of a share's channels.  False: given up.
+template <bool BWD> __device__ __forceinline__ bool finish(const Args& a, int n, int part_of, float* scratch, float* partial, Meeting& meet)
 {
     const Plan& q = a.q;
     const int lo = (int)((long long)a.G * part_of / q.fin), hi = (int)((long long)a.G * (part_of + 1) / q.fin);
@@ -170,14 +193,14 @@ template <bool BWD> __device__ __forceinline__ void finish(const Args& a, int n,
                 else scratch[col] = v;
             }
         }
-        consumers();
+        if (!meet()) return false;
         if (split > 1) {
             for (int col = threadIdx.x; col < cols; col += T) {
                 float v = partial[col];
                 for (int k = 1; k < split; ++k) v += partial[k * cols + col];
                 scratch[col] = v;
             }
-            consumers();
+            if (!meet()) return false;
         }
         for (int g = lo + warp; g < hi; g += T / 32) {
             float c1 = 0.0f, c2 = 0.0f;
@@ -198,6 +221,7 @@ template <bool BWD> __device__ __forceinline__ void finish(const Args& a, int n,
             if (lane == 0) put_coef(a.coef + (size_t)n * a.G + g, -r * c1 * a.inv_count, -r * r * r * c2 * a.inv_count);
         }
     }
+    return true;
 }
 
 template <typename X, bool ALIGNED, bool BWD, bool KEPT>
@@ -212,7 +236,8 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) { tc::mbar_init(tc::smem_u32(&c.full[s]), 1); tc::mbar_init(tc::smem_u32(&c.empty[s]), T / 32); }
-        for (int i = 0; i < POSTS; ++i) tc::mbar_init(tc::smem_u32(&c.stored[i]), T / 32);
+        for (int i = 0; i < POSTS; ++i) { tc::mbar_init(tc::smem_u32(&c.stored[i]), T / 32); c.post[i] = -1; }
+        tc::mbar_init(tc::smem_u32(&c.meeting), T / 32);
         c.abort = 0;
         c.posted = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -243,7 +268,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
             const int vend = min(v + q.tile, nvec);
             int flags = HEAD_FIRST | it.flags;
             for (;;) {
-                if (!tc::mbar_wait(tc::smem_u32(&c.empty[s]), ph)) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); return; }
+                if (!tc::mbar_wait(tc::smem_u32(&c.empty[s]), ph, abort_flag)) { give_up(abort_flag, a.status); return; }
                 const int n = loads && vend > v ? min(vend - v, chunk) : 0;
                 if (!loads || v + n >= vend) flags |= HEAD_LAST;
                 c.head[s] = {at + front, v, n, it.n, it.tile, vend, flags, it.tile == 0 ? front : 0, it.tile == q.nt - 1 ? back : 0,
@@ -263,9 +288,12 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 flags &= ~HEAD_FIRST;
                 v += n;
             }
-            if (end) return;
+            if (end) {
+                if (*abort_flag) give_up(abort_flag, a.status);
+                return;
+            }
             const int w = awaited_chunk(first, sent, stages);
-            if (w >= 0 && !tc::mbar_wait(tc::smem_u32(&c.empty[w % stages]), (uint32_t)(w / stages) & 1u)) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); return; }
+            if (w >= 0 && !tc::mbar_wait(tc::smem_u32(&c.empty[w % stages]), (uint32_t)(w / stages) & 1u, abort_flag)) { give_up(abort_flag, a.status); return; }
         }
     }
 
@@ -274,7 +302,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
         // among them, some microseconds: not to be done by those who compute.
         if (lane != 0) return;
         for (int t = 0;; ++t) {
-            if (!tc::mbar_wait(tc::smem_u32(&c.stored[t % POSTS]), (uint32_t)(t / POSTS) & 1u)) return;
+            if (!tc::mbar_wait(tc::smem_u32(&c.stored[t % POSTS]), (uint32_t)(t / POSTS) & 1u, abort_flag)) { give_up(abort_flag, a.status); return; }
             const int n = c.post[t % POSTS];
             if (n < 0) return;
             asm volatile("fence.acq_rel.gpu;" ::: "memory");
@@ -308,30 +336,39 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
     f2 k0[ALIGNED ? 1 : VP], k1[ALIGNED ? 1 : VP];                 // backward, apply: dx = k t + k1 (x - mean) + k0
     float pivot = 0.0f;
     int count = 0;
-    bool skip = false;
     float scale[K];
 
-    // the warp's part of a tile's sums is stored (n: its image; -1: there are no more tiles)
+    Meeting meet{tc::smem_u32(&c.meeting), 0u, abort_flag};
+    // the warp's part of a tile's sums is stored (n: its image; -1: there are no more tiles); false: given up, nothing is counted
     int posts = 0;
     auto post = [&](int n) {
         __syncwarp();
+        bool room = true;
         if (lane == 0) {
             const uint32_t limit = tc::c_wait_limit;
-            for (uint32_t i = 0; i < limit && posts - *const_cast<volatile int*>(&c.posted) >= POSTS; ++i) __nanosleep(64);
-            if (warp == 0) c.post[posts % POSTS] = n;
-            tc::mbar_arrive(tc::smem_u32(&c.stored[posts % POSTS]));
+            room = posts - *const_cast<volatile int*>(&c.posted) < POSTS;
+            for (uint32_t i = 0; i < limit && !room && !*abort_flag; ++i) {
+                __nanosleep(64);
+                room = posts - *const_cast<volatile int*>(&c.posted) < POSTS;
+            }
+            if (room) {
+                if (warp == 0) c.post[posts % POSTS] = n;
+                tc::mbar_arrive(tc::smem_u32(&c.stored[posts % POSTS]));
+            }
         }
         ++posts;
+        return __all_sync(0xFFFFFFFFu, room) != 0;
     };
     int s = 0;
     uint32_t ph = 0;
     for (;;) {
-        if (!tc::mbar_wait(tc::smem_u32(&c.full[s]), ph)) {        // cannot be: the copies were issued
-            if (lane == 0) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); }
+        const bool here = tc::mbar_wait(tc::smem_u32(&c.full[s]), ph, abort_flag);
+        if (!__all_sync(0xFFFFFFFFu, here)) { give_up(abort_flag, a.status); return; }
+        const Head h = c.head[s];
+        if (h.flags & HEAD_END) {
+            if (!post(-1)) give_up(abort_flag, a.status);
             return;
         }
-        const Head h = c.head[s];
-        if (h.flags & HEAD_END) { post(-1); return; }
         const bool applying = (h.flags & HEAD_APPLY) != 0;
         // (asked for one chunk ahead)
         auto scales_of = [&](int ahead) {
@@ -357,11 +394,9 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     ok = load_acquire(a.ctl + 1 + h.n) == want;
                     if (!ok) __nanosleep(64);
                 }
-                if (!ok) { *abort_flag = 1; atomicExch(a.status, (int)WCC_ERR_TIMEOUT); }
+                c.go = ok;
             }
-            consumers();
-            if (!*abort_flag) finish<BWD>(a, h.n, h.tile, scratch, c.partial);
-            consumers();
+            if (!meet() || !*const_cast<volatile int*>(&c.go) || !finish<BWD>(a, h.n, h.tile, scratch, c.partial, meet) || !meet()) { give_up(abort_flag, a.status); return; }
             continue;
         }
         if (h.flags & HEAD_FIRST) {
@@ -383,8 +418,8 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     const long long f = lane < h.front ? (long long)lane : (long long)a.P * a.C - h.back + (lane - h.front);
                     where_edge = coef + (int)(f % a.C) / a.D;
                 }
-                for (uint32_t i = 0; i < limit; ++i) {
-                    if (!ALIGNED && !__all_sync(0xFFFFFFFFu, is_there(load_coef(where[0]))) && !*abort_flag) { __nanosleep(256); continue; }
+                for (uint32_t i = 0; i < limit && !all && !__any_sync(0xFFFFFFFFu, *abort_flag != 0); ++i) {
+                    if (!ALIGNED && !__all_sync(0xFFFFFFFFu, is_there(load_coef(where[0])))) { __nanosleep(256); continue; }
                     unsigned long long w[NG], we = ~0ull;          // (all on their way at once)
 #pragma unroll
                     for (int e = 0; e < NG; ++e) w[e] = load_coef(where[e]);
@@ -399,11 +434,9 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                         k1[j] = pair(p0.y, p1.y);
                     }
                     all = __all_sync(0xFFFFFFFFu, ok);
-                    if (all || *abort_flag) break;
-                    __nanosleep(128);
+                    if (!all) __nanosleep(128);
                 }
-                if (!all) { *abort_flag = 1; if (lane == 0) atomicExch(a.status, (int)WCC_ERR_TIMEOUT); }
-                skip = !__all_sync(0xFFFFFFFFu, all);
+                if (!all) { give_up(abort_flag, a.status); return; }
             }
             if (BWD || applying) {
                 const float *mp = BWD ? a.mean + (size_t)h.n * a.G : nullptr, *rp = BWD ? a.rstd + (size_t)h.n * a.G : nullptr;
@@ -522,7 +555,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
             else chunk_of(std::integral_constant<int, WCC_ACT_NONE>(), final);
         };
         if (applying) {
-            if (!skip) by_act(std::true_type());
+            by_act(std::true_type());
         } else if constexpr (BWD) {
             by_act(std::false_type());
         } else {
@@ -569,7 +602,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
         }
         const float2* const coef = a.coef + (size_t)h.n * a.G;
         if (applying) {
-            if (!ALIGNED && warp == 0 && edge_ch >= 0 && !skip) {
+            if (!ALIGNED && warp == 0 && edge_ch >= 0) {
                 const int g = edge_ch / a.D;
                 const float2 cf = decode(load_coef(coef + g));
                 const float w = a.gamma ? __ldg(a.gamma + edge_ch) : 1.0f, be = a.beta ? __ldg(a.beta + edge_ch) : 0.0f;
@@ -588,7 +621,6 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 }
                 out[edge_at] = (X)r[0];
             }
-            skip = false;
             continue;
         }
         uint8_t* const mine = buffers + buffer * buffer_bytes;
@@ -610,7 +642,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     }
                 }
             }
-            consumers();
+            if (!meet()) { give_up(abort_flag, a.status); return; }
             // The tile's groups: first the mean, then the squared deviations from it.  The group's channels among the entries: value f of a
             // period is channel (f + shift) mod C.
             Stat* part = reinterpret_cast<Stat*>(a.part) + ((size_t)h.n * q.nt + h.tile) * a.G;
@@ -644,7 +676,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 m2 = warp_sum(m2);
                 if (lane == 0) part[g] = {n, mu, m2};
             }
-            post(h.n);
+            if (!post(h.n)) { give_up(abort_flag, a.status); return; }
         } else {
             float* sums = reinterpret_cast<float*>(mine);
             const int second = rows * width;
@@ -665,7 +697,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     *reinterpret_cast<unsigned long long*>(sums + second + row + 2 * i) = s2.v[i].w;
                 }
             }
-            consumers();
+            if (!meet()) { give_up(abort_flag, a.status); return; }
             float et = 0.0f, etx = 0.0f;
             if (!ALIGNED && edge_ch >= 0) {
                 const int g = edge_ch / a.D;
@@ -704,7 +736,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     part[a.C + ch] = v2;
                 }
             }
-            post(h.n);
+            if (!post(h.n)) { give_up(abort_flag, a.status); return; }
         }
     }
 }
