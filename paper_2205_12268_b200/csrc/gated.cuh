@@ -354,6 +354,11 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                     if (++s == ST) { s = 0; ph ^= 1u; }
                 }
             }
+            // the products' arrivals at this CTA's barriers (PAIR: from the other CTA) are all there before it goes
+            for (int i = 0; i < ST && !failed; ++i) {
+                failed = !mbar_wait(smem_u32(&ctl->empty[s]), ph, abort_flag);
+                if (++s == ST) { s = 0; ph ^= 1u; }
+            }
         }
         __syncwarp();
     } else if (warp == 1) {
