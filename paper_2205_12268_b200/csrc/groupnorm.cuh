@@ -813,14 +813,16 @@ inline bool rows_path(int P, int C, int G, int es, bool whole_rows)
     const int V = 16 / es, D = C / G, lanes = D / V;
     return P == 1 && D % V == 0 && lanes <= 32 && (lanes & (lanes - 1)) == 0 && (!whole_rows || C % 16 == 0);
 }
-struct RowsGrid { int each, slots, blocks; };                  // rows of a CTA at once, CTAs side by side along a row, CTAs along the rows
-inline RowsGrid rows_grid(int N, int C, int es, int sms, bool backward)
+// Rows of a CTA at once, CTAs side by side along a row, CTAs along the rows: by the sizes alone, so that the order of the gradients' sums is, and their rows of
+// partial sums fit a workspace (laid out without a device).
+struct RowsGrid { int each, slots, blocks; };
+inline RowsGrid rows_grid(int N, int C, int es, bool backward)
 {
     RowsGrid g;
     const int per = C * es / 16;
     g.each = per < T ? T / per : 1;
     g.slots = (per + T - 1) / T;
-    const int want = (N + g.each - 1) / g.each, most = sms * (backward ? CTAS_BWD : 8) / g.slots;
+    const int want = (N + g.each - 1) / g.each, most = B200_SMS * (backward ? CTAS_BWD : 8) / g.slots;
     g.blocks = want < most ? want : most > 0 ? most : 1;
     return g;
 }
@@ -1026,7 +1028,7 @@ wcc_status forward(const Args& a, const DeviceInfo& di, cudaStream_t st)
 {
     const Plan& q = a.q;
     if (rows_path(a.P, a.C, a.G, (int)sizeof(X), false)) {
-        const RowsGrid g = rows_grid(a.N, a.C, (int)sizeof(X), di.sms, false);
+        const RowsGrid g = rows_grid(a.N, a.C, (int)sizeof(X), false);
         return launch_overlapped(rows_forward<X>, dim3((unsigned)g.blocks, (unsigned)g.slots), dim3(T), 0, st, true, 1, a, g.each);
     }
     if constexpr (sizeof(X) == 2)
@@ -1052,7 +1054,7 @@ wcc_status backward(const Args& a, const DeviceInfo& di, int grid, cudaStream_t 
     const Plan& q = a.q;
     const bool kept = a.x == nullptr;
     if (rows_path(a.P, a.C, a.G, (int)sizeof(X), kept)) {
-        const RowsGrid g = rows_grid(a.N, a.C, (int)sizeof(X), di.sms, true);
+        const RowsGrid g = rows_grid(a.N, a.C, (int)sizeof(X), true);
         return launch_overlapped(kept ? rows_backward<X, true> : rows_backward<X, false>, dim3((unsigned)g.blocks, (unsigned)g.slots), dim3(T), 0, st, true, 1, a, g.each);
     }
     if constexpr (sizeof(X) == 2)

@@ -130,13 +130,13 @@ wcc_status wcc_groupnorm_bwd(const void* dy, const void* x, const int8_t* codes,
     gn::Args a = groupnorm_args(N, P, C, groups, act, q, l, ws, di);
     a.dy = dy; a.x = x; a.codes = codes; a.scales = scales; a.out = dx; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.params = dgamma || dbeta;
-    const int grid = gn::grid_of(q, N, di.sms < B200_SMS ? di.sms : B200_SMS, true);
+    const int grid = gn::grid_of(q, N, B200_SMS, true);
     a.img_beta = 0; a.img_gamma = C; a.img_row = 2LL * C;
     if (!q.solo && (s = launch_clear(a.ctl, l.part - l.ctl, st)) != WCC_OK) return s;
     if (q.ring) s = dt == WCC_BF16 ? gn::ring_backward<__nv_bfloat16>(a, di, st) : gn::ring_backward<float>(a, di, st);
     else s = dt == WCC_BF16 ? gn::backward<__nv_bfloat16>(a, di, grid, st) : gn::backward<float>(a, di, grid, st);
     if (s != WCC_OK || !a.params) return s;
-    const int es = dt == WCC_BF16 ? 2 : 4, rows = gn::rows_path(P, C, groups, es, x == nullptr) ? gn::rows_grid(N, C, es, di.sms, true).blocks : q.solo ? grid : N;
+    const int es = dt == WCC_BF16 ? 2 : 4, rows = gn::rows_path(P, C, groups, es, x == nullptr) ? gn::rows_grid(N, C, es, true).blocks : q.solo ? grid : N;
     return launch_overlapped(gn::reduce_kernel, dim3((unsigned)ceil_div(2 * C, 32)), dim3(256), 0, st, true, 1, a.img, rows, C, dgamma, dbeta);
 }
 
