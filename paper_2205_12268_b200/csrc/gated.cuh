@@ -182,8 +182,8 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ Act2 act_of(f2 z)
     if constexpr (ACT == WCC_ACT_RELU)
         return {pair(z.x() < 0.0f ? 0.0f : z.x(), z.y() < 0.0f ? 0.0f : z.y()), pair(z.x() > 0.0f ? 1.0f : 0.0f, z.y() > 0.0f ? 1.0f : 0.0f)};
     if constexpr (ACT == WCC_ACT_SILU) {
-        const f2 s = sigmoid2(z), a = mul2(z, s);
-        return {a, SLOPE ? fma2(a, fma2(s, both(-1.0f), one), s) : one};
+        const Sigmoid2 q = sigmoid2(z);
+        return {mul2(z, q.s), SLOPE ? silu_slope2(z, q) : one};
     }
     if constexpr (ACT == WCC_ACT_GELU) {
         const f2 x = pair(fminf(fabsf(z.x()), 42.0f), fminf(fabsf(z.y()), 42.0f));

@@ -891,7 +891,7 @@ __global__ void __launch_bounds__(T) rows_forward(const __grid_constant__ Args a
             for (int i = 0; i < VP; ++i) {
                 f2 z = fma2(f.v[i], mul2(w[i], both(rstd)), b[i]);
                 if (a.act == WCC_ACT_RELU) z = pair(z.x() < 0.0f ? 0.0f : z.x(), z.y() < 0.0f ? 0.0f : z.y());
-                else if (a.act == WCC_ACT_SILU) z = mul2(z, sigmoid2(z));
+                else if (a.act == WCC_ACT_SILU) z = silu2(z);
                 f.v[i] = z;
             }
             *reinterpret_cast<uint4*>(y + r * a.C + c) = pack2(f, X());
@@ -951,8 +951,7 @@ __global__ void __launch_bounds__(T, CTAS_BWD) rows_backward(const __grid_consta
                 if (a.act == WCC_ACT_RELU) {
                     t.v[i] = pair(z.x() > 0.0f ? t.v[i].x() : 0.0f, z.y() > 0.0f ? t.v[i].y() : 0.0f);
                 } else {
-                    const f2 e = sigmoid2(z);
-                    t.v[i] = mul2(t.v[i], fma2(mul2(z, e), fma2(e, both(-1.0f), both(1.0f)), e));
+                    t.v[i] = mul2(t.v[i], silu_slope2(z, sigmoid2(z)));
                 }
             }
             s0[i] = add2(s0[i], t.v[i]);

@@ -523,8 +523,8 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                             const f2 z = fma2(xc.v[i], k.v[i], b.v[i]);
                             t.v[i] = pair(z.x() > 0.0f ? t.v[i].x() : 0.0f, z.y() > 0.0f ? t.v[i].y() : 0.0f);
                         } else if constexpr (ACT == WCC_ACT_SILU) {
-                            const f2 z = fma2(xc.v[i], k.v[i], b.v[i]), g = sigmoid2(z);
-                            t.v[i] = mul2(t.v[i], fma2(mul2(z, g), fma2(g, both(-1.0f), both(1.0f)), g));
+                            const f2 z = fma2(xc.v[i], k.v[i], b.v[i]);
+                            t.v[i] = mul2(t.v[i], silu_slope2(z, sigmoid2(z)));
                         }
                         if constexpr (!APPLY) {
                             s1.v[i] = add2(s1.v[i], t.v[i]);
@@ -543,7 +543,7 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                     for (int i = 0; i < VP; ++i) {
                         f.v[i] = fma2(f.v[i], k.v[i], b.v[i]);
                         if constexpr (ACT == WCC_ACT_RELU) f.v[i] = pair(f.v[i].x() < 0.0f ? 0.0f : f.v[i].x(), f.v[i].y() < 0.0f ? 0.0f : f.v[i].y());
-                        else if constexpr (ACT == WCC_ACT_SILU) f.v[i] = mul2(f.v[i], sigmoid2(f.v[i]));
+                        else if constexpr (ACT == WCC_ACT_SILU) f.v[i] = silu2(f.v[i]);
                     }
                     *reinterpret_cast<uint4*>(dst + v * V) = pack2(f, X());
                 });

@@ -128,12 +128,27 @@ template <int V> __device__ __forceinline__ void pack(Vec<__nv_bfloat16, V>& v, 
 __device__ __forceinline__ float sigmoid(float z) { return rcp_approx(1.0f + exp2_approx(-1.4426950408889634f * z)); }
 
 // Two at once with one reciprocal, 1/a = b / (a b): the unit of 2^x and of reciprocals gives 16 results a clock and SM and bounds the backward pass of
-// group norm with its four a value (three this way).  Below z = -43 the result stays e^-43 = 2e-19, so that a b does not overflow.
-__device__ __forceinline__ f2 sigmoid2(f2 z)
+// group norm with its four a value (three this way).  With t = e^z: 1 - s = 1 / (1 + t), s = t (1 - s), both to fp32's digits however small.  Above z = 43 t stays
+// e^43, so that a b does not overflow: s is 1 long since.  (Held from below instead, as 1 / (1 + e^-z), s does not fall under e^-43, and z s is anything.)
+struct Sigmoid2 { f2 s, rest; };           // sigmoid, 1 - sigmoid
+__device__ __forceinline__ Sigmoid2 sigmoid2(f2 z)
 {
-    const f2 v = mul2(pair(fmaxf(z.x(), -43.0f), fmaxf(z.y(), -43.0f)), both(-1.4426950408889634f));
-    const f2 a = add2(pair(exp2_approx(v.x()), exp2_approx(v.y())), both(1.0f));
-    return mul2(both(rcp_approx(a.x() * a.y())), pair(a.y(), a.x()));
+    const f2 v = mul2(pair(fminf(z.x(), 43.0f), fminf(z.y(), 43.0f)), both(1.4426950408889634f));
+    const f2 t = pair(exp2_approx(v.x()), exp2_approx(v.y())), a = add2(t, both(1.0f));
+    const f2 rest = mul2(both(rcp_approx(a.x() * a.y())), pair(a.y(), a.x()));
+    return {mul2(t, rest), rest};
+}
+__device__ __forceinline__ float min_nan(float a, float b)
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ f2 silu2(f2 z) { return mul2(z, sigmoid2(z).s); }
+// s + z s (1 - s), z held at 43 as well: 1 - s is.  (A NaN stays one, and is its own value's alone.)
+__device__ __forceinline__ f2 silu_slope2(f2 z, const Sigmoid2& q)
+{
+    return fma2(mul2(pair(min_nan(z.x(), 43.0f), min_nan(z.y(), 43.0f)), q.s), q.rest, q.s);
 }
 
 // Values of a vector as pairs.
