@@ -12,9 +12,12 @@
 //
 // dG and dU are fp16 with a power of two for each row, and so are x and the weights as operands of DX and DW.  Rounded to bf16, dG would add an error as large as
 // the results' own rounding (2.4e-3 instead of 1.7e-3 against 64 bits); fp16 has three more bits at the same rate of the tensor cores, and bf16 values fit it
-// exactly once the largest is near its end.  Row r's factor 2^k(r) comes from bounds, |dG|, |dU| < 1.13 Cin max|dy_r| max|x_r| max|W|, so nothing overflows,
-// and what lies 2^-25 and more below a row's bound loses bits.  Products of the rows' sums DW need one factor for all: x_r is scaled by 2^(c - k(r)), with
-// the c that brings the largest |dy_r| max|x_r|^2 to the end of fp16; rows that lose bits of x are those that the sum does not notice.
+// exactly once the largest is near its end.  Row r's factor 2^k(r) comes from bounds, |dG| < 1.13 Cin max|dy_r| max|x_r| max|Wu| and |dU| the same with Wg (one for
+// each: with the larger weights' bound for both, the other's part has fewer digits the more the two differ, none at 10^8).  With Cin and the maxima rounded up to
+// powers of two the bound lies between 2^9 and 2^13.2, so nothing overflows, and a value has all of fp16's digits down to 2^-14: 2^-23 to 2^-27 of the bound.
+// The weights have a factor each, their largest between 2^14 and 2^15; the products of DX then have the same power of two in both halves.  DW's need one
+// for all rows: x_r is scaled by 2^(c - k(r)), with the c that brings the largest |dy_r| max|x_r|^2 to the end of fp16; x has all of its bits (bf16: eight) in rows
+// where that is 2^-29 of the largest and more, times what x itself lies below its row's largest.
 //
 // Where the contraction is long, tiles of 256 columns are the work of two CTAs on neighbouring SMs (PAIR, cta_group::2): 128 rows each, and each brings in half
 // of B for both, 32 KB a step instead of 48.  What bounds the loop then is the bytes that a ring can have on their way (192 KB at 1.5 us or so from L2):
@@ -68,9 +71,9 @@ struct Ctl {
     int abort_flag;
 };
 
-// Exponents E, |v| < 2^E, with BIAS added: of the weights, and the largest over the rows of what they bring to DW, |dy_r| |x_r|^2.  (A row's own, of |dy_r| |x_r|,
-// are a list.)
-struct Exps { unsigned weights, rows; };
+// Exponents E, |v| < 2^E, with BIAS added: of either weights and of x, and the largest over the rows of what they bring to DW, |dy_r| |x_r|^2.  (A row's own,
+// E(r) of |dy_r| |x_r|, are a list.)
+struct Exps { unsigned Wg, Wu, rows, x; };
 constexpr int BIAS = 512;
 
 struct Args {
@@ -144,17 +147,30 @@ template <bool PR> __device__ __forceinline__ void commit(uint32_t bar)
 
 // ---- powers of two
 __device__ __forceinline__ float power(int n) { return __int_as_float((min(max(n, -126), 127) + 127) << 23); }
+// With row r's E(r): dG is scaled by 2^(dG - E(r)), dU by 2^(dU - E(r)), x of DW by 2^(x + E(r)), the weights by 2^Wg and 2^Wu.  No power is held to what fp32 has:
+// where one goes beyond it (tiny rows, weights of zeros), it is multiplied by in two steps, dG's and dU's by way of dy.  What these do not reach is 0: of the sums
+// u (or g) of rows where Cin max|x_r| max|Wu| is below 2^-114.
+// With row r's e = row(E(r)): dG is scaled by 2^(dG - e), dU by 2^(dU - e), x of DW by 2^(x + e), the weights by 2^Wg and 2^Wu.  row() keeps dG's and dU's powers
+// in fp32: below, for values that are larger than the bound allows; above, rows for which one of the two bounds is less than 2^-114 are scaled by less.  Weights of
+// zeros go as large as the others.
 struct Scales {
-    int base = 0, weights = 0, all = 0;    // k(r) = base - E(r); of the weights; c
+    int dG = 0, dU = 0, Wg = 0, Wu = 0, x = 0, lo = 0, hi = 0;
     __device__ __forceinline__ Scales() {}
     __device__ __forceinline__ Scales(const Exps* e, int log_cin)
     {
-        const int ew = (int)__ldcg(&e->weights) - BIAS, er = (int)__ldcg(&e->rows) - BIAS;
-        base = 13 - log_cin - ew;
-        weights = 15 - ew;
-        all = min(base + 15 - er, 100);
+        int eg = (int)__ldcg(&e->Wg) - BIAS, eu = (int)__ldcg(&e->Wu) - BIAS;
+        const int least = -126, er = (int)__ldcg(&e->rows) - BIAS, ex = (int)__ldcg(&e->x) - BIAS;
+        if (eg == least) eg = eu;
+        if (eu == least) eu = eg;
+        dG = 13 - log_cin - eu;
+        dU = 13 - log_cin - eg;
+        Wg = 15 - eg;
+        Wu = 15 - eu;
+        lo = max(dG, dU) - 127;
+        hi = min(dG, dU) + 126;
+        x = 15 - max(er, lo + ex);
     }
-    __device__ __forceinline__ int row(int e) const { return min(max(base - e, -120), 120); }
+    __device__ __forceinline__ int row(int E) const { return min(max(E, lo), hi); }
 };
 __device__ __forceinline__ uint32_t pack_half2(float a, float b)
 {
@@ -226,9 +242,9 @@ __device__ __forceinline__ void store16(__nv_bfloat16* p, const uint32_t* w, int
     }
 }
 
-// 16 columns of gates and their partners: y, or with dy (`d`, bf16 pairs) dG and dU times the row's factor.
+// 16 columns of gates and their partners: y, or with dy (`d`, bf16 pairs) dG and dU times the row's factors.
 template <int USE, int ACT>
-__device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t (&u)[16], const uint32_t* d, float factor, uint32_t* o, uint32_t* o2)
+__device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t (&u)[16], const uint32_t* d, float fg, float fu, uint32_t* o, uint32_t* o2)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -239,7 +255,7 @@ __device__ __forceinline__ void gates16(const uint32_t (&g)[16], const uint32_t 
             o[i] = pack_bf16x2(r.x(), r.y());
         } else {
             // (the factor last: dy alone times it might be too large)
-            const f2 t = pair(bf16lo(d[i]), bf16hi(d[i])), r = mul2(mul2(mul2(t, w), v.d), both(factor)), r2 = mul2(mul2(t, v.a), both(factor));
+            const f2 t = pair(bf16lo(d[i]), bf16hi(d[i])), r = mul2(mul2(mul2(t, w), v.d), both(fg)), r2 = mul2(mul2(t, v.a), both(fu));
             o[i] = pack_half2(r.x(), r.y());
             o2[i] = pack_half2(r2.x(), r2.y());
         }
@@ -434,12 +450,11 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                     d[i / 2] = v.x; d[i / 2 + 1] = v.y; d[i / 2 + 2] = v.z; d[i / 2 + 3] = v.w;
                 }
             }
-            // the row's factor: of dG and dU, or what takes it (and the other operand's) away again
-            int n = 0;
-            if constexpr (USE == PARTS || USE == DX) n = on ? scales.row(a.row_exp[row]) : 0;
-            if constexpr (USE == DX) n = -(n + scales.weights);
-            if constexpr (USE == DW) n = -scales.all;
-            const float factor = power(USE == PARTS ? n : n / 2), second = power(n - n / 2);
+            // the row's factors of dG and dU, or what takes them and the other operands' away again (DX: the same of both halves)
+            const int e = (USE == PARTS || USE == DX) && on ? scales.row(a.row_exp[row]) : 0;
+            const int n = USE == DX ? e - scales.dG - scales.Wg : USE == DW ? -(up ? scales.dU : scales.dG) - scales.x : 0;
+            [[maybe_unused]] const float factor = power(n / 2), second = power(n - n / 2);
+            [[maybe_unused]] const float fg = power(scales.dG - e), fu = power(scales.dU - e);
             const int buf = item & 1;
             const uint32_t bph = (uint32_t)(item >> 1) & 1u;
             int ok = mbar_wait(smem_u32(&ctl->tfull[buf]), bph, abort_flag) ? 1 : 0;
@@ -466,7 +481,7 @@ contract(const __grid_constant__ CUtensorMap tA0, const __grid_constant__ CUtens
                 auto all = [&](auto act) {
 #pragma unroll
                     for (int c = 0; c < MINE / N; ++c)
-                        gates16<USE, decltype(act)::value>(v[c], p[c], USE == PARTS ? d + c * 8 : d, factor, o + c * 8, USE == PARTS ? o2 + c * 8 : o2);
+                        gates16<USE, decltype(act)::value>(v[c], p[c], USE == PARTS ? d + c * 8 : d, fg, fu, o + c * 8, USE == PARTS ? o2 + c * 8 : o2);
                 };
                 if (a.act == WCC_ACT_SILU) all(std::integral_constant<int, WCC_ACT_SILU>());
                 else if (a.act == WCC_ACT_GELU) all(std::integral_constant<int, WCC_ACT_GELU>());
@@ -555,15 +570,15 @@ template <int LANES>
 __global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __restrict__ dy, const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg,
                                                         const __nv_bfloat16* __restrict__ Wu, int rows, int Cin, int F, short* __restrict__ row_exp, Exps* exps)
 {
-    __shared__ unsigned most[2];
+    __shared__ unsigned most[4];
     pdl_wait();
     pdl_launch();
-    if (threadIdx.x < 2) most[threadIdx.x] = 0;
+    if (threadIdx.x < 4) most[threadIdx.x] = 0;
     __syncthreads();
     constexpr int EACH = 256 / LANES;
     const int lane = threadIdx.x & (LANES - 1);
     const long long all = (long long)rows + 2 * F, step = (long long)gridDim.x * EACH;
-    unsigned top_w = 0, top_r = 0;
+    unsigned top_g = 0, top_u = 0, top_r = 0, top_x = 0;
     for (long long r0 = (long long)blockIdx.x * EACH; r0 < all; r0 += step) {
         // (lanes without a row go along with the last one)
         const long long r = min(r0 + threadIdx.x / LANES, all - 1), f = r - rows;
@@ -573,17 +588,21 @@ __global__ void __launch_bounds__(256) exponents(const __nv_bfloat16* __restrict
         if (row) {
             if (lane == 0) row_exp[r] = (short)(ey + ex);
             top_r = max(top_r, (unsigned)(ey + 2 * ex + BIAS));
+            top_x = max(top_x, (unsigned)(ex + BIAS));
+        } else if (f < F) {
+            top_g = max(top_g, (unsigned)(ex + BIAS));
         } else {
-            top_w = max(top_w, (unsigned)(ex + BIAS));
+            top_u = max(top_u, (unsigned)(ex + BIAS));
         }
     }
     if (lane == 0) {
-        if (top_w) atomicMax(&most[0], top_w);
-        if (top_r) atomicMax(&most[1], top_r);
+        if (top_g) atomicMax(&most[0], top_g);
+        if (top_u) atomicMax(&most[1], top_u);
+        if (top_r) atomicMax(&most[2], top_r);
+        if (top_x) atomicMax(&most[3], top_x);
     }
     __syncthreads();
-    if (threadIdx.x == 0 && most[0]) atomicMax(&exps->weights, most[0]);
-    if (threadIdx.x == 1 && most[1]) atomicMax(&exps->rows, most[1]);
+    if (threadIdx.x < 4 && most[threadIdx.x]) atomicMax(reinterpret_cast<unsigned*>(exps) + threadIdx.x, most[threadIdx.x]);
 }
 // x and the weights in fp16 with their factors; x16 or W16 NULL: not wanted.
 static __global__ void __launch_bounds__(256) to_half(const __nv_bfloat16* __restrict__ x, const __nv_bfloat16* __restrict__ Wg, const __nv_bfloat16* __restrict__ Wu,
@@ -597,14 +616,15 @@ static __global__ void __launch_bounds__(256) to_half(const __nv_bfloat16* __res
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < nx + 2 * nw; i += (long long)gridDim.x * 256) {
         const uint4* from;
         uint4* to;
-        int n = s.weights;
+        int n;
         if (i < nx) {
             const long long row = nx < (1LL << 31) ? (long long)by_row.div((int)i) : i / per;
-            n = s.all - s.row(row_exp[row]);
+            n = s.x + s.row(row_exp[row]);
             from = reinterpret_cast<const uint4*>(x) + i;
             to = x16 + i;
         } else {
             const long long j = i - nx;
+            n = j < nw ? s.Wg : s.Wu;
             from = j < nw ? reinterpret_cast<const uint4*>(Wg) + j : reinterpret_cast<const uint4*>(Wu) + (j - nw);
             to = W16 + j;
         }
