@@ -631,7 +631,8 @@ __global__ void __launch_bounds__(T + 64, 2) ring_kernel(const __grid_constant__
                 if constexpr (ALIGNED) {
                     const f2 sa = add2(s1.v[0], s1.v[1]), sb = add2(s2.v[0], s2.v[1]);
                     const float n = (float)(count * V), sum = sa.x() + sa.y(), m = count ? __fdividef(sum, n) : 0.0f;
-                    entries[v_mine] = {n, pivot + m, fmaxf(sb.x() + sb.y() - sum * m, 0.0f)};
+                    // (a thread without a vector here has the pivot of another tile)
+                    entries[v_mine] = {n, count ? pivot + m : 0.0f, fmaxf(sb.x() + sb.y() - sum * m, 0.0f)};
                 } else {
                     const float n = (float)count;
 #pragma unroll
