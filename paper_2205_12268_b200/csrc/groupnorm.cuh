@@ -690,7 +690,14 @@ __device__ __forceinline__ void dx_of(const Args& a, int n, long long at, int nv
     else dx_tile<X, V, KEPT, WCC_ACT_NONE>(a, n, at, nvec, coef);
 }
 
-// From the channel sums of image n: dx = rstd gamma t + k1 (x - mean) + k0 with k0 = -rstd mean(g), k1 = -rstd^2 mean(g xh).
+// The terms of a group's dx = rstd gamma t + k1 (x - mean) + k0 from its sums of g and g (x - mean): k0 = -rstd mean(g), k1 = -rstd^2 mean(g xh).  The mean of g xh
+// comes first: it is of g's size, where rstd^3 alone would leave fp32 with a spread of 10^-13 or 10^13.
+__device__ __forceinline__ float2 terms_of(const Args& a, float r, float c1, float c2)
+{
+    const float m = r * (c2 * a.inv_count);
+    return make_float2(-r * (c1 * a.inv_count), -r * m * r);
+}
+// Of image n, from the sums of its channels.
 __device__ __forceinline__ void group_terms(const Args& a, int n, const float* chan, float2* coef)
 {
     for (int g = threadIdx.x >> 5; g < a.G; g += T / 32) {
@@ -705,7 +712,7 @@ __device__ __forceinline__ void group_terms(const Args& a, int n, const float* c
         c2 = warp_sum(c2);
         if ((threadIdx.x & 31) == 0) {
             const float r = __ldg(a.rstd + (size_t)n * a.G + g);
-            coef[g] = make_float2(-r * c1 * a.inv_count, -r * r * r * c2 * a.inv_count);
+            coef[g] = terms_of(a, r, c1, c2);
         }
     }
 }

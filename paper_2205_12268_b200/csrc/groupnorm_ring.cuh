@@ -218,7 +218,10 @@ template <bool BWD> __device__ __forceinline__ bool finish(const Args& a, int n,
             }
             c1 = warp_sum(c1);
             c2 = warp_sum(c2);
-            if (lane == 0) put_coef(a.coef + (size_t)n * a.G + g, -r * c1 * a.inv_count, -r * r * r * c2 * a.inv_count);
+            if (lane == 0) {
+                const float2 k = terms_of(a, r, c1, c2);
+                put_coef(a.coef + (size_t)n * a.G + g, k.x, k.y);
+            }
         }
     }
     return true;
