@@ -162,8 +162,10 @@ template <int V> constexpr int LOADS_BWD = V >= 4 ? 2 : 8 / V;
 struct Stat { float n, mean, m2; };
 __device__ __forceinline__ Stat merge(Stat a, Stat b)
 {
+    // (what is of no values adds nothing: its distance's square may be no fp32 number)
+    if (b.n == 0.0f) return a;
+    if (a.n == 0.0f) return b;
     const float n = a.n + b.n;
-    if (n == 0.0f) return a;
     const float d = b.mean - a.mean, f = __fdividef(b.n, n);
     return {n, __fmaf_rn(d, f, a.mean), a.m2 + b.m2 + d * d * a.n * f};
 }
