@@ -159,21 +159,23 @@ template <int V> constexpr int LOADS_FWD = V == 1 ? 8 : 4;
 template <int V> constexpr int LOADS_BWD = V >= 4 ? 2 : 8 / V;
 
 // ---- pieces ----------------------------------------------------------------------------------------
-struct Stat { float n, mean, m2; };
-__device__ __forceinline__ Stat merge(Stat a, Stat b)
+struct Stat { float n, mean, m2; };       // (ring)
+// Values put together: their number, their mean in two parts, base + off, and the sum of their squared deviations from it.  base is one of the values: between
+// groups of a few values differences of means go into the deviations at first order, and the mean of values far from zero, rounded, has lost too much for
+// that (a mean of 10^4 spreads: rstd of 23 values was off by 10^-4; one by one its parts lose what is of the spread's size).
+struct Part { float n, base, off, m2; };
+__device__ __forceinline__ Part merge(Part a, Part b)
 {
-    // (what is of no values adds nothing: its distance's square may be no fp32 number)
-    if (b.n == 0.0f) return a;
-    if (a.n == 0.0f) return b;
-    const float n = a.n + b.n;
-    const float d = b.mean - a.mean, f = __fdividef(b.n, n);
-    return {n, __fmaf_rn(d, f, a.mean), a.m2 + b.m2 + d * d * a.n * f};
+    // (what is of no values adds nothing: the square of its distance may be no fp32 number.  By selections: with branches 3 x 40 x 200 x 1023 fp32 takes 253 us, so 185.)
+    const bool none = a.n == 0.0f, both = !none && b.n != 0.0f;
+    const float n = a.n + b.n, f = both ? __fdividef(b.n, n) : 0.0f, d = both ? (b.base - a.base) + (b.off - a.off) : 0.0f;
+    return {n, none ? b.base : a.base, none ? b.off : __fmaf_rn(d, f, a.off), a.m2 + b.m2 + d * d * a.n * f};
 }
-__device__ __forceinline__ Stat warp_merge(Stat s)
+__device__ __forceinline__ Part warp_merge(Part s)
 {
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-        Stat b{__shfl_xor_sync(0xFFFFFFFFu, s.n, o), __shfl_xor_sync(0xFFFFFFFFu, s.mean, o), __shfl_xor_sync(0xFFFFFFFFu, s.m2, o)};
+        Part b{__shfl_xor_sync(0xFFFFFFFFu, s.n, o), __shfl_xor_sync(0xFFFFFFFFu, s.base, o), __shfl_xor_sync(0xFFFFFFFFu, s.off, o), __shfl_xor_sync(0xFFFFFFFFu, s.m2, o)};
         // the lower lane's part first on both sides: the same bits on all lanes
         s = (threadIdx.x & o) ? merge(b, s) : merge(s, b);
     }
@@ -196,9 +198,9 @@ template <int V> __device__ __forceinline__ int channel(const Args& a, int q, in
 // ---- forward ---------------------------------------------------------------------------------------
 // Sums of a tile.  Deviations are taken from the thread's first value (of the channel, or of its group), so a common offset costs nothing: a
 // thread's sum of squares holds the pivot's own distance squared, and loses at most (values of the thread) * 2^-24 of itself.  Threads and tiles
-// are then put together as (count, mean, sum of squared deviations).
+// are then put together (Part).
 template <typename X, int V, bool ALIGNED>
-__device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, Stat* entries)
+__device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, Part* entries)
 {
     const Plan& q = a.q;
     const int sub = threadIdx.x / q.lanes, lane = threadIdx.x - sub * q.lanes;
@@ -235,7 +237,7 @@ __device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, 
                 }
             }
             const float n = (float)(k * V), sum = s.x() + s.y() + s1, sq = ss.x() + ss.y() + ss1, m = k ? __fdividef(sum, n) : 0.0f;
-            entries[v0] = {n, pivot + m, fmaxf(sq - sum * m, 0.0f)};
+            entries[v0] = {n, pivot, m, fmaxf(sq - sum * m, 0.0f)};
         } else {
             float s[V], ss[V], pivot[V];
 #pragma unroll
@@ -261,7 +263,7 @@ __device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, 
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float n = (float)k, m = k ? __fdividef(s[e], n) : 0.0f;
-                entries[v0 * V + e] = {n, pivot[e] + m, fmaxf(ss[e] - s[e] * m, 0.0f)};
+                entries[v0 * V + e] = {n, pivot[e], m, fmaxf(ss[e] - s[e] * m, 0.0f)};
             }
         }
     }
@@ -269,12 +271,12 @@ __device__ __forceinline__ void stats_tile(const Args& a, const X* x, int nvec, 
 
 // Group g of the CTA's entries; the whole warp calls it.
 template <int V, bool ALIGNED>
-__device__ __forceinline__ Stat group_of(const Args& a, int g, const Stat* entries)
+__device__ __forceinline__ Part group_of(const Args& a, int g, const Part* entries)
 {
     const Plan& q = a.q;
     constexpr int W = ALIGNED ? V : 1;
     const int period = q.p * V / W, Cw = a.C / W, Dw = a.D / W, copies = period / Cw, each = copies * Dw, total = q.reps * each;
-    Stat s{0.0f, 0.0f, 0.0f};
+    Part s{0.0f, 0.0f, 0.0f, 0.0f};
     for (int m = threadIdx.x & 31; m < total; m += 32) {
         const int sub = m / each, rest = m - sub * each, i = rest / Dw;
         s = merge(s, entries[sub * period + i * Cw + g * Dw + (rest - i * Dw)]);
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(T, CTAS_FWD) forward_kernel(const __grid_const
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ long long s_item;
     __shared__ int s_flag;
-    Stat* entries = reinterpret_cast<Stat*>(smem);
+    Part* entries = reinterpret_cast<Part*>(smem);
     const Plan& q = a.q;
     const int warp = threadIdx.x >> 5;
     const X* x = static_cast<const X*>(a.x);
@@ -410,17 +412,17 @@ __global__ void __launch_bounds__(T, CTAS_FWD) forward_kernel(const __grid_const
     pdl_launch();
     if (q.solo) {
         const int words = q.slots > 1 ? q.p * V / (ALIGNED ? V : 1) : q.reps * q.p * (ALIGNED ? 1 : V);
-        float2* coef = reinterpret_cast<float2*>(entries + words + (words & 1));
+        float2* coef = reinterpret_cast<float2*>(entries + words);
         const int nvec = (int)(E / V);
         for (int n = blockIdx.x; n < a.N; n += gridDim.x) {
             stats_tile<X, V, ALIGNED>(a, x + n * E, nvec, entries);
             __syncthreads();
             for (int g = warp; g < a.G; g += T / 32) {
-                const Stat s = group_of<V, ALIGNED>(a, g, entries);
+                const Part s = group_of<V, ALIGNED>(a, g, entries);
                 if ((threadIdx.x & 31) == 0) {
-                    const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps));
-                    coef[g] = make_float2(s.mean, r);
-                    if (a.mean_out) a.mean_out[(size_t)n * a.G + g] = s.mean;
+                    const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps)), mean = s.base + s.off;
+                    coef[g] = make_float2(mean, r);
+                    if (a.mean_out) a.mean_out[(size_t)n * a.G + g] = mean;
                     if (a.rstd_out) a.rstd_out[(size_t)n * a.G + g] = r;
                 }
             }
@@ -448,21 +450,22 @@ __global__ void __launch_bounds__(T, CTAS_FWD) forward_kernel(const __grid_const
             stats_tile<X, V, ALIGNED>(a, x + at, nvec, entries);
             __syncthreads();
             for (int g = warp; g < a.G; g += T / 32) {
-                const Stat s = group_of<V, ALIGNED>(a, g, entries);
-                if ((threadIdx.x & 31) == 0) part[(size_t)it.tile * a.G + g] = make_float2(s.mean, s.m2);
+                const Part s = group_of<V, ALIGNED>(a, g, entries);
+                // (a tile's mean in one number: the tile's values are many, and what their mean loses goes into the whole by less than a value's own rounding)
+                if ((threadIdx.x & 31) == 0) part[(size_t)it.tile * a.G + g] = make_float2(s.base + s.off, s.m2);
             }
             if (arrive_last(ctl, (unsigned)q.nt, &s_flag)) {
                 for (int g = warp; g < a.G; g += T / 32) {
-                    Stat s{0.0f, 0.0f, 0.0f};
+                    Part s{0.0f, 0.0f, 0.0f, 0.0f};
                     for (int t = threadIdx.x & 31; t < q.nt; t += 32) {
                         const float2 v = __ldcg(part + (size_t)t * a.G + g);
-                        s = merge(s, {(float)((long long)min(q.tile, a.P - t * q.tile) * a.D), v.x, v.y});
+                        s = merge(s, {(float)((long long)min(q.tile, a.P - t * q.tile) * a.D), v.x, 0.0f, v.y});
                     }
                     s = warp_merge(s);
                     if ((threadIdx.x & 31) == 0) {
-                        const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps));
-                        coef[g] = make_float2(s.mean, r);
-                        if (a.mean_out) a.mean_out[(size_t)it.n * a.G + g] = s.mean;
+                        const float r = __fdiv_rn(1.0f, __fsqrt_rn(s.m2 * a.inv_count + a.eps)), mean = s.base + s.off;
+                        coef[g] = make_float2(mean, r);
+                        if (a.mean_out) a.mean_out[(size_t)it.n * a.G + g] = mean;
                         if (a.rstd_out) a.rstd_out[(size_t)it.n * a.G + g] = r;
                     }
                 }
@@ -1023,7 +1026,7 @@ wcc_status launch_forward(const Args& a, const DeviceInfo& di, cudaStream_t st)
 {
     const Plan& q = a.q;
     const int words = (q.slots > 1 ? q.p : q.reps * q.p) * (ALIGNED ? 1 : V);
-    size_t smem = (size_t)(words + (words & 1)) * sizeof(Stat) + (q.solo ? (size_t)a.G * 8 : 0);
+    size_t smem = (size_t)words * sizeof(Part) + (q.solo ? (size_t)a.G * 8 : 0);
     if (smem < (size_t)a.G * 8) smem = (size_t)a.G * 8;
     if (smem > 48 * 1024) {
         const wcc_status s = allow_smem<forward_kernel<X, V, ALIGNED>>(di.dev, (int)smem);
