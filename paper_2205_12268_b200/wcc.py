@@ -512,8 +512,7 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
     """The gradients of ``layernorm``: (dx, dgamma, dbeta), the last two fp32 [C] and None without ``params``.
     ``dx`` may be dy or x.  ``ws`` is a ``Workspace.for_layernorm_backward``, allocated here if it is not given.
     ``x`` may be a ``Checkpoint`` of the map; its values are brought back first."""
-    if isinstance(x, Checkpoint):
-        x = x.restore()
+    x, kept = _brought_back(x)
     N, Cc, H, W = _map_shape(x, "x")
     dt, dev = _dt(x), _here(x)
     pdy, pg = _same(dy, x, dev, "dy", "x"), _floats(gamma, Cc, dev, "gamma")
@@ -530,6 +529,8 @@ def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rs
         if ws is None:
             ws = Workspace.for_layernorm_backward(x)
         pdg, pdb, pw, nw = dgamma.data_ptr(), dbeta.data_ptr(), ws.buf.data_ptr(), ws.nbytes
+    if kept is not None:
+        kept.restore(out=x)
     _check(lib().wcc_layernorm_bwd(pdy, x.data_ptr(), pg, pm, pr, N, Cc, H, W, dt, pdx, pdg, pdb, pw, nw, _stream()), "wcc_layernorm_bwd")
     return dx, dgamma, dbeta
 
@@ -578,6 +579,11 @@ class Checkpoint:
         _check(lib().wcc_checkpoint_restore(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.L, _dt(out), out.data_ptr(), _stream()),
                "wcc_checkpoint_restore")
         return out
+
+
+def _brought_back(x):
+    """(x, None), or of a ``Checkpoint`` room for its values and itself: they are brought back once nothing is left to refuse here."""
+    return (x.codes.new_empty(x.codes.shape, dtype=x.dtype), x) if isinstance(x, Checkpoint) else (x, None)
 
 
 def checkpoint(x: torch.Tensor, into: Checkpoint | None = None) -> Checkpoint:
@@ -715,9 +721,9 @@ def gated_backward(dy: torch.Tensor, x, Wg: torch.Tensor, Wu: torch.Tensor, act=
                    ws: Workspace | None = None):
     """The gradients of ``gated``: (dx, dWg, dWu), all bfloat16, the last two None without ``params``.  Nothing is needed of the forward pass but x, which
     may be a ``Checkpoint`` (its values are brought back first).  ``ws``: a ``Workspace.for_gated_backward``, allocated here if it is not given."""
-    if isinstance(x, Checkpoint):
-        x = x.restore()
+    x, kept = _brought_back(x)
     rows, Cin, F, dev = _gated_shape(x, Wg, Wu)
+    code = _act(act)
     if not (dy.get_device() == dev and dy.is_contiguous() and dy.dtype == x.dtype and dy.shape == tuple(x.shape[:-1]) + (F,)):
         raise ValueError("dy must be contiguous bfloat16 [...][F] with x's rows on its device")
     if dx is None:
@@ -732,7 +738,9 @@ def gated_backward(dy: torch.Tensor, x, Wg: torch.Tensor, Wu: torch.Tensor, act=
         dWg, dWu = torch.empty_like(Wg), torch.empty_like(Wu)
     if ws is None:
         ws = Workspace.for_gated_backward(x, Wg)
-    _check(lib().wcc_gated_bwd(dy.data_ptr(), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), rows, Cin, F, _act(act), pdx, _ptr(dWg), _ptr(dWu),
+    if kept is not None:
+        kept.restore(out=x)
+    _check(lib().wcc_gated_bwd(dy.data_ptr(), x.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), rows, Cin, F, code, pdx, _ptr(dWg), _ptr(dWu),
                                ws.buf.data_ptr(), ws.nbytes, _stream()), "wcc_gated_bwd")
     return dx, dWg, dWu
 
@@ -822,8 +830,7 @@ class Adapters:
                  params: bool = True, ws: Workspace | None = None):
         """(dx, dA, dB): dx = base + the adapters' part of the map's gradient, dA and dB fp32 in the factors' shapes (None without ``params``).
         ``x`` may be a ``Checkpoint`` of the map; its values are brought back first."""
-        if isinstance(x, Checkpoint):
-            x = x.restore()
+        x, kept = _brought_back(x)
         N, _, H, W = self._shape(x)
         dev, px = _here(x), x.data_ptr()
         pi, pdy, pb = self._ids(ids, N, dev), self._map(dy, x, self.Cout, dev, "dy"), self._map(base, x, self.Cin, dev, "base")
@@ -835,6 +842,8 @@ class Adapters:
         dA = x.new_empty(self.A.shape, dtype=torch.float32) if params else None
         dB = x.new_empty(self.B.shape, dtype=torch.float32) if params else None
         buf, n = self._scratch(x, N, H, W, True, ws)
+        if kept is not None:
+            kept.restore(out=x)
         _check(lib().wcc_adapters_bwd(pdy, px, self.A.data_ptr(), self.B.data_ptr(), _ptr(self.scale), pi, pb, N, self.Cin, self.Cout, H, W, self.R,
                                       self.rank, self.dt, pdx, _ptr(dA), _ptr(dB), buf.data_ptr(), n, _stream()), "wcc_adapters_bwd")
         return dx, dA, dB
