@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(256, 5) pack_vectors(const T* __restrict__ x, 
                                                     float* __restrict__ scales)
 {
     constexpr int V = 16 / (int)sizeof(T), EACH = 256 / LANES, U = 4;
+    static_assert(LANES >= U, "a lane divides for each of the U blocks");
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x % LANES, col = lane * V;
@@ -113,20 +114,10 @@ __global__ void __launch_bounds__(256, 5) pack_vectors(const T* __restrict__ x, 
         // each of four lanes divides for one of the four blocks
         float inv[U];
         const int j = lane & (U - 1);
-        Scale s{0.0f, 0.0f};
-        if constexpr (LANES >= U) {
-            s = scale_of(j == 1 ? top[1] : j == 2 ? top[2] : j == 3 ? top[3] : top[0]);
+        const Scale s = scale_of(j == 1 ? top[1] : j == 2 ? top[2] : j == 3 ? top[3] : top[0]);
 #pragma unroll
-            for (int u = 0; u < U; ++u) inv[u] = __shfl_sync(0xFFFFFFFFu, s.inv, u, LANES);
-            if (lane < U && b0 + j * EACH < blocks) scales[b0 + j * EACH] = s.scale;
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                s = scale_of(top[u]);
-                inv[u] = s.inv;
-                if (lane == 0 && b0 + u * EACH < blocks) scales[b0 + u * EACH] = s.scale;
-            }
-        }
+        for (int u = 0; u < U; ++u) inv[u] = __shfl_sync(0xFFFFFFFFu, s.inv, u, LANES);
+        if (lane < U && b0 + j * EACH < blocks) scales[b0 + j * EACH] = s.scale;
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (on[u]) {
