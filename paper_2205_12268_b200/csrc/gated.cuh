@@ -73,7 +73,7 @@ struct Ctl {
 
 // Exponents E, |v| < 2^E, with BIAS added: of either weights and of x, and the largest over the rows of what they bring to DW, |dy_r| |x_r|^2.  (A row's own,
 // E(r) of |dy_r| |x_r|, are a list.)
-struct Exps { unsigned Wg, Wu, rows, x; };
+struct alignas(16) Exps { unsigned Wg, Wu, rows, x; };
 constexpr int BIAS = 512;
 
 struct Args {
@@ -158,8 +158,9 @@ struct Scales {
     __device__ __forceinline__ Scales() {}
     __device__ __forceinline__ Scales(const Exps* e, int log_cin)
     {
-        int eg = (int)__ldcg(&e->Wg) - BIAS, eu = (int)__ldcg(&e->Wu) - BIAS;
-        const int least = -126, er = (int)__ldcg(&e->rows) - BIAS, ex = (int)__ldcg(&e->x) - BIAS;
+        const uint4 all = __ldcg(reinterpret_cast<const uint4*>(e));
+        const int least = -126, er = (int)all.z - BIAS, ex = (int)all.w - BIAS;
+        int eg = (int)all.x - BIAS, eu = (int)all.y - BIAS;
         if (eg == least) eg = eu;
         if (eu == least) eu = eg;
         dG = 13 - log_cin - eu;
