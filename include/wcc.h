@@ -393,14 +393,16 @@ wcc_status wcc_checkpoint_restore(const int8_t* codes, const float* scales, long
 /*
  * Group norm with an activation: the channels of an image in `groups` groups of D = C / groups, each normalised over its D channels at all P positions,
  *     mean = 1/(P D) sum x,  rstd = (1/(P D) sum (x - mean)^2 + eps)^-1/2,  z = (x - mean) * rstd * gamma[c] + beta[c],  y = act(z)
- * (of each image and group).  act: WCC_ACT_NONE, WCC_ACT_RELU or WCC_ACT_SILU (z / (1 + exp(-z))).
+ * (of each image and group).  act: WCC_ACT_NONE, WCC_ACT_RELU or WCC_ACT_SILU (z / (1 + exp(-z)); 0 where exp(z) is below fp32's normal numbers); others are
+ * refused as WCC_ERR_SHAPE.
  *   x     in : [N][P][C] of dt             gamma, beta in: fp32 [C], each may be NULL (1 and 0)
  *   y     out: as x; may be x itself       mean, rstd out: fp32 [N][groups], each may be NULL; the backward pass reads them
- *   codes, scales out: the checkpoint of x as wcc_checkpoint(x, N * P, C, ...) writes it; both NULL: not wanted
+ *   codes, scales out: the checkpoint of x as wcc_checkpoint(x, N * P, C, ...) writes it (in a launch of its own, which reads x once more); both NULL: not wanted
  *   eps      : >= 0 and finite.  With eps = 0 a group whose values are all equal gives NaN, as the formula does.
  *   ws       : scratch of at least wcc_groupnorm_workspace_bytes(..., 0) bytes of this call's sizes, 16-byte aligned
  * groups divides C, C <= WCC_MAX_CHANNELS, N * P <= 2^30, N * P * C <= 2^40.  fp32 arithmetic; the variance is put together from squared deviations from a value of the
- * data or a mean, so a large common offset costs it no digits.  The order of the sums depends on the sizes alone: the same call gives the same bits.
+ * data or a mean, never from squares of x: a mean of 2^k spreads costs rstd at most 2^(k - 23) / sqrt(values of the group) of itself.  What one image or group
+ * holds changes no other's results.  The order of the sums depends on the sizes alone: the same call gives the same bits.
  */
 size_t wcc_groupnorm_workspace_bytes(int N, int P, int C, int groups, wcc_dtype dt, int backward);
 wcc_status wcc_groupnorm_fwd(const void* x, const float* gamma, const float* beta, int N, int P, int C, int groups, float eps, wcc_act act,
@@ -408,7 +410,7 @@ wcc_status wcc_groupnorm_fwd(const void* x, const float* gamma, const float* bet
 /*
  * Its backward pass.  With xh = (x - mean) * rstd, t = dy * act'(xh gamma + beta) and g = t * gamma[c]:
  *     dx = rstd * (g - 1/(P D) sum g - xh * 1/(P D) sum g xh),   dgamma[c] = sum_{n,p} t xh,   dbeta[c] = sum_{n,p} t
- * (relu: act'(z) = 1 for z > 0, else 0).
+ * (relu: act'(z) = 1 for z > 0, else 0).  fp32 arithmetic; rstd^2 times the mean of g xh has to be an fp32 number (a spread between 10^-17 and 10^17).
  *   dy    in : [N][P][C] of dt             x in: as the forward pass had it, or NULL: then codes and scales are its checkpoint
  *   gamma, beta in: as in the forward pass (beta is read only with an activation)
  *   mean, rstd  in: what the forward pass returned
@@ -422,7 +424,7 @@ wcc_status wcc_groupnorm_bwd(const void* dy, const void* x, const int8_t* codes,
 /*
  * The gated pointwise block on rows of channels (positions of a channels-last map, tokens): both projections, the activation and the product,
  *     g = x Wg^T,  u = x Wu^T,  y = act(g) * u
- * act: any wcc_act (gelu: g * Phi(g) with the normal distribution function).  bf16 only, sums in fp32 on the tensor cores; y is rounded once.
+ * act: any wcc_act (gelu: g * Phi(g) with the normal distribution function, Phi to 10^-7 absolute).  bf16 only, sums in fp32 on the tensor cores; y is rounded once.
  *   x  in : bf16 [rows][Cin]          Wg, Wu in: bf16 [F][Cin]          y out: bf16 [rows][F], must not overlap the inputs
  * Cin and F are multiples of 8, at most WCC_MAX_GATED; 1 <= rows <= 2^30.
  */
@@ -431,9 +433,13 @@ wcc_status wcc_gated_fwd(const void* x, const void* Wg, const void* Wu, int rows
 /*
  * Its backward pass.  Nothing is kept of the forward pass but x: g and u are computed again.
  *     dG = dy * u * act'(g),  dU = dy * act(g),   dx = dG Wg + dU Wu,   dWg = dG^T x,   dWu = dU^T x
- * dG, dU, x and the weights enter the products as fp16 with a power of two for each row (of x, dy) and for the weights, from bounds, so that nothing
- * overflows: a rounding of 2^-12 of a term at most, of what is at least 2^-28 of its row's bound 1.13 Cin max|dy_r| max|x_r| max|W|, on top of the results' own.
- * A row with a NaN or an infinity gives such in its own row of dx and in the weights' gradients.
+ * dG, dU, x and the weights enter the products as fp16 with powers of two in front, from bounds, so that nothing overflows.  On top of the results' own rounding:
+ *   dG  of row r is off by at most 2^-11 of itself or 2^-34 of B_r = 1.13 Cin max|dy_r| max|x_r| max|Wu|, whichever is more; dU the same with max|Wg|;
+ *   Wg and Wu in dx are exact, or off by 2^-39 of their own largest value, whichever is more;
+ *   x in dWg and dWu is exact, or off by so much that its row's term is by 2^-34 of the largest B_r max|x_r| of all rows, whichever is more: rows (or columns f of dy)
+ *   that lie further than that below the others do not show in the weights' gradients.
+ * (The bounds of a row's dG and dU are at least 2^-114; below, the second figures grow.)  A row with a NaN or an infinity gives such in its own row of dx and in
+ * the weights' gradients.
  *   dy in : bf16 [rows][F]            dx out: bf16 [rows][Cin], must not overlap the inputs; NULL: not wanted
  *   dWg, dWu out: bf16 [F][Cin], both NULL: not wanted
  *   ws    : scratch of at least wcc_gated_bwd_workspace_bytes(...) bytes of this call's sizes, 16-byte aligned

@@ -819,7 +819,7 @@ __global__ void __launch_bounds__(T, CTAS_BWD) backward_kernel(const __grid_cons
 
 // ---- images of one position ------------------------------------------------------------------------
 // Rows of tokens: a group is D neighbouring values, 2^k lanes with a vector each, so its sums are shuffles and nothing is read twice.  A thread keeps its channels
-// from row to row.  (us, 8192 x 1024 bf16, an image a CTA as above / this way: forward 198 / 15, backward 343 / 27.)
+// from row to row.  (us, 8192 x 1024 bf16, an image a CTA as above / this way: forward 198 / 13, backward 343 / 23.)
 inline bool rows_path(int P, int C, int G, int es, bool whole_rows)
 {
     const int V = 16 / es, D = C / G, lanes = D / V;
